@@ -79,12 +79,12 @@ enum {
     LAPLEX_OK = 0,
     LAPLEX_ERR_NULL = -1,      /* a required pointer is NULL */
     LAPLEX_ERR_SIZE = -2,      /* negative size, or k + n above LAPLEX_MAX_MERGED */
-    LAPLEX_ERR_LD = -3,        /* a leading dimension below batch */
+    LAPLEX_ERR_LD = -3,        /* a leading dimension below the length of a row (batch) */
     LAPLEX_ERR_WORKSPACE = -4, /* ws_bytes below laplex_workspace_bytes(...) */
     LAPLEX_ERR_FLAGS = -5,     /* unknown bit, or a bit that has no meaning for this call */
     LAPLEX_ERR_HIP = -6,       /* a HIP launch failed; see laplex_last_hip_error() */
     LAPLEX_ERR_ALIGN = -7,     /* a float pointer not 4-byte, or ws not 256-byte, aligned */
-    LAPLEX_ERR_VALUE = -8      /* a scalar argument is out of range (inverse temperature not positive and finite) */
+    LAPLEX_ERR_VALUE = -8      /* a scalar argument is out of range (inverse temperature not positive and finite, unknown type) */
 };
 
 enum {
@@ -357,6 +357,134 @@ int laplex_get_perm(const void* ws, size_t ws_bytes, int64_t count, uint32_t* pe
  */
 int laplex_get_plan_status(const void* ws, size_t ws_bytes, int64_t count, uint32_t* status_out,
                            laplex_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Operators for token models: what stands before and behind a LAPLEX^(r) head that is taught to predict tokens.  The
+ * rules above hold, with these differences: matrices are of one of the types below (`type`), a row of one holds what
+ * belongs to one TOKEN ([heads][numbers of a head], ld >= their product, so that the parts of a fused projection's result
+ * are read where they lie), and floats named `float*` are fp32 whatever the type.  Sums, states and statistics are held
+ * in fp32 at least and rounded once, when they are written.
+ * ------------------------------------------------------------------------- */
+enum {
+    LAPLEX_F32 = 0,
+    LAPLEX_BF16 = 1     /* 2-byte aligned pointers instead of 4-byte aligned ones */
+};
+
+enum {
+    LAPLEX_ROTARY_INTERLEAVED = 16u,   /* pairs are (0, 1), (2, 3), ...; without: (0, r/2), (1, r/2 + 1), ... */
+    LAPLEX_ROTARY_INVERSE = 32u        /* turn the other way: what carries gradients back */
+};
+
+enum { /* laplex_rotary_frequencies */
+    LAPLEX_ROTARY_PLAIN = 0,
+    LAPLEX_ROTARY_LINEAR = 1,
+    LAPLEX_ROTARY_BASE = 2,
+    LAPLEX_ROTARY_PARTS = 3
+};
+
+#define LAPLEX_TOKEN_MAX_HEADS 65535LL
+#define LAPLEX_TOKEN_MAX_TOKENS 67108864LL  /* tokens (rows, and the columns of logits) of a call */
+#define LAPLEX_TOKEN_MAX_SEQUENCES 1048576LL
+#define LAPLEX_ROTARY_MAX_DIM 4096LL        /* numbers of a head */
+#define LAPLEX_ATTENTION_MAX_DIM 256LL      /* numbers of a head in q and k, and in v */
+#define LAPLEX_LOGPROB_MAX_TOP 64LL         /* alternatives of a token */
+
+/*
+ * Rotary positions: the first rotary_dim numbers of every head of x[tokens][heads][head_dim] are r/2 pairs, and pair i of
+ * token t is turned by the angle positions[t] * frequencies[i] and scaled by `magnitude`:
+ *   y1 = magnitude * (x1 cos - x2 sin),  y2 = magnitude * (x2 cos + x1 sin);
+ * the numbers behind them are copied.  positions[tokens] (int64, 8-byte aligned, any sign) and frequencies[rotary_dim / 2]
+ * are device arrays; the angle is formed in fp64 and brought below one turn before it is rounded, so positions of many
+ * millions keep their precision.  y may be x (in place; with another ld the matrices must not overlap).  The gradient is the same call
+ * on gy with LAPLEX_ROTARY_INVERSE.  Queries and keys that lie side by side in one matrix are turned by one call.
+ * rotary_dim even, 0 <= rotary_dim <= head_dim <= LAPLEX_ROTARY_MAX_DIM; magnitude finite.
+ */
+int laplex_rotary(const void* x, int64_t ldx, void* y, int64_t ldy, int type, int64_t tokens, int64_t heads, int64_t head_dim,
+                  int64_t rotary_dim, const int64_t* positions, const float* frequencies, float magnitude, uint32_t flags,
+                  laplex_stream_t stream);
+
+/*
+ * frequencies[i] = base^(-2 i / rotary_dim), i < rotary_dim / 2, for contexts `factor` times the original one:
+ *   PLAIN: as they are;  LINEAR: divided by factor;  BASE: with the base times factor^(r / (r - 2)), r = rotary_dim, so that the
+ *   slowest pair is slowed by factor and the fastest not at all;  PARTS: pairs that turn at least high_turns times within
+ *   original_context are kept, those with at most low_turns are divided by factor, and between them keep = (turns - low) / (high - low)
+ *   of the one and 1 - keep of the other.  Formed in fp64.  base and factor positive and finite; PARTS: original_context
+ *   positive, low_turns < high_turns.  What a scaling does not use is not looked at.
+ */
+int laplex_rotary_frequencies(float* frequencies, int64_t rotary_dim, double base, int scaling, double factor,
+                              double original_context, double low_turns, double high_turns, laplex_stream_t stream);
+
+/*
+ * Linear attention with a decay for each head: the causal Laplace kernel over token positions, weighted by q . k.  Per head
+ * of a sequence of n tokens, with l = exp(-rates[head]) and the state S0 (dk x dv):
+ *   y_t = scale * ( sum_{s <= t} l^(t-s) (q_t . k_s) v_s  +  l^(t+1) q_t S0 ),        t = 0 .. n-1
+ *   Sn  = l^n S0 + sum_s l^(n-1-s) k_s v_s^T
+ * q, k [tokens][heads][dk], v, y [tokens][heads][dv].  The sequences lie one behind the other: sequence b has the rows
+ * starts[b] .. starts[b+1]-1 (int64 device array of sequences + 1 ascending values from 0 to tokens; 8-byte aligned), or, with starts NULL,
+ * all have tokens / sequences rows.  Sequences may be empty.  Values in starts that are out of order or of range give wrong values, never a fault.
+ * rates[heads] >= 0 in device memory (constants of the layer: they get no gradient; +inf: every token sees only itself).
+ * state_in, state_out: fp32 [sequences][heads][dk][dv]; state_in NULL = zeros, state_out NULL = not wanted; they may be the same buffer.
+ * An empty sequence hands its state through.  1 <= dk, dv <= LAPLEX_ATTENTION_MAX_DIM; scale positive and finite.
+ * Rows before a value that is not finite are not touched by it; from its token on everything that it is weighted into is not finite.
+ */
+int laplex_decay_attention_workspace_bytes(int type, int64_t tokens, int64_t sequences, int64_t heads, int64_t dk, int64_t dv,
+                                           size_t* out /* host; enough for the forward and the backward call */);
+
+int laplex_decay_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                           int64_t tokens, int64_t sequences, const int64_t* starts, int64_t heads, int64_t dk, int64_t dv,
+                           const float* rates, float scale, const float* state_in, void* y, int64_t ldy, float* state_out,
+                           void* ws, size_t ws_bytes, laplex_stream_t stream);
+
+/*
+ * Gradients of sum(gy * y) + sum(gstate_out * Sn) with respect to q, k, v and S0:
+ *   gq_t  = scale * ( sum_{s <= t} l^(t-s) (gy_t . v_s) k_s + l^(t+1) S0 gy_t )
+ *   gk_s  = scale * sum_{t >= s} l^(t-s) (gy_t . v_s) q_t + l^(n-1-s) G v_s              (G = gstate_out)
+ *   gv_s  = scale * sum_{t >= s} l^(t-s) (q_t . k_s) gy_t + l^(n-1-s) G^T k_s
+ *   gS0   = scale * sum_t l^(t+1) q_t gy_t^T + l^n G
+ * gq, gk, gv may each be NULL (not wanted), and so may gstate_in; gstate_out NULL = zeros; state_in as in the forward call.
+ * No output may overlap an input or another output.  The call stands alone: nothing is kept from the forward call.
+ */
+int laplex_decay_attention_backward(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                                    int64_t tokens, int64_t sequences, const int64_t* starts, int64_t heads, int64_t dk, int64_t dv,
+                                    const float* rates, float scale, const float* state_in, const void* gy, int64_t ldgy,
+                                    const float* gstate_out, void* gq, int64_t ldgq, void* gk, int64_t ldgk, void* gv, int64_t ldgv,
+                                    float* gstate_in, void* ws, size_t ws_bytes, laplex_stream_t stream);
+
+/*
+ * The same for one token of every sequence, as when tokens are written one by one: row b of q, k, v, y belongs to sequence b, and
+ *   state[b] <- l state[b] + k v^T,   y = scale * q state[b]          (state fp32 [sequences][heads][dk][dv], updated in place).
+ */
+int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                                int64_t sequences, int64_t heads, int64_t dk, int64_t dv, const float* rates, float scale,
+                                float* state, void* y, int64_t ldy, laplex_stream_t stream);
+
+/*
+ * Log probabilities over logits y[k][batch] in the layout of this library's products (row = vocabulary entry, column = token),
+ * z = tau * y (tau an inverse temperature as above):
+ *   lse[t] = log sum_i exp z[i,t],  logp[t] = z[targets[t], t] - lse[t],  entropy[t] = -sum_i p log p,  p = exp(z - lse)
+ * and, with top > 0, the `top` largest logits of each column in descending order, of equal ones the lowest row first:
+ *   top_ids[r * batch + t] (int64), top_logp[r * batch + t] = z - lse,  r < top <= min(k, LAPLEX_LOGPROB_MAX_TOP).
+ * logp, lse, entropy may each be NULL; targets (int64 device array) may be NULL if logp is.  A target outside 0 .. k-1 (padding) has
+ * logp 0.  Logits of -inf (banned entries) have probability 0 and add nothing to the entropy; a column of nothing else has
+ * lse = logp = top_logp = -inf and entropy 0.  A column with a NaN or +inf gives NaN; NaN counts as the largest logit.
+ * k == 0 gives lse = -inf, entropy 0, logp 0.
+ */
+int laplex_logprob_workspace_bytes(int64_t k, int64_t batch, int64_t top, size_t* out /* host */);
+
+int laplex_logprob(const void* y, int64_t ldy, int type, int64_t k, int64_t batch, const int64_t* targets, float tau,
+                   float* logp, float* lse, float* entropy, int64_t top, int64_t* top_ids, float* top_logp,
+                   void* ws, size_t ws_bytes, laplex_stream_t stream);
+
+/*
+ * Gradient of sum_t glogp[t] logp[t] + gentropy[t] entropy[t] + glse[t] lse[t] with respect to the logits:
+ *   gy[i,t] = tau * ( glogp[t] (1[i == targets[t]] - p) - gentropy[t] p (log p + entropy[t]) + glse[t] p )
+ * glogp, gentropy, glse may each be NULL (= zeros).  lse and, if gentropy is given, entropy are the forward call's; targets are needed with glogp, and
+ * a target outside 0 .. k-1 contributes nothing.  gy (same type as y) may be y itself (in place).  No gradient flows through top_logp.
+ * A column of -inf alone has gradient 0; a column with a NaN or +inf gets NaN.
+ */
+int laplex_logprob_backward(const void* y, int64_t ldy, int type, int64_t k, int64_t batch, const int64_t* targets, float tau,
+                            const float* lse, const float* entropy, const float* glogp, const float* gentropy, const float* glse,
+                            void* gy, int64_t ldgy, laplex_stream_t stream);
 
 /* Host: static text for a status code. */
 const char* laplex_status_string(int status);

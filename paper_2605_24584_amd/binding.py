@@ -27,7 +27,23 @@ LAPLEX_B_SORTED = 2
 LAPLEX_REUSE_PLAN = 4
 LAPLEX_SAVE_SCANS = 8
 
+LAPLEX_F32 = 0
+LAPLEX_BF16 = 1
+
+LAPLEX_ROTARY_INTERLEAVED = 16
+LAPLEX_ROTARY_INVERSE = 32
+LAPLEX_ROTARY_PLAIN = 0
+LAPLEX_ROTARY_LINEAR = 1
+LAPLEX_ROTARY_BASE = 2
+LAPLEX_ROTARY_PARTS = 3
+
 LAPLEX_MAX_MERGED = 4294967294
+LAPLEX_TOKEN_MAX_HEADS = 65535
+LAPLEX_TOKEN_MAX_TOKENS = 67108864
+LAPLEX_TOKEN_MAX_SEQUENCES = 1048576
+LAPLEX_ROTARY_MAX_DIM = 4096
+LAPLEX_ATTENTION_MAX_DIM = 256
+LAPLEX_LOGPROB_MAX_TOP = 64
 
 EXPORTS = (
     "laplex_workspace_bytes", "laplex_apply", "laplex_apply_backward", "laplex_gram",
@@ -38,6 +54,10 @@ EXPORTS = (
     "laplex_wgram_workspace_bytes", "laplex_wgram",
     "laplex_mix_workspace_bytes", "laplex_mix_apply", "laplex_mix_apply_backward",
     "laplex_wgram_f64_workspace_bytes", "laplex_wgram_f64",
+    "laplex_rotary", "laplex_rotary_frequencies",
+    "laplex_decay_attention_workspace_bytes", "laplex_decay_attention", "laplex_decay_attention_backward",
+    "laplex_decay_attention_step",
+    "laplex_logprob_workspace_bytes", "laplex_logprob", "laplex_logprob_backward",
 )
 
 # include/laplex_diag.h: hooks for benchmarks and tests
@@ -106,6 +126,17 @@ def lib() -> ctypes.CDLL:
         L.laplex_mix_apply.argtypes = [_P, _P, _P, _I, _I, _I, _P, _I, _I, _P, _I, _P, _Z, _U, _P]
         L.laplex_mix_apply_backward.argtypes = [_P, _P, _P, _I, _I, _I, _P, _I, _P, _I, _I, _P, _I, _P, _P, _P,
                                                 _P, _Z, _U, _P]
+        _C, _D = ctypes.c_int, ctypes.c_double
+        L.laplex_rotary.argtypes = [_P, _I, _P, _I, _C, _I, _I, _I, _I, _P, _P, _F, _U, _P]
+        L.laplex_rotary_frequencies.argtypes = [_P, _I, _D, _C, _D, _D, _D, _D, _P]
+        L.laplex_decay_attention_workspace_bytes.argtypes = [_C, _I, _I, _I, _I, _I, ctypes.POINTER(_Z)]
+        L.laplex_decay_attention.argtypes = [_P, _I, _P, _I, _P, _I, _C, _I, _I, _P, _I, _I, _I, _P, _F, _P, _P, _I, _P, _P, _Z, _P]
+        L.laplex_decay_attention_backward.argtypes = [_P, _I, _P, _I, _P, _I, _C, _I, _I, _P, _I, _I, _I, _P, _F, _P, _P, _I, _P,
+                                                      _P, _I, _P, _I, _P, _I, _P, _P, _Z, _P]
+        L.laplex_decay_attention_step.argtypes = [_P, _I, _P, _I, _P, _I, _C, _I, _I, _I, _I, _P, _F, _P, _P, _I, _P]
+        L.laplex_logprob_workspace_bytes.argtypes = [_I, _I, _I, ctypes.POINTER(_Z)]
+        L.laplex_logprob.argtypes = [_P, _I, _C, _I, _I, _P, _F, _P, _P, _P, _I, _P, _P, _P, _Z, _P]
+        L.laplex_logprob_backward.argtypes = [_P, _I, _C, _I, _I, _P, _F, _P, _P, _P, _P, _P, _P, _I, _P]
         for name in EXPORTS + DIAG_EXPORTS:
             if name not in ("laplex_status_string", "laplex_last_hip_error"):
                 getattr(L, name).restype = ctypes.c_int
@@ -334,3 +365,144 @@ def laplex_wgram_f64(a, b, d, m, ws, flags: int = 0, stream=None) -> None:
     """m (k, k) fp64 <- A diag(d) A^T, fp32 anchors, fp64 weights and arithmetic."""
     _check(lib().laplex_wgram_f64(_ptr(a), a.numel(), _ptr(b), b.numel(), _ptr(d), _ptr(m), _ld(m),
                                   _ptr(ws), ws.numel(), flags, _stream(stream)))
+
+
+# --- operators for token models ----------------------------------------------------------------------------------------
+
+def _type(dtype):
+    """The library's name of a torch type."""
+    import torch
+    if dtype == torch.float32:
+        return LAPLEX_F32
+    if dtype == torch.bfloat16:
+        return LAPLEX_BF16
+    raise LaplexError(LAPLEX_ERR_VALUE)
+
+
+def _same_type(first, *others):
+    for t in others:
+        if t is not None and t.dtype != first.dtype:
+            raise LaplexError(LAPLEX_ERR_VALUE)
+    return _type(first.dtype)
+
+
+def _whole(t, shape, dtype):
+    """An array that the library reads or writes from end to end."""
+    if t is None:
+        return None
+    assert tuple(t.shape) == tuple(shape), f"shape {tuple(t.shape)}, not {tuple(shape)}"
+    assert t.dtype == dtype, f"type {t.dtype}, not {dtype}"
+    assert t.is_contiguous(), "must be contiguous"
+    return t.data_ptr()
+
+
+def _ld_tokens(t, shape):
+    """Row stride of a (tokens, heads, numbers) tensor whose rows are contiguous."""
+    if t is None:
+        return 0
+    assert tuple(t.shape) == tuple(shape), f"shape {tuple(t.shape)}, not {tuple(shape)}"
+    n, h, d = t.shape
+    assert d <= 1 or h == 0 or n == 0 or t.stride(2) == 1, "a head's numbers must be contiguous"
+    assert h <= 1 or d == 0 or n == 0 or t.stride(1) == d, "the heads of a token must be contiguous"
+    return t.stride(0) if n > 1 else max(h * d, 1)
+
+
+def laplex_rotary(x, positions, frequencies, y, magnitude: float = 1.0, flags: int = 0, stream=None) -> None:
+    """y <- x (tokens, heads, numbers) with the first 2 * len(frequencies) numbers of every head turned by the token's position."""
+    import torch
+    n, h, d = x.shape
+    _check(lib().laplex_rotary(_ptr(x), _ld_tokens(x, x.shape), _ptr(y), _ld_tokens(y, x.shape), _same_type(x, y), n, h, d,
+                               2 * frequencies.numel(), _whole(positions, (n,), torch.int64),
+                               _whole(frequencies, (frequencies.numel(),), torch.float32), magnitude, flags, _stream(stream)))
+
+
+def laplex_rotary_frequencies(frequencies, base: float = 10000.0, scaling: int = LAPLEX_ROTARY_PLAIN, factor: float = 1.0,
+                              original_context: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0, stream=None) -> None:
+    """frequencies (rotary_dim / 2,) <- radians per position of each pair."""
+    import torch
+    _check(lib().laplex_rotary_frequencies(_whole(frequencies, (frequencies.numel(),), torch.float32), 2 * frequencies.numel(), base,
+                                           scaling, factor, original_context, low_turns, high_turns, _stream(stream)))
+
+
+def laplex_decay_attention_workspace_bytes(dtype, tokens: int, sequences: int, heads: int, dk: int, dv: int) -> int:
+    out = _Z(0)
+    _check(lib().laplex_decay_attention_workspace_bytes(_type(dtype), tokens, sequences, heads, dk, dv, ctypes.byref(out)))
+    return out.value
+
+
+def _sequences(sequences, starts):
+    import torch
+    if starts is None:
+        return sequences, None
+    return starts.numel() - 1, _whole(starts, (starts.numel(),), torch.int64)
+
+
+def laplex_decay_attention(q, k, v, rates, y, ws, scale: float = 1.0, sequences: int = 1, starts=None, state_in=None, state_out=None,
+                           stream=None) -> None:
+    """y (tokens, heads, dv) <- linear attention of q, k (tokens, heads, dk) and v with the decay exp(-rates[head]) per token.
+    The sequences lie one behind the other, of equal lengths or from row starts[b] to starts[b + 1]; states are
+    (sequences, heads, dk, dv) fp32."""
+    import torch
+    n, h, dk = q.shape
+    dv = v.shape[2]
+    b, at = _sequences(sequences, starts)
+    state = (b, h, dk, dv)
+    _check(lib().laplex_decay_attention(
+        _ptr(q), _ld_tokens(q, (n, h, dk)), _ptr(k), _ld_tokens(k, (n, h, dk)), _ptr(v), _ld_tokens(v, (n, h, dv)), _same_type(q, k, v, y),
+        n, b, at, h, dk, dv, _whole(rates, (h,), torch.float32), scale, _whole(state_in, state, torch.float32),
+        _ptr(y), _ld_tokens(y, (n, h, dv)), _whole(state_out, state, torch.float32), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def laplex_decay_attention_backward(q, k, v, rates, gy, gq, gk, gv, ws, scale: float = 1.0, sequences: int = 1, starts=None,
+                                    state_in=None, gstate_out=None, gstate_in=None, stream=None) -> None:
+    """gq, gk, gv, gstate_in (any may be None) <- gradients of sum(gy * y) + sum(gstate_out * state_out)."""
+    import torch
+    n, h, dk = q.shape
+    dv = v.shape[2]
+    b, at = _sequences(sequences, starts)
+    state = (b, h, dk, dv)
+    _check(lib().laplex_decay_attention_backward(
+        _ptr(q), _ld_tokens(q, (n, h, dk)), _ptr(k), _ld_tokens(k, (n, h, dk)), _ptr(v), _ld_tokens(v, (n, h, dv)),
+        _same_type(q, k, v, gy, gq, gk, gv), n, b, at, h, dk, dv, _whole(rates, (h,), torch.float32), scale,
+        _whole(state_in, state, torch.float32), _ptr(gy), _ld_tokens(gy, (n, h, dv)), _whole(gstate_out, state, torch.float32),
+        _ptr(gq), _ld_tokens(gq, (n, h, dk)), _ptr(gk), _ld_tokens(gk, (n, h, dk)), _ptr(gv), _ld_tokens(gv, (n, h, dv)),
+        _whole(gstate_in, state, torch.float32), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def laplex_decay_attention_step(q, k, v, rates, state, y, scale: float = 1.0, stream=None) -> None:
+    """One token of every sequence: state (sequences, heads, dk, dv) is updated in place, y (sequences, heads, dv) written."""
+    import torch
+    b, h, dk = q.shape
+    dv = v.shape[2]
+    _check(lib().laplex_decay_attention_step(
+        _ptr(q), _ld_tokens(q, (b, h, dk)), _ptr(k), _ld_tokens(k, (b, h, dk)), _ptr(v), _ld_tokens(v, (b, h, dv)), _same_type(q, k, v, y),
+        b, h, dk, dv, _whole(rates, (h,), torch.float32), scale, _whole(state, (b, h, dk, dv), torch.float32),
+        _ptr(y), _ld_tokens(y, (b, h, dv)), _stream(stream)))
+
+
+def laplex_logprob_workspace_bytes(k: int, batch: int, top: int = 0) -> int:
+    out = _Z(0)
+    _check(lib().laplex_logprob_workspace_bytes(k, batch, top, ctypes.byref(out)))
+    return out.value
+
+
+def laplex_logprob(y, targets, logp, lse, entropy, top_ids, top_logp, ws, tau: float = 1.0, stream=None) -> None:
+    """Log probabilities of the targets, log-sum-exp and entropy of tau * y (k, batch) per column, and its largest logits
+    (top_ids, top_logp: (top, batch)); whatever is not wanted is None."""
+    import torch
+    k, t = (y.shape[0], _batch(y))
+    top = 0 if top_ids is None else top_ids.shape[0]
+    f = lambda x: _whole(x, (t,), torch.float32)
+    _check(lib().laplex_logprob(_ptr(y), _ld(y), _type(y.dtype), k, t, _whole(targets, (t,), torch.int64), tau, f(logp), f(lse), f(entropy),
+                                top, _whole(top_ids, (top, t), torch.int64), _whole(top_logp, (top, t), torch.float32),
+                                _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def laplex_logprob_backward(y, targets, lse, entropy, glogp, gentropy, glse, gy, tau: float = 1.0, stream=None) -> None:
+    """gy (k, batch) <- gradient of sum(glogp * logp + gentropy * entropy + glse * lse); gy may be y."""
+    import torch
+    k, t = (y.shape[0], _batch(y))
+    assert tuple(gy.shape) == tuple(y.shape)
+    f = lambda x: _whole(x, (t,), torch.float32)
+    _check(lib().laplex_logprob_backward(_ptr(y), _ld(y), _same_type(y, gy), k, t, _whole(targets, (t,), torch.int64), tau, f(lse), f(entropy),
+                                         f(glogp), f(gentropy), f(glse), _ptr(gy), _ld(gy), _stream(stream)))

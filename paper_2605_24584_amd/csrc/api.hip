@@ -4,6 +4,7 @@
 #include "../../include/laplex.h"
 #include "../../include/laplex_diag.h"
 #include "laplex_internal.h"
+#include "token_internal.h"
 
 #include <atomic>
 #include <cmath>
@@ -60,6 +61,12 @@ int hip_fail(hipError_t e)
     g_hip_error = hipGetErrorString(e);
     return LAPLEX_ERR_HIP;
 }
+
+}  // namespace
+
+int laplex::hip_failed(hipError_t e) { return hip_fail(e); }
+
+namespace {
 
 #define LAPLEX_HIP(expr)                                   \
     do {                                                   \

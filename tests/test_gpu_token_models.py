@@ -1,0 +1,453 @@
+"""Operators for token models against the oracle in 64 bits: rotary positions, attention with a decay for each head,
+log probabilities; sizes and masks where they can go wrong.
+
+Tolerances.  U = 2^-24 is the unit rounding of fp32 (24 bits), H = 2^-8 that of bf16 (8 bits).  An error is compared with the same sum over absolute values:
+ - rotary: a result is two products with a cosine or sine; angle, function, products and sum are at most 8 roundings.
+ - attention: sums over up to n tokens and dk numbers with roundings of either sign, and weights whose exponent (at most 20
+   where they matter) is rounded once: 16 sqrt(n + dk + 64) U.  In bf16 the map of a stretch of tokens is rounded before its second
+   product, and the result once: 2 H.  States are fp32 sums of exact products whatever the type.
+ - log probabilities: logits and sums of magnitude z are off by 4 U |z| each; the sums over k by 16 sqrt(log) U; see there.
+"""
+import numpy as np
+import pytest
+
+from oracle import token_oracle as O
+from paper_2605_24584_amd import binding as B
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U, H = 2.0 ** -24, 2.0 ** -8
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def seeded(*what):
+    import zlib
+    return np.random.default_rng(zlib.crc32(repr(what).encode()))
+
+
+def dev(v, dtype=F32):
+    return torch.from_numpy(np.ascontiguousarray(v)).to("cuda").to(dtype)
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def rounded(r, shape, dtype):
+    """(device tensor, its values in 64 bits)"""
+    t = dev(r.normal(size=shape).astype(np.float32), dtype)
+    return t, host(t)
+
+
+def within(name, got, want, bound):
+    assert got.shape == want.shape, name
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (f"{name}: {int(bad.sum())} of {bad.size} off, first at {tuple(np.argwhere(bad)[0])}: "
+                           f"{got[bad][0]} instead of {want[bad][0]}, may be off by {np.broadcast_to(bound, bad.shape)[bad][0]}")
+
+
+# --- rotary positions ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,dim,turned", [
+    (1, 1, 2, 2), (1, 32, 128, 128), (3, 5, 7, 4), (17, 3, 80, 20), (64, 2, 64, 64), (65, 1, 96, 0), (5, 4, 9, 8), (33, 6, 256, 128),
+    (2, 2, 130, 66), (257, 18, 80, 36), (4, 1, 4096, 4096)])
+def test_rotary(dtype, interleaved, tokens, heads, dim, turned):
+    r = seeded("rotary", tokens, heads, dim, turned)
+    x, hx = rounded(r, (tokens, heads, dim), dtype)
+    positions = r.integers(-1000, 2000000, tokens)
+    freq = (10000.0 ** (-np.arange(turned // 2) * 2.0 / max(turned, 1))).astype(np.float32)
+    for inverse in (False, True):
+        y = torch.full_like(x, float("nan"))
+        flags = (B.LAPLEX_ROTARY_INTERLEAVED if interleaved else 0) | (B.LAPLEX_ROTARY_INVERSE if inverse else 0)
+        B.laplex_rotary(x, dev(positions, torch.int64), dev(freq), y, 1.25, flags)
+        want, size = O.rotary(hx, positions, freq, 1.25, interleaved, inverse)
+        within("y", host(y), want, 8 * U * size + (H * np.abs(want) if dtype == BF16 else 0.0))
+        assert torch.equal(y[..., turned:], x[..., turned:])
+
+
+def test_rotary_in_place_on_a_part_of_a_matrix():
+    """Queries and keys inside a fused matrix, ld beyond their width; what lies beside them stays; the inverse brings them back."""
+    r = seeded("rotary in place")
+    n, heads, dim = 37, 6, 40
+    m, hm = rounded(r, (n, 11 + heads * dim + 5), F32)
+    x = m[:, 11:11 + heads * dim].unflatten(1, (heads, dim))
+    positions = np.arange(n) * 1001
+    freq = (100.0 ** -np.linspace(0, 1, 15)).astype(np.float32)
+    B.laplex_rotary(x, dev(positions, torch.int64), dev(freq), x)
+    want, size = O.rotary(hm[:, 11:11 + heads * dim].reshape(n, heads, dim), positions, freq)
+    within("y", host(x), want, 8 * U * size)
+    assert np.array_equal(host(m)[:, :11], hm[:, :11]) and np.array_equal(host(m)[:, -5:], hm[:, -5:])
+    B.laplex_rotary(x, dev(positions, torch.int64), dev(freq), x, 1.0, B.LAPLEX_ROTARY_INVERSE)
+    within("back", host(m), hm, 32 * U * np.maximum(np.abs(hm), np.abs(hm).max()))
+
+
+@pytest.mark.parametrize("scaling,turned", [(0, 128), (1, 128), (2, 128), (3, 128), (2, 2), (3, 20), (0, 2)])
+def test_rotary_frequencies(scaling, turned):
+    f = torch.full((turned // 2,), float("nan"), device="cuda")
+    B.laplex_rotary_frequencies(f, 10000.0, scaling, 8.0, 4096.0, 1.0, 32.0)
+    want = O.frequencies(turned, 10000.0, scaling, 8.0, 4096.0, 1.0, 32.0)
+    within("f", host(f), want, 2 * U * want)
+
+
+# --- attention with a decay for each head ----------------------------------------------------------------------------------
+
+def attention_bound(size, n, dk, dtype, want=None):
+    b = 16 * np.sqrt(n + dk + 64.0) * U * size
+    return b + 1.05 * H * (np.abs(want) + size) if dtype == BF16 else b
+
+
+def attention_inputs(r, lengths, heads, dk, dv, dtype, states):
+    n, b = int(sum(lengths)), len(lengths)
+    # q, k, v side by side in one matrix, as a projection leaves them
+    m, hm = rounded(r, (n, heads * (2 * dk + dv) + 3), dtype)
+    cut = lambda t, a, d: t[:, a:a + heads * d].reshape(n, heads, d) if isinstance(t, np.ndarray) else t[:, a:a + heads * d].unflatten(1, (heads, d))
+    parts = [(cut(m, a, d), cut(hm, a, d)) for a, d in ((0, dk), (heads * dk, dk), (2 * heads * dk, dv))]
+    rates = np.resize(np.array([0.03, 0.7, 0.0, 0.002, 3.0, 0.25], np.float32), heads)
+    state = rounded(r, (b, heads, dk, dv), F32) if states else (None, None)
+    return parts, rates, state
+
+
+def run_forward(parts, rates, state, lengths, dv, scale, packed, want_state=True):
+    (q, _), (k, _), (v, _) = parts
+    n, heads, dk = q.shape
+    b = len(lengths)
+    y = torch.full((n, heads, dv), float("nan"), device="cuda", dtype=q.dtype)
+    last = torch.full((b, heads, dk, dv), float("nan"), device="cuda") if want_state else None
+    starts = dev(np.concatenate([[0], np.cumsum(lengths)]), torch.int64) if packed else None
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(q.dtype, n, b, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    B.laplex_decay_attention(q, k, v, dev(rates), y, ws, scale, b, starts, state, last)
+    return y, last
+
+
+SHAPES = [
+    # lengths, heads, dk, dv, packed
+    ([1], 1, 1, 1, False), ([1, 1, 1], 2, 16, 16, False), ([5], 3, 7, 9, False), ([16], 1, 32, 32, False), ([17, 0, 1, 64, 65], 2, 20, 33, True),
+    ([63], 2, 64, 64, False), ([64, 64], 2, 64, 64, False), ([130], 1, 128, 128, False), ([200, 3, 0, 0, 129], 3, 96, 80, True),
+    ([300], 1, 256, 256, False), ([70], 2, 256, 40, False), ([95], 1, 40, 256, False), ([0, 0], 2, 8, 8, True), ([1000, 513], 1, 48, 100, True),
+    ([257, 255], 1, 129, 65, True), ([2100], 2, 64, 128, False),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths,heads,dk,dv,packed", SHAPES)
+@pytest.mark.parametrize("states", [False, True])
+def test_attention(dtype, lengths, heads, dk, dv, packed, states):
+    r = seeded("attention", lengths, heads, dk, dv)
+    parts, rates, (state, hstate) = attention_inputs(r, lengths, heads, dk, dv, dtype, states)
+    scale = float(np.float32(dk ** -0.5))
+    y, last = run_forward(parts, rates, state, lengths, dv, scale, packed)
+    at = 0
+    for b, n in enumerate(lengths):
+        for h in range(heads):
+            q, k, v = (p[1][at:at + n, h] for p in parts)
+            wy, ws, sy, ss = O.attention_sequence(q, k, v, rates[h], scale, None if hstate is None else hstate[b, h])
+            within(f"y[{b},{h}]", host(y[at:at + n, h]), wy, attention_bound(sy, n, dk, dtype, wy))
+            within(f"state[{b},{h}]", host(last[b, h]), ws, attention_bound(ss, n, dk, F32))
+        at += n
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths,heads,dk,dv,packed", SHAPES)
+@pytest.mark.parametrize("states", [False, True])
+def test_attention_backward(dtype, lengths, heads, dk, dv, packed, states):
+    r = seeded("attention backward", lengths, heads, dk, dv)
+    parts, rates, (state, hstate) = attention_inputs(r, lengths, heads, dk, dv, dtype, states)
+    scale = float(np.float32(dk ** -0.5))
+    n, b = sum(lengths), len(lengths)
+    gy, hgy = rounded(r, (n, heads, dv), dtype)
+    gs, hgs = rounded(r, (b, heads, dk, dv), F32) if states else (None, None)
+    new = lambda *s, t=dtype: torch.full(s, float("nan"), device="cuda", dtype=t)
+    gq, gk, gv, g0 = new(n, heads, dk), new(n, heads, dk), new(n, heads, dv), new(b, heads, dk, dv, t=F32)
+    starts = dev(np.concatenate([[0], np.cumsum(lengths)]), torch.int64) if packed else None
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(dtype, n, b, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    (q, _), (k, _), (v, _) = parts
+    B.laplex_decay_attention_backward(q, k, v, dev(rates), gy, gq, gk, gv, ws, scale, b, starts, state, gs, g0)
+    at = 0
+    for i, m in enumerate(lengths):
+        for h in range(heads):
+            hq, hk, hv = (p[1][at:at + m, h] for p in parts)
+            want, size = O.attention_sequence_backward(hq, hk, hv, rates[h], scale, None if hstate is None else hstate[i, h],
+                                                       hgy[at:at + m, h], None if hgs is None else hgs[i, h])
+            for name, got, w, s, d in zip(("gq", "gk", "gv"), (gq, gk, gv), want, size, (dv, dv, dk)):
+                within(f"{name}[{i},{h}]", host(got[at:at + m, h]), w, attention_bound(s, m, d, dtype, w))
+            within(f"g0[{i},{h}]", host(g0[i, h]), want[3], attention_bound(size[3], m, dk, F32))
+        at += m
+    # any gradient can be left out without a change to the others
+    for left in range(4):
+        some = [None if j == left else torch.full_like(t, float("nan")) for j, t in enumerate((gq, gk, gv, g0))]
+        B.laplex_decay_attention_backward(q, k, v, dev(rates), gy, *some[:3], ws, scale, b, starts, state, gs, some[3])
+        for t, full in zip(some, (gq, gk, gv, g0)):
+            assert t is None or torch.equal(t, full)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("sequences,heads,dk,dv", [(1, 1, 1, 1), (1, 16, 128, 128), (3, 2, 20, 33), (5, 1, 256, 256), (70, 8, 64, 64), (2, 3, 96, 80), (9, 2, 129, 130), (600, 1, 32, 40)])
+def test_attention_step(dtype, sequences, heads, dk, dv):
+    r = seeded("step", sequences, heads, dk, dv)
+    parts, rates, (state, hstate) = attention_inputs(r, [1] * sequences, heads, dk, dv, dtype, True)
+    (q, hq), (k, hk), (v, hv) = parts
+    scale = 0.37
+    y = torch.full((sequences, heads, dv), float("nan"), device="cuda", dtype=dtype)
+    B.laplex_decay_attention_step(q, k, v, dev(rates), state, y, scale)
+    for b in range(sequences):
+        for h in range(heads):
+            wy, ws, sy, ss = O.attention_sequence(hq[b:b + 1, h], hk[b:b + 1, h], hv[b:b + 1, h], rates[h], scale, hstate[b, h])
+            within("y", host(y[b:b + 1, h]), wy, 16 * np.sqrt(dk + 1.0) * U * sy + (H * np.abs(wy) if dtype == BF16 else 0.0))
+            within("state", host(state[b, h]), ws, 8 * U * ss)
+
+
+def test_attention_prompt_then_steps_is_the_longer_prompt():
+    """A state handed from a prompt to steps and to a second prompt (in place) ends where one prompt over all tokens ends."""
+    r = seeded("hand over")
+    heads, dk, dv, first, steps, second = 2, 48, 64, 133, 3, 70
+    n = first + steps + second
+    parts, rates, _ = attention_inputs(r, [n], heads, dk, dv, F32, False)
+    y, last = run_forward(parts, rates, None, [n], dv, 0.5, False)
+    state = torch.empty(1, heads, dk, dv, device="cuda")
+    got = torch.empty_like(y)
+    cut = lambda a, b: [p[0][a:b] for p in parts]
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(F32, n, 1, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    B.laplex_decay_attention(*cut(0, first), dev(rates), got[:first], ws, 0.5, state_out=state)
+    for t in range(first, first + steps):
+        B.laplex_decay_attention_step(*cut(t, t + 1), dev(rates), state, got[t:t + 1], 0.5)
+    B.laplex_decay_attention(*cut(first + steps, n), dev(rates), got[first + steps:], ws, 0.5, state_in=state, state_out=state)
+    for h in range(heads):
+        _, _, sy, ss = O.attention_sequence(*(p[1][:, h] for p in parts), rates[h], 0.5)
+        within("y", host(got[:, h]), host(y[:, h]), 2 * attention_bound(sy, n, dk, F32))
+        within("state", host(state[0, h]), host(last[0, h]), 2 * attention_bound(ss, n, dk, F32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_rates_at_their_ends(dtype):
+    """Rate 0: plain causal sums.  Infinite and huge rates: every token sees only itself, and 0 * inf is no NaN."""
+    r = seeded("rates")
+    n, heads, dk, dv = 150, 4, 32, 48
+    parts, _, (state, hstate) = attention_inputs(r, [n], heads, dk, dv, dtype, True)
+    rates = np.array([0.0, np.inf, 1e6, 200.0], np.float32)
+    y, last = run_forward(parts, rates, state, [n], dv, 1.0, False)
+    for h in range(heads):
+        wy, ws, sy, ss = O.attention_sequence(*(p[1][:, h] for p in parts), min(float(rates[h]), 1e30), 1.0, hstate[0, h])
+        within("y", host(y[:, h]), wy, attention_bound(sy, n, dk, dtype, wy))
+        within("state", host(last[0, h]), ws, attention_bound(ss, n, dk, F32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_attention_values_that_are_not_finite_stay_where_they_reach(dtype, what, value):
+    """Rows before the token, other sequences and other columns are the same bits as without it."""
+    r = seeded("odd", what)
+    lengths, heads, dk, dv, at, col = [100, 90, 40], 2, 64, 64, 137, 21      # token 37 of the second sequence
+    parts, rates, _ = attention_inputs(r, lengths, heads, dk, dv, dtype, False)
+    y, last = run_forward(parts, rates, None, lengths, dv, 1.0, True)
+    parts["qkv".index(what)][0][at, 1, col] = value
+    y2, last2 = run_forward(parts, rates, None, lengths, dv, 1.0, True)
+    same = torch.ones(y.shape, dtype=torch.bool)
+    if what == "q":
+        same[at, 1] = False
+        assert not torch.isfinite(y2[at, 1]).any() or dtype == BF16 or not torch.isfinite(y2[at, 1]).all()
+    elif what == "k":
+        same[at:190, 1] = False
+        assert not torch.isfinite(last2[1, 1, col]).any()
+    else:
+        same[at:190, 1, col] = False
+        assert not torch.isfinite(y2[at:190, 1, col]).any() and not torch.isfinite(last2[1, 1, :, col]).any()
+    assert torch.equal(y.cpu()[same], y2.cpu()[same])
+    assert torch.equal(last[[0, 2]], last2[[0, 2]]) and torch.equal(last[1, 0], last2[1, 0])
+
+
+def test_attention_starts_out_of_range_touch_nothing_outside():
+    """Garbage in starts gives wrong values; rows beyond the matrices are neither read nor written."""
+    r = seeded("starts")
+    heads, dk, dv, n = 1, 32, 32, 100
+    parts, rates, _ = attention_inputs(r, [n], heads, dk, dv, F32, False)
+    guard = torch.full((n + 200, heads, dv), 7.0, device="cuda")
+    y = guard[100:100 + n]
+    starts = dev(np.array([-50, 40, 30, 10 ** 12, -10 ** 15, 60]), torch.int64)
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(F32, n, 5, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    B.laplex_decay_attention(*(p[0] for p in parts), dev(rates), y, ws, 1.0, starts=starts)
+    assert (guard[:100] == 7.0).all() and (guard[100 + n:] == 7.0).all()
+
+
+# --- log probabilities ---------------------------------------------------------------------------------------------------
+
+def logprob_bounds(f, y, tau):
+    """Roundings of numbers as large as the largest logits and sums in play, 16 of them at most, and 64 U for the sums."""
+    z = np.where(np.isfinite(y), np.abs(tau * y), 0.0).max(axis=0, initial=0.0)
+    lse = np.where(np.isfinite(f["lse"]), np.abs(f["lse"]), 0.0)
+    return U * (16 * (z + lse) + 64)
+
+
+def run_logprob(y, targets, tau, top, ws_fill=None):
+    k, t = y.shape
+    new = lambda *s, d=F32: torch.full(s, -77, device="cuda", dtype=d)
+    out = dict(logp=new(t), lse=new(t), entropy=new(t), top_ids=new(top, t, d=torch.int64), top_logp=new(top, t))
+    ws = torch.empty(B.laplex_logprob_workspace_bytes(k, t, top), dtype=torch.uint8, device="cuda")
+    B.laplex_logprob(y, targets, out["logp"], out["lse"], out["entropy"], out["top_ids"] if top else None, out["top_logp"] if top else None, ws, tau)
+    return out
+
+
+def check_logprob(y, hy, targets, tau, top):
+    out = run_logprob(y, dev(targets, torch.int64), tau, top)
+    want = O.logprob(hy, targets, tau, top)
+    bound = logprob_bounds(want, hy, tau)
+    for name in ("logp", "lse", "entropy", "top_logp"):
+        got, w = host(out[name]), want[name]
+        odd = ~np.isfinite(w)
+        assert np.array_equal(got[odd], w[odd], equal_nan=True), name
+        within(name, got[~odd], w[~odd], np.broadcast_to(bound, w.shape)[~odd])
+    assert np.array_equal(out["top_ids"].cpu().numpy(), want["top_ids"])
+    return out
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,batch,top", [
+    (1, 1, 1), (2, 3, 2), (10, 1, 5), (17, 5, 0), (100, 64, 8), (333, 65, 20), (1000, 256, 5), (1000, 31, 64), (4096, 2, 33), (5001, 7, 1),
+    (32000, 1, 8), (32000, 4, 20), (20011, 12, 64), (16, 300, 16), (15, 130, 15), (131072, 1, 20), (140001, 2, 3), (64, 64, 64)])
+def test_logprob(dtype, k, batch, top):
+    r = seeded("logprob", k, batch)
+    y, hy = rounded(r, (k, batch), dtype)
+    y = y * 3; hy = host(y)
+    targets = r.integers(0, k, batch); targets[::5] = r.choice([-1, -100, k, 2 ** 40], len(targets[::5]))
+    check_logprob(y, hy, targets, 1.0, top)
+    check_logprob(y, hy, targets, 0.7, top)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,batch,ld", [(500, 12, 16), (500, 12, 17), (1000, 1, 5), (300, 64, 68), (700, 8, 8)])
+def test_logprob_leading_dimensions_and_offsets(dtype, k, batch, ld):
+    r = seeded("ld", k, batch, ld)
+    for offset in (0, 1, 4):
+        m, _ = rounded(r, (k * ld + offset,), dtype)
+        y = m[offset:].view(k, ld)[:, :batch]
+        targets = r.integers(0, k, batch)
+        check_logprob(y, host(y), targets, 1.0, 7)
+
+
+def odd_columns(r, k, dtype):
+    """Columns with masks and values where sums can go wrong."""
+    low = float(torch.finfo(dtype).min)
+    c = [np.full(k, -np.inf), np.full(k, low), np.full(k, 0.0), r.normal(size=k)]
+    one = np.full(k, -np.inf); one[k // 2] = 3.0; c.append(one)
+    some = r.normal(size=k); some[r.random(k) < 0.7] = -np.inf; c.append(some)
+    late = np.full(k, -np.inf); late[-1] = -5.0; c.append(late)
+    c.append(np.where(r.random(k) < 0.5, low, r.normal(size=k)))
+    c.append(r.normal(size=k) * 1e4)
+    zero = np.zeros(k); zero[::2] = -0.0; c.append(zero)
+    big = r.normal(size=k); big[k // 3] = 2e30; c.append(big)
+    for v in (np.nan, np.inf):
+        w = r.normal(size=k); w[(2 * k) // 3] = v; c.append(w)
+    two = r.normal(size=k); two[5] = np.inf; two[9] = np.nan; two[11] = np.nan; c.append(two)
+    return np.stack(c, axis=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k", [13, 64, 1000, 9000])
+def test_logprob_masks_ties_and_values_that_are_not_finite(dtype, k):
+    r = seeded("odd columns", k)
+    y = dev(odd_columns(r, k, dtype).astype(np.float32), dtype)
+    hy = host(y)
+    t = y.shape[1]
+    for targets in (np.zeros(t, np.int64), np.full(t, k // 2), np.full(t, k - 1)):
+        check_logprob(y, hy, targets, 1.0, 12)
+    ties = dev(r.integers(0, 3, (k, 20)).astype(np.float32), dtype)      # many equal values: the lowest rows come first
+    check_logprob(ties, host(ties), r.integers(0, k, 20), 1.0, 13)
+
+
+def check_logprob_backward(y, hy, targets, tau, in_place=False):
+    k, t = hy.shape
+    r = seeded("weights", k, t)
+    glogp, gent, glse = (r.normal(size=t).astype(np.float32) for _ in range(3))
+    out = run_logprob(y, dev(targets, torch.int64), tau, 0)
+    gy = y if in_place else torch.full_like(y, float("nan"))
+    B.laplex_logprob_backward(y, dev(targets, torch.int64), out["lse"], out["entropy"], dev(glogp), dev(gent), dev(glse), gy, tau)
+    want = O.logprob_backward(hy, targets, glogp, gent, glse, tau)
+    f = O.logprob(hy, targets, tau)
+    rel = logprob_bounds(f, hy, tau)
+    with np.errstate(all="ignore"):
+        logp = tau * hy - f["lse"]
+        p = np.where(np.isfinite(logp), np.exp(logp), 0.0)
+        size = tau * (np.abs(glogp) * p + np.abs(gent) * p * (np.abs(np.where(p > 0, logp, 0.0)) + np.abs(f["entropy"]) + 1.0) + np.abs(glse) * p)
+        for c in range(t):
+            if 0 <= targets[c] < k and np.isfinite(f["lse"][c]):
+                size[targets[c], c] += tau * abs(glogp[c])
+    odd = np.isnan(want)
+    got = host(gy)
+    assert np.array_equal(np.isnan(got), odd)
+    within("gy", got[~odd], want[~odd], (2 * np.broadcast_to(rel, want.shape) * size + (H * np.abs(want) if y.dtype == BF16 else 0.0) + 1e-37)[~odd])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,batch", [(1, 1), (2, 3), (10, 1), (100, 64), (333, 65), (1000, 256), (5001, 7), (32000, 4)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_logprob_backward(dtype, k, batch, in_place):
+    r = seeded("logprob backward", k, batch)
+    y = rounded(r, (k, batch), dtype)[0] * 3
+    targets = r.integers(0, k, batch); targets[::5] = r.choice([-1, k, -2 ** 40], len(targets[::5]))
+    check_logprob_backward(y, host(y), targets, 1.3, in_place)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logprob_backward_masks_and_values_that_are_not_finite(dtype):
+    r = seeded("odd columns backward")
+    y = dev(odd_columns(r, 500, dtype).astype(np.float32), dtype)
+    t = y.shape[1]
+    for targets in (np.zeros(t, np.int64), np.full(t, 250), np.full(t, -1)):
+        check_logprob_backward(y, host(y), targets, 1.0)
+
+
+def test_logprob_empty_vocabulary():
+    y = torch.empty(0, 3, device="cuda")
+    out = run_logprob(y, dev(np.zeros(3), torch.int64), 1.0, 0)
+    assert (out["lse"] == -float("inf")).all() and (out["entropy"] == 0).all() and (out["logp"] == 0).all()
+
+
+# --- streams and graphs ----------------------------------------------------------------------------------------------------
+
+def test_calls_run_on_the_stream_they_are_given_and_in_graphs():
+    """Everything once eagerly, then captured and replayed with other work between the replays: the same bits."""
+    r = seeded("graph")
+    heads, dk, dv, n, k = 2, 64, 64, 700, 3000
+    parts, rates, (state, _) = attention_inputs(r, [n], heads, dk, dv, BF16, True)
+    (q, _), (kk, _), (v, _) = parts
+    drates, freq = dev(rates), dev((10000.0 ** -np.linspace(0, 1, dk // 2)).astype(np.float32))
+    positions = dev(np.arange(n), torch.int64)
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(BF16, n, 1, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    logits = rounded(r, (k, 40), F32)[0]
+    targets = dev(r.integers(0, k, 40), torch.int64)
+    lws = torch.empty(B.laplex_logprob_workspace_bytes(k, 40, 5), dtype=torch.uint8, device="cuda")
+    new = lambda *s, d=F32: torch.empty(s, device="cuda", dtype=d)
+    turned, y, last = torch.empty(n, heads, dk, device="cuda", dtype=BF16), new(n, heads, dv, d=BF16), new(1, heads, dk, dv)
+    gq, gk, gv, g0 = new(n, heads, dk, d=BF16), new(n, heads, dk, d=BF16), new(n, heads, dv, d=BF16), new(1, heads, dk, dv)
+    step_state, step_y = new(1, heads, dk, dv), new(1, heads, dv, d=BF16)
+    logp, lse, ent, ids, top, gl = new(40), new(40), new(40), new(5, 40, d=torch.int64), new(5, 40), torch.empty_like(logits)
+    outs = (turned, y, last, gq, gk, gv, g0, step_state, step_y, logp, lse, ent, ids, top, gl)
+
+    def work():
+        B.laplex_rotary(q, positions, freq, turned)
+        B.laplex_decay_attention(turned, kk, v, drates, y, ws, 0.125, state_in=state, state_out=last)
+        B.laplex_decay_attention_backward(turned, kk, v, drates, y, gq, gk, gv, ws, 0.125, state_in=state, gstate_out=last, gstate_in=g0)
+        step_state.copy_(last)
+        B.laplex_decay_attention_step(q[:1], kk[:1], v[:1], drates, step_state, step_y, 0.125)
+        B.laplex_logprob(logits, targets, logp, lse, ent, ids, top, lws)
+        B.laplex_logprob_backward(logits, targets, lse, ent, logp, ent, lse, gl)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        work()
+    side.synchronize()
+    want = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for _ in range(3):
+        for t in outs:
+            t.zero_()
+        noise = torch.randn(1000, 1000, device="cuda") @ torch.randn(1000, 1000, device="cuda")
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)) and torch.isfinite(noise).all()
