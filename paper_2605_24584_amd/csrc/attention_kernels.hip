@@ -1,5 +1,13 @@
 // Linear attention with a decay for each head: the causal Laplace kernel exp(-rate (t - s)), s <= t, over token positions,
-// weighted by (q_t . k_s).
+// weighted by (q_t . k_s):  y_t = sum_{s <= t} l^(t-s) (q_t . k_s) v_s + l^(t+1) q_t S0,  l = exp(-rate).
+//
+// A walk (token_internal.h) is computed in chunks of C tokens with the state S (dk x dv) carried from chunk to chunk:
+//   inside a chunk   P_ij = l^(i-j) (q_i . k_j), j <= i;     out_i = l^(i+lead) q_i S + sum_j P_ij v_j
+//   and its end      S <- l^C S + sum_j l^(C-j-lead) k_j v_j^T
+// All four products run on the matrix cores.  A workgroup of four wavefronts walks one head of one stretch of a sequence; a
+// wavefront owns 16 NT columns of the result and of the state, which stays in its accumulator registers from the first chunk to
+// the last: as it leaves an accumulator a pair of tiles IS a fragment of the product q S (over the state's rows in a
+// permuted order, which the rows of q in LDS share), so the state never passes through memory.
 #include "token_internal.h"
 
 namespace laplex {
@@ -7,72 +15,585 @@ namespace laplex {
 namespace {
 
 constexpr int kStepThreads = 256;
+constexpr int kWalkThreads = 256;
 
 __device__ __forceinline__ float rate_of(const float* rates, int h)
 {
     return fminf(rates[h], 1.0e30f);      // an infinite rate: nothing but the token itself, and 0 * rate stays 0
 }
 
-__device__ __forceinline__ void sequence_rows(const int64_t* starts, int64_t tokens, int64_t sequences, int64_t b, int64_t* begin, int64_t* count)
+__device__ __forceinline__ int64_t start_of(const int64_t* starts, int64_t tokens, int64_t sequences, int64_t b)
 {
-    if (!starts) { *count = tokens / sequences; *begin = b * *count; return; }
-    int64_t lo = starts[b], hi = starts[b + 1];                       // whatever they hold, no row outside the matrices is touched
-    lo = lo < 0 ? 0 : lo > tokens ? tokens : lo;
-    hi = hi < lo ? lo : hi > tokens ? tokens : hi;
-    *begin = lo; *count = hi - lo;
+    if (!starts) return sequences > 0 ? tokens / sequences * b : 0;
+    const int64_t v = starts[b];                       // whatever it holds, no row outside the matrices is touched
+    return v < 0 ? 0 : v > tokens ? tokens : v;
 }
 
-// The recurrence S <- l S + k v^T token by token: 16 columns of one head of one sequence, 16 lanes of a wavefront share a
-// column, each with every 16th row of it.
-template <typename T>
-__global__ void __launch_bounds__(256)
-k_attention_recurrent(AttentionArgs A)
+// ----------------------------------------------------------------------------
+// Fragments: 16 bytes of a row, K numbers of the contraction per step of the matrix cores (16 x 16 results; lane l holds
+// row or column l % 16 and the numbers of group l / 16; of a result, column l % 16 and rows 4 (l / 16) .. + 3).
+// ----------------------------------------------------------------------------
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Num;
+template <> struct Num<float> {
+    typedef f32x4 frag;
+    typedef f32x4 quad;                  // four numbers
+    static constexpr int E = 4, K = 16;
+};
+template <> struct Num<__bf16> {
+    typedef bf16x8 frag;
+    typedef bf16x4 quad;
+    static constexpr int E = 8, K = 32;
+};
+
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c)
 {
-    const Walk W = A.walk[blockIdx.z];
-    const int slices = (W.dv + 15) / 16;
-    const int64_t b = blockIdx.x / slices;
-    const int slice = blockIdx.x % slices, h = blockIdx.y;
-    if (b >= A.sequences) return;
-    const int part = threadIdx.x & 15, col = slice * 16 + (threadIdx.x >> 4);
-    const float rate = rate_of(A.rates, h), decay = expf(-rate);
-    int64_t begin, count;
-    sequence_rows(A.starts, A.tokens, A.sequences, b, &begin, &count);
-    const bool live = col < W.dv;
-    float S[16];
-    const int64_t at = (b * A.heads + h) * (int64_t)W.dk * W.dv;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int row = i * 16 + part;
-        S[i] = 0.0f;
-        if (W.state_in && live && row < W.dk)
-            S[i] = W.in_scale * W.state_in[at + (W.transposed ? (int64_t)col * W.dk + row : (int64_t)row * W.dv + col)];
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// A tile in LDS: rows of SLOTS times 16 bytes.  The slots of a row are permuted by its number, so that eight lanes that read
+// the same slot of eight rows, or write a column's pieces of eight rows, meet eight different groups of banks.
+template <int SLOTS>
+__device__ __forceinline__ int twist(int row)
+{
+    return SLOTS >= 8 ? (row ^ (row >> 3)) & 7 : ((row >> 1) ^ (row >> 3)) & 3;
+}
+template <int SLOTS>
+__device__ __forceinline__ int slot_at(int row, int slot) { return row * SLOTS + (slot ^ twist<SLOTS>(row)); }
+
+// Keeps the compiler from forming everything that follows from v outside the loop over chunks, where it would fill the registers.
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// A lane's part of the place of slot 4 m + g of row 16 t + r16: the rest of the permutation depends on t and m alone.
+template <int SLOTS>
+struct Reader {
+    static constexpr int kMask = SLOTS >= 8 ? 7 : 3;
+    int base, low;
+    __device__ __forceinline__ Reader(int r16, int g) : base(r16 * SLOTS * 16), low((g ^ twist<SLOTS>(r16)) * 16) {}
+    __device__ __forceinline__ int at(int t, int m) const
+    {
+        const int fixed = (4 * m ^ 2 * t) & kMask;
+        return base + (low ^ (fixed * 16)) + ((4 * m) & ~kMask) * 16 + t * 16 * SLOTS * 16;
     }
-    for (int64_t u = 0; u < count; ++u) {
-        const int64_t t = begin + (W.reverse ? count - 1 - u : u);
-        const T* q = static_cast<const T*>(W.q) + t * W.ldq + (int64_t)h * W.dk;
-        const T* k = static_cast<const T*>(W.k) + t * W.ldk + (int64_t)h * W.dk;
-        const float v = live ? to_float(static_cast<const T*>(W.v)[t * W.ldv + (int64_t)h * W.dv + col]) : 0.0f;
-        const float d = (u == 0 && W.lead == 0) ? 1.0f : decay;
-        float o = 0.0f;
+};
+
+// four rows of E numbers each
+template <typename T> struct Patch { typename Num<T>::frag r[4]; };
+
+// rows first .. first + 3 of `valid` (p: the first of them), numbers at .. at + E - 1 of `width`; zeros beyond.  wide: all rows allow
+// 16-byte accesses.
+template <typename T>
+__device__ __forceinline__ void load_patch(Patch<T>& out, const T* p, int64_t stride, int first, int valid, int at, int width, bool wide)
+{
+    constexpr int E = Num<T>::E;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int row = i * 16 + part;
-            if (row < W.dk) {
-                S[i] = S[i] * d + to_float(k[row]) * v;
-                o += S[i] * to_float(q[row]);
+    for (int i = 0; i < 4; ++i) {
+        typename Num<T>::frag v = {};
+        const bool there = first + i < valid;
+        if (wide) {
+            if (there && at < width) v = *reinterpret_cast<const typename Num<T>::frag*>(p);
+        } else if (there) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (at + e < width) v[e] = p[e];
+        }
+        out.r[i] = v;
+        p += stride;
+    }
+}
+
+// Rows as they are, numbers along the slots (first: a multiple of 4).  In bf16 the quads of 32 numbers lie in the order 0 4 1 5 2 6 3 7: group g of a
+// fragment then holds numbers 4 g .. + 3 and 16 + 4 g .. + 3, which are the rows of a pair of accumulator tiles that the group holds.
+template <int SLOTS>
+__device__ __forceinline__ void put_rows(char* tile, const Patch<__bf16>& p, int first, int piece)
+{
+    const int low = here(((piece >> 2) * 4 + 2 * (piece & 1)) ^ twist<SLOTS>(first));
+    char* const at = tile + first * SLOTS * 16 + 8 * ((piece >> 1) & 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const bf16x4 v = {p.r[i][4 * half], p.r[i][4 * half + 1], p.r[i][4 * half + 2], p.r[i][4 * half + 3]};
+            *reinterpret_cast<bf16x4*>(at + i * SLOTS * 16 + 16 * (low ^ i ^ half)) = v;
+        }
+}
+template <int SLOTS>
+__device__ __forceinline__ void put_rows(char* tile, const Patch<float>& p, int first, int piece)
+{
+    const int low = here(piece ^ twist<SLOTS>(first));
+    char* const at = tile + first * SLOTS * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(at + i * SLOTS * 16 + 16 * (low ^ i)) = p.r[i];
+}
+
+// The patch's columns as rows, tokens along the slots.
+template <int SLOTS>
+__device__ __forceinline__ void put_columns(char* tile, const Patch<__bf16>& p, int first, int piece)
+{
+    const int low = here((first >> 3) ^ twist<SLOTS>(piece * 8));
+    char* const at = tile + piece * 8 * SLOTS * 16 + 8 * ((first >> 2) & 1);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bf16x4 v = {p.r[0][e], p.r[1][e], p.r[2][e], p.r[3][e]};
+        *reinterpret_cast<bf16x4*>(at + e * SLOTS * 16 + 16 * (low ^ (SLOTS >= 8 ? e : (e >> 1)))) = v;
+    }
+}
+template <int SLOTS>
+__device__ __forceinline__ void put_columns(char* tile, const Patch<float>& p, int first, int piece)
+{
+    const int low = here((first >> 2) ^ twist<SLOTS>(piece * 4));
+    char* const at = tile + piece * 4 * SLOTS * 16;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const f32x4 v = {p.r[0][e], p.r[1][e], p.r[2][e], p.r[3][e]};
+        *reinterpret_cast<f32x4*>(at + e * SLOTS * 16 + 16 * (low ^ (SLOTS >= 8 ? e : (e >> 1)))) = v;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ typename Num<T>::frag get(const char* tile, int place)
+{
+    return *reinterpret_cast<const typename Num<T>::frag*>(tile + place);
+}
+
+// x = hi + mid + lo: bf16 holds 8 bits, so three of them all 24 of an fp32 number
+__device__ __forceinline__ void split3(const float* x, bf16x8& hi, bf16x8& mid, bf16x8& lo)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        hi[e] = (__bf16)x[e];
+        const float r = x[e] - (float)hi[e];
+        mid[e] = (__bf16)r;
+        lo[e] = (__bf16)(r - (float)mid[e]);
+    }
+}
+
+__device__ __forceinline__ bool finite_bits(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
+template <typename T>
+__device__ __forceinline__ bool finite_patch(const Patch<T>& p)
+{
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < Num<T>::E; ++e) fine = fine && finite_bits((float)p.r[i][e]);
+    return fine;
+}
+
+// ----------------------------------------------------------------------------
+// Which stretch of which sequence: sequences are cut into stretches of `stretch` tokens (a multiple of every C).  Sequence b has the slots
+// from start / stretch + b on: at least one, and as many as it has stretches; a slot beyond those has nothing to do.
+// ----------------------------------------------------------------------------
+struct Stretch {
+    int64_t b;                        // sequence
+    int64_t begin, count;             // its rows
+    int64_t lo, hi;                   // tokens of the stretch, in the order of the walk
+    bool there, last;
+    int64_t index;
+};
+
+__device__ __forceinline__ Stretch find_stretch(const AttentionArgs& A, int64_t slot)
+{
+    Stretch s;
+    // the last sequence whose first slot is at most this one: 64 candidates at a time
+    int64_t lo = 0, hi = A.sequences;                  // in [lo, hi)
+    const int lane = threadIdx.x & 63;
+    if (A.starts) {
+        while (hi - lo > 1) {
+            const int64_t step = (hi - lo + 63) / 64;
+            const int64_t c = lo + lane * step;
+            const bool mine = c < hi && start_of(A.starts, A.tokens, A.sequences, c) / A.stretch + c <= slot;
+            const uint64_t votes = __ballot(mine);
+            const int at = votes ? 63 - __builtin_clzll(votes) : 0;
+            lo += at * step;
+            hi = lo + step < hi ? lo + step : hi;
+        }
+    } else {
+        const int64_t n = A.tokens / A.sequences;
+        // first slot of b: b n / stretch + b, between b (n + stretch) / stretch - 1 and that
+        lo = slot * A.stretch / (n + A.stretch);
+        while (lo + 1 < A.sequences && (lo + 1) * n / A.stretch + lo + 1 <= slot) ++lo;
+    }
+    s.b = lo;
+    s.begin = start_of(A.starts, A.tokens, A.sequences, lo);
+    const int64_t end = start_of(A.starts, A.tokens, A.sequences, lo + 1);
+    s.count = end > s.begin ? end - s.begin : 0;
+    s.index = slot - (s.begin / A.stretch + lo);
+    s.lo = s.index * A.stretch;
+    s.there = s.index >= 0 && (s.lo < s.count || s.index == 0);
+    s.hi = s.lo + A.stretch < s.count ? s.lo + A.stretch : s.count;
+    s.last = s.hi == s.count;
+    return s;
+}
+
+__device__ __forceinline__ float state_value(const Walk& W, int64_t at, int row, int col)
+{
+    return W.in_scale * W.state_in[at + (W.transposed ? (int64_t)col * W.dk + row : (int64_t)row * W.dv + col)];
+}
+
+// Sizes of a walk's kernel: DK the padded rows of the state, NT tiles of 16 columns for each of four wavefronts.
+template <typename T, int DK, int NT>
+struct Geometry {
+    static constexpr int E = Num<T>::E, K = Num<T>::K;
+    static constexpr int C = (DK > 128 ? 32 : 64) * 2 / (int)sizeof(T);      // tokens of a chunk
+    static constexpr int COLS = 64 * NT;                                     // columns of a workgroup
+    static constexpr int ROW = DK * (int)sizeof(T) / 16, SEQ = C * (int)sizeof(T) / 16;   // slots of a row of numbers, of tokens
+    static constexpr int CT = C / 16, DT = DK / 16, KD = DK / K, KC = C / K;
+    static constexpr int kBytesRows = C * ROW * 16, kBytesK = DK * SEQ * 16, kBytesV = COLS * SEQ * 16, kBytesP = C * SEQ * 16;
+    static constexpr int kLds = 2 * kBytesRows + kBytesK + kBytesV + kBytesP;
+};
+
+// STATES: only what a stretch adds to the state, for the stretches behind it (U below).
+template <typename T, int DK, int NT, bool STATES>
+__global__ void __launch_bounds__(kWalkThreads, 2)
+k_attention_walk(AttentionArgs A)
+{
+    typedef Geometry<T, DK, NT> G;
+    typedef typename Num<T>::frag frag;
+    constexpr int E = G::E, C = G::C, ROW = G::ROW, SEQ = G::SEQ, CT = G::CT, DT = G::DT, KD = G::KD, KC = G::KC;
+    __shared__ __attribute__((aligned(16))) char lds[STATES ? G::kBytesK + G::kBytesV : G::kLds];
+    __shared__ float power[C + 1], weight[C];          // l^d, and the weights of the chunk's tokens in the state
+    __shared__ int odd[2];
+    char* const Kt = lds;                              // [DK][C]
+    char* const Vt = Kt + G::kBytesK;                  // [COLS][C]
+    char* const Qs = Vt + G::kBytesV;                  // [C][DK], as Ks
+    char* const Ks = Qs + G::kBytesRows;
+    char* const Ps = Ks + G::kBytesRows;               // [C][C]
+
+    const Walk W = A.walk[blockIdx.z];
+    const int slice = blockIdx.x % A.slices;
+    const int64_t slot = blockIdx.x / A.slices;
+    const int h = blockIdx.y, col0 = slice * G::COLS;
+    if (col0 >= W.dv) return;
+    const Stretch s = find_stretch(A, slot);
+    if (!s.there || (STATES && s.last)) return;
+
+    const int x = threadIdx.x, lane = x & 63, wave = x >> 6, r16 = lane & 15, g = lane >> 4;
+    const double rate = (double)rate_of(A.rates, h);
+    for (int d = x; d <= C; d += kWalkThreads) power[d] = (float)exp(-rate * d);
+    if (!STATES)
+        for (int i = x; i < G::kBytesP / 16; i += kWalkThreads) reinterpret_cast<f32x4*>(Ps)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (x < 2) odd[x] = 0;
+    // a chunk's decay in two floats: rounded to one it would be off the same way in every chunk
+    const double full_decay = exp(-rate * C);
+    float decay_hi = (float)full_decay, decay_lo = (float)(full_decay - (double)decay_hi);
+
+    const int64_t back = W.reverse ? -1 : 1;
+    const int64_t first_row = s.begin + (W.reverse ? s.count - 1 - s.lo : s.lo);
+    const int64_t sq = back * W.ldq, sk = back * W.ldk, sv = back * W.ldv;
+    const bool wq = A.wide[blockIdx.z] & 1, wk = A.wide[blockIdx.z] & 2, wv = A.wide[blockIdx.z] & 4, wo = A.wide[blockIdx.z] & 8;
+
+    // the state: rows 16 t + 4 g .. + 3, column col0 + (wave NT + c) 16 + r16
+    f32x4 S[DT][NT];
+    const int64_t state_at = (s.b * A.heads + h) * (int64_t)W.dk * W.dv;
+    f32x4* const U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * (DK * G::COLS / 4);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (!STATES) {
+                if (s.index > 0) v4 = U[((wave * DT + t) * NT + c) * 64 + lane];
+                else if (W.state_in) {
+                    const int col = col0 + (wave * NT + c) * 16 + r16;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (col < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col);
+                }
+            }
+            S[t][c] = v4;
+        }
+
+    // patches of a chunk: four rows by 16 bytes
+    constexpr int kRowPatches = (C / 4) * (DK / E), kColPatches = (C / 4) * (G::COLS / E);
+    constexpr int NR = (kRowPatches + kWalkThreads - 1) / kWalkThreads, NV = (kColPatches + kWalkThreads - 1) / kWalkThreads;
+    Patch<T> pq[NR], pk[NR], pv[NV];
+    const T *tq[NR], *tk[NR], *tv[NV];                 // a thread's first row of the chunk that is loaded next
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const int p = x + i * kWalkThreads, row = (p / (DK / E)) * 4, at = (p % (DK / E)) * E;
+        tq[i] = static_cast<const T*>(W.q) + (first_row + back * row) * W.ldq + (int64_t)h * W.dk + at;
+        tk[i] = static_cast<const T*>(W.k) + (first_row + back * row) * W.ldk + (int64_t)h * W.dk + at;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int p = x + i * kWalkThreads, row = (p / (G::COLS / E)) * 4, at = col0 + (p % (G::COLS / E)) * E;
+        tv[i] = static_cast<const T*>(W.v) + (first_row + back * row) * W.ldv + (int64_t)h * W.dv + at;
+    }
+    auto load = [&](int64_t u) {
+        const int valid = (int)(s.hi - u < C ? s.hi - u : C);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int p = x + i * kWalkThreads;
+            if (kRowPatches % kWalkThreads == 0 || p < kRowPatches) {
+                const int at = (p % (DK / E)) * E, row = (p / (DK / E)) * 4;
+                if (!STATES) load_patch(pq[i], tq[i], sq, row, valid, at, W.dk, wq);
+                load_patch(pk[i], tk[i], sk, row, valid, at, W.dk, wk);
+                tq[i] += C * sq; tk[i] += C * sk;
             }
         }
 #pragma unroll
-        for (int m = 8; m >= 1; m >>= 1) o += __shfl_xor(o, m);
-        if (W.out && live && part == 0) static_cast<T*>(W.out)[t * W.ldo + (int64_t)h * W.dv + col] = (T)(o * W.out_scale);
-    }
-    if (W.state_out && live) {
-        const float d = (W.lead == 0 && count > 0) ? decay : 1.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int row = i * 16 + part;
-            if (row < W.dk) W.state_out[at + (int64_t)row * W.dv + col] = W.last_scale * (S[i] * d);
+        for (int i = 0; i < NV; ++i) {
+            const int p = x + i * kWalkThreads;
+            if (kColPatches % kWalkThreads == 0 || p < kColPatches) {
+                load_patch(pv[i], tv[i], sv, (p / (G::COLS / E)) * 4, valid, col0 + (p % (G::COLS / E)) * E, W.dv, wv);
+                tv[i] += C * sv;
+            }
         }
+    };
+    if (s.lo < s.hi) load(s.lo);
+    __syncthreads();                                   // the powers are there
+    float ahead[CT];                                   // weights of the state in the rows
+    if (!STATES)
+#pragma unroll
+        for (int t = 0; t < CT; ++t) ahead[t] = power[16 * t + r16 + W.lead];
+
+    Reader<ROW> rows(r16, g);
+    Reader<SEQ> columns(r16, g);
+    Reader<SEQ> values(r16, g);                        // columns of this wavefront: tiles wave NT + c
+    values.base += wave * NT * 16 * SEQ * 16;
+    values.low ^= ((2 * wave * NT) & Reader<SEQ>::kMask) * 16;
+    T* out = static_cast<T*>(W.out) + (first_row + back * r16) * W.ldo + (int64_t)h * W.dv;
+    const int64_t out_step = back * 16 * W.ldo;
+
+    int turn = 0;
+    for (int64_t u = s.lo; u < s.hi; u += C, turn ^= 1) {
+        const int valid = (int)(s.hi - u < C ? s.hi - u : C);
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int p = x + i * kWalkThreads;
+            if (kRowPatches % kWalkThreads == 0 || p < kRowPatches) {
+                const int piece = p % (DK / E), row = (p / (DK / E)) * 4;
+                if (!STATES) { put_rows<ROW>(Qs, pq[i], row, piece); put_rows<ROW>(Ks, pk[i], row, piece); }
+                put_columns<SEQ>(Kt, pk[i], row, piece);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int p = x + i * kWalkThreads;
+            if (kColPatches % kWalkThreads == 0 || p < kColPatches) {
+                put_columns<SEQ>(Vt, pv[i], (p / (G::COLS / E)) * 4, p % (G::COLS / E));
+                if (!STATES) fine = fine && finite_patch(pv[i]);
+            }
+        }
+        if (!STATES && !fine) odd[turn] = 1;
+        if (u == s.lo || valid < C) {
+            if (x < C) weight[x] = power[x < valid ? valid - x - W.lead : 0];
+            const double d = exp(-rate * valid);
+            decay_hi = (float)d; decay_lo = (float)(d - (double)decay_hi);
+        }
+        if (u + C < s.hi) load(u + C);
+        __syncthreads();
+
+        rows.low = here(rows.low); columns.low = here(columns.low); values.low = here(values.low);
+        f32x4 O[CT][NT];
+        if (!STATES) {
+            // P: tiles on and below the diagonal, dealt to the wavefronts; as it leaves the accumulator a lane holds P[i][j .. j + 3]
+#pragma unroll
+            for (int n = 0; n < (CT * (CT + 1) / 2 + 3) / 4; ++n) {
+                const int tile = n * 4 + wave;
+                int it = 0, jt = tile;
+                while (jt > it) { jt -= it + 1; ++it; }
+                if (it < CT) {
+                    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int m = 0; m < KD; ++m) acc = mma(get<T>(Ks, rows.at(jt, m)), get<T>(Qs, rows.at(it, m)), acc);
+                    typename Num<T>::quad w;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int d = 16 * (it - jt) + r16 - 4 * g - r;
+                        w[r] = (T)(d >= 0 ? acc[r] * power[d < 0 ? 0 : d] : 0.0f);
+                    }
+                    const int j = 16 * jt + 4 * g;
+                    *reinterpret_cast<typename Num<T>::quad*>(Ps + 16 * slot_at<SEQ>(16 * it + r16, j / E) + (j % E) * (int)sizeof(T)) = w;
+                }
+            }
+            // q S, weighted by the rows
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int c = 0; c < NT; ++c) O[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int m = 0; m < KD; ++m) {
+                __builtin_amdgcn_sched_barrier(0);     // (all steps' fragments at once do not fit the registers)
+#pragma unroll
+                for (int c = 0; c < NT; ++c) {
+                    if constexpr (sizeof(T) == 2) {
+                        bf16x8 sf;                     // rounded for this product alone, as P is for its own: the result is rounded as much again
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sf[e] = (__bf16)S[2 * m + (e >> 2)][c][e & 3];
+#pragma unroll
+                        for (int t = 0; t < CT; ++t) O[t][c] = mma(sf, get<T>(Qs, rows.at(t, m)), O[t][c]);
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < CT; ++t) O[t][c] = mma(S[m][c], get<T>(Qs, rows.at(t, m)), O[t][c]);
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int c = 0; c < NT; ++c) O[t][c] *= ahead[t];
+        }
+        // the state at the chunk's end
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[t][c][r] = fmaf(S[t][c][r], decay_hi, S[t][c][r] * decay_lo);
+#pragma unroll
+        for (int m = 0; m < KC; ++m) {
+            __builtin_amdgcn_sched_barrier(0);
+            float w[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) w[e] = weight[(4 * m + g) * E + e];
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                const frag vf = get<T>(Vt, values.at(c, m));
+                float xs[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) xs[e] = w[e] * (float)vf[e];
+                if constexpr (sizeof(T) == 2) {
+                    bf16x8 hi, mid, lo;
+                    split3(xs, hi, mid, lo);
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        const frag kf = get<T>(Kt, columns.at(t, m));
+                        S[t][c] = mma(kf, hi, S[t][c]);
+                        S[t][c] = mma(kf, mid, S[t][c]);
+                        S[t][c] = mma(kf, lo, S[t][c]);
+                    }
+                } else {
+                    const f32x4 b = {xs[0], xs[1], xs[2], xs[3]};
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) S[t][c] = mma(get<T>(Kt, columns.at(t, m)), b, S[t][c]);
+                }
+            }
+        }
+        if (!STATES) {
+            __syncthreads();                           // P is there
+            const bool slow = odd[turn] != 0;          // a value of v is not finite: 0 * v of the tokens behind a row must not reach it
+            if (x == 0) odd[turn ^ 1] = 0;
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int m = 0; m < KC; ++m) {
+                    frag vf = get<T>(Vt, values.at(c, m));
+                    if (slow)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
+#pragma unroll
+                    for (int t = 0; t < CT; ++t)
+                        if (16 * t + 15 >= m * G::K) O[t][c] = mma(vf, get<T>(Ps, columns.at(t, m)), O[t][c]);
+                }
+            if (slow)
+                for (int j = 0; j < C; ++j)
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int n = (wave * NT + c) * 16 + 4 * g + r;
+                            const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n, j / E) + (j % E) * (int)sizeof(T));
+                            if (finite_bits(vj)) continue;
+#pragma unroll
+                            for (int t = 0; t < CT; ++t)
+                                if (16 * t + r16 >= j)
+                                    O[t][c][r] += vj * (float)*reinterpret_cast<const T*>(Ps + 16 * slot_at<SEQ>(16 * t + r16, j / E) + (j % E) * (int)sizeof(T));
+                        }
+            if (W.out) {
+#pragma unroll
+                for (int t = 0; t < CT; ++t) {
+                    const int i = 16 * t + r16;
+                    if (i < valid) {
+                        T* row = out + t * out_step;
+#pragma unroll
+                        for (int c = 0; c < NT; ++c) {
+                            const int n = col0 + (wave * NT + c) * 16 + 4 * g;
+                            typename Num<T>::quad w;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
+                            if (wo) {
+                                if (n < W.dv) *reinterpret_cast<typename Num<T>::quad*>(row + n) = w;
+                            } else {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (n + r < W.dv) row[n + r] = w[r];
+                            }
+                        }
+                    }
+                }
+            }
+        }
+        out += CT * out_step;
+        __syncthreads();                               // the tiles may be written again
+    }
+
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            if (STATES) U[((wave * DT + t) * NT + c) * 64 + lane] = S[t][c];
+            else if (W.state_out && s.last) {
+                const int col = col0 + (wave * NT + c) * 16 + r16;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * t + 4 * g + r;
+                    if (col < W.dv && row < W.dk) W.state_out[state_at + (int64_t)row * W.dv + col] = W.last_scale * S[t][c][r];
+                }
+            }
+        }
+}
+
+// What enters every stretch but the first: carry_n = l^stretch carry_(n-1) + U_(n-1), carry_0 = the initial state, in the places of the U.
+// A thread per four rows of a column of the state.
+template <int DK, int COLS>
+__global__ void __launch_bounds__(256)
+k_attention_carry(AttentionArgs A)
+{
+    constexpr int kPieces = DK * COLS / 4, kBlocks = kPieces / 256;
+    const Walk W = A.walk[blockIdx.z];
+    const int64_t b = blockIdx.x / (A.slices * kBlocks);
+    const int rest = (int)(blockIdx.x % (A.slices * kBlocks)), slice = rest / kBlocks, piece = (rest % kBlocks) * 256 + threadIdx.x;
+    const int h = blockIdx.y, col0 = slice * COLS;
+    if (col0 >= W.dv) return;
+    constexpr int DT = DK / 16, NT = COLS / 64;
+    const int lane = piece & 63, c = (piece >> 6) % NT, t = (piece / (64 * NT)) % DT, wave = piece / (64 * NT * DT);
+    const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
+    const int64_t count = end > begin ? end - begin : 0, stretches = (count + A.stretch - 1) / A.stretch;
+    const int64_t slot = begin / A.stretch + b;
+    if (stretches < 2 || slot + stretches > A.slots) return;
+    const double d = exp(-(double)rate_of(A.rates, h) * (double)A.stretch);
+    const float hi = (float)d, lo = (float)(d - (double)hi);
+    f32x4 carry = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (W.state_in) {
+        const int col = col0 + (wave * NT + c) * 16 + (lane & 15);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * t + 4 * (lane >> 4) + r;
+            if (col < W.dv && row < W.dk) carry[r] = state_value(W, (b * A.heads + h) * (int64_t)W.dk * W.dv, row, col);
+        }
+    }
+    const int64_t step = (int64_t)A.heads * A.slices * kPieces;
+    f32x4* U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * kPieces + piece;
+    f32x4 next = U[0];
+    for (int64_t n = 1; n < stretches; ++n) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) carry[r] = fmaf(carry[r], hi, fmaf(carry[r], lo, next[r]));
+        if (n + 1 < stretches) next = U[n * step];
+        U[n * step] = carry;
     }
 }
 
@@ -100,20 +621,81 @@ k_attention_step(AttentionStepArgs A)
     }
 }
 
+struct Plan {
+    int dk, cols, slices;              // padded rows of the state, columns of a workgroup, workgroups side by side
+    int64_t stretch, slots;
+    bool cut;                          // some sequence may have more than one stretch
+};
+
+// By the sizes alone, so that the workspace query and both calls agree (walks: those of the backward call).
+Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv)
+{
+    Plan P;
+    const int most = dk > dv ? dk : dv;
+    P.dk = most <= 64 ? 64 : most <= 128 ? 128 : 256;
+    P.cols = P.dk == 128 ? 128 : 64;
+    P.slices = (most + P.cols - 1) / P.cols;
+    const int64_t workgroups = sequences * heads * P.slices;
+    P.stretch = 512;
+    if (workgroups >= 512) P.stretch = tokens > 512 ? (tokens + 511) / 512 * 512 : 512;
+    P.cut = tokens > P.stretch;
+    P.slots = tokens / P.stretch + sequences;
+    return P;
+}
+
+bool allows(const void* p, int64_t ld, int d, int size, int bytes)
+{
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0 && d * size % bytes == 0;
+}
+
+template <typename T, int DK, int NT>
+hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
+{
+    const dim3 grid((unsigned)(P.slots * P.slices), (unsigned)A.heads, (unsigned)A.walks);
+    if (P.cut) {
+        profile_before("attention_states", st);
+        hipLaunchKernelGGL((k_attention_walk<T, DK, NT, true>), grid, dim3(kWalkThreads), 0, st, A);
+        profile_after("attention_states", st);
+        profile_before("attention_carry", st);
+        hipLaunchKernelGGL((k_attention_carry<DK, 64 * NT>), dim3((unsigned)(A.sequences * P.slices * (DK * 64 * NT / 1024)), (unsigned)A.heads, (unsigned)A.walks),
+                           dim3(256), 0, st, A);
+        profile_after("attention_carry", st);
+    }
+    profile_before("attention_walk", st);
+    hipLaunchKernelGGL((k_attention_walk<T, DK, NT, false>), grid, dim3(kWalkThreads), 0, st, A);
+    profile_after("attention_walk", st);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t walk_of(const AttentionArgs& A, const Plan& P, hipStream_t st)
+{
+    if (P.dk == 64) return walk_with<T, 64, 1>(A, P, st);
+    if (P.dk == 128) return walk_with<T, 128, 2>(A, P, st);
+    return walk_with<T, 256, 1>(A, P, st);
+}
+
 }  // namespace
 
-size_t attention_workspace(bool, int64_t, int64_t, int, int, int) { return 0; }
-
-hipError_t launch_attention(const AttentionArgs& A, hipStream_t st)
+size_t attention_workspace(bool, int64_t tokens, int64_t sequences, int heads, int dk, int dv)
 {
-    int most = 0;
-    for (int w = 0; w < A.walks; ++w) most = A.walk[w].dv > most ? A.walk[w].dv : most;
-    const dim3 grid((unsigned)(A.sequences * ((most + 15) / 16)), (unsigned)A.heads, (unsigned)A.walks);
-    profile_before("attention", st);
-    if (A.bf16) hipLaunchKernelGGL((k_attention_recurrent<__bf16>), grid, dim3(256), 0, st, A);
-    else hipLaunchKernelGGL((k_attention_recurrent<float>), grid, dim3(256), 0, st, A);
-    profile_after("attention", st);
-    return hipGetLastError();
+    const Plan P = plan_of(tokens, sequences, heads, dk, dv);
+    if (!P.cut || sequences == 0) return 0;
+    return (size_t)3 * P.slots * heads * P.slices * P.dk * P.cols * sizeof(float);
+}
+
+hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
+{
+    AttentionArgs A = given;
+    const Plan P = plan_of(A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv);
+    A.stretch = P.stretch; A.slots = P.slots; A.slices = P.slices;
+    const int size = A.bf16 ? 2 : 4;
+    for (int w = 0; w < A.walks; ++w) {
+        const Walk& W = A.walk[w];
+        A.wide[w] = (allows(W.q, W.ldq, W.dk, size, 16) ? 1 : 0) | (allows(W.k, W.ldk, W.dk, size, 16) ? 2 : 0) |
+                    (allows(W.v, W.ldv, W.dv, size, 16) ? 4 : 0) | (allows(W.out, W.ldo, W.dv, size, 4 * size) ? 8 : 0);
+    }
+    return A.bf16 ? walk_of<__bf16>(A, P, st) : walk_of<float>(A, P, st);
 }
 
 hipError_t launch_attention_step(const AttentionStepArgs& A, hipStream_t st)
