@@ -1,4 +1,5 @@
-// Rotary positions: pairs of a head's numbers are turned by position * frequency.
+// Rotary positions: pairs of a head's numbers are turned by position * frequency.  Memory bound: a read and a write per number.
+// A workgroup takes a few tokens, forms their cosines and sines once, in LDS, for all heads, and then streams the heads.
 #include "token_internal.h"
 
 namespace laplex {
@@ -6,6 +7,7 @@ namespace laplex {
 namespace {
 
 constexpr int kRotaryThreads = 256;
+constexpr int64_t kRotaryMaxBlocks = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
 
 // cos and sin of position * frequency.  The product passes what fp32 holds (position 10^6 at one radian per position leaves
 // 0.06 radians): it is formed and brought below a turn in fp64, and only the rest is rounded.
@@ -19,31 +21,100 @@ __device__ __forceinline__ void turn_of(int64_t position, float frequency, float
     *s = (inverse ? -sn : sn) * magnitude;
 }
 
-// one thread per (token, pair or number that passes through): all heads
-template <typename T>
-__global__ void __launch_bounds__(kRotaryThreads)
-k_rotary(RotaryArgs A)
+// n / d for n < 2^31 by a product (d >= 1)
+struct Divisor {
+    uint32_t d, factor, shift;
+    Divisor() = default;
+    explicit Divisor(uint32_t by) : d(by), factor(0), shift(0)
+    {
+        while (shift < 31 && (uint64_t(1) << shift) < by) ++shift;
+        factor = (uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - by)) / by + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, factor) + n) >> shift; }
+};
+
+struct RotaryTiles {
+    RotaryArgs A;
+    int tile;                        // tokens of a workgroup
+    int pairs, rest;                 // units of a head: those that turn, those that pass through
+    Divisor token, head;             // by the units of a token, of a head
+};
+
+template <typename T, int VEC> struct Vec { typedef T type __attribute__((ext_vector_type(VEC))); };
+template <typename T> struct Vec<T, 1> { typedef T type; };
+
+template <typename T, int VEC>
+__device__ __forceinline__ void load_vec(float* out, const T* p)
 {
-    const int units = A.half + (A.dim - 2 * A.half);
-    const int64_t total = A.tokens * units;
-    for (int64_t i = (int64_t)blockIdx.x * kRotaryThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kRotaryThreads) {
-        const int64_t token = i / units;
-        const int unit = (int)(i - token * units);
-        const T* x = static_cast<const T*>(A.x) + token * A.ldx;
-        T* y = static_cast<T*>(A.y) + token * A.ldy;
-        if (unit < A.half) {
-            const int first = A.interleaved ? 2 * unit : unit, second = A.interleaved ? first + 1 : unit + A.half;
+    const typename Vec<T, VEC>::type v = *reinterpret_cast<const typename Vec<T, VEC>::type*>(p);
+    if constexpr (VEC == 1) out[0] = to_float(v);
+    else
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) out[i] = to_float((T)v[i]);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_vec(T* p, const float* in)
+{
+    typename Vec<T, VEC>::type v;
+    if constexpr (VEC == 1) v = (T)in[0];
+    else
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = (T)in[i];
+    *reinterpret_cast<typename Vec<T, VEC>::type*>(p) = v;
+}
+
+// A unit of the first half of a head is VEC pairs: VEC numbers from either half, or (INTERLEAVED) VEC pairs side by side, in two
+// pieces of VEC numbers.
+template <typename T, int VEC, bool INTERLEAVED>
+__global__ void __launch_bounds__(kRotaryThreads)
+k_rotary(RotaryTiles R)
+{
+    extern __shared__ float2 table[];                  // [tile][half]
+    const RotaryArgs& A = R.A;
+    const uint32_t per_head = R.pairs + R.rest, per_token = per_head * A.heads;
+    for (int64_t token0 = (int64_t)blockIdx.x * R.tile; token0 < A.tokens; token0 += (int64_t)gridDim.x * R.tile) {
+        const int tokens = A.tokens - token0 < R.tile ? (int)(A.tokens - token0) : R.tile;
+        for (int i = threadIdx.x; i < tokens * A.half; i += kRotaryThreads) {
+            const int t = i / A.half;
             float c, s;
-            turn_of(A.positions[token], A.frequencies[unit], A.magnitude, A.inverse, &c, &s);
-            for (int h = 0; h < A.heads; ++h) {
-                const float u = to_float(x[h * A.dim + first]), v = to_float(x[h * A.dim + second]);
-                y[h * A.dim + first] = (T)(u * c - v * s);
-                y[h * A.dim + second] = (T)(v * c + u * s);
-            }
-        } else {
-            const int at = unit + A.half;
-            for (int h = 0; h < A.heads; ++h) y[h * A.dim + at] = x[h * A.dim + at];
+            turn_of(A.positions[token0 + t], A.frequencies[i - t * A.half], A.magnitude, A.inverse, &c, &s);
+            table[i] = float2{c, s};
         }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < per_token * tokens; i += kRotaryThreads) {
+            const uint32_t t = R.token.of(i), in_token = i - t * per_token, h = R.head.of(in_token), unit = in_token - h * per_head;
+            const T* x = static_cast<const T*>(A.x) + (token0 + t) * A.ldx + h * A.dim;
+            T* y = static_cast<T*>(A.y) + (token0 + t) * A.ldy + h * A.dim;
+            if (unit < (uint32_t)R.pairs) {
+                const float2* turns = table + t * A.half + unit * VEC;
+                const int first = INTERLEAVED ? 2 * unit * VEC : unit * VEC, second = INTERLEAVED ? first + VEC : first + A.half;
+                float u[VEC], v[VEC];
+                load_vec<T, VEC>(u, x + first);
+                load_vec<T, VEC>(v, x + second);
+                float nu[VEC], nv[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float2 w = turns[j];
+                    // the j-th pair of the unit: numbers j of both pieces, or numbers 2 j and 2 j + 1 of the two pieces as one
+                    const float p = INTERLEAVED ? (2 * j < VEC ? u[(2 * j) % VEC] : v[(2 * j) % VEC]) : u[j];
+                    const float q = INTERLEAVED ? (2 * j + 1 < VEC ? u[(2 * j + 1) % VEC] : v[(2 * j + 1) % VEC]) : v[j];
+                    const float a = p * w.x - q * w.y, b = q * w.x + p * w.y;
+                    if (INTERLEAVED) {
+                        (2 * j < VEC ? nu : nv)[(2 * j) % VEC] = a;
+                        (2 * j + 1 < VEC ? nu : nv)[(2 * j + 1) % VEC] = b;
+                    } else {
+                        nu[j] = a;
+                        nv[j] = b;
+                    }
+                }
+                store_vec<T, VEC>(y + first, nu);
+                store_vec<T, VEC>(y + second, nv);
+            } else {
+                const int at = 2 * A.half + (unit - R.pairs) * VEC;
+                *reinterpret_cast<typename Vec<T, VEC>::type*>(y + at) = *reinterpret_cast<const typename Vec<T, VEC>::type*>(x + at);
+            }
+        }
+        __syncthreads();                               // the table may be written again
     }
 }
 
@@ -68,14 +139,60 @@ __global__ void k_rotary_frequencies(float* out, int64_t pairs, double base, int
 
 }  // namespace
 
+namespace {
+
+template <typename T, int VEC>
+void rotary_with(const RotaryTiles& R, dim3 grid, size_t lds, hipStream_t st)
+{
+    if (R.A.interleaved) hipLaunchKernelGGL((k_rotary<T, VEC, true>), grid, dim3(kRotaryThreads), lds, st, R);
+    else hipLaunchKernelGGL((k_rotary<T, VEC, false>), grid, dim3(kRotaryThreads), lds, st, R);
+}
+
+template <typename T>
+void rotary_of(const RotaryTiles& R, int vec, dim3 grid, size_t lds, hipStream_t st)
+{
+    if (vec * sizeof(T) == 16) rotary_with<T, 16 / sizeof(T)>(R, grid, lds, st);
+    else if (vec * sizeof(T) == 8) rotary_with<T, 8 / sizeof(T)>(R, grid, lds, st);
+    else rotary_with<T, 1>(R, grid, lds, st);
+}
+
+}  // namespace
+
 hipError_t launch_rotary(const RotaryArgs& A, hipStream_t st)
 {
-    const int64_t total = A.tokens * (A.dim - A.half);
-    int64_t blocks = (total + kRotaryThreads - 1) / kRotaryThreads;
-    if (blocks > (1 << 20)) blocks = 1 << 20;
+    // in place the numbers that pass through are there
+    const bool copies = A.x != A.y || A.ldx != A.ldy;
+    if (A.half == 0 && !copies) return hipSuccess;
+    const int size = A.bf16 ? 2 : 4, rest = A.dim - 2 * A.half;
+    // the widest pieces that every row, head and part of a head is a whole number of
+    int vec = 16 / size;
+    const auto fits = [&](int v) {
+        const int64_t bytes = (int64_t)v * size;
+        return reinterpret_cast<uintptr_t>(A.x) % bytes == 0 && reinterpret_cast<uintptr_t>(A.y) % bytes == 0 && A.ldx * size % bytes == 0 &&
+               A.ldy * size % bytes == 0 && A.dim % v == 0 && A.half % v == 0;
+    };
+    if (!fits(vec)) vec /= 2;
+    if (!fits(vec)) vec = 1;
+    RotaryTiles R{};
+    R.A = A;
+    R.pairs = A.half / vec;
+    R.rest = copies ? rest / vec : 0;
+    const int64_t units = (int64_t)(R.pairs + R.rest) * A.heads;
+    R.head = Divisor((uint32_t)(R.pairs + R.rest));
+    R.token = Divisor((uint32_t)units);
+    // about four units a thread, as long as there are tokens for two thousand workgroups; the table at most 16 KB
+    int64_t tile = (4 * kRotaryThreads + units - 1) / units;
+    if (tile > A.tokens / 2048) tile = A.tokens / 2048;
+    if (A.half && tile > 2048 / A.half) tile = 2048 / A.half;
+    if (tile > 1024) tile = 1024;
+    if (tile < 1) tile = 1;
+    R.tile = (int)tile;
+    const int64_t tiles = (A.tokens + tile - 1) / tile;
+    const dim3 grid((unsigned)(tiles < kRotaryMaxBlocks ? tiles : kRotaryMaxBlocks));
+    const size_t lds = (size_t)tile * A.half * sizeof(float2);
     profile_before("rotary", st);
-    if (A.bf16) hipLaunchKernelGGL((k_rotary<__bf16>), dim3((unsigned)blocks), dim3(kRotaryThreads), 0, st, A);
-    else hipLaunchKernelGGL((k_rotary<float>), dim3((unsigned)blocks), dim3(kRotaryThreads), 0, st, A);
+    if (A.bf16) rotary_of<__bf16>(R, vec, grid, lds, st);
+    else rotary_of<float>(R, vec, grid, lds, st);
     profile_after("rotary", st);
     return hipGetLastError();
 }
