@@ -383,7 +383,7 @@ enum { /* laplex_rotary_frequencies */
 };
 
 #define LAPLEX_TOKEN_MAX_HEADS 65535LL
-#define LAPLEX_TOKEN_MAX_TOKENS 67108864LL  /* tokens (rows, and the columns of logits) of a call */
+#define LAPLEX_TOKEN_MAX_TOKENS 33554432LL  /* tokens (rows, and the columns of logits) of a call */
 #define LAPLEX_TOKEN_MAX_SEQUENCES 1048576LL
 #define LAPLEX_ROTARY_MAX_DIM 4096LL        /* numbers of a head */
 #define LAPLEX_ATTENTION_MAX_DIM 256LL      /* numbers of a head in q and k, and in v */

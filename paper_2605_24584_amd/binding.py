@@ -39,7 +39,7 @@ LAPLEX_ROTARY_PARTS = 3
 
 LAPLEX_MAX_MERGED = 4294967294
 LAPLEX_TOKEN_MAX_HEADS = 65535
-LAPLEX_TOKEN_MAX_TOKENS = 67108864
+LAPLEX_TOKEN_MAX_TOKENS = 33554432
 LAPLEX_TOKEN_MAX_SEQUENCES = 1048576
 LAPLEX_ROTARY_MAX_DIM = 4096
 LAPLEX_ATTENTION_MAX_DIM = 256

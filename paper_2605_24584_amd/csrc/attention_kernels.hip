@@ -565,59 +565,98 @@ k_attention_carry(AttentionArgs A)
 {
     constexpr int kPieces = DK * COLS / 4, kBlocks = kPieces / 256;
     const Walk W = A.walk[blockIdx.z];
-    const int64_t b = blockIdx.x / (A.slices * kBlocks);
-    const int rest = (int)(blockIdx.x % (A.slices * kBlocks)), slice = rest / kBlocks, piece = (rest % kBlocks) * 256 + threadIdx.x;
-    const int h = blockIdx.y, col0 = slice * COLS;
-    if (col0 >= W.dv) return;
-    constexpr int DT = DK / 16, NT = COLS / 64;
-    const int lane = piece & 63, c = (piece >> 6) % NT, t = (piece / (64 * NT)) % DT, wave = piece / (64 * NT * DT);
-    const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
-    const int64_t count = end > begin ? end - begin : 0, stretches = (count + A.stretch - 1) / A.stretch;
-    const int64_t slot = begin / A.stretch + b;
-    if (stretches < 2 || slot + stretches > A.slots) return;
-    const double d = exp(-(double)rate_of(A.rates, h) * (double)A.stretch);
-    const float hi = (float)d, lo = (float)(d - (double)hi);
-    f32x4 carry = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (W.state_in) {
-        const int col = col0 + (wave * NT + c) * 16 + (lane & 15);
+    for (int64_t block = blockIdx.x; block < A.sequences * A.slices * kBlocks; block += gridDim.x) {
+        const int64_t b = block / (A.slices * kBlocks);
+        const int rest = (int)(block % (A.slices * kBlocks)), slice = rest / kBlocks, piece = (rest % kBlocks) * 256 + threadIdx.x;
+        const int h = blockIdx.y, col0 = slice * COLS;
+        if (col0 >= W.dv) continue;
+        constexpr int DT = DK / 16, NT = COLS / 64;
+        const int lane = piece & 63, c = (piece >> 6) % NT, t = (piece / (64 * NT)) % DT, wave = piece / (64 * NT * DT);
+        const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
+        const int64_t count = end > begin ? end - begin : 0, stretches = (count + A.stretch - 1) / A.stretch;
+        const int64_t slot = begin / A.stretch + b;
+        if (stretches < 2 || slot + stretches > A.slots) continue;
+        const double d = exp(-(double)rate_of(A.rates, h) * (double)A.stretch);
+        const float hi = (float)d, lo = (float)(d - (double)hi);
+        f32x4 carry = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (W.state_in) {
+            const int col = col0 + (wave * NT + c) * 16 + (lane & 15);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = 16 * t + 4 * (lane >> 4) + r;
-            if (col < W.dv && row < W.dk) carry[r] = state_value(W, (b * A.heads + h) * (int64_t)W.dk * W.dv, row, col);
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * t + 4 * (lane >> 4) + r;
+                if (col < W.dv && row < W.dk) carry[r] = state_value(W, (b * A.heads + h) * (int64_t)W.dk * W.dv, row, col);
+            }
         }
-    }
-    const int64_t step = (int64_t)A.heads * A.slices * kPieces;
-    f32x4* U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * kPieces + piece;
-    f32x4 next = U[0];
-    for (int64_t n = 1; n < stretches; ++n) {
+        const int64_t step = (int64_t)A.heads * A.slices * kPieces;
+        f32x4* U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * kPieces + piece;
+        f32x4 next = U[0];
+        for (int64_t n = 1; n < stretches; ++n) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) carry[r] = fmaf(carry[r], hi, fmaf(carry[r], lo, next[r]));
-        if (n + 1 < stretches) next = U[n * step];
-        U[n * step] = carry;
+            for (int r = 0; r < 4; ++r) carry[r] = fmaf(carry[r], hi, fmaf(carry[r], lo, next[r]));
+            if (n + 1 < stretches) next = U[n * step];
+            U[n * step] = carry;
+        }
     }
 }
 
-// One token for every sequence: a workgroup per (sequence, head), a thread per column and part of the rows.
-template <typename T>
+// One token for every sequence: the state is read and written once, everything else is a few hundred numbers.  A workgroup takes `lanes` times VEC columns of one
+// state, a lane VEC of them, the rest of the lanes its rows.
+template <typename T, int VEC>
 __global__ void __launch_bounds__(kStepThreads)
-k_attention_step(AttentionStepArgs A)
+k_attention_step(AttentionStepArgs A, int lanes_log2, int slices)
 {
-    const int64_t b = blockIdx.x;
-    const int h = blockIdx.y;
-    const float decay = expf(-rate_of(A.rates, h));
-    const T* q = static_cast<const T*>(A.q) + b * A.ldq + (int64_t)h * A.dk;
-    const T* k = static_cast<const T*>(A.k) + b * A.ldk + (int64_t)h * A.dk;
-    const T* v = static_cast<const T*>(A.v) + b * A.ldv + (int64_t)h * A.dv;
-    float* S = A.state + (b * A.heads + h) * (int64_t)A.dk * A.dv;
-    for (int col = threadIdx.x; col < A.dv; col += kStepThreads) {
-        const float vc = to_float(v[col]);
-        float o = 0.0f;
-        for (int row = 0; row < A.dk; ++row) {
-            const float s = S[(int64_t)row * A.dv + col] * decay + to_float(k[row]) * vc;
-            S[(int64_t)row * A.dv + col] = s;
-            o += to_float(q[row]) * s;
+    constexpr int kAhead = 4;                          // rows that a thread has asked for at a time
+    __shared__ float qs[256], ks[256], side[kStepThreads / 64][64][VEC];
+    const int x = threadIdx.x, lanes = 1 << lanes_log2, rows = kStepThreads >> lanes_log2;
+    const int64_t b = blockIdx.x / slices;
+    const int slice = blockIdx.x % slices, h = blockIdx.y, col = (slice * lanes + (x & (lanes - 1))) * VEC;
+    // the decay in two floats: rounded to one it would be off the same way at every token
+    const double exact = exp(-(double)rate_of(A.rates, h));
+    const float hi = (float)exact, lo = (float)(exact - (double)hi);
+    if (x < A.dk) {
+        qs[x] = to_float(static_cast<const T*>(A.q)[b * A.ldq + (int64_t)h * A.dk + x]);
+        ks[x] = to_float(static_cast<const T*>(A.k)[b * A.ldk + (int64_t)h * A.dk + x]);
+    }
+    const bool live = col < A.dv;
+    float v[VEC], o[VEC];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+        v[c] = live ? to_float(static_cast<const T*>(A.v)[b * A.ldv + (int64_t)h * A.dv + col + c]) : 0.0f;
+        o[c] = 0.0f;
+    }
+    __syncthreads();
+    typedef float vec __attribute__((ext_vector_type(VEC)));
+    float* const S = A.state + (b * A.heads + h) * (int64_t)A.dk * A.dv + col;
+    if (live)
+        for (int r0 = x >> lanes_log2; r0 < A.dk; r0 += kAhead * rows) {
+            vec s[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (r0 + i * rows < A.dk) s[i] = *reinterpret_cast<const vec*>(S + (int64_t)(r0 + i * rows) * A.dv);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int r = r0 + i * rows;
+                if (r < A.dk) {
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) {
+                        s[i][c] = fmaf(s[i][c], hi, fmaf(s[i][c], lo, ks[r] * v[c]));
+                        o[c] = fmaf(qs[r], s[i][c], o[c]);
+                    }
+                    *reinterpret_cast<vec*>(S + (int64_t)r * A.dv) = s[i];
+                }
+            }
         }
-        static_cast<T*>(A.y)[b * A.ldy + (int64_t)h * A.dv + col] = (T)(A.scale * o);
+    for (int step = lanes; step < 64; step <<= 1)
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) o[c] += __shfl_xor(o[c], step);
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) side[x >> 6][x & 63][c] = o[c];
+    __syncthreads();
+    if (x < lanes && live) {
+        T* const y = static_cast<T*>(A.y) + b * A.ldy + (int64_t)h * A.dv + col;
+#pragma unroll
+        for (int c = 0; c < VEC; ++c)
+            y[c] = (T)(A.scale * ((side[0][x][c] + side[1][x][c]) + (side[2][x][c] + side[3][x][c])));
     }
 }
 
@@ -657,7 +696,8 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
         hipLaunchKernelGGL((k_attention_walk<T, DK, NT, true>), grid, dim3(kWalkThreads), 0, st, A);
         profile_after("attention_states", st);
         profile_before("attention_carry", st);
-        hipLaunchKernelGGL((k_attention_carry<DK, 64 * NT>), dim3((unsigned)(A.sequences * P.slices * (DK * 64 * NT / 1024)), (unsigned)A.heads, (unsigned)A.walks),
+        const int64_t blocks = A.sequences * P.slices * (DK * 64 * NT / 1024), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+        hipLaunchKernelGGL((k_attention_carry<DK, 64 * NT>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.walks),
                            dim3(256), 0, st, A);
         profile_after("attention_carry", st);
     }
@@ -700,10 +740,22 @@ hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
 
 hipError_t launch_attention_step(const AttentionStepArgs& A, hipStream_t st)
 {
-    const dim3 grid((unsigned)A.sequences, (unsigned)A.heads);
+    const int vec = A.dv % 4 == 0 && reinterpret_cast<uintptr_t>(A.state) % 16 == 0 ? 4 : 1;
+    const int wide = (A.dv + vec - 1) / vec;
+    // few states: narrower slices of them, so that more compute units take part
+    const int most = A.sequences * A.heads >= 1024 ? 6 : 3;
+    int lanes_log2 = 0;
+    while (lanes_log2 < most && (1 << lanes_log2) < wide) ++lanes_log2;
+    const int slices = (wide + (1 << lanes_log2) - 1) >> lanes_log2;
+    const dim3 grid((unsigned)(A.sequences * slices), (unsigned)A.heads), block(kStepThreads);
     profile_before("attention_step", st);
-    if (A.bf16) hipLaunchKernelGGL((k_attention_step<__bf16>), grid, dim3(kStepThreads), 0, st, A);
-    else hipLaunchKernelGGL((k_attention_step<float>), grid, dim3(kStepThreads), 0, st, A);
+    if (A.bf16) {
+        if (vec == 4) hipLaunchKernelGGL((k_attention_step<__bf16, 4>), grid, block, 0, st, A, lanes_log2, slices);
+        else hipLaunchKernelGGL((k_attention_step<__bf16, 1>), grid, block, 0, st, A, lanes_log2, slices);
+    } else {
+        if (vec == 4) hipLaunchKernelGGL((k_attention_step<float, 4>), grid, block, 0, st, A, lanes_log2, slices);
+        else hipLaunchKernelGGL((k_attention_step<float, 1>), grid, block, 0, st, A, lanes_log2, slices);
+    }
     profile_after("attention_step", st);
     return hipGetLastError();
 }
