@@ -74,6 +74,9 @@ __device__ __forceinline__ int here(int v)
     return v;
 }
 
+// a value that all lanes hold
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+
 // A lane's part of the place of slot 4 m + g of row 16 t + r16: the rest of the permutation depends on t and m alone.
 template <int SLOTS>
 struct Reader {
@@ -284,9 +287,10 @@ k_attention_walk(AttentionArgs A)
     if (!STATES)
         for (int i = x; i < G::kBytesP / 16; i += kWalkThreads) reinterpret_cast<f32x4*>(Ps)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (x < 2) odd[x] = 0;
-    // a chunk's decay in two floats: rounded to one it would be off the same way in every chunk
-    const double full_decay = exp(-rate * C);
-    float decay_hi = (float)full_decay, decay_lo = (float)(full_decay - (double)decay_hi);
+    // a chunk's decay in two floats: rounded to one it would be off the same way in every chunk.  The last chunk may be shorter.
+    const double full_decay = exp(-rate * C), end_decay = exp(-rate * (int)((s.hi - s.lo) % C));
+    float decay_hi = uniform((float)full_decay), decay_lo = uniform((float)(full_decay - (double)(float)full_decay));
+    const float end_hi = uniform((float)end_decay), end_lo = uniform((float)(end_decay - (double)(float)end_decay));
 
     const int64_t back = W.reverse ? -1 : 1;
     const int64_t first_row = s.begin + (W.reverse ? s.count - 1 - s.lo : s.lo);
@@ -353,11 +357,6 @@ k_attention_walk(AttentionArgs A)
     };
     if (s.lo < s.hi) load(s.lo);
     __syncthreads();                                   // the powers are there
-    float ahead[CT];                                   // weights of the state in the rows
-    if (!STATES)
-#pragma unroll
-        for (int t = 0; t < CT; ++t) ahead[t] = power[16 * t + r16 + W.lead];
-
     Reader<ROW> rows(r16, g);
     Reader<SEQ> columns(r16, g);
     Reader<SEQ> values(r16, g);                        // columns of this wavefront: tiles wave NT + c
@@ -390,8 +389,7 @@ k_attention_walk(AttentionArgs A)
         if (!STATES && !fine) odd[turn] = 1;
         if (u == s.lo || valid < C) {
             if (x < C) weight[x] = power[x < valid ? valid - x - W.lead : 0];
-            const double d = exp(-rate * valid);
-            decay_hi = (float)d; decay_lo = (float)(d - (double)decay_hi);
+            if (valid < C) { decay_hi = end_hi; decay_lo = end_lo; }
         }
         if (u + C < s.hi) load(u + C);
         __syncthreads();
@@ -443,9 +441,68 @@ k_attention_walk(AttentionArgs A)
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < CT; ++t)
+            for (int t = 0; t < CT; ++t) {
+                const float ahead = power[16 * t + r16 + W.lead];
 #pragma unroll
-                for (int c = 0; c < NT; ++c) O[t][c] *= ahead[t];
+                for (int c = 0; c < NT; ++c) O[t][c] *= ahead;
+            }
+        }
+        if (!STATES) {
+            __syncthreads();                           // P is there
+            const bool slow = odd[turn] != 0;          // a value of v is not finite: 0 * v of the tokens behind a row must not reach it
+            if (x == 0) odd[turn ^ 1] = 0;
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int m = 0; m < KC; ++m) {
+                    frag vf = get<T>(Vt, values.at(c, m));
+                    if (slow)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
+#pragma unroll
+                    for (int t = 0; t < CT; ++t)
+                        if (16 * t + 15 >= m * G::K) O[t][c] = mma(vf, get<T>(Ps, columns.at(t, m)), O[t][c]);
+                }
+            if (slow)
+                for (int j = 0; j < C; ++j) {
+                    const int i0 = here(r16), n0 = here(wave * NT * 16 + 4 * g);
+                    float p[CT];
+#pragma unroll
+                    for (int t = 0; t < CT; ++t)
+                        p[t] = (float)*reinterpret_cast<const T*>(Ps + 16 * slot_at<SEQ>(16 * t + i0, j / E) + (j % E) * (int)sizeof(T));
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n0 + 16 * c + r, j / E) + (j % E) * (int)sizeof(T));
+#pragma unroll
+                            for (int t = 0; t < CT; ++t)
+                                if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][c][r] += vj * p[t];
+                        }
+                }
+            if (W.out) {
+#pragma unroll
+                for (int t = 0; t < CT; ++t) {
+                    const int i = 16 * t + r16;
+                    if (i < valid) {
+                        T* row = out + t * out_step;
+#pragma unroll
+                        for (int c = 0; c < NT; ++c) {
+                            const int n = col0 + (wave * NT + c) * 16 + 4 * g;
+                            typename Num<T>::quad w;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
+                            if (wo) {
+                                if (n < W.dv) *reinterpret_cast<typename Num<T>::quad*>(row + n) = w;
+                            } else {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (n + r < W.dv) row[n + r] = w[r];
+                            }
+                        }
+                    }
+                }
+            }
         }
         // the state at the chunk's end
 #pragma unroll
@@ -480,60 +537,6 @@ k_attention_walk(AttentionArgs A)
                     const f32x4 b = {xs[0], xs[1], xs[2], xs[3]};
 #pragma unroll
                     for (int t = 0; t < DT; ++t) S[t][c] = mma(get<T>(Kt, columns.at(t, m)), b, S[t][c]);
-                }
-            }
-        }
-        if (!STATES) {
-            __syncthreads();                           // P is there
-            const bool slow = odd[turn] != 0;          // a value of v is not finite: 0 * v of the tokens behind a row must not reach it
-            if (x == 0) odd[turn ^ 1] = 0;
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int m = 0; m < KC; ++m) {
-                    frag vf = get<T>(Vt, values.at(c, m));
-                    if (slow)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
-#pragma unroll
-                    for (int t = 0; t < CT; ++t)
-                        if (16 * t + 15 >= m * G::K) O[t][c] = mma(vf, get<T>(Ps, columns.at(t, m)), O[t][c]);
-                }
-            if (slow)
-                for (int j = 0; j < C; ++j)
-#pragma unroll
-                    for (int c = 0; c < NT; ++c)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int n = (wave * NT + c) * 16 + 4 * g + r;
-                            const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n, j / E) + (j % E) * (int)sizeof(T));
-                            if (finite_bits(vj)) continue;
-#pragma unroll
-                            for (int t = 0; t < CT; ++t)
-                                if (16 * t + r16 >= j)
-                                    O[t][c][r] += vj * (float)*reinterpret_cast<const T*>(Ps + 16 * slot_at<SEQ>(16 * t + r16, j / E) + (j % E) * (int)sizeof(T));
-                        }
-            if (W.out) {
-#pragma unroll
-                for (int t = 0; t < CT; ++t) {
-                    const int i = 16 * t + r16;
-                    if (i < valid) {
-                        T* row = out + t * out_step;
-#pragma unroll
-                        for (int c = 0; c < NT; ++c) {
-                            const int n = col0 + (wave * NT + c) * 16 + 4 * g;
-                            typename Num<T>::quad w;
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
-                            if (wo) {
-                                if (n < W.dv) *reinterpret_cast<typename Num<T>::quad*>(row + n) = w;
-                            } else {
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (n + r < W.dv) row[n + r] = w[r];
-                            }
-                        }
-                    }
                 }
             }
         }
