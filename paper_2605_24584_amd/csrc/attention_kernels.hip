@@ -4,8 +4,8 @@
 // A walk (token_internal.h) is computed in chunks of C tokens with the state S (dk x dv) carried from chunk to chunk:
 //   inside a chunk   P_ij = l^(i-j) (q_i . k_j), j <= i;     out_i = l^(i+lead) q_i S + sum_j P_ij v_j
 //   and its end      S <- l^C S + sum_j l^(C-j-lead) k_j v_j^T
-// All four products run on the matrix cores.  A workgroup of four wavefronts walks one head of one stretch of a sequence; a
-// wavefront owns 16 NT columns of the result and of the state, which stays in its accumulator registers from the first chunk to
+// All four products run on the matrix cores.  A workgroup of eight wavefronts walks one head of one stretch of a sequence; a
+// wavefront owns 16 columns of the result and of the state, which stays in its accumulator registers from the first chunk to
 // the last: as it leaves an accumulator a pair of tiles IS a fragment of the product q S (over the state's rows in a
 // permuted order, which the rows of q in LDS share), so the state never passes through memory.
 #include "token_internal.h"
@@ -15,7 +15,6 @@ namespace laplex {
 namespace {
 
 constexpr int kStepThreads = 256;
-constexpr int kWalkThreads = 256;
 
 __device__ __forceinline__ float rate_of(const float* rates, int h)
 {
@@ -33,7 +32,10 @@ __device__ __forceinline__ int64_t start_of(const int64_t* starts, int64_t token
 // Fragments: 16 bytes of a row, K numbers of the contraction per step of the matrix cores (16 x 16 results; lane l holds
 // row or column l % 16 and the numbers of group l / 16; of a result, column l % 16 and rows 4 (l / 16) .. + 3).
 // ----------------------------------------------------------------------------
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
@@ -90,24 +92,54 @@ struct Reader {
     }
 };
 
-// four rows of E numbers each
-template <typename T> struct Patch { typename Num<T>::frag r[4]; };
-
-// rows first .. first + 3 of `valid` (p: the first of them), numbers at .. at + E - 1 of `width`; zeros beyond.  wide: all rows allow
-// 16-byte accesses.
+// R rows of four numbers each
 template <typename T>
-__device__ __forceinline__ void load_patch(Patch<T>& out, const T* p, int64_t stride, int first, int valid, int at, int width, bool wide)
+struct Patch {
+    static constexpr int R = sizeof(T) == 2 ? 4 : 2;
+    typename Num<T>::quad r[R];
+};
+
+// Rows first .. first + R - 1 of a chunk of `valid` rows from `base` on, numbers at .. at + 3 of `width`, which may be read four at a time and lie
+// within 2^31 bytes of the chunk's lowest row.  CLAMP: where some do not exist others are read in their place (no branch, so that nothing waits for the loads
+// here), and keep_patch zeroes them before they are used.
+template <typename T, bool CLAMP>
+__device__ __forceinline__ void load_wide(Patch<T>& out, const T* base, int64_t stride, int first, int valid, int at, int width)
 {
-    constexpr int E = Num<T>::E;
+    typedef typename Num<T>::quad quad;
+    const bool down = stride < 0;                      // an unsigned 32-bit place from the row that lies lowest
+    const char* const low = reinterpret_cast<const char*>(down ? base + stride * (valid - 1) : base);
+    const uint32_t step = (uint32_t)((down ? -stride : stride) * (int)sizeof(T));
+    if (CLAMP) at = at < width - 4 ? at : width - 4;
+    const uint32_t place = (down ? valid - 1 - first : first) * step + at * (int)sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        typename Num<T>::frag v = {};
-        const bool there = first + i < valid;
-        if (wide) {
-            if (there && at < width) v = *reinterpret_cast<const typename Num<T>::frag*>(p);
-        } else if (there) {
+    for (int i = 0; i < Patch<T>::R; ++i) {
+        if (CLAMP) {
+            const int row = first + i < valid ? first + i : valid - 1;
+            out.r[i] = *reinterpret_cast<const quad*>(low + ((down ? valid - 1 - row : row) * step + at * (int)sizeof(T)));
+        } else {
+            out.r[i] = *reinterpret_cast<const quad*>(low + (down ? place - i * step : place + i * step));
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void keep_patch(Patch<T>& p, int first, int valid, int at, int width)
+{
 #pragma unroll
-            for (int e = 0; e < E; ++e)
+    for (int i = 0; i < Patch<T>::R; ++i)
+        if (first + i >= valid || at >= width) p.r[i] = typename Num<T>::quad{};
+}
+
+// Rows of any alignment and width.
+template <typename T>
+__device__ __forceinline__ void load_some(Patch<T>& out, const T* base, int64_t stride, int first, int valid, int at, int width)
+{
+    const T* p = base + first * stride + at;
+#pragma unroll
+    for (int i = 0; i < Patch<T>::R; ++i) {
+        typename Num<T>::quad v = {};
+        if (first + i < valid) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
                 if (at + e < width) v[e] = p[e];
         }
         out.r[i] = v;
@@ -115,20 +147,16 @@ __device__ __forceinline__ void load_patch(Patch<T>& out, const T* p, int64_t st
     }
 }
 
-// Rows as they are, numbers along the slots (first: a multiple of 4).  In bf16 the quads of 32 numbers lie in the order 0 4 1 5 2 6 3 7: group g of a
-// fragment then holds numbers 4 g .. + 3 and 16 + 4 g .. + 3, which are the rows of a pair of accumulator tiles that the group holds.
+// Rows as they are, numbers along the slots (first: a multiple of R, piece: which four numbers).  In bf16 the quads of 32 numbers lie in the order
+// 0 4 1 5 2 6 3 7: group g of a fragment then holds numbers 4 g .. + 3 and 16 + 4 g .. + 3, which are the rows of a pair of accumulator
+// tiles that the group holds.
 template <int SLOTS>
 __device__ __forceinline__ void put_rows(char* tile, const Patch<__bf16>& p, int first, int piece)
 {
-    const int low = here(((piece >> 2) * 4 + 2 * (piece & 1)) ^ twist<SLOTS>(first));
-    char* const at = tile + first * SLOTS * 16 + 8 * ((piece >> 1) & 1);
+    const int low = here(((piece >> 3) * 4 + (piece & 3)) ^ twist<SLOTS>(first));
+    char* const at = tile + first * SLOTS * 16 + 8 * ((piece >> 2) & 1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const bf16x4 v = {p.r[i][4 * half], p.r[i][4 * half + 1], p.r[i][4 * half + 2], p.r[i][4 * half + 3]};
-            *reinterpret_cast<bf16x4*>(at + i * SLOTS * 16 + 16 * (low ^ i ^ half)) = v;
-        }
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<bf16x4*>(at + i * SLOTS * 16 + 16 * (low ^ i)) = p.r[i];
 }
 template <int SLOTS>
 __device__ __forceinline__ void put_rows(char* tile, const Patch<float>& p, int first, int piece)
@@ -136,17 +164,17 @@ __device__ __forceinline__ void put_rows(char* tile, const Patch<float>& p, int 
     const int low = here(piece ^ twist<SLOTS>(first));
     char* const at = tile + first * SLOTS * 16;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(at + i * SLOTS * 16 + 16 * (low ^ i)) = p.r[i];
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(at + i * SLOTS * 16 + 16 * (low ^ i)) = p.r[i];
 }
 
 // The patch's columns as rows, tokens along the slots.
 template <int SLOTS>
 __device__ __forceinline__ void put_columns(char* tile, const Patch<__bf16>& p, int first, int piece)
 {
-    const int low = here((first >> 3) ^ twist<SLOTS>(piece * 8));
-    char* const at = tile + piece * 8 * SLOTS * 16 + 8 * ((first >> 2) & 1);
+    const int low = here((first >> 3) ^ twist<SLOTS>(piece * 4));
+    char* const at = tile + piece * 4 * SLOTS * 16 + 8 * ((first >> 2) & 1);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 4; ++e) {
         const bf16x4 v = {p.r[0][e], p.r[1][e], p.r[2][e], p.r[3][e]};
         *reinterpret_cast<bf16x4*>(at + e * SLOTS * 16 + 16 * (low ^ (SLOTS >= 8 ? e : (e >> 1)))) = v;
     }
@@ -155,11 +183,11 @@ template <int SLOTS>
 __device__ __forceinline__ void put_columns(char* tile, const Patch<float>& p, int first, int piece)
 {
     const int low = here((first >> 2) ^ twist<SLOTS>(piece * 4));
-    char* const at = tile + piece * 4 * SLOTS * 16;
+    char* const at = tile + piece * 4 * SLOTS * 16 + 8 * ((first >> 1) & 1);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const f32x4 v = {p.r[0][e], p.r[1][e], p.r[2][e], p.r[3][e]};
-        *reinterpret_cast<f32x4*>(at + e * SLOTS * 16 + 16 * (low ^ (SLOTS >= 8 ? e : (e >> 1)))) = v;
+        const f32x2 v = {p.r[0][e], p.r[1][e]};
+        *reinterpret_cast<f32x2*>(at + e * SLOTS * 16 + 16 * (low ^ (SLOTS >= 8 ? e : (e >> 1)))) = v;
     }
 }
 
@@ -169,28 +197,45 @@ __device__ __forceinline__ typename Num<T>::frag get(const char* tile, int place
     return *reinterpret_cast<const typename Num<T>::frag*>(tile + place);
 }
 
-// x = hi + mid + lo: bf16 holds 8 bits, so three of them all 24 of an fp32 number
+// x = hi + mid + lo, exactly: bf16 holds 8 bits, so three of them hold all 24 of an fp32 number.  The upper half of an fp32 number is a bf16 one.
+__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
+__device__ __forceinline__ bf16x8 uppers(const float* x)
+{
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(__float_as_uint(x[2 * e + 1]), __float_as_uint(x[2 * e]), 0x07060302u);
+    return __builtin_bit_cast(bf16x8, v);
+}
 __device__ __forceinline__ void split3(const float* x, bf16x8& hi, bf16x8& mid, bf16x8& lo)
 {
+    float r[8], q[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        hi[e] = (__bf16)x[e];
-        const float r = x[e] - (float)hi[e];
-        mid[e] = (__bf16)r;
-        lo[e] = (__bf16)(r - (float)mid[e]);
+        r[e] = x[e] - upper(x[e]);
+        q[e] = r[e] - upper(r[e]);
     }
+    hi = uppers(x); mid = uppers(r); lo = uppers(q);
 }
 
 __device__ __forceinline__ bool finite_bits(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
-template <typename T>
-__device__ __forceinline__ bool finite_patch(const Patch<T>& p)
+__device__ __forceinline__ bool finite_patch(const Patch<float>& p)
 {
-    bool fine = true;
+    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < Num<T>::E; ++e) fine = fine && finite_bits((float)p.r[i][e]);
-    return fine;
+        for (int e = 0; e < 4; ++e) { const uint32_t v = __float_as_uint(p.r[i][e]) & 0x7F800000u; most = v > most ? v : most; }
+    return most != 0x7F800000u;
+}
+__device__ __forceinline__ bool finite_patch(const Patch<__bf16>& p)
+{
+    uint32_t odd = 0;                                  // an exponent of ones carries into the sign's place
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u32x2 v = __builtin_bit_cast(u32x2, p.r[i]);
+        odd |= ((v[0] & 0x7F807F80u) + 0x00800080u) | ((v[1] & 0x7F807F80u) + 0x00800080u);
+    }
+    return (odd & 0x80008000u) == 0;
 }
 
 // ----------------------------------------------------------------------------
@@ -244,12 +289,12 @@ __device__ __forceinline__ float state_value(const Walk& W, int64_t at, int row,
     return W.in_scale * W.state_in[at + (W.transposed ? (int64_t)col * W.dk + row : (int64_t)row * W.dv + col)];
 }
 
-// Sizes of a walk's kernel: DK the padded rows of the state, NT tiles of 16 columns for each of four wavefronts.
-template <typename T, int DK, int NT>
+// Sizes of a walk's kernel: DK the padded rows of the state; every wavefront has 16 columns.
+template <typename T, int DK, int WAVES>
 struct Geometry {
-    static constexpr int E = Num<T>::E, K = Num<T>::K;
+    static constexpr int E = Num<T>::E, K = Num<T>::K, R = Patch<T>::R, THREADS = 64 * WAVES;
     static constexpr int C = (DK > 128 ? 32 : 64) * 2 / (int)sizeof(T);      // tokens of a chunk
-    static constexpr int COLS = 64 * NT;                                     // columns of a workgroup
+    static constexpr int COLS = 16 * WAVES;                                  // columns of a workgroup
     static constexpr int ROW = DK * (int)sizeof(T) / 16, SEQ = C * (int)sizeof(T) / 16;   // slots of a row of numbers, of tokens
     static constexpr int CT = C / 16, DT = DK / 16, KD = DK / K, KC = C / K;
     static constexpr int kBytesRows = C * ROW * 16, kBytesK = DK * SEQ * 16, kBytesV = COLS * SEQ * 16, kBytesP = C * SEQ * 16;
@@ -257,13 +302,14 @@ struct Geometry {
 };
 
 // STATES: only what a stretch adds to the state, for the stretches behind it (U below).
-template <typename T, int DK, int NT, bool STATES>
-__global__ void __launch_bounds__(kWalkThreads, 2)
+template <typename T, int DK, int WAVES, bool STATES>
+__global__ void __launch_bounds__(64 * WAVES, (DK > 128 ? 2 : DK > 64 ? 4 : 3))      // as many as LDS and, at 256 rows, the state leave room for
 k_attention_walk(AttentionArgs A)
 {
-    typedef Geometry<T, DK, NT> G;
+    typedef Geometry<T, DK, WAVES> G;
     typedef typename Num<T>::frag frag;
-    constexpr int E = G::E, C = G::C, ROW = G::ROW, SEQ = G::SEQ, CT = G::CT, DT = G::DT, KD = G::KD, KC = G::KC;
+    typedef typename Num<T>::quad quad;
+    constexpr int E = G::E, C = G::C, R = G::R, ROW = G::ROW, SEQ = G::SEQ, CT = G::CT, DT = G::DT, KD = G::KD, KC = G::KC, THREADS = G::THREADS;
     __shared__ __attribute__((aligned(16))) char lds[STATES ? G::kBytesK + G::kBytesV : G::kLds];
     __shared__ float power[C + 1], weight[C];          // l^d, and the weights of the chunk's tokens in the state
     __shared__ int odd[2];
@@ -281,283 +327,270 @@ k_attention_walk(AttentionArgs A)
     const Stretch s = find_stretch(A, slot);
     if (!s.there || (STATES && s.last)) return;
 
-    const int x = threadIdx.x, lane = x & 63, wave = x >> 6, r16 = lane & 15, g = lane >> 4;
+    const int x = threadIdx.x, lane = x & 63, wave = __builtin_amdgcn_readfirstlane(x >> 6), r16 = lane & 15, g = lane >> 4;
     const double rate = (double)rate_of(A.rates, h);
-    for (int d = x; d <= C; d += kWalkThreads) power[d] = (float)exp(-rate * d);
+    for (int d = x; d <= C; d += THREADS) power[d] = (float)exp(-rate * d);
     if (!STATES)
-        for (int i = x; i < G::kBytesP / 16; i += kWalkThreads) reinterpret_cast<f32x4*>(Ps)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = x; i < G::kBytesP / 16; i += THREADS) reinterpret_cast<f32x4*>(Ps)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (x < 2) odd[x] = 0;
-    // a chunk's decay in two floats: rounded to one it would be off the same way in every chunk.  The last chunk may be shorter.
-    const double full_decay = exp(-rate * C), end_decay = exp(-rate * (int)((s.hi - s.lo) % C));
-    float decay_hi = uniform((float)full_decay), decay_lo = uniform((float)(full_decay - (double)(float)full_decay));
-    const float end_hi = uniform((float)end_decay), end_lo = uniform((float)(end_decay - (double)(float)end_decay));
+    // A chunk's decay as an fp32 number and what its rounding leaves out, in parts of it: the same rounding in every chunk would add up, so the
+    // next number up or down is taken whenever what has been left out reaches half of their distance.  The last chunk may be shorter.
+    const double full_decay = exp(-rate * C);
+    const float decay = uniform((float)full_decay), end_decay = uniform((float)exp(-rate * (int)((s.hi - s.lo) % C)));
+    const float ulp = uniform(__uint_as_float(__float_as_uint(decay) + 1) - decay), rest = uniform((float)(full_decay - (double)decay));
+    float left = 0.0f;
 
     const int64_t back = W.reverse ? -1 : 1;
     const int64_t first_row = s.begin + (W.reverse ? s.count - 1 - s.lo : s.lo);
     const int64_t sq = back * W.ldq, sk = back * W.ldk, sv = back * W.ldv;
-    const bool wq = A.wide[blockIdx.z] & 1, wk = A.wide[blockIdx.z] & 2, wv = A.wide[blockIdx.z] & 4, wo = A.wide[blockIdx.z] & 8;
+    const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;      // rows further apart need 64-bit places
+    const bool wide = (A.wide[blockIdx.z] & 7) == 7 && W.ldq < near && W.ldk < near && W.ldv < near, wo = A.wide[blockIdx.z] & 8;
+    const bool whole = wide && W.dk == DK && col0 + G::COLS <= W.dv;
 
-    // the state: rows 16 t + 4 g .. + 3, column col0 + (wave NT + c) 16 + r16
-    f32x4 S[DT][NT];
+    // the state: rows 16 t + 4 g .. + 3, column col0 + 16 wave + r16
+    f32x4 S[DT];
+    const int col = col0 + 16 * wave + r16;
     const int64_t state_at = (s.b * A.heads + h) * (int64_t)W.dk * W.dv;
-    f32x4* const U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * (DK * G::COLS / 4);
+    f32x4* const U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * (DK * G::COLS / 4) +
+                     wave * DT * 64 + lane;
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+    for (int t = 0; t < DT; ++t) {
+        f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (!STATES) {
+            if (s.index > 0) v4 = U[t * 64];
+            else if (W.state_in) {
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (!STATES) {
-                if (s.index > 0) v4 = U[((wave * DT + t) * NT + c) * 64 + lane];
-                else if (W.state_in) {
-                    const int col = col0 + (wave * NT + c) * 16 + r16;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (col < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col);
-                }
+                for (int r = 0; r < 4; ++r)
+                    if (col < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col);
             }
-            S[t][c] = v4;
         }
+        S[t] = v4;
+    }
 
-    // patches of a chunk: four rows by 16 bytes
-    constexpr int kRowPatches = (C / 4) * (DK / E), kColPatches = (C / 4) * (G::COLS / E);
-    constexpr int NR = (kRowPatches + kWalkThreads - 1) / kWalkThreads, NV = (kColPatches + kWalkThreads - 1) / kWalkThreads;
+    // a chunk's patches
+    constexpr int kRowPatches = (C / R) * (DK / 4), kColPatches = (C / R) * (G::COLS / 4);
+    constexpr int NR = (kRowPatches + THREADS - 1) / THREADS, NV = (kColPatches + THREADS - 1) / THREADS;
     Patch<T> pq[NR], pk[NR], pv[NV];
-    const T *tq[NR], *tk[NR], *tv[NV];                 // a thread's first row of the chunk that is loaded next
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-        const int p = x + i * kWalkThreads, row = (p / (DK / E)) * 4, at = (p % (DK / E)) * E;
-        tq[i] = static_cast<const T*>(W.q) + (first_row + back * row) * W.ldq + (int64_t)h * W.dk + at;
-        tk[i] = static_cast<const T*>(W.k) + (first_row + back * row) * W.ldk + (int64_t)h * W.dk + at;
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int p = x + i * kWalkThreads, row = (p / (G::COLS / E)) * 4, at = col0 + (p % (G::COLS / E)) * E;
-        tv[i] = static_cast<const T*>(W.v) + (first_row + back * row) * W.ldv + (int64_t)h * W.dv + at;
-    }
+    const T* q = static_cast<const T*>(W.q) + first_row * W.ldq + (int64_t)h * W.dk;       // the first row of the chunk that is loaded next
+    const T* k = static_cast<const T*>(W.k) + first_row * W.ldk + (int64_t)h * W.dk;
+    const T* v = static_cast<const T*>(W.v) + first_row * W.ldv + (int64_t)h * W.dv;
     auto load = [&](int64_t u) {
-        const int valid = (int)(s.hi - u < C ? s.hi - u : C);
+        const int valid = (int)(s.hi - u < C ? s.hi - u : C), y = here(x);
+        auto each = [&](auto rows_of, auto columns_of) {
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            const int p = x + i * kWalkThreads;
-            if (kRowPatches % kWalkThreads == 0 || p < kRowPatches) {
-                const int at = (p % (DK / E)) * E, row = (p / (DK / E)) * 4;
-                if (!STATES) load_patch(pq[i], tq[i], sq, row, valid, at, W.dk, wq);
-                load_patch(pk[i], tk[i], sk, row, valid, at, W.dk, wk);
-                tq[i] += C * sq; tk[i] += C * sk;
+            for (int i = 0; i < NR; ++i) {
+                const int p = y + i * THREADS;
+                if (kRowPatches % THREADS == 0 || p < kRowPatches) rows_of(i, (p / (DK / 4)) * R, (p % (DK / 4)) * 4);
             }
-        }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int p = x + i * kWalkThreads;
-            if (kColPatches % kWalkThreads == 0 || p < kColPatches) {
-                load_patch(pv[i], tv[i], sv, (p / (G::COLS / E)) * 4, valid, col0 + (p % (G::COLS / E)) * E, W.dv, wv);
-                tv[i] += C * sv;
+            for (int i = 0; i < NV; ++i) {
+                const int p = y + i * THREADS;
+                if (kColPatches % THREADS == 0 || p < kColPatches) columns_of(i, (p / (G::COLS / 4)) * R, col0 + (p % (G::COLS / 4)) * 4);
             }
-        }
+        };
+        // (one branch for all: a wait for the loads of one matrix where the other branch has its own would hold up the next one's)
+        if (whole && valid == C)
+            each([&](int i, int row, int at) {
+                     if (!STATES) load_wide<T, false>(pq[i], q, sq, row, C, at, DK);
+                     load_wide<T, false>(pk[i], k, sk, row, C, at, DK);
+                 },
+                 [&](int i, int row, int at) { load_wide<T, false>(pv[i], v, sv, row, C, at, W.dv); });
+        else if (wide)
+            each([&](int i, int row, int at) {
+                     if (!STATES) load_wide<T, true>(pq[i], q, sq, row, valid, at, W.dk);
+                     load_wide<T, true>(pk[i], k, sk, row, valid, at, W.dk);
+                 },
+                 [&](int i, int row, int at) { load_wide<T, true>(pv[i], v, sv, row, valid, at, W.dv); });
+        else
+            each([&](int i, int row, int at) {
+                     if (!STATES) load_some(pq[i], q, sq, row, valid, at, W.dk);
+                     load_some(pk[i], k, sk, row, valid, at, W.dk);
+                 },
+                 [&](int i, int row, int at) { load_some(pv[i], v, sv, row, valid, at, W.dv); });
+        q += C * sq; k += C * sk; v += C * sv;
     };
     if (s.lo < s.hi) load(s.lo);
     __syncthreads();                                   // the powers are there
-    Reader<ROW> rows(r16, g);
-    Reader<SEQ> columns(r16, g);
-    Reader<SEQ> values(r16, g);                        // columns of this wavefront: tiles wave NT + c
-    values.base += wave * NT * 16 * SEQ * 16;
-    values.low ^= ((2 * wave * NT) & Reader<SEQ>::kMask) * 16;
-    T* out = static_cast<T*>(W.out) + (first_row + back * r16) * W.ldo + (int64_t)h * W.dv;
-    const int64_t out_step = back * 16 * W.ldo;
+    T* out = static_cast<T*>(W.out) + first_row * W.ldo + (int64_t)h * W.dv + col0 + 16 * wave;      // the chunk's first row
+    const int64_t so = back * W.ldo;
 
     int turn = 0;
     for (int64_t u = s.lo; u < s.hi; u += C, turn ^= 1) {
         const int valid = (int)(s.hi - u < C ? s.hi - u : C);
         bool fine = true;
+        const int y = here(x);
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int p = x + i * kWalkThreads;
-            if (kRowPatches % kWalkThreads == 0 || p < kRowPatches) {
-                const int piece = p % (DK / E), row = (p / (DK / E)) * 4;
+            const int p = y + i * THREADS;
+            if (kRowPatches % THREADS == 0 || p < kRowPatches) {
+                const int piece = p % (DK / 4), row = (p / (DK / 4)) * R;
+                if (!(whole && valid == C)) {
+                    if (!STATES) keep_patch(pq[i], row, valid, piece * 4, W.dk);
+                    keep_patch(pk[i], row, valid, piece * 4, W.dk);
+                }
                 if (!STATES) { put_rows<ROW>(Qs, pq[i], row, piece); put_rows<ROW>(Ks, pk[i], row, piece); }
                 put_columns<SEQ>(Kt, pk[i], row, piece);
             }
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int p = x + i * kWalkThreads;
-            if (kColPatches % kWalkThreads == 0 || p < kColPatches) {
-                put_columns<SEQ>(Vt, pv[i], (p / (G::COLS / E)) * 4, p % (G::COLS / E));
+            const int p = y + i * THREADS;
+            if (kColPatches % THREADS == 0 || p < kColPatches) {
+                const int piece = p % (G::COLS / 4), row = (p / (G::COLS / 4)) * R;
+                if (!(whole && valid == C)) keep_patch(pv[i], row, valid, col0 + piece * 4, W.dv);
+                put_columns<SEQ>(Vt, pv[i], row, piece);
                 if (!STATES) fine = fine && finite_patch(pv[i]);
             }
         }
         if (!STATES && !fine) odd[turn] = 1;
-        if (u == s.lo || valid < C) {
+        if (u == s.lo || valid < C)
             if (x < C) weight[x] = power[x < valid ? valid - x - W.lead : 0];
-            if (valid < C) { decay_hi = end_hi; decay_lo = end_lo; }
-        }
         if (u + C < s.hi) load(u + C);
         __syncthreads();
 
-        rows.low = here(rows.low); columns.low = here(columns.low); values.low = here(values.low);
-        f32x4 O[CT][NT];
+        const int l = here(lane), r16 = l & 15, g = l >> 4;
+        const Reader<ROW> rows(r16, g);
+        const Reader<SEQ> columns(r16, g);
+        Reader<SEQ> values(r16, g);                    // the columns of this wavefront: tile `wave`
+        values.base += wave * 16 * SEQ * 16;
+        values.low ^= ((2 * wave) & Reader<SEQ>::kMask) * 16;
         if (!STATES) {
             // P: tiles on and below the diagonal, dealt to the wavefronts; as it leaves the accumulator a lane holds P[i][j .. j + 3]
 #pragma unroll
-            for (int n = 0; n < (CT * (CT + 1) / 2 + 3) / 4; ++n) {
-                const int tile = n * 4 + wave;
+            for (int n = 0; n < (CT * (CT + 1) / 2 + WAVES - 1) / WAVES; ++n) {
+                const int tile = n * WAVES + wave;
                 int it = 0, jt = tile;
                 while (jt > it) { jt -= it + 1; ++it; }
                 if (it < CT) {
                     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int m = 0; m < KD; ++m) acc = mma(get<T>(Ks, rows.at(jt, m)), get<T>(Qs, rows.at(it, m)), acc);
-                    typename Num<T>::quad w;
+                    quad w;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int d = 16 * (it - jt) + r16 - 4 * g - r;
                         w[r] = (T)(d >= 0 ? acc[r] * power[d < 0 ? 0 : d] : 0.0f);
                     }
                     const int j = 16 * jt + 4 * g;
-                    *reinterpret_cast<typename Num<T>::quad*>(Ps + 16 * slot_at<SEQ>(16 * it + r16, j / E) + (j % E) * (int)sizeof(T)) = w;
+                    *reinterpret_cast<quad*>(Ps + 16 * slot_at<SEQ>(16 * it + r16, j / E) + (j % E) * (int)sizeof(T)) = w;
                 }
             }
             // q S, weighted by the rows
+            f32x4 O[CT];
 #pragma unroll
-            for (int t = 0; t < CT; ++t)
-#pragma unroll
-                for (int c = 0; c < NT; ++c) O[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < CT; ++t) O[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int m = 0; m < KD; ++m) {
-                __builtin_amdgcn_sched_barrier(0);     // (all steps' fragments at once do not fit the registers)
+                if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);     // (all steps' fragments at once do not fit the registers)
+                frag sf;
+                if constexpr (sizeof(T) == 2) {
+                    // rounded for this product alone, as P is for its own: the result is rounded as much again
 #pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    if constexpr (sizeof(T) == 2) {
-                        bf16x8 sf;                     // rounded for this product alone, as P is for its own: the result is rounded as much again
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sf[e] = (__bf16)S[2 * m + (e >> 2)][c][e & 3];
-#pragma unroll
-                        for (int t = 0; t < CT; ++t) O[t][c] = mma(sf, get<T>(Qs, rows.at(t, m)), O[t][c]);
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < CT; ++t) O[t][c] = mma(S[m][c], get<T>(Qs, rows.at(t, m)), O[t][c]);
-                    }
+                    for (int e = 0; e < 8; ++e) sf[e] = (__bf16)S[2 * m + (e >> 2)][e & 3];
+                } else {
+                    sf = S[m];
                 }
+#pragma unroll
+                for (int t = 0; t < CT; ++t) O[t] = mma(sf, get<T>(Qs, rows.at(t, m)), O[t]);
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                const float ahead = power[16 * t + r16 + W.lead];
-#pragma unroll
-                for (int c = 0; c < NT; ++c) O[t][c] *= ahead;
-            }
-        }
-        if (!STATES) {
+            for (int t = 0; t < CT; ++t) O[t] *= power[16 * t + r16 + W.lead];
             __syncthreads();                           // P is there
             const bool slow = odd[turn] != 0;          // a value of v is not finite: 0 * v of the tokens behind a row must not reach it
             if (x == 0) odd[turn ^ 1] = 0;
 #pragma unroll
-            for (int c = 0; c < NT; ++c)
+            for (int m = 0; m < KC; ++m) {
+                frag vf = get<T>(Vt, values.at(0, m));
+                if (slow)
 #pragma unroll
-                for (int m = 0; m < KC; ++m) {
-                    frag vf = get<T>(Vt, values.at(c, m));
-                    if (slow)
+                    for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
 #pragma unroll
-                        for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
-#pragma unroll
-                    for (int t = 0; t < CT; ++t)
-                        if (16 * t + 15 >= m * G::K) O[t][c] = mma(vf, get<T>(Ps, columns.at(t, m)), O[t][c]);
-                }
+                for (int t = 0; t < CT; ++t)
+                    if (16 * t + 15 >= m * G::K) O[t] = mma(vf, get<T>(Ps, columns.at(t, m)), O[t]);
+            }
             if (slow)
                 for (int j = 0; j < C; ++j) {
-                    const int i0 = here(r16), n0 = here(wave * NT * 16 + 4 * g);
+                    const int i0 = here(r16), n0 = here(wave * 16 + 4 * g);
                     float p[CT];
 #pragma unroll
                     for (int t = 0; t < CT; ++t)
                         p[t] = (float)*reinterpret_cast<const T*>(Ps + 16 * slot_at<SEQ>(16 * t + i0, j / E) + (j % E) * (int)sizeof(T));
 #pragma unroll
-                    for (int c = 0; c < NT; ++c)
+                    for (int r = 0; r < 4; ++r) {
+                        const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n0 + r, j / E) + (j % E) * (int)sizeof(T));
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n0 + 16 * c + r, j / E) + (j % E) * (int)sizeof(T));
-#pragma unroll
-                            for (int t = 0; t < CT; ++t)
-                                if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][c][r] += vj * p[t];
-                        }
+                        for (int t = 0; t < CT; ++t)
+                            if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][r] += vj * p[t];
+                    }
                 }
             if (W.out) {
+                const int n = col0 + 16 * wave + 4 * g;
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
-                    const int i = 16 * t + r16;
-                    if (i < valid) {
-                        T* row = out + t * out_step;
+                    if (16 * t + r16 < valid) {
+                        T* row = out + (16 * t + r16) * so + 4 * g;
+                        quad w;
 #pragma unroll
-                        for (int c = 0; c < NT; ++c) {
-                            const int n = col0 + (wave * NT + c) * 16 + 4 * g;
-                            typename Num<T>::quad w;
+                        for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][r] * W.out_scale);
+                        if (wo) {
+                            if (n < W.dv) *reinterpret_cast<quad*>(row) = w;
+                        } else {
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
-                            if (wo) {
-                                if (n < W.dv) *reinterpret_cast<typename Num<T>::quad*>(row + n) = w;
-                            } else {
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (n + r < W.dv) row[n + r] = w[r];
-                            }
+                            for (int r = 0; r < 4; ++r)
+                                if (n + r < W.dv) row[r] = w[r];
                         }
                     }
                 }
             }
+            out += C * so;
         }
         // the state at the chunk's end
+        float d = decay;
+        left += rest;
+        if (left >= 0.5f * ulp) { d = decay + ulp; left -= ulp; }
+        else if (left <= -0.5f * ulp) { d = decay - ulp; left += ulp; }
+        if (valid < C) d = end_decay;
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][c][r] = fmaf(S[t][c][r], decay_hi, S[t][c][r] * decay_lo);
+        for (int t = 0; t < DT; ++t) S[t] *= d;
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
             __builtin_amdgcn_sched_barrier(0);
-            float w[E];
+            const frag vf = get<T>(Vt, values.at(0, m));
+            float xs[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) w[e] = weight[(4 * m + g) * E + e];
+            for (int e = 0; e < E; ++e) xs[e] = weight[(4 * m + g) * E + e] * (float)vf[e];
+            if constexpr (sizeof(T) == 2) {
+                bf16x8 hi, mid, lo;                    // the state is an fp32 sum of fp32 products whatever the type
+                split3(xs, hi, mid, lo);
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                const frag vf = get<T>(Vt, values.at(c, m));
-                float xs[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) xs[e] = w[e] * (float)vf[e];
-                if constexpr (sizeof(T) == 2) {
-                    bf16x8 hi, mid, lo;
-                    split3(xs, hi, mid, lo);
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) {
-                        const frag kf = get<T>(Kt, columns.at(t, m));
-                        S[t][c] = mma(kf, hi, S[t][c]);
-                        S[t][c] = mma(kf, mid, S[t][c]);
-                        S[t][c] = mma(kf, lo, S[t][c]);
-                    }
-                } else {
-                    const f32x4 b = {xs[0], xs[1], xs[2], xs[3]};
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) S[t][c] = mma(get<T>(Kt, columns.at(t, m)), b, S[t][c]);
+                for (int t = 0; t < DT; ++t) {
+                    const frag kf = get<T>(Kt, columns.at(t, m));
+                    S[t] = mma(kf, hi, S[t]);
+                    S[t] = mma(kf, mid, S[t]);
+                    S[t] = mma(kf, lo, S[t]);
                 }
+            } else {
+                const f32x4 b = {xs[0], xs[1], xs[2], xs[3]};
+#pragma unroll
+                for (int t = 0; t < DT; ++t) S[t] = mma(get<T>(Kt, columns.at(t, m)), b, S[t]);
             }
         }
-        out += CT * out_step;
         __syncthreads();                               // the tiles may be written again
     }
 
+    if (STATES) {
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+        for (int t = 0; t < DT; ++t) U[t * 64] = S[t];
+    } else if (W.state_out && s.last) {
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            if (STATES) U[((wave * DT + t) * NT + c) * 64 + lane] = S[t][c];
-            else if (W.state_out && s.last) {
-                const int col = col0 + (wave * NT + c) * 16 + r16;
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * t + 4 * g + r;
-                    if (col < W.dv && row < W.dk) W.state_out[state_at + (int64_t)row * W.dv + col] = W.last_scale * S[t][c][r];
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * t + 4 * g + r;
+                if (col < W.dv && row < W.dk) W.state_out[state_at + (int64_t)row * W.dv + col] = W.last_scale * S[t][r];
             }
-        }
+    }
 }
 
 // What enters every stretch but the first: carry_n = l^stretch carry_(n-1) + U_(n-1), carry_0 = the initial state, in the places of the U.
@@ -573,8 +606,8 @@ k_attention_carry(AttentionArgs A)
         const int rest = (int)(block % (A.slices * kBlocks)), slice = rest / kBlocks, piece = (rest % kBlocks) * 256 + threadIdx.x;
         const int h = blockIdx.y, col0 = slice * COLS;
         if (col0 >= W.dv) continue;
-        constexpr int DT = DK / 16, NT = COLS / 64;
-        const int lane = piece & 63, c = (piece >> 6) % NT, t = (piece / (64 * NT)) % DT, wave = piece / (64 * NT * DT);
+        constexpr int DT = DK / 16;
+        const int lane = piece & 63, t = (piece >> 6) % DT, wave = piece / (64 * DT);
         const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
         const int64_t count = end > begin ? end - begin : 0, stretches = (count + A.stretch - 1) / A.stretch;
         const int64_t slot = begin / A.stretch + b;
@@ -583,7 +616,7 @@ k_attention_carry(AttentionArgs A)
         const float hi = (float)d, lo = (float)(d - (double)hi);
         f32x4 carry = {0.0f, 0.0f, 0.0f, 0.0f};
         if (W.state_in) {
-            const int col = col0 + (wave * NT + c) * 16 + (lane & 15);
+            const int col = col0 + wave * 16 + (lane & 15);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * t + 4 * (lane >> 4) + r;
@@ -675,7 +708,7 @@ Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv)
     Plan P;
     const int most = dk > dv ? dk : dv;
     P.dk = most <= 64 ? 64 : most <= 128 ? 128 : 256;
-    P.cols = P.dk == 128 ? 128 : 64;
+    P.cols = P.dk == 64 ? 64 : 128;
     P.slices = (most + P.cols - 1) / P.cols;
     const int64_t workgroups = sequences * heads * P.slices;
     P.stretch = 512;
@@ -690,22 +723,22 @@ bool allows(const void* p, int64_t ld, int d, int size, int bytes)
     return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0 && d * size % bytes == 0;
 }
 
-template <typename T, int DK, int NT>
+template <typename T, int DK, int WAVES>
 hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
     const dim3 grid((unsigned)(P.slots * P.slices), (unsigned)A.heads, (unsigned)A.walks);
     if (P.cut) {
         profile_before("attention_states", st);
-        hipLaunchKernelGGL((k_attention_walk<T, DK, NT, true>), grid, dim3(kWalkThreads), 0, st, A);
+        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, true>), grid, dim3(64 * WAVES), 0, st, A);
         profile_after("attention_states", st);
         profile_before("attention_carry", st);
-        const int64_t blocks = A.sequences * P.slices * (DK * 64 * NT / 1024), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
-        hipLaunchKernelGGL((k_attention_carry<DK, 64 * NT>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.walks),
+        const int64_t blocks = A.sequences * P.slices * (DK * 16 * WAVES / 1024), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+        hipLaunchKernelGGL((k_attention_carry<DK, 16 * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.walks),
                            dim3(256), 0, st, A);
         profile_after("attention_carry", st);
     }
     profile_before("attention_walk", st);
-    hipLaunchKernelGGL((k_attention_walk<T, DK, NT, false>), grid, dim3(kWalkThreads), 0, st, A);
+    hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, false>), grid, dim3(64 * WAVES), 0, st, A);
     profile_after("attention_walk", st);
     return hipGetLastError();
 }
@@ -713,9 +746,9 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 template <typename T>
 hipError_t walk_of(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
-    if (P.dk == 64) return walk_with<T, 64, 1>(A, P, st);
-    if (P.dk == 128) return walk_with<T, 128, 2>(A, P, st);
-    return walk_with<T, 256, 1>(A, P, st);
+    if (P.dk == 64) return walk_with<T, 64, 4>(A, P, st);
+    if (P.dk == 128) return walk_with<T, 128, 8>(A, P, st);
+    return walk_with<T, 256, 8>(A, P, st);
 }
 
 }  // namespace
@@ -735,8 +768,8 @@ hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
     const int size = A.bf16 ? 2 : 4;
     for (int w = 0; w < A.walks; ++w) {
         const Walk& W = A.walk[w];
-        A.wide[w] = (allows(W.q, W.ldq, W.dk, size, 16) ? 1 : 0) | (allows(W.k, W.ldk, W.dk, size, 16) ? 2 : 0) |
-                    (allows(W.v, W.ldv, W.dv, size, 16) ? 4 : 0) | (allows(W.out, W.ldo, W.dv, size, 4 * size) ? 8 : 0);
+        A.wide[w] = (allows(W.q, W.ldq, W.dk, size, 4 * size) ? 1 : 0) | (allows(W.k, W.ldk, W.dk, size, 4 * size) ? 2 : 0) |
+                    (allows(W.v, W.ldv, W.dv, size, 4 * size) ? 4 : 0) | (allows(W.out, W.ldo, W.dv, size, 4 * size) ? 8 : 0);
     }
     return A.bf16 ? walk_of<__bf16>(A, P, st) : walk_of<float>(A, P, st);
 }

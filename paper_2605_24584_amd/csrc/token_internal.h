@@ -56,7 +56,7 @@ struct AttentionArgs {
     // filled in by launch_attention
     int64_t stretch, slots;          // tokens of a stretch that one workgroup walks; stretches of all sequences, at most
     int slices;                      // workgroups side by side over the columns
-    int wide[3];                     // per walk, a bit each for q, k, v, out: its rows allow 16-byte accesses (out: four numbers at once)
+    int wide[3];                     // per walk, a bit each for q, k, v, out: its rows may be accessed four numbers at a time
 };
 size_t attention_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv);
 hipError_t launch_attention(const AttentionArgs& A, hipStream_t st);
