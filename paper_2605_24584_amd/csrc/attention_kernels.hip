@@ -239,9 +239,12 @@ __device__ __forceinline__ bool finite_patch(const Patch<__bf16>& p)
 }
 
 // ----------------------------------------------------------------------------
-// Which stretch of which sequence: sequences are cut into stretches of `stretch` tokens (a multiple of every C).  Sequence b has the slots
-// from start / stretch + b on: at least one, and as many as it has stretches; a slot beyond those has nothing to do.
+// Which stretch of which sequence: sequences are cut into stretches of `stretch` tokens (a multiple of every C), each with a slot.  Of equal lengths
+// every sequence has its slots; otherwise sequence b has those from start / stretch + b on: at least one, and as many as it has stretches, and a
+// slot beyond those has nothing to do.
 // ----------------------------------------------------------------------------
+constexpr int64_t kSlotRows = 32768;      // slots along a grid's second axis
+
 struct Stretch {
     int64_t b;                        // sequence
     int64_t begin, count;             // its rows
@@ -250,13 +253,19 @@ struct Stretch {
     int64_t index;
 };
 
+__device__ __forceinline__ int64_t first_slot(const AttentionArgs& A, int64_t b, int64_t begin)
+{
+    return A.starts ? begin / A.stretch + b : b * A.per_sequence;
+}
+
 __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& A, int64_t slot)
 {
     Stretch s;
-    // the last sequence whose first slot is at most this one: 64 candidates at a time
-    int64_t lo = 0, hi = A.sequences;                  // in [lo, hi)
-    const int lane = threadIdx.x & 63;
+    int64_t lo = 0;
     if (A.starts) {
+        // the last sequence whose first slot is at most this one: 64 candidates at a time
+        int64_t hi = A.sequences;                      // in [lo, hi)
+        const int lane = threadIdx.x & 63;
         while (hi - lo > 1) {
             const int64_t step = (hi - lo + 63) / 64;
             const int64_t c = lo + lane * step;
@@ -267,16 +276,13 @@ __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& A, int64_t 
             hi = lo + step < hi ? lo + step : hi;
         }
     } else {
-        const int64_t n = A.tokens / A.sequences;
-        // first slot of b: b n / stretch + b, between b (n + stretch) / stretch - 1 and that
-        lo = slot * A.stretch / (n + A.stretch);
-        while (lo + 1 < A.sequences && (lo + 1) * n / A.stretch + lo + 1 <= slot) ++lo;
+        lo = slot / A.per_sequence;
     }
     s.b = lo;
     s.begin = start_of(A.starts, A.tokens, A.sequences, lo);
     const int64_t end = start_of(A.starts, A.tokens, A.sequences, lo + 1);
     s.count = end > s.begin ? end - s.begin : 0;
-    s.index = slot - (s.begin / A.stretch + lo);
+    s.index = slot - first_slot(A, lo, s.begin);
     s.lo = s.index * A.stretch;
     s.there = s.index >= 0 && (s.lo < s.count || s.index == 0);
     s.hi = s.lo + A.stretch < s.count ? s.lo + A.stretch : s.count;
@@ -289,12 +295,12 @@ __device__ __forceinline__ float state_value(const Walk& W, int64_t at, int row,
     return W.in_scale * W.state_in[at + (W.transposed ? (int64_t)col * W.dk + row : (int64_t)row * W.dv + col)];
 }
 
-// Sizes of a walk's kernel: DK the padded rows of the state; every wavefront has 16 columns.
-template <typename T, int DK, int WAVES>
+// Sizes of a walk's kernel: DK the padded rows of the state; every wavefront has NT tiles of 16 columns.
+template <typename T, int DK, int WAVES, int NT>
 struct Geometry {
     static constexpr int E = Num<T>::E, K = Num<T>::K, R = Patch<T>::R, THREADS = 64 * WAVES;
     static constexpr int C = (DK > 128 ? 32 : 64) * 2 / (int)sizeof(T);      // tokens of a chunk
-    static constexpr int COLS = 16 * WAVES;                                  // columns of a workgroup
+    static constexpr int COLS = 16 * NT * WAVES;                                  // columns of a workgroup
     static constexpr int ROW = DK * (int)sizeof(T) / 16, SEQ = C * (int)sizeof(T) / 16;   // slots of a row of numbers, of tokens
     static constexpr int CT = C / 16, DT = DK / 16, KD = DK / K, KC = C / K;
     static constexpr int kBytesRows = C * ROW * 16, kBytesK = DK * SEQ * 16, kBytesV = COLS * SEQ * 16, kBytesP = C * SEQ * 16;
@@ -302,11 +308,11 @@ struct Geometry {
 };
 
 // STATES: only what a stretch adds to the state, for the stretches behind it (U below).
-template <typename T, int DK, int WAVES, bool STATES>
-__global__ void __launch_bounds__(64 * WAVES, (DK > 128 ? 2 : DK > 64 ? 4 : 3))      // as many as LDS and, at 256 rows, the state leave room for
+template <typename T, int DK, int WAVES, int NT, bool STATES>
+__global__ void __launch_bounds__(64 * WAVES, (NT > 1 || DK > 128 ? 2 : DK > 64 ? 4 : 3))      // as many as LDS and the state leave room for
 k_attention_walk(AttentionArgs A)
 {
-    typedef Geometry<T, DK, WAVES> G;
+    typedef Geometry<T, DK, WAVES, NT> G;
     typedef typename Num<T>::frag frag;
     typedef typename Num<T>::quad quad;
     constexpr int E = G::E, C = G::C, R = G::R, ROW = G::ROW, SEQ = G::SEQ, CT = G::CT, DT = G::DT, KD = G::KD, KC = G::KC, THREADS = G::THREADS;
@@ -319,11 +325,11 @@ k_attention_walk(AttentionArgs A)
     char* const Ks = Qs + G::kBytesRows;
     char* const Ps = Ks + G::kBytesRows;               // [C][C]
 
-    const Walk W = A.walk[blockIdx.z];
-    const int slice = blockIdx.x % A.slices;
-    const int64_t slot = blockIdx.x / A.slices;
-    const int h = blockIdx.y, col0 = slice * G::COLS;
-    if (col0 >= W.dv) return;
+    // heads side by side: the slots that have nothing to do are then spread over the chiplets, which take workgroups in turn
+    const int walk = blockIdx.z % A.walks, slice = blockIdx.x % A.slices, h = blockIdx.x / A.slices, col0 = slice * G::COLS;
+    const int64_t slot = (int64_t)(blockIdx.z / A.walks) * kSlotRows + blockIdx.y;
+    const Walk W = A.walk[walk];
+    if (slot >= A.slots || col0 >= W.dv) return;
     const Stretch s = find_stretch(A, slot);
     if (!s.there || (STATES && s.last)) return;
 
@@ -344,28 +350,30 @@ k_attention_walk(AttentionArgs A)
     const int64_t first_row = s.begin + (W.reverse ? s.count - 1 - s.lo : s.lo);
     const int64_t sq = back * W.ldq, sk = back * W.ldk, sv = back * W.ldv;
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;      // rows further apart need 64-bit places
-    const bool wide = (A.wide[blockIdx.z] & 7) == 7 && W.ldq < near && W.ldk < near && W.ldv < near, wo = A.wide[blockIdx.z] & 8;
+    const bool wide = (A.wide[walk] & 7) == 7 && W.ldq < near && W.ldk < near && W.ldv < near, wo = A.wide[walk] & 8;
     const bool whole = wide && W.dk == DK && col0 + G::COLS <= W.dv;
 
-    // the state: rows 16 t + 4 g .. + 3, column col0 + 16 wave + r16
-    f32x4 S[DT];
-    const int col = col0 + 16 * wave + r16;
+    // the state: rows 16 t + 4 g .. + 3, columns col0 + 16 (wave NT + c) + r16
+    f32x4 S[DT][NT];
+    const int col = col0 + 16 * wave * NT + r16;
     const int64_t state_at = (s.b * A.heads + h) * (int64_t)W.dk * W.dv;
-    f32x4* const U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * (DK * G::COLS / 4) +
-                     wave * DT * 64 + lane;
+    f32x4* const U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)walk * A.slots + slot) * A.heads + h) * A.slices + slice) * (DK * G::COLS / 4) +
+                     wave * NT * DT * 64 + lane;
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-        f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (!STATES) {
-            if (s.index > 0) v4 = U[t * 64];
-            else if (W.state_in) {
+    for (int c = 0; c < NT; ++c)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (col < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col);
+        for (int t = 0; t < DT; ++t) {
+            f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (!STATES) {
+                if (s.index > 0) v4 = U[(c * DT + t) * 64];
+                else if (W.state_in) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (col + 16 * c < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col + 16 * c);
+                }
             }
+            S[t][c] = v4;
         }
-        S[t] = v4;
-    }
 
     // a chunk's patches
     constexpr int kRowPatches = (C / R) * (DK / 4), kColPatches = (C / R) * (G::COLS / 4);
@@ -411,7 +419,7 @@ k_attention_walk(AttentionArgs A)
     };
     if (s.lo < s.hi) load(s.lo);
     __syncthreads();                                   // the powers are there
-    T* out = static_cast<T*>(W.out) + first_row * W.ldo + (int64_t)h * W.dv + col0 + 16 * wave;      // the chunk's first row
+    T* out = static_cast<T*>(W.out) + first_row * W.ldo + (int64_t)h * W.dv + col0 + 16 * wave * NT;      // the chunk's first row
     const int64_t so = back * W.ldo;
 
     int turn = 0;
@@ -451,9 +459,9 @@ k_attention_walk(AttentionArgs A)
         const int l = here(lane), r16 = l & 15, g = l >> 4;
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
-        Reader<SEQ> values(r16, g);                    // the columns of this wavefront: tile `wave`
-        values.base += wave * 16 * SEQ * 16;
-        values.low ^= ((2 * wave) & Reader<SEQ>::kMask) * 16;
+        Reader<SEQ> values(r16, g);                    // the columns of this wavefront: tiles wave NT + c
+        values.base += wave * NT * 16 * SEQ * 16;
+        values.low ^= ((2 * wave * NT) & Reader<SEQ>::kMask) * 16;
         if (!STATES) {
             // P: tiles on and below the diagonal, dealt to the wavefronts; as it leaves the accumulator a lane holds P[i][j .. j + 3]
 #pragma unroll
@@ -476,72 +484,97 @@ k_attention_walk(AttentionArgs A)
                 }
             }
             // q S, weighted by the rows
-            f32x4 O[CT];
+            f32x4 O[CT][NT];
 #pragma unroll
-            for (int t = 0; t < CT; ++t) O[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int c = 0; c < NT; ++c) O[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int m = 0; m < KD; ++m) {
                 if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);     // (all steps' fragments at once do not fit the registers)
-                frag sf;
-                if constexpr (sizeof(T) == 2) {
-                    // rounded for this product alone, as P is for its own: the result is rounded as much again
+                frag sf[NT];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sf[e] = (__bf16)S[2 * m + (e >> 2)][e & 3];
-                } else {
-                    sf = S[m];
+                for (int c = 0; c < NT; ++c) {
+                    if constexpr (sizeof(T) == 2) {
+                        // rounded for this product alone, as P is for its own: the result is rounded as much again
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sf[c][e] = (__bf16)S[2 * m + (e >> 2)][c][e & 3];
+                    } else {
+                        sf[c] = S[m][c];
+                    }
                 }
 #pragma unroll
-                for (int t = 0; t < CT; ++t) O[t] = mma(sf, get<T>(Qs, rows.at(t, m)), O[t]);
+                for (int t = 0; t < CT; ++t) {
+                    const frag qf = get<T>(Qs, rows.at(t, m));
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) O[t][c] = mma(sf[c], qf, O[t][c]);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < CT; ++t) O[t] *= power[16 * t + r16 + W.lead];
+            for (int t = 0; t < CT; ++t) {
+                const float ahead = power[16 * t + r16 + W.lead];
+#pragma unroll
+                for (int c = 0; c < NT; ++c) O[t][c] *= ahead;
+            }
             __syncthreads();                           // P is there
             const bool slow = odd[turn] != 0;          // a value of v is not finite: 0 * v of the tokens behind a row must not reach it
             if (x == 0) odd[turn ^ 1] = 0;
 #pragma unroll
             for (int m = 0; m < KC; ++m) {
-                frag vf = get<T>(Vt, values.at(0, m));
-                if (slow)
+                frag vf[NT];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
+                for (int c = 0; c < NT; ++c) {
+                    vf[c] = get<T>(Vt, values.at(c, m));
+                    if (slow)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) vf[c][e] = finite_bits((float)vf[c][e]) ? vf[c][e] : (T)0.0f;
+                }
 #pragma unroll
                 for (int t = 0; t < CT; ++t)
-                    if (16 * t + 15 >= m * G::K) O[t] = mma(vf, get<T>(Ps, columns.at(t, m)), O[t]);
+                    if (16 * t + 15 >= m * G::K) {
+                        const frag pf = get<T>(Ps, columns.at(t, m));
+#pragma unroll
+                        for (int c = 0; c < NT; ++c) O[t][c] = mma(vf[c], pf, O[t][c]);
+                    }
             }
             if (slow)
                 for (int j = 0; j < C; ++j) {
-                    const int i0 = here(r16), n0 = here(wave * 16 + 4 * g);
+                    const int i0 = here(r16), n0 = here(wave * NT * 16 + 4 * g);
                     float p[CT];
 #pragma unroll
                     for (int t = 0; t < CT; ++t)
                         p[t] = (float)*reinterpret_cast<const T*>(Ps + 16 * slot_at<SEQ>(16 * t + i0, j / E) + (j % E) * (int)sizeof(T));
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n0 + r, j / E) + (j % E) * (int)sizeof(T));
+                    for (int c = 0; c < NT; ++c)
 #pragma unroll
-                        for (int t = 0; t < CT; ++t)
-                            if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][r] += vj * p[t];
-                    }
+                        for (int r = 0; r < 4; ++r) {
+                            const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n0 + 16 * c + r, j / E) + (j % E) * (int)sizeof(T));
+#pragma unroll
+                            for (int t = 0; t < CT; ++t)
+                                if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][c][r] += vj * p[t];
+                        }
                 }
             if (W.out) {
-                const int n = col0 + 16 * wave + 4 * g;
 #pragma unroll
-                for (int t = 0; t < CT; ++t) {
+                for (int t = 0; t < CT; ++t)
                     if (16 * t + r16 < valid) {
                         T* row = out + (16 * t + r16) * so + 4 * g;
-                        quad w;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][r] * W.out_scale);
-                        if (wo) {
-                            if (n < W.dv) *reinterpret_cast<quad*>(row) = w;
-                        } else {
+                        for (int c = 0; c < NT; ++c) {
+                            const int n = col0 + 16 * (wave * NT + c) + 4 * g;
+                            quad w;
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (n + r < W.dv) row[r] = w[r];
+                            for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
+                            if (wo) {
+                                if (n < W.dv) *reinterpret_cast<quad*>(row + 16 * c) = w;
+                            } else {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (n + r < W.dv) row[16 * c + r] = w[r];
+                            }
                         }
                     }
-                }
             }
             out += C * so;
         }
@@ -552,45 +585,52 @@ k_attention_walk(AttentionArgs A)
         else if (left <= -0.5f * ulp) { d = decay - ulp; left += ulp; }
         if (valid < C) d = end_decay;
 #pragma unroll
-        for (int t = 0; t < DT; ++t) S[t] *= d;
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int c = 0; c < NT; ++c) S[t][c] *= d;
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
             __builtin_amdgcn_sched_barrier(0);
-            const frag vf = get<T>(Vt, values.at(0, m));
-            float xs[E];
+            float w[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) xs[e] = weight[(4 * m + g) * E + e] * (float)vf[e];
-            if constexpr (sizeof(T) == 2) {
-                bf16x8 hi, mid, lo;                    // the state is an fp32 sum of fp32 products whatever the type
-                split3(xs, hi, mid, lo);
+            for (int e = 0; e < E; ++e) w[e] = weight[(4 * m + g) * E + e];
+            // the state is an fp32 sum of fp32 products whatever the type
+            constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
+            frag part[TERMS][NT];
 #pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    const frag kf = get<T>(Kt, columns.at(t, m));
-                    S[t] = mma(kf, hi, S[t]);
-                    S[t] = mma(kf, mid, S[t]);
-                    S[t] = mma(kf, lo, S[t]);
-                }
-            } else {
-                const f32x4 b = {xs[0], xs[1], xs[2], xs[3]};
+            for (int c = 0; c < NT; ++c) {
+                const frag vf = get<T>(Vt, values.at(c, m));
+                float xs[E];
 #pragma unroll
-                for (int t = 0; t < DT; ++t) S[t] = mma(get<T>(Kt, columns.at(t, m)), b, S[t]);
+                for (int e = 0; e < E; ++e) xs[e] = w[e] * (float)vf[e];
+                if constexpr (sizeof(T) == 2) split3(xs, part[0][c], part[1][c], part[2][c]);
+                else part[0][c] = f32x4{xs[0], xs[1], xs[2], xs[3]};
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                const frag kf = get<T>(Kt, columns.at(t, m));
+#pragma unroll
+                for (int p = 0; p < TERMS; ++p)
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) S[t][c] = mma(kf, part[p][c], S[t][c]);
             }
         }
         __syncthreads();                               // the tiles may be written again
     }
 
-    if (STATES) {
 #pragma unroll
-        for (int t = 0; t < DT; ++t) U[t * 64] = S[t];
-    } else if (W.state_out && s.last) {
+    for (int c = 0; c < NT; ++c)
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+        for (int t = 0; t < DT; ++t) {
+            if (STATES) U[(c * DT + t) * 64] = S[t][c];
+            else if (W.state_out && s.last) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * t + 4 * g + r;
-                if (col < W.dv && row < W.dk) W.state_out[state_at + (int64_t)row * W.dv + col] = W.last_scale * S[t][r];
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * t + 4 * g + r, column = col + 16 * c;
+                    if (column < W.dv && row < W.dk) W.state_out[state_at + (int64_t)row * W.dv + column] = W.last_scale * S[t][c][r];
+                }
             }
-    }
+        }
 }
 
 // What enters every stretch but the first: carry_n = l^stretch carry_(n-1) + U_(n-1), carry_0 = the initial state, in the places of the U.
@@ -610,7 +650,7 @@ k_attention_carry(AttentionArgs A)
         const int lane = piece & 63, t = (piece >> 6) % DT, wave = piece / (64 * DT);
         const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
         const int64_t count = end > begin ? end - begin : 0, stretches = (count + A.stretch - 1) / A.stretch;
-        const int64_t slot = begin / A.stretch + b;
+        const int64_t slot = first_slot(A, b, begin);
         if (stretches < 2 || slot + stretches > A.slots) continue;
         const double d = exp(-(double)rate_of(A.rates, h) * (double)A.stretch);
         const float hi = (float)d, lo = (float)(d - (double)hi);
@@ -698,24 +738,38 @@ k_attention_step(AttentionStepArgs A, int lanes_log2, int slices)
 
 struct Plan {
     int dk, cols, slices;              // padded rows of the state, columns of a workgroup, workgroups side by side
-    int64_t stretch, slots;
+    int64_t stretch, per_sequence, slots;
     bool cut;                          // some sequence may have more than one stretch
 };
 
-// By the sizes alone, so that the workspace query and both calls agree (walks: those of the backward call).
-Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv)
+// By the sizes alone.
+Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv, int walks, bool equal)
 {
     Plan P;
     const int most = dk > dv ? dk : dv;
     P.dk = most <= 64 ? 64 : most <= 128 ? 128 : 256;
     P.cols = P.dk == 64 ? 64 : 128;
     P.slices = (most + P.cols - 1) / P.cols;
-    const int64_t workgroups = sequences * heads * P.slices;
-    P.stretch = 512;
-    if (workgroups >= 512) P.stretch = tokens > 512 ? (tokens + 511) / 512 * 512 : 512;
-    P.cut = tokens > P.stretch;
-    P.slots = tokens / P.stretch + sequences;
+    const int64_t longest = equal && sequences > 0 ? tokens / sequences : tokens;
+    // Two workgroups for every compute unit, where cutting is worth its two further launches and the second read of k and v: not where whole sequences
+    // give every compute unit one or nearly (a stretch would be half a sequence or more).  Of unknown lengths four times as many, since the longest
+    // stretch is what the others wait for.  us, stretches of 256 / 512 / 1024 / 2048 / whole sequences: 4 x 2048 tokens, 16 heads 82 / 80 / 128 / - / 164; 65536
+    // tokens, 8 heads 369 / 283 / 258 / 318 / 5155; 8 x 4096, 16 heads 294 / 250 / 229 / 264 / 344, their gradients 835 / 698 / 632 / 592 / 492; 24 sequences of
+    // 1250 tokens on average, 6 heads, fp32 277 / 286 / 530 / 604 / 641, their gradients 694 / 699 / 902 / 1050 / 1061.
+    const int64_t work = tokens * heads * P.slices * walks, workgroups = equal ? 512 : 2048;
+    P.stretch = (work / workgroups + 63) / 64 * 64;
+    if (P.stretch < 256) P.stretch = 256;
+    P.cut = longest > 2 * P.stretch;
+    if (!P.cut) P.stretch = longest < 64 ? 64 : (longest + 63) / 64 * 64;
+    P.per_sequence = equal ? (longest + P.stretch - 1) / P.stretch : 0;
+    if (equal && P.per_sequence < 1) P.per_sequence = 1;
+    P.slots = equal ? sequences * P.per_sequence : tokens / P.stretch + sequences;
     return P;
+}
+
+size_t plan_bytes(const Plan& P, int heads, int walks)
+{
+    return P.cut ? (size_t)walks * P.slots * heads * P.slices * P.dk * P.cols * sizeof(float) : 0;
 }
 
 bool allows(const void* p, int64_t ld, int d, int size, int bytes)
@@ -723,22 +777,23 @@ bool allows(const void* p, int64_t ld, int d, int size, int bytes)
     return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0 && d * size % bytes == 0;
 }
 
-template <typename T, int DK, int WAVES>
+template <typename T, int DK, int WAVES, int NT>
 hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
-    const dim3 grid((unsigned)(P.slots * P.slices), (unsigned)A.heads, (unsigned)A.walks);
+    const int64_t deep = (P.slots + kSlotRows - 1) / kSlotRows;
+    const dim3 grid((unsigned)(A.heads * P.slices), (unsigned)(deep > 1 ? kSlotRows : P.slots), (unsigned)(deep * A.walks));
     if (P.cut) {
         profile_before("attention_states", st);
-        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, true>), grid, dim3(64 * WAVES), 0, st, A);
+        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, NT, true>), grid, dim3(64 * WAVES), 0, st, A);
         profile_after("attention_states", st);
         profile_before("attention_carry", st);
-        const int64_t blocks = A.sequences * P.slices * (DK * 16 * WAVES / 1024), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
-        hipLaunchKernelGGL((k_attention_carry<DK, 16 * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.walks),
+        const int64_t blocks = A.sequences * P.slices * (DK * 16 * NT * WAVES / 1024), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+        hipLaunchKernelGGL((k_attention_carry<DK, 16 * NT * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.walks),
                            dim3(256), 0, st, A);
         profile_after("attention_carry", st);
     }
     profile_before("attention_walk", st);
-    hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, false>), grid, dim3(64 * WAVES), 0, st, A);
+    hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, NT, false>), grid, dim3(64 * WAVES), 0, st, A);
     profile_after("attention_walk", st);
     return hipGetLastError();
 }
@@ -746,25 +801,31 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 template <typename T>
 hipError_t walk_of(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
-    if (P.dk == 64) return walk_with<T, 64, 4>(A, P, st);
-    if (P.dk == 128) return walk_with<T, 128, 8>(A, P, st);
-    return walk_with<T, 256, 8>(A, P, st);
+    if (P.dk == 64) return walk_with<T, 64, 4, 1>(A, P, st);
+    if (P.dk == 128) return walk_with<T, 128, 8, 1>(A, P, st);
+    return walk_with<T, 256, 8, 1>(A, P, st);
 }
 
 }  // namespace
 
 size_t attention_workspace(bool, int64_t tokens, int64_t sequences, int heads, int dk, int dv)
 {
-    const Plan P = plan_of(tokens, sequences, heads, dk, dv);
-    if (!P.cut || sequences == 0) return 0;
-    return (size_t)3 * P.slots * heads * P.slices * P.dk * P.cols * sizeof(float);
+    // the forward and the backward call, with lengths that are equal or not
+    size_t most = 0;
+    for (int walks = 1; walks <= 3; ++walks)
+        for (int equal = 0; equal < 2; ++equal) {
+            if (equal && (sequences == 0 || tokens % sequences != 0)) continue;
+            const size_t bytes = plan_bytes(plan_of(tokens, sequences, heads, dk, dv, walks, equal != 0), heads, walks);
+            most = bytes > most ? bytes : most;
+        }
+    return sequences > 0 && heads > 0 ? most : 0;
 }
 
 hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
 {
     AttentionArgs A = given;
-    const Plan P = plan_of(A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv);
-    A.stretch = P.stretch; A.slots = P.slots; A.slices = P.slices;
+    const Plan P = plan_of(A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv, A.walks, A.starts == nullptr);
+    A.stretch = P.stretch; A.per_sequence = P.per_sequence; A.slots = P.slots; A.slices = P.slices;
     const int size = A.bf16 ? 2 : 4;
     for (int w = 0; w < A.walks; ++w) {
         const Walk& W = A.walk[w];
