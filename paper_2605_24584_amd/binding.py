@@ -173,6 +173,9 @@ def _batch(t):
 def _stream(stream):
     if stream is None:
         import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same handle without an object around it (2.7 us a call)
+        if raw is not None and torch.cuda.is_initialized():
+            return raw(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
@@ -380,17 +383,18 @@ def _type(dtype):
 
 
 def _same_type(first, *others):
+    dtype = first.dtype
     for t in others:
-        if t is not None and t.dtype != first.dtype:
+        if t is not None and t.dtype != dtype:
             raise LaplexError(LAPLEX_ERR_VALUE)
-    return _type(first.dtype)
+    return _type(dtype)
 
 
 def _whole(t, shape, dtype):
     """An array that the library reads or writes from end to end."""
     if t is None:
         return None
-    assert tuple(t.shape) == tuple(shape), f"shape {tuple(t.shape)}, not {tuple(shape)}"
+    assert t.shape == shape, f"shape {tuple(t.shape)}, not {shape}"
     assert t.dtype == dtype, f"type {t.dtype}, not {dtype}"
     assert t.is_contiguous(), "must be contiguous"
     return t.data_ptr()
@@ -400,11 +404,14 @@ def _ld_tokens(t, shape):
     """Row stride of a (tokens, heads, numbers) tensor whose rows are contiguous."""
     if t is None:
         return 0
-    assert tuple(t.shape) == tuple(shape), f"shape {tuple(t.shape)}, not {tuple(shape)}"
-    n, h, d = t.shape
-    assert d <= 1 or h == 0 or n == 0 or t.stride(2) == 1, "a head's numbers must be contiguous"
-    assert h <= 1 or d == 0 or n == 0 or t.stride(1) == d, "the heads of a token must be contiguous"
-    return t.stride(0) if n > 1 else max(h * d, 1)
+    assert t.shape == shape, f"shape {tuple(t.shape)}, not {tuple(shape)}"
+    n, h, d = shape
+    row, head, number = t.stride()
+    if n > 1 and number == 1 and head == d:
+        return row
+    assert d <= 1 or h == 0 or n == 0 or number == 1, "a head's numbers must be contiguous"
+    assert h <= 1 or d == 0 or n == 0 or head == d, "the heads of a token must be contiguous"
+    return row if n > 1 else max(h * d, 1)
 
 
 def laplex_rotary(x, positions, frequencies, y, magnitude: float = 1.0, flags: int = 0, stream=None) -> None:

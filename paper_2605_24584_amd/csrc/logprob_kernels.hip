@@ -17,11 +17,11 @@ namespace laplex {
 
 namespace {
 
-constexpr int kGroup = 16;            // rows whose maximum is kept
-constexpr int kSuper = 8;             // groups that are looked at together first
+constexpr int kGroupBits = 4, kGroup = 1 << kGroupBits;      // rows whose maximum is kept
+constexpr int kSuperBits = 3, kSuper = 1 << kSuperBits;      // groups that are looked at together first
 constexpr int kPick = 16;             // values per lane that a choice is made among
 constexpr int kDirect = 64 * kPick;   // rows that need no groups
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 256, kRowThreadsFew = 64;   // of a workgroup; where those would leave compute units without one
 
 // ----------------------------------------------------------------------------
 // Up to four neighbouring logits; rows need not be aligned to more than one.
@@ -86,13 +86,13 @@ struct RowsArgs {
     float *parts, *maxima;
 };
 
-template <typename T, int VEC, bool TOP>
-__global__ void __launch_bounds__(kRowThreads)
+template <typename T, int VEC, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 k_logprob_rows(RowsArgs A)
 {
-    __shared__ Stats side[kRowThreads / 64][64][VEC];
+    __shared__ Stats side[THREADS / 64][64][VEC];
     const int lanes = 1 << A.lanes_log2, x = threadIdx.x, column_lane = x & (lanes - 1), row_lane = x >> A.lanes_log2;
-    const int row_lanes = kRowThreads >> A.lanes_log2;
+    const int row_lanes = THREADS >> A.lanes_log2;
     const int64_t slab = blockIdx.x % A.slabs, block = blockIdx.x / A.slabs;
     const int64_t t = (slab * lanes + column_lane) * VEC;
     const int have = A.batch - t >= VEC ? VEC : A.batch > t ? (int)(A.batch - t) : 0;
@@ -158,15 +158,15 @@ k_logprob_rows(RowsArgs A)
 #pragma unroll
         for (int c = 0; c < VEC; ++c) {
             Stats all = side[0][x][c];
-            for (int wave = 1; wave < kRowThreads / 64; ++wave) all = join(all, side[wave][x][c], A.c);
+            for (int wave = 1; wave < THREADS / 64; ++wave) all = join(all, side[wave][x][c], A.c);
             if (c < have) { out[c] = all.m; out[A.batch + c] = all.s; out[2 * A.batch + c] = all.w; }
         }
     }
 }
 
 // ----------------------------------------------------------------------------
-// A wavefront chooses the `want` largest of up to 64 N values: keys in the order of the values, key[r] of lane l is value
-// 64 r + l, and of equal ones the first are taken; key 0: no value.
+// A wavefront chooses the `want` largest of up to 64 N values: keys in the order of the values, and of equal ones the first are
+// taken; key 0: no value.
 // ----------------------------------------------------------------------------
 
 // A logit as a whole number in the order of the values: -0 equals +0, NaN comes before all numbers; never 0.
@@ -184,43 +184,72 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
+// The largest bound that at least `want` of the keys reach (0: there are fewer keys but 0), two bits at a time.
+template <int N>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[N], int want)
+{
+    uint32_t bound = 0;
+#pragma unroll 1
+    for (int bit = 30; bit >= 0; bit -= 2) {
+        const uint32_t low = bound | (1u << bit), mid = bound | (2u << bit), high = bound | (3u << bit);
+        int at_low = 0, at_mid = 0, at_high = 0;
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            at_low += __popcll(__ballot(key[r] >= low));
+            at_mid += __popcll(__ballot(key[r] >= mid));
+            at_high += __popcll(__ballot(key[r] >= high));
+        }
+        bound = at_high >= want ? high : at_mid >= want ? mid : at_low >= want ? low : bound;
+    }
+    return bound;
+}
+
 // chosen[0 .. count) <- numbers of the chosen values, ascending; keys[] <- their keys (may be null).  Returns count (uniform).
-__device__ __forceinline__ int choose(const uint32_t (&key)[kPick], int used, int want, int* chosen, uint32_t* keys)
+template <int N>
+__device__ __forceinline__ int choose_among(const uint32_t* stage, int want, int* chosen, uint32_t* keys)
 {
     const int lane = threadIdx.x & 63;
     const uint64_t below = (1ull << lane) - 1ull;
-    // the largest bound that `want` values reach, bit by bit
-    uint32_t bound = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t trial = bound | (1u << bit);
-        int count = 0;
+    uint32_t key[N];
 #pragma unroll
-        for (int r = 0; r < kPick; ++r)
-            if (r < used) count += __popcll(__ballot(key[r] >= trial));
-        if (count >= want) bound = trial;
-    }
+    for (int r = 0; r < N; ++r) key[r] = stage[r * 64 + lane];
+    const uint32_t bound = bound_of(key, want);
     int above = 0;
 #pragma unroll
-    for (int r = 0; r < kPick; ++r)
-        if (r < used) above += __popcll(__ballot(key[r] > bound));
+    for (int r = 0; r < N; ++r) above += __popcll(__ballot(key[r] > bound));
     int equal = bound == 0 ? 0 : want - above, count = 0;      // how many of those at the bound are taken
 #pragma unroll
-    for (int r = 0; r < kPick; ++r)
-        if (r < used) {
-            const uint64_t same = __ballot(key[r] == bound);
-            const bool mine = key[r] > bound || (key[r] == bound && __popcll(same & below) < equal);
-            equal -= __popcll(same);
-            equal = equal < 0 ? 0 : equal;
-            const uint64_t all = __ballot(mine);
-            if (mine) {
-                const int at = count + __popcll(all & below);
-                chosen[at] = r * 64 + lane;
-                if (keys) keys[at] = key[r];
-            }
-            count += __popcll(all);
+    for (int r = 0; r < N; ++r) {
+        const uint64_t same = __ballot(key[r] == bound);
+        const bool mine = key[r] > bound || (key[r] == bound && __popcll(same & below) < equal);
+        equal -= __popcll(same);
+        equal = equal < 0 ? 0 : equal;
+        const uint64_t all = __ballot(mine);
+        if (mine) {
+            const int at = count + __popcll(all & below);
+            chosen[at] = r * 64 + lane;
+            keys[at] = key[r];
         }
+        count += __popcll(all);
+    }
     wave_sync();
     return count;
+}
+
+// `used` times 64 keys in `stage` (room for kDirect; what lies behind those is overwritten)
+__device__ __forceinline__ int choose(uint32_t* stage, int used, int want, int* chosen, uint32_t* keys)
+{
+    const int lane = threadIdx.x & 63;
+    const int padded = used <= 1 ? 1 : used <= 2 ? 2 : used <= 4 ? 4 : used <= 8 ? 8 : kPick;
+    for (int n = used * 64 + lane; n < padded * 64; n += 64) stage[n] = 0;
+    wave_sync();
+    switch (padded) {
+        case 1: return choose_among<1>(stage, want, chosen, keys);
+        case 2: return choose_among<2>(stage, want, chosen, keys);
+        case 4: return choose_among<4>(stage, want, chosen, keys);
+        case 8: return choose_among<8>(stage, want, chosen, keys);
+        default: return choose_among<kPick>(stage, want, chosen, keys);
+    }
 }
 
 struct FinishArgs {
@@ -230,27 +259,72 @@ struct FinishArgs {
     float c;
 };
 
-constexpr int kFinishWaves = 4;
+constexpr int kColumns = 4;             // of a workgroup: read together, finished by a wavefront each
+constexpr int kAhead = 4;               // parts that a lane has asked for at a time
 constexpr int kMaxTop = 64;
 
-template <typename T>
-__global__ void __launch_bounds__(kFinishWaves * 64)
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kColumns * 64)
 k_logprob_finish(FinishArgs F)
 {
-    __shared__ int list_a[kFinishWaves][kMaxTop], list_b[kFinishWaves][kMaxTop];
-    __shared__ uint32_t stage[kFinishWaves][kDirect];      // keys on their way into the registers
-    __shared__ uint32_t keys_a[kFinishWaves][kMaxTop], best_key[kFinishWaves][2 * kMaxTop], best_row[kFinishWaves][2 * kMaxTop];
+    __shared__ Stats side[kColumns * 64][kColumns];
     const LogprobArgs& A = F.L;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t = (int64_t)blockIdx.x * kFinishWaves + wave;
+    const int x = threadIdx.x, lane = x & 63, wave = x >> 6;
+    const int64_t t0 = (int64_t)blockIdx.x * kColumns, t = t0 + wave;
+    const int have = A.batch - t0 < kColumns ? (int)(A.batch - t0) : kColumns;
+
+    {
+        Stats st[kColumns];
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) st[c] = Stats{-INFINITY, 0.0f, 0.0f};
+        for (int64_t p0 = x; p0 < F.part_count; p0 += kColumns * 64 * kAhead) {
+            float m[kAhead][kColumns], s[kAhead][kColumns], w[kAhead][kColumns];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t p = p0 + i * kColumns * 64;
+                if (p < F.part_count) {
+                    const float* const at = F.parts + p * 3 * A.batch + t0;
+                    load_columns<float, kColumns>(m[i], at, have);
+                    load_columns<float, kColumns>(s[i], at + A.batch, have);
+                    load_columns<float, kColumns>(w[i], at + 2 * A.batch, have);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (p0 + i * kColumns * 64 < F.part_count)
+#pragma unroll
+                    for (int c = 0; c < kColumns; ++c) st[c] = join(st[c], Stats{m[i][c], s[i][c], w[i][c]}, F.c);
+        }
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) side[x][c] = st[c];
+    }
+    // groups of groups: what the first level of each column's choice is made among
+    constexpr int kSpan = TOP ? kDirect : 4;
+    __shared__ __attribute__((aligned(16))) uint32_t stage[kColumns][kSpan];      // keys on their way into the registers
+    if (TOP && A.k > kDirect) {
+        const int64_t supers = (F.groups + kSuper - 1) / kSuper;
+        for (int n = x; n < kDirect && n < supers; n += kColumns * 64) {
+            uint32_t most[kColumns] = {};
+            float v[kSuper][kColumns];
+#pragma unroll
+            for (int i = 0; i < kSuper; ++i)
+                if (n * kSuper + i < F.groups) load_columns<float, kColumns>(v[i], F.maxima + (int64_t)(n * kSuper + i) * A.batch + t0, have);
+#pragma unroll
+            for (int i = 0; i < kSuper; ++i)
+                if (n * kSuper + i < F.groups)
+#pragma unroll
+                    for (int c = 0; c < kColumns; ++c) { const uint32_t o = order_of(v[i][c]); most[c] = o > most[c] ? o : most[c]; }
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) stage[c][n] = most[c];
+        }
+    }
+    __syncthreads();
     if (t >= A.batch) return;                        // (nothing below is for the whole workgroup)
     const T* const y = static_cast<const T*>(A.y) + t;
 
-    Stats st{-INFINITY, 0.0f, 0.0f};
-    for (int64_t p = lane; p < F.part_count; p += 64) {
-        const float* const at = F.parts + p * 3 * A.batch + t;
-        st = join(st, Stats{at[0], at[A.batch], at[2 * A.batch]}, F.c);
-    }
+    Stats st = side[lane][wave];
+#pragma unroll
+    for (int n = 1; n < kColumns; ++n) st = join(st, side[n * 64 + lane][wave], F.c);
     for (int step = 32; step >= 1; step >>= 1) {
         const Stats other{__shfl_xor(st.m, step), __shfl_xor(st.s, step), __shfl_xor(st.w, step)};
         st = join(st, other, F.c);
@@ -266,90 +340,73 @@ k_logprob_finish(FinishArgs F)
             A.logp[t] = target >= 0 && target < A.k ? logp_of(to_float(y[target * A.ldy])) : 0.0f;
         }
     }
-    if (A.top == 0) return;
-
-    int *const la = list_a[wave], *const lb = list_b[wave];
-    uint32_t *const ka = keys_a[wave], *const bk = best_key[wave], *const br = best_row[wave];
-    uint32_t* const sk = stage[wave];
-    int best = 0;                                    // values chosen so far, by row, in bk and br
-    auto take = [&](uint32_t (&key)[kPick], int used) {
-        wave_sync();
+    if constexpr (TOP) {
+        __shared__ int lists[kColumns][2][kMaxTop];
+        __shared__ uint32_t keys_a[kColumns][kMaxTop], best_key[kColumns][2 * kMaxTop], best_row[kColumns][2 * kMaxTop];
+        int *const ids = lists[wave][0], *const chosen = lists[wave][1];
+        uint32_t *const ka = keys_a[wave], *const bk = best_key[wave], *const br = best_row[wave], *const sk = stage[wave];
+        int best = 0;                                  // values chosen so far, by row, in bk and br
+        const int want = A.top;
+        // stretches of kDirect groups of groups; a turn for each level, the last of them the rows (a single one where they are few).  One loop, so that the
+        // levels share their instructions: a wavefront goes through them once, and fetching them is most of the time.
+        const int64_t span = (int64_t)kDirect * kSuper * kGroup;
+        for (int64_t first = 0; first < A.k; first += span) {
+            const int64_t left = A.k - first < span ? A.k - first : span, groups = (left + kGroup - 1) / kGroup;
+            const float* const maxima = F.maxima + first / kGroup * A.batch + t;
+            const T* const rows = y + first * A.ldy;
+            int count = 0;
+#pragma unroll 1
+            for (int level = A.k > kDirect ? 0 : 2; level < 3; ++level) {
+                // what is opened (bits of its size), how many there are, and the limit of their numbers
+                const bool whole = level == 0 || A.k <= kDirect;
+                const int bits = level == 1 ? kSuperBits : kGroupBits;
+                const int64_t limit = level == 0 ? (groups + kSuper - 1) / kSuper : level == 1 ? groups : left;
+                const int candidates = whole ? (int)limit : count << bits;
+                const auto number = [&](int n) { return whole ? n : (ids[n >> bits] << bits) + (n & ((1 << bits) - 1)); };
+                if (level == 0) {
+                    for (int n = lane; n < candidates && first > 0; n += 64) {       // (the first stretch's are there)
+                        uint32_t most = 0;
 #pragma unroll
-        for (int r = 0; r < kPick; ++r) key[r] = r < used ? sk[r * 64 + lane] : 0;
-        wave_sync();
-    };
-    const int want = A.top;
-    uint32_t key[kPick];
-    // stretches of kDirect rows, or of kDirect groups of groups
-    const int64_t span = A.k <= kDirect ? kDirect : (int64_t)kDirect * kSuper * kGroup;
-    for (int64_t first = 0; first < A.k; first += span) {
-        int used, count;
-        if (A.k > kDirect) {
-            const int64_t group0 = first / kGroup, left = F.groups - group0;
-            const float* const maxima = F.maxima + group0 * A.batch + t;
-            const int supers = (int)((left + kSuper - 1) / kSuper < kDirect ? (left + kSuper - 1) / kSuper : kDirect);
-            used = (supers + 63) / 64;
-#pragma unroll 2
-            for (int r = 0; r < used; ++r) {
-                const int64_t g = (int64_t)(r * 64 + lane) * kSuper;
-                float v[kSuper];
-#pragma unroll
-                for (int i = 0; i < kSuper; ++i) v[i] = g + i < left ? maxima[(g + i) * A.batch] : -INFINITY;
-                uint32_t most = 0;
-#pragma unroll
-                for (int i = 0; i < kSuper; ++i) { const uint32_t o = order_of(v[i]); most = o > most ? o : most; }
-                sk[r * 64 + lane] = g < left ? most : 0;
-            }
-            take(key, used);
-            count = choose(key, used, want, la, nullptr);
-            const int groups = count * kSuper;
-            used = (groups + 63) / 64;
+                        for (int i = 0; i < kSuper; ++i) {
+                            const uint32_t o = n * kSuper + i < groups ? order_of(maxima[(int64_t)(n * kSuper + i) * A.batch]) : 0;
+                            most = o > most ? o : most;
+                        }
+                        sk[n] = most;
+                    }
+                } else {
 #pragma unroll 4
-            for (int n = lane; n < used * 64; n += 64) {
-                const int64_t g = n < groups ? (int64_t)la[n / kSuper] * kSuper + n % kSuper : left;
-                sk[n] = g < left ? order_of(maxima[g * A.batch]) : 0;
+                    for (int n = lane; n < candidates; n += 64) {
+                        const int id = number(n);
+                        sk[n] = id < limit ? order_of(level == 1 ? maxima[(int64_t)id * A.batch] : to_float(rows[(int64_t)id * A.ldy])) : 0;
+                    }
+                }
+                const int used = (candidates + 63) / 64;
+                for (int n = candidates + lane; n < used * 64; n += 64) sk[n] = 0;
+                count = choose(sk, used, want, chosen, ka);
+                const int id = lane < count ? number(chosen[lane]) : 0;
+                wave_sync();
+                if (lane < count) ids[lane] = id;
+                wave_sync();
             }
-            take(key, used);
-            count = choose(key, used, want, lb, nullptr);
-            for (int n = lane; n < count; n += 64) lb[n] = la[lb[n] / kSuper] * kSuper + lb[n] % kSuper;
+            if (lane < count) { br[best + lane] = (uint32_t)(first + ids[lane]); bk[best + lane] = ka[lane]; }
             wave_sync();
-            const int rows = count * kGroup;
-            used = (rows + 63) / 64;
-#pragma unroll 4
-            for (int n = lane; n < used * 64; n += 64) {
-                const int64_t row = n < rows ? first + (int64_t)lb[n / kGroup] * kGroup + n % kGroup : A.k;
-                sk[n] = row < A.k ? order_of(to_float(y[row * A.ldy])) : 0;
+            best += count;
+            if (best > want) {                         // more than one stretch: the earlier one's rows come first
+                for (int n = lane; n < 128; n += 64) sk[n] = n < best ? bk[n] : 0;
+                best = choose(sk, 2, want, chosen, ka);
+                const uint32_t row = lane < best ? br[chosen[lane]] : 0;
+                wave_sync();
+                if (lane < best) { br[lane] = row; bk[lane] = ka[lane]; }
+                wave_sync();
             }
-        } else {
-            used = (int)((A.k + 63) / 64);
-#pragma unroll 4
-            for (int n = lane; n < used * 64; n += 64) sk[n] = n < A.k ? order_of(to_float(y[n * A.ldy])) : 0;
         }
-        take(key, used);
-        count = choose(key, used, want, la, ka);
-        for (int n = lane; n < count; n += 64) {
-            const int c = la[n];
-            br[best + n] = (uint32_t)(A.k > kDirect ? first + (int64_t)lb[c / kGroup] * kGroup + c % kGroup : c);
-            bk[best + n] = ka[n];
+        if (lane < best) {
+            const uint32_t mine = bk[lane], row = br[lane];
+            int rank = 0;
+            for (int n = 0; n < best; ++n) rank += bk[n] > mine || (bk[n] == mine && n < lane);
+            A.top_ids[rank * A.batch + t] = row;
+            A.top_logp[rank * A.batch + t] = logp_of(to_float(y[row * A.ldy]));
         }
-        wave_sync();
-        best += count;
-        if (best > want) {                           // more than one stretch: the earlier one's rows come first
-#pragma unroll
-            for (int r = 0; r < kPick; ++r) key[r] = r < 2 && r * 64 + lane < best ? bk[r * 64 + lane] : 0;
-            best = choose(key, 2, want, la, ka);
-            const uint32_t row = lane < best ? br[la[lane]] : 0;
-            wave_sync();
-            if (lane < best) { br[lane] = row; bk[lane] = ka[lane]; }
-            wave_sync();
-        }
-    }
-    if (lane < best) {
-        const uint32_t mine = bk[lane], row = br[lane];
-        int rank = 0;
-        for (int n = 0; n < best; ++n) rank += bk[n] > mine || (bk[n] == mine && n < lane);
-        A.top_ids[rank * A.batch + t] = row;
-        A.top_logp[rank * A.batch + t] = logp_of(to_float(y[row * A.ldy]));
     }
 }
 
@@ -422,21 +479,25 @@ k_logprob_backward(BackwardArgs F)
     }
 }
 
+constexpr int64_t kFewWorkgroups = 256;      // compute units
+
 // Lanes across the columns, and how often a thread takes rows: about kTarget workgroups, if there are rows for them.
 struct Shape {
-    int vec, lanes_log2, turns;
+    int vec, lanes_log2, turns, threads;
     int64_t slabs, blocks;
 };
 
 Shape shape_of(int64_t k, int64_t batch, int rows, int64_t target)
 {
     Shape S;
+    S.threads = kRowThreads;
     S.vec = batch >= 4 ? 4 : 1;
     const int64_t wide = (batch + S.vec - 1) / S.vec;
     S.lanes_log2 = 0;
     while (S.lanes_log2 < 6 && (int64_t(1) << S.lanes_log2) < wide) ++S.lanes_log2;
     S.slabs = (wide + (int64_t(1) << S.lanes_log2) - 1) >> S.lanes_log2;
-    const int64_t row_lanes = kRowThreads >> S.lanes_log2, turn = row_lanes * rows, all = (k + turn - 1) / turn;
+    if (rows == kGroup && S.slabs * ((k * (int64_t(1) << S.lanes_log2)) / (kRowThreads * rows)) < kFewWorkgroups) S.threads = kRowThreadsFew;
+    const int64_t row_lanes = S.threads >> S.lanes_log2, turn = row_lanes * rows, all = (k + turn - 1) / turn;
     int64_t blocks = target / S.slabs;
     blocks = blocks < 1 ? 1 : blocks > all ? all : blocks;
     S.turns = (int)((all + blocks - 1) / (blocks ? blocks : 1));
@@ -466,9 +527,14 @@ Plan plan_of(int64_t k, int64_t batch, int64_t top)
 template <typename T, int VEC>
 void rows_with(const RowsArgs& R, bool top, const Plan& P, hipStream_t st)
 {
-    const dim3 grid((unsigned)(P.rows.blocks * P.rows.slabs));
-    if (top) hipLaunchKernelGGL((k_logprob_rows<T, VEC, true>), grid, dim3(kRowThreads), 0, st, R);
-    else hipLaunchKernelGGL((k_logprob_rows<T, VEC, false>), grid, dim3(kRowThreads), 0, st, R);
+    const dim3 grid((unsigned)(P.rows.blocks * P.rows.slabs)), block(P.rows.threads);
+    if (P.rows.threads == kRowThreadsFew) {
+        if (top) hipLaunchKernelGGL((k_logprob_rows<T, VEC, true, kRowThreadsFew>), grid, block, 0, st, R);
+        else hipLaunchKernelGGL((k_logprob_rows<T, VEC, false, kRowThreadsFew>), grid, block, 0, st, R);
+    } else {
+        if (top) hipLaunchKernelGGL((k_logprob_rows<T, VEC, true, kRowThreads>), grid, block, 0, st, R);
+        else hipLaunchKernelGGL((k_logprob_rows<T, VEC, false, kRowThreads>), grid, block, 0, st, R);
+    }
 }
 
 }  // namespace
@@ -490,10 +556,15 @@ hipError_t launch_logprob(const LogprobArgs& A, hipStream_t st)
     }
     FinishArgs F{};
     F.L = A; F.parts = R.parts; F.maxima = R.maxima; F.part_count = A.k > 0 ? P.rows.blocks : 0; F.groups = P.groups; F.c = R.c;
-    const dim3 grid((unsigned)((A.batch + kFinishWaves - 1) / kFinishWaves));
     profile_before("logprob_finish", st);
-    if (A.bf16) hipLaunchKernelGGL((k_logprob_finish<__bf16>), grid, dim3(kFinishWaves * 64), 0, st, F);
-    else hipLaunchKernelGGL((k_logprob_finish<float>), grid, dim3(kFinishWaves * 64), 0, st, F);
+    const dim3 grid((unsigned)((A.batch + kColumns - 1) / kColumns)), block(kColumns * 64);
+    if (A.bf16) {
+        if (A.top > 0) hipLaunchKernelGGL((k_logprob_finish<__bf16, true>), grid, block, 0, st, F);
+        else hipLaunchKernelGGL((k_logprob_finish<__bf16, false>), grid, block, 0, st, F);
+    } else {
+        if (A.top > 0) hipLaunchKernelGGL((k_logprob_finish<float, true>), grid, block, 0, st, F);
+        else hipLaunchKernelGGL((k_logprob_finish<float, false>), grid, block, 0, st, F);
+    }
     profile_after("logprob_finish", st);
     return hipGetLastError();
 }
