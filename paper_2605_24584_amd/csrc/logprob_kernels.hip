@@ -184,13 +184,13 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-// The largest bound that at least `want` of the keys reach (0: there are fewer keys but 0), two bits at a time.
-template <int N>
+// The largest bound, a multiple of 2^LOW, that at least `want` of the keys reach (0: there are fewer keys but 0), two bits at a time.
+template <int N, int LOW>
 __device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[N], int want)
 {
     uint32_t bound = 0;
 #pragma unroll 1
-    for (int bit = 30; bit >= 0; bit -= 2) {
+    for (int bit = 30; bit >= LOW; bit -= 2) {
         const uint32_t low = bound | (1u << bit), mid = bound | (2u << bit), high = bound | (3u << bit);
         int at_low = 0, at_mid = 0, at_high = 0;
 #pragma unroll
@@ -213,7 +213,7 @@ __device__ __forceinline__ int choose_among(const uint32_t* stage, int want, int
     uint32_t key[N];
 #pragma unroll
     for (int r = 0; r < N; ++r) key[r] = stage[r * 64 + lane];
-    const uint32_t bound = bound_of(key, want);
+    const uint32_t bound = bound_of<N, 0>(key, want);
     int above = 0;
 #pragma unroll
     for (int r = 0; r < N; ++r) above += __popcll(__ballot(key[r] > bound));
@@ -252,6 +252,24 @@ __device__ __forceinline__ int choose(uint32_t* stage, int used, int want, int* 
     }
 }
 
+// A bound that at least `want` of `used` times 64 keys in `stage` reach, and few more: the upper halves of the keys alone are looked at.  At least 1.
+template <int N>
+__device__ __forceinline__ uint32_t coarse_among(const uint32_t* stage, int want)
+{
+    uint32_t key[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) key[r] = stage[r * 64 + (threadIdx.x & 63)];
+    const uint32_t bound = bound_of<N, 16>(key, want);
+    return bound ? bound : 1u;
+}
+__device__ __forceinline__ uint32_t coarse(uint32_t* stage, int used, int want)
+{
+    const int padded = used <= 4 ? 4 : kPick;
+    for (int n = used * 64 + (threadIdx.x & 63); n < padded * 64; n += 64) stage[n] = 0;
+    wave_sync();
+    return padded == 4 ? coarse_among<4>(stage, want) : coarse_among<kPick>(stage, want);
+}
+
 struct FinishArgs {
     LogprobArgs L;
     const float *parts, *maxima;
@@ -259,76 +277,101 @@ struct FinishArgs {
     float c;
 };
 
-constexpr int kColumns = 4;             // of a workgroup: read together, finished by a wavefront each
+constexpr int kChiplets = 8;
+constexpr int kFinishThreads = 256;
 constexpr int kAhead = 4;               // parts that a lane has asked for at a time
-constexpr int kMaxTop = 64;
+constexpr int kMaxTop = 64, kOpen = 128, kFound = 192;      // groups that are opened; values among which the places are given: kMaxTop and 128 new ones
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kColumns * 64)
+// COLS columns of a workgroup are read together, and finished by a wavefront each.
+template <typename T, bool TOP, int COLS>
+__global__ void __launch_bounds__(kFinishThreads)
 k_logprob_finish(FinishArgs F)
 {
-    __shared__ Stats side[kColumns * 64][kColumns];
+    __shared__ Stats side[kFinishThreads][COLS];
     const LogprobArgs& A = F.L;
     const int x = threadIdx.x, lane = x & 63, wave = x >> 6;
-    const int64_t t0 = (int64_t)blockIdx.x * kColumns, t = t0 + wave;
-    const int have = A.batch - t0 < kColumns ? (int)(A.batch - t0) : kColumns;
+    // neighbouring columns share lines: they go to one chiplet (workgroups are dealt to the chiplets in turn)
+    const int64_t t0 = ((int64_t)(blockIdx.x % kChiplets) * (gridDim.x / kChiplets) + blockIdx.x / kChiplets) * COLS, t = t0 + wave;
+    if (t0 >= A.batch) return;
+    const int have = A.batch - t0 < COLS ? (int)(A.batch - t0) : COLS;
 
-    {
-        Stats st[kColumns];
+    // groups of groups: what the first level of each column's choice is made among (asked for before the parts are waited for)
+    constexpr int kSpan = TOP ? kDirect : 4;
+    __shared__ __attribute__((aligned(16))) uint32_t stage[COLS][kSpan];      // keys on their way into the registers
+    const int64_t all_supers = (F.groups + kSuper - 1) / kSuper;
+    const int supers = TOP && A.k > kDirect ? (int)(all_supers < kDirect ? all_supers : kDirect) : 0;
+    float v[2][kSuper][COLS];
+    const auto ask = [&](int n0) {
 #pragma unroll
-        for (int c = 0; c < kColumns; ++c) st[c] = Stats{-INFINITY, 0.0f, 0.0f};
-        for (int64_t p0 = x; p0 < F.part_count; p0 += kColumns * 64 * kAhead) {
-            float m[kAhead][kColumns], s[kAhead][kColumns], w[kAhead][kColumns];
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int i = 0; i < kSuper; ++i) {
+                const int n = n0 + a * kFinishThreads;
+                if (n < supers && n * kSuper + i < F.groups)
+                    load_columns<float, COLS>(v[a][i], F.maxima + (int64_t)(n * kSuper + i) * A.batch + t0, have);
+            }
+    };
+    const auto put = [&](int n0) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const int n = n0 + a * kFinishThreads;
+            if (n < supers)
+#pragma unroll
+                for (int c = 0; c < COLS; ++c) {
+                    uint32_t most = 0;
+#pragma unroll
+                    for (int i = 0; i < kSuper; ++i) { const uint32_t o = n * kSuper + i < F.groups ? order_of(v[a][i][c]) : 0; most = o > most ? o : most; }
+                    stage[c][n] = most;
+                }
+        }
+    };
+    if (TOP) ask(x);
+    {
+        Stats st[COLS];
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) st[c] = Stats{-INFINITY, 0.0f, 0.0f};
+        for (int64_t p0 = x; p0 < F.part_count; p0 += kFinishThreads * kAhead) {
+            float m[kAhead][COLS], s[kAhead][COLS], w[kAhead][COLS];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int64_t p = p0 + i * kColumns * 64;
+                const int64_t p = p0 + i * kFinishThreads;
                 if (p < F.part_count) {
                     const float* const at = F.parts + p * 3 * A.batch + t0;
-                    load_columns<float, kColumns>(m[i], at, have);
-                    load_columns<float, kColumns>(s[i], at + A.batch, have);
-                    load_columns<float, kColumns>(w[i], at + 2 * A.batch, have);
+                    load_columns<float, COLS>(m[i], at, have);
+                    load_columns<float, COLS>(s[i], at + A.batch, have);
+                    load_columns<float, COLS>(w[i], at + 2 * A.batch, have);
                 }
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
-                if (p0 + i * kColumns * 64 < F.part_count)
+                if (p0 + i * kFinishThreads < F.part_count)
 #pragma unroll
-                    for (int c = 0; c < kColumns; ++c) st[c] = join(st[c], Stats{m[i][c], s[i][c], w[i][c]}, F.c);
+                    for (int c = 0; c < COLS; ++c) st[c] = join(st[c], Stats{m[i][c], s[i][c], w[i][c]}, F.c);
         }
 #pragma unroll
-        for (int c = 0; c < kColumns; ++c) side[x][c] = st[c];
+        for (int c = 0; c < COLS; ++c) side[x][c] = st[c];
     }
-    // groups of groups: what the first level of each column's choice is made among
-    constexpr int kSpan = TOP ? kDirect : 4;
-    __shared__ __attribute__((aligned(16))) uint32_t stage[kColumns][kSpan];      // keys on their way into the registers
-    if (TOP && A.k > kDirect) {
-        const int64_t supers = (F.groups + kSuper - 1) / kSuper;
-        for (int n = x; n < kDirect && n < supers; n += kColumns * 64) {
-            uint32_t most[kColumns] = {};
-            float v[kSuper][kColumns];
-#pragma unroll
-            for (int i = 0; i < kSuper; ++i)
-                if (n * kSuper + i < F.groups) load_columns<float, kColumns>(v[i], F.maxima + (int64_t)(n * kSuper + i) * A.batch + t0, have);
-#pragma unroll
-            for (int i = 0; i < kSuper; ++i)
-                if (n * kSuper + i < F.groups)
-#pragma unroll
-                    for (int c = 0; c < kColumns; ++c) { const uint32_t o = order_of(v[i][c]); most[c] = o > most[c] ? o : most[c]; }
-#pragma unroll
-            for (int c = 0; c < kColumns; ++c) stage[c][n] = most[c];
-        }
+    if (TOP) {
+        put(x);
+        for (int n = x + 2 * kFinishThreads; n < supers; n += 2 * kFinishThreads) { ask(n); put(n); }
     }
     __syncthreads();
-    if (t >= A.batch) return;                        // (nothing below is for the whole workgroup)
+    if (wave >= COLS || t >= A.batch) return;        // (nothing below is for the whole workgroup)
     const T* const y = static_cast<const T*>(A.y) + t;
 
-    Stats st = side[lane][wave];
+    // the column's maximum, then every lane's sums brought to it, then their sum
+    constexpr int kShares = kFinishThreads / 64;
+    Stats some[kShares], st{-INFINITY, 0.0f, 0.0f};
 #pragma unroll
-    for (int n = 1; n < kColumns; ++n) st = join(st, side[n * 64 + lane][wave], F.c);
-    for (int step = 32; step >= 1; step >>= 1) {
-        const Stats other{__shfl_xor(st.m, step), __shfl_xor(st.s, step), __shfl_xor(st.w, step)};
-        st = join(st, other, F.c);
+    for (int n = 0; n < kShares; ++n) { some[n] = side[n * 64 + lane][wave]; st.m = fmaxf(st.m, some[n].m); }
+    for (int step = 32; step >= 1; step >>= 1) st.m = fmaxf(st.m, __shfl_xor(st.m, step));
+#pragma unroll
+    for (int n = 0; n < kShares; ++n) {
+        rebase(some[n], st.m, F.c);
+        st.s += some[n].s;
+        st.w += some[n].w;
     }
+    for (int step = 32; step >= 1; step >>= 1) { st.s += __shfl_xor(st.s, step); st.w += __shfl_xor(st.w, step); }
     const bool empty = st.m == -INFINITY && st.s == 0.0f;
     const float log_sum = logf(st.s);
     auto logp_of = [&](float v) { return empty ? -INFINITY : (v - st.m) * A.tau - log_sum; };
@@ -341,71 +384,169 @@ k_logprob_finish(FinishArgs F)
         }
     }
     if constexpr (TOP) {
-        __shared__ int lists[kColumns][2][kMaxTop];
-        __shared__ uint32_t keys_a[kColumns][kMaxTop], best_key[kColumns][2 * kMaxTop], best_row[kColumns][2 * kMaxTop];
-        int *const ids = lists[wave][0], *const chosen = lists[wave][1];
-        uint32_t *const ka = keys_a[wave], *const bk = best_key[wave], *const br = best_row[wave], *const sk = stage[wave];
-        int best = 0;                                  // values chosen so far, by row, in bk and br
+        __shared__ int lists[COLS][2][kMaxTop], open[COLS][2][kOpen];
+        __shared__ uint32_t keys[COLS][kMaxTop];
+        __shared__ __attribute__((aligned(16))) uint32_t found_key[COLS][kFound], found_row[COLS][kFound];
+        uint32_t *const fk = found_key[wave], *const fr = found_row[wave], *const sk = stage[wave];
+        int *const ol = open[wave][0], *const op = open[wave][1];
+        int best = 0;                                  // fk, fr [0, best): the largest so far, in their order
         const int want = A.top;
-        // stretches of kDirect groups of groups; a turn for each level, the last of them the rows (a single one where they are few).  One loop, so that the
-        // levels share their instructions: a wavefront goes through them once, and fetching them is most of the time.
+        const uint64_t below = (1ull << lane) - 1ull;
+        // stretches of kDirect groups of groups
         const int64_t span = (int64_t)kDirect * kSuper * kGroup;
         for (int64_t first = 0; first < A.k; first += span) {
             const int64_t left = A.k - first < span ? A.k - first : span, groups = (left + kGroup - 1) / kGroup;
             const float* const maxima = F.maxima + first / kGroup * A.batch + t;
             const T* const rows = y + first * A.ldy;
-            int count = 0;
-#pragma unroll 1
-            for (int level = A.k > kDirect ? 0 : 2; level < 3; ++level) {
-                // what is opened (bits of its size), how many there are, and the limit of their numbers
-                const bool whole = level == 0 || A.k <= kDirect;
-                const int bits = level == 1 ? kSuperBits : kGroupBits;
-                const int64_t limit = level == 0 ? (groups + kSuper - 1) / kSuper : level == 1 ? groups : left;
-                const int candidates = whole ? (int)limit : count << bits;
-                const auto number = [&](int n) { return whole ? n : (ids[n >> bits] << bits) + (n & ((1 << bits) - 1)); };
-                if (level == 0) {
-                    for (int n = lane; n < candidates && first > 0; n += 64) {       // (the first stretch's are there)
-                        uint32_t most = 0;
+            const bool direct = A.k <= kDirect;
+            const auto group_key = [&](int g) { return order_of(maxima[(int64_t)g * A.batch]); };
+            const auto super_key = [&](int n) {
+                uint32_t most = 0;
 #pragma unroll
-                        for (int i = 0; i < kSuper; ++i) {
-                            const uint32_t o = n * kSuper + i < groups ? order_of(maxima[(int64_t)(n * kSuper + i) * A.batch]) : 0;
-                            most = o > most ? o : most;
-                        }
-                        sk[n] = most;
+                for (int i = 0; i < kSuper; ++i) {
+                    const uint32_t o = n * kSuper + i < groups ? group_key(n * kSuper + i) : 0;
+                    most = o > most ? o : most;
+                }
+                return most;
+            };
+            const auto row_key = [&](int r) { return order_of(to_float(rows[(int64_t)r * A.ldy])); };
+            // sk[n] <- f(n), n < total: eight of a lane's loads at a time
+            const auto gather = [&](int total, auto f) {
+                for (int n0 = lane; n0 < total; n0 += 64 * 8) {
+                    uint32_t k[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) k[i] = n0 + i * 64 < total ? f(n0 + i * 64) : 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (n0 + i * 64 < total) sk[n0 + i * 64] = k[i];
+                }
+                wave_sync();
+            };
+            // keys of the groups of groups (the first stretch's are there), or of the rows where they are few
+            const int whole = direct ? (int)left : (int)((groups + kSuper - 1) / kSuper);
+            if (direct) {
+                gather(whole, row_key);
+            } else if (first > 0) {
+                for (int n = lane; n < whole; n += 64) sk[n] = super_key(n);
+            }
+            const int used = (whole + 63) / 64;
+            for (int n = whole + lane; n < used * 64; n += 64) sk[n] = 0;
+            // What reaches a bound that `want` of them reach: those are opened, and again what reaches it.  Where many values are equal it may be more
+            // than there is room for.
+            const uint32_t bound = coarse(sk, used, want);
+            int found = best;
+            bool fits = true;
+            if (direct) {
+                for (int n = lane; n < used * 64; n += 64) {
+                    const uint32_t k = sk[n];
+                    const uint64_t all = __ballot(k >= bound);
+                    const int at = found + __popcll(all & below);
+                    if (k >= bound && at < kFound) { fk[at] = k; fr[at] = (uint32_t)n; }
+                    found += __popcll(all);
+                }
+            } else {
+                int listed = 0, opened = 0;
+                for (int n = lane; n < used * 64; n += 64) {
+                    const bool in = sk[n] >= bound;
+                    const uint64_t all = __ballot(in);
+                    const int at = listed + __popcll(all & below);
+                    if (in && at < kOpen) ol[at] = n;
+                    listed += __popcll(all);
+                }
+                wave_sync();
+                fits = listed <= kOpen;
+                // (all loads of a level at a time, then what of it is kept)
+                for (int n0 = 0; fits && n0 < listed * kSuper; n0 += kDirect) {
+                    const int some = listed * kSuper - n0 < kDirect ? listed * kSuper - n0 : kDirect;
+                    gather(some, [&](int n) {
+                        const int g = ol[(n0 + n) >> kSuperBits] * kSuper + (n & (kSuper - 1));
+                        return g < groups ? group_key(g) : 0;
+                    });
+                    for (int n = lane; n < (some + 63) / 64 * 64; n += 64) {
+                        const bool in = n < some && sk[n] >= bound;
+                        const uint64_t all = __ballot(in);
+                        const int at = opened + __popcll(all & below);
+                        if (in && at < kOpen) op[at] = ol[(n0 + n) >> kSuperBits] * kSuper + (n & (kSuper - 1));
+                        opened += __popcll(all);
                     }
-                } else {
+                    wave_sync();
+                }
+                fits = fits && opened <= kOpen;
+                for (int n0 = 0; fits && n0 < opened * kGroup; n0 += kDirect) {
+                    const int some = opened * kGroup - n0 < kDirect ? opened * kGroup - n0 : kDirect;
+                    gather(some, [&](int n) {
+                        const int row = op[(n0 + n) >> kGroupBits] * kGroup + (n & (kGroup - 1));
+                        return row < left ? row_key(row) : 0;
+                    });
+                    for (int n = lane; n < (some + 63) / 64 * 64; n += 64) {
+                        const uint32_t k = n < some ? sk[n] : 0;
+                        const uint64_t all = __ballot(k >= bound);
+                        const int at = found + __popcll(all & below);
+                        if (k >= bound && at < kFound) { fk[at] = k; fr[at] = (uint32_t)(first + op[(n0 + n) >> kGroupBits] * kGroup + (n & (kGroup - 1))); }
+                        found += __popcll(all);
+                    }
+                    wave_sync();
+                }
+            }
+            if (!fits || found > kFound) {
+                // Level by level, the `want` first ones of each: no more than that are ever held.
+                int *const ids = lists[wave][0], *const chosen = lists[wave][1];
+                int count = 0;
+#pragma unroll 1
+                for (int level = direct ? 2 : 0; level < 3; ++level) {
+                    // what is opened (bits of its size), how many there are, and the limit of their numbers
+                    const bool all = level == 0 || direct;
+                    const int bits = level == 1 ? kSuperBits : kGroupBits;
+                    const int64_t limit = level == 1 ? groups : left;
+                    const int candidates = all ? whole : count << bits;
+                    const auto number = [&](int n) { return all ? n : (ids[n >> bits] << bits) + (n & ((1 << bits) - 1)); };
 #pragma unroll 4
                     for (int n = lane; n < candidates; n += 64) {
                         const int id = number(n);
-                        sk[n] = id < limit ? order_of(level == 1 ? maxima[(int64_t)id * A.batch] : to_float(rows[(int64_t)id * A.ldy])) : 0;
+                        sk[n] = level == 0 ? super_key(id) : id >= limit ? 0 : level == 1 ? group_key(id) : row_key(id);
                     }
+                    const int some = (candidates + 63) / 64;
+                    for (int n = candidates + lane; n < some * 64; n += 64) sk[n] = 0;
+                    count = choose(sk, some, want, chosen, keys[wave]);
+                    const int id = lane < count ? number(chosen[lane]) : 0;
+                    wave_sync();
+                    if (lane < count) ids[lane] = id;
+                    wave_sync();
                 }
-                const int used = (candidates + 63) / 64;
-                for (int n = candidates + lane; n < used * 64; n += 64) sk[n] = 0;
-                count = choose(sk, used, want, chosen, ka);
-                const int id = lane < count ? number(chosen[lane]) : 0;
-                wave_sync();
-                if (lane < count) ids[lane] = id;
-                wave_sync();
+                if (lane < count) { fr[best + lane] = (uint32_t)(first + ids[lane]); fk[best + lane] = keys[wave][lane]; }
+                found = best + count;
             }
-            if (lane < count) { br[best + lane] = (uint32_t)(first + ids[lane]); bk[best + lane] = ka[lane]; }
             wave_sync();
-            best += count;
-            if (best > want) {                         // more than one stretch: the earlier one's rows come first
-                for (int n = lane; n < 128; n += 64) sk[n] = n < best ? bk[n] : 0;
-                best = choose(sk, 2, want, chosen, ka);
-                const uint32_t row = lane < best ? br[chosen[lane]] : 0;
-                wave_sync();
-                if (lane < best) { br[lane] = row; bk[lane] = ka[lane]; }
-                wave_sync();
+            // the places of all that was found, those of earlier stretches among it
+            for (int n = found + lane; n < (found + 63) / 64 * 64; n += 64) { fk[n] = 0; fr[n] = 0xFFFFFFFFu; }
+            wave_sync();
+            uint32_t k[kFound / 64], row[kFound / 64];
+            int place[kFound / 64];
+#pragma unroll
+            for (int i = 0; i < kFound / 64; ++i) {
+                place[i] = kFound;
+                if (i * 64 >= found) continue;
+                k[i] = fk[i * 64 + lane];
+                row[i] = fr[i * 64 + lane];
+                int before = 0;
+#pragma unroll 2
+                for (int j = 0; j < found; j += 4) {
+                    const uint4 ok = *reinterpret_cast<const uint4*>(fk + j), orow = *reinterpret_cast<const uint4*>(fr + j);
+                    before += (ok.x > k[i] || (ok.x == k[i] && orow.x < row[i])) + (ok.y > k[i] || (ok.y == k[i] && orow.y < row[i])) +
+                              (ok.z > k[i] || (ok.z == k[i] && orow.z < row[i])) + (ok.w > k[i] || (ok.w == k[i] && orow.w < row[i]));
+                }
+                if (i * 64 + lane < found) place[i] = before;
             }
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < kFound / 64; ++i)
+                if (place[i] < want) { fk[place[i]] = k[i]; fr[place[i]] = row[i]; }
+            best = found < want ? found : want;
+            wave_sync();
         }
         if (lane < best) {
-            const uint32_t mine = bk[lane], row = br[lane];
-            int rank = 0;
-            for (int n = 0; n < best; ++n) rank += bk[n] > mine || (bk[n] == mine && n < lane);
-            A.top_ids[rank * A.batch + t] = row;
-            A.top_logp[rank * A.batch + t] = logp_of(to_float(y[row * A.ldy]));
+            A.top_ids[lane * A.batch + t] = fr[lane];
+            A.top_logp[lane * A.batch + t] = logp_of(to_float(y[fr[lane] * A.ldy]));
         }
     }
 }
@@ -537,6 +678,15 @@ void rows_with(const RowsArgs& R, bool top, const Plan& P, hipStream_t st)
     }
 }
 
+template <typename T, int COLS>
+void finish_with(const FinishArgs& F, hipStream_t st)
+{
+    const int64_t blocks = (F.L.batch + COLS - 1) / COLS;
+    const dim3 grid((unsigned)((blocks + kChiplets - 1) / kChiplets * kChiplets)), block(kFinishThreads);
+    if (F.L.top > 0) hipLaunchKernelGGL((k_logprob_finish<T, true, COLS>), grid, block, 0, st, F);
+    else hipLaunchKernelGGL((k_logprob_finish<T, false, COLS>), grid, block, 0, st, F);
+}
+
 }  // namespace
 
 size_t logprob_workspace(int64_t k, int64_t batch, int64_t top) { return batch ? plan_of(k, batch, top).total : 0; }
@@ -557,14 +707,8 @@ hipError_t launch_logprob(const LogprobArgs& A, hipStream_t st)
     FinishArgs F{};
     F.L = A; F.parts = R.parts; F.maxima = R.maxima; F.part_count = A.k > 0 ? P.rows.blocks : 0; F.groups = P.groups; F.c = R.c;
     profile_before("logprob_finish", st);
-    const dim3 grid((unsigned)((A.batch + kColumns - 1) / kColumns)), block(kColumns * 64);
-    if (A.bf16) {
-        if (A.top > 0) hipLaunchKernelGGL((k_logprob_finish<__bf16, true>), grid, block, 0, st, F);
-        else hipLaunchKernelGGL((k_logprob_finish<__bf16, false>), grid, block, 0, st, F);
-    } else {
-        if (A.top > 0) hipLaunchKernelGGL((k_logprob_finish<float, true>), grid, block, 0, st, F);
-        else hipLaunchKernelGGL((k_logprob_finish<float, false>), grid, block, 0, st, F);
-    }
+    if (A.bf16) { if (P.rows.vec == 4) finish_with<__bf16, 4>(F, st); else finish_with<__bf16, 1>(F, st); }
+    else { if (P.rows.vec == 4) finish_with<float, 4>(F, st); else finish_with<float, 1>(F, st); }
     profile_after("logprob_finish", st);
     return hipGetLastError();
 }
