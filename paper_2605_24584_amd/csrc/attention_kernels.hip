@@ -217,6 +217,16 @@ __device__ __forceinline__ void split3(const float* x, bf16x8& hi, bf16x8& mid, 
     hi = uppers(x); mid = uppers(r); lo = uppers(q);
 }
 
+__device__ __forceinline__ void split2(const float* x, bf16x8& hi, bf16x8& mid)
+{
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = x[e] - upper(x[e]);
+    hi = uppers(x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mid[e] = (__bf16)r[e];
+}
+
 __device__ __forceinline__ bool finite_bits(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
 __device__ __forceinline__ bool finite_patch(const Patch<float>& p)
 {
@@ -301,7 +311,7 @@ struct Geometry {
     static constexpr int E = Num<T>::E, K = Num<T>::K, R = Patch<T>::R, THREADS = 64 * WAVES;
     static constexpr int C = (DK > 128 ? 32 : 64) * 2 / (int)sizeof(T);      // tokens of a chunk
     static constexpr int COLS = 16 * NT * WAVES;                                  // columns of a workgroup
-    static constexpr int ROW = DK * (int)sizeof(T) / 16, SEQ = C * (int)sizeof(T) / 16;   // slots of a row of numbers, of tokens
+    static constexpr int ROW = (DK * (int)sizeof(T) / 16 + 7) / 8 * 8, SEQ = C * (int)sizeof(T) / 16;   // slots of a row of numbers (a multiple of 8: they are permuted by eights), of tokens
     static constexpr int CT = C / 16, DT = DK / 16, KD = DK / K, KC = C / K;
     static constexpr int kBytesRows = C * ROW * 16, kBytesK = DK * SEQ * 16, kBytesV = COLS * SEQ * 16, kBytesP = C * SEQ * 16;
     static constexpr int kLds = 2 * kBytesRows + kBytesK + kBytesV + kBytesP;
@@ -309,7 +319,7 @@ struct Geometry {
 
 // STATES: only what a stretch adds to the state, for the stretches behind it (U below).
 template <typename T, int DK, int WAVES, int NT, bool STATES>
-__global__ void __launch_bounds__(64 * WAVES, (NT > 1 || DK > 128 ? 2 : DK > 64 ? 4 : 3))      // as many as LDS and the state leave room for
+__global__ void __launch_bounds__(64 * WAVES, (NT > 1 || DK > 128 ? 2 : DK > 96 ? 4 : DK > 64 && sizeof(T) == 4 ? 5 : 3))      // as many as LDS and the state leave room for
 k_attention_walk(AttentionArgs A)
 {
     typedef Geometry<T, DK, WAVES, NT> G;
@@ -594,7 +604,6 @@ k_attention_walk(AttentionArgs A)
             float w[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) w[e] = weight[(4 * m + g) * E + e];
-            // the state is an fp32 sum of fp32 products whatever the type
             constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
             frag part[TERMS][NT];
 #pragma unroll
@@ -603,16 +612,20 @@ k_attention_walk(AttentionArgs A)
                 float xs[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) xs[e] = w[e] * (float)vf[e];
-                if constexpr (sizeof(T) == 2) split3(xs, part[0][c], part[1][c], part[2][c]);
-                else part[0][c] = f32x4{xs[0], xs[1], xs[2], xs[3]};
+                if constexpr (sizeof(T) == 2) {
+                    // all 24 bits where the state can be asked for, 16 where it only goes on into results of 8
+                    if (W.exact) split3(xs, part[0][c], part[1][c], part[2][c]);
+                    else split2(xs, part[0][c], part[1][c]);
+                } else part[0][c] = f32x4{xs[0], xs[1], xs[2], xs[3]};
             }
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
                 const frag kf = get<T>(Kt, columns.at(t, m));
 #pragma unroll
                 for (int p = 0; p < TERMS; ++p)
+                    if (p < 2 || W.exact)
 #pragma unroll
-                    for (int c = 0; c < NT; ++c) S[t][c] = mma(kf, part[p][c], S[t][c]);
+                        for (int c = 0; c < NT; ++c) S[t][c] = mma(kf, part[p][c], S[t][c]);
             }
         }
         __syncthreads();                               // the tiles may be written again
@@ -639,13 +652,13 @@ template <int DK, int COLS>
 __global__ void __launch_bounds__(256)
 k_attention_carry(AttentionArgs A)
 {
-    constexpr int kPieces = DK * COLS / 4, kBlocks = kPieces / 256;
+    constexpr int kPieces = DK * COLS / 4, kBlocks = (kPieces + 255) / 256;
     const Walk W = A.walk[blockIdx.z];
     for (int64_t block = blockIdx.x; block < A.sequences * A.slices * kBlocks; block += gridDim.x) {
         const int64_t b = block / (A.slices * kBlocks);
         const int rest = (int)(block % (A.slices * kBlocks)), slice = rest / kBlocks, piece = (rest % kBlocks) * 256 + threadIdx.x;
         const int h = blockIdx.y, col0 = slice * COLS;
-        if (col0 >= W.dv) continue;
+        if (col0 >= W.dv || piece >= kPieces) continue;
         constexpr int DT = DK / 16;
         const int lane = piece & 63, t = (piece >> 6) % DT, wave = piece / (64 * DT);
         const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
@@ -747,8 +760,8 @@ Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv, int w
 {
     Plan P;
     const int most = dk > dv ? dk : dv;
-    P.dk = most <= 64 ? 64 : most <= 128 ? 128 : 256;
-    P.cols = P.dk == 64 ? 64 : 128;
+    P.dk = most <= 64 ? 64 : most <= 96 ? 96 : most <= 128 ? 128 : most <= 192 ? 192 : 256;
+    P.cols = P.dk == 64 ? 64 : P.dk == 96 || P.dk == 192 ? 96 : 128;
     P.slices = (most + P.cols - 1) / P.cols;
     const int64_t longest = equal && sequences > 0 ? tokens / sequences : tokens;
     // Two workgroups for every compute unit, where cutting is worth its two further launches and the second read of k and v: not where whole sequences
@@ -787,7 +800,7 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
         hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, NT, true>), grid, dim3(64 * WAVES), 0, st, A);
         profile_after("attention_states", st);
         profile_before("attention_carry", st);
-        const int64_t blocks = A.sequences * P.slices * (DK * 16 * NT * WAVES / 1024), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+        const int64_t blocks = A.sequences * P.slices * ((DK * 16 * NT * WAVES / 4 + 255) / 256), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
         hipLaunchKernelGGL((k_attention_carry<DK, 16 * NT * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.walks),
                            dim3(256), 0, st, A);
         profile_after("attention_carry", st);
@@ -802,7 +815,9 @@ template <typename T>
 hipError_t walk_of(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
     if (P.dk == 64) return walk_with<T, 64, 4, 1>(A, P, st);
+    if (P.dk == 96) return walk_with<T, 96, 6, 1>(A, P, st);
     if (P.dk == 128) return walk_with<T, 128, 8, 1>(A, P, st);
+    if (P.dk == 192) return walk_with<T, 192, 6, 1>(A, P, st);
     return walk_with<T, 256, 8, 1>(A, P, st);
 }
 

@@ -138,7 +138,7 @@ int laplex_decay_attention(const void* q, int64_t ldq, const void* k, int64_t ld
     A.bf16 = type == LAPLEX_BF16; A.ws = static_cast<char*>(ws);
     Walk& W = A.walk[A.walks++];
     W.q = q; W.ldq = ldq; W.k = k; W.ldk = ldk; W.v = v; W.ldv = ldv; W.out = y; W.ldo = ldy;
-    W.dk = (int)dk; W.dv = (int)dv; W.lead = 1;
+    W.dk = (int)dk; W.dv = (int)dv; W.lead = 1; W.exact = 1;
     W.state_in = state_in; W.in_scale = 1.0f;
     W.state_out = state_out; W.last_scale = 1.0f;
     W.out_scale = scale;
@@ -180,7 +180,7 @@ int laplex_decay_attention_backward(const void* q, int64_t ldq, const void* k, i
     if (gv || gstate_in) {      // back: queries k, keys q, values gy
         Walk& W = A.walk[A.walks++];
         W.q = k; W.ldq = ldk; W.k = q; W.ldk = ldq; W.v = gy; W.ldv = ldgy; W.out = gv; W.ldo = ldgv;
-        W.dk = (int)dk; W.dv = (int)dv; W.reverse = 1;
+        W.dk = (int)dk; W.dv = (int)dv; W.reverse = 1; W.exact = 1;
         W.state_in = gstate_out; W.in_scale = 1.0f / scale; W.out_scale = scale;
         W.state_out = gstate_in; W.last_scale = scale;
     }

@@ -39,6 +39,7 @@ struct Walk {
     int64_t ldq, ldk, ldv, ldo;
     int dk, dv;                      // of this walk: the state is dk x dv
     int reverse, lead, transposed;   // transposed: state_in lies as dv x dk
+    int exact;                       // the walk's state can be asked for: an fp32 sum of fp32 products, whether it is or not (so that `out` has the same bits)
     const float* state_in;           // [sequences][heads][dk][dv] (or [dv][dk]) or null
     float* state_out;                // the same, never transposed, or null
     float in_scale, out_scale, last_scale;
