@@ -361,7 +361,7 @@ k_attention_walk(AttentionArgs A)
     const int64_t sq = back * W.ldq, sk = back * W.ldk, sv = back * W.ldv;
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;      // rows further apart need 64-bit places
     const bool wide = (A.wide[walk] & 7) == 7 && W.ldq < near && W.ldk < near && W.ldv < near, wo = A.wide[walk] & 8;
-    const bool whole = wide && W.dk == DK && col0 + G::COLS <= W.dv;
+    const bool whole = wide && W.dk == DK && col0 + G::COLS <= W.dv, whole_out = W.out && wo && col0 + G::COLS <= W.dv;
 
     // the state: rows 16 t + 4 g .. + 3, columns col0 + 16 (wave NT + c) + r16
     f32x4 S[DT][NT];
@@ -565,26 +565,34 @@ k_attention_walk(AttentionArgs A)
                                 if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][c][r] += vj * p[t];
                         }
                 }
-            if (W.out) {
+            const auto result = [&](int t, int c) {
+                quad w;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
+                return w;
+            };
+            if (whole_out && valid == C) {
 #pragma unroll
                 for (int t = 0; t < CT; ++t)
-                    if (16 * t + r16 < valid) {
-                        T* row = out + (16 * t + r16) * so + 4 * g;
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) *reinterpret_cast<quad*>(out + (16 * t + r16) * so + 4 * g + 16 * c) = result(t, c);
+            } else if (W.out) {
+#pragma unroll
+                for (int t = 0; t < CT; ++t)
+                    if (16 * t + r16 < valid)
 #pragma unroll
                         for (int c = 0; c < NT; ++c) {
                             const int n = col0 + 16 * (wave * NT + c) + 4 * g;
-                            quad w;
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
+                            T* const at = out + (16 * t + r16) * so + 4 * g + 16 * c;
+                            const quad w = result(t, c);
                             if (wo) {
-                                if (n < W.dv) *reinterpret_cast<quad*>(row + 16 * c) = w;
+                                if (n < W.dv) *reinterpret_cast<quad*>(at) = w;
                             } else {
 #pragma unroll
                                 for (int r = 0; r < 4; ++r)
-                                    if (n + r < W.dv) row[16 * c + r] = w[r];
+                                    if (n + r < W.dv) at[r] = w[r];
                             }
                         }
-                    }
             }
             out += C * so;
         }
