@@ -375,7 +375,8 @@ k_attention_walk(AttentionArgs A)
         for (int t = 0; t < DT; ++t) {
             f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
             if (!STATES) {
-                if (s.index > 0) v4 = U[(c * DT + t) * 64];
+                // (of sequences that are cut the initial state, too, comes from U: another workgroup may already write the last state, in its place)
+                if (A.cut ? s.index > 0 || W.state_in : 0) v4 = U[(c * DT + t) * 64];
                 else if (W.state_in) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
@@ -654,7 +655,7 @@ k_attention_walk(AttentionArgs A)
         }
 }
 
-// What enters every stretch but the first: carry_n = l^stretch carry_(n-1) + U_(n-1), carry_0 = the initial state, in the places of the U.
+// What enters the stretches: carry_n = l^stretch carry_(n-1) + U_(n-1), carry_0 = the initial state, in the places of the U.
 // A thread per four rows of a column of the state.
 template <int DK, int COLS>
 __global__ void __launch_bounds__(256)
@@ -672,7 +673,7 @@ k_attention_carry(AttentionArgs A)
         const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
         const int64_t count = end > begin ? end - begin : 0, stretches = (count + A.stretch - 1) / A.stretch;
         const int64_t slot = first_slot(A, b, begin);
-        if (stretches < 2 || slot + stretches > A.slots) continue;
+        if ((stretches < 2 && !W.state_in) || slot >= A.slots || slot + stretches > A.slots) continue;
         const double d = exp(-(double)rate_of(A.rates, h) * (double)A.stretch);
         const float hi = (float)d, lo = (float)(d - (double)hi);
         f32x4 carry = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -686,7 +687,9 @@ k_attention_carry(AttentionArgs A)
         }
         const int64_t step = (int64_t)A.heads * A.slices * kPieces;
         f32x4* U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * kPieces + piece;
-        f32x4 next = U[0];
+        f32x4 next = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (stretches > 1) next = U[0];
+        if (W.state_in) U[0] = carry;
         for (int64_t n = 1; n < stretches; ++n) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) carry[r] = fmaf(carry[r], hi, fmaf(carry[r], lo, next[r]));
@@ -848,7 +851,7 @@ hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
 {
     AttentionArgs A = given;
     const Plan P = plan_of(A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv, A.walks, A.starts == nullptr);
-    A.stretch = P.stretch; A.per_sequence = P.per_sequence; A.slots = P.slots; A.slices = P.slices;
+    A.cut = P.cut; A.stretch = P.stretch; A.per_sequence = P.per_sequence; A.slots = P.slots; A.slices = P.slices;
     const int size = A.bf16 ? 2 : 4;
     for (int w = 0; w < A.walks; ++w) {
         const Walk& W = A.walk[w];

@@ -55,6 +55,7 @@ struct AttentionArgs {
     bool bf16;
     char* ws;
     // filled in by launch_attention
+    int cut;                         // some sequence may have more than one stretch
     int64_t stretch, per_sequence, slots;   // tokens of a stretch that one workgroup walks; stretches of a sequence (equal lengths), of all, at most
     int slices;                      // workgroups side by side over the columns
     int wide[3];                     // per walk, a bit each for q, k, v, out: its rows may be accessed four numbers at a time

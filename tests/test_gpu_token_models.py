@@ -221,6 +221,30 @@ def test_attention_prompt_then_steps_is_the_longer_prompt():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths", [[5000], [1, 0, 3000, 700, 2, 1500], [64] * 3 + [2800]])
+def test_attention_state_in_place_of_sequences_in_stretches(dtype, lengths):
+    """The state that a long prompt begins from and leaves in one buffer: the same bits as in two."""
+    r = seeded("in place", lengths)
+    heads, dk, dv = 2, 64, 48
+    parts, rates, (state, _) = attention_inputs(r, lengths, heads, dk, dv, dtype, True)
+    (q, _), (k, _), (v, _) = parts
+    n, b = sum(lengths), len(lengths)
+    starts = dev(np.concatenate([[0], np.cumsum(lengths)]), torch.int64)
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(dtype, n, b, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    y, last = run_forward(parts, rates, state, lengths, dv, 0.3, True)
+    for _ in range(3):
+        same, z = state.clone(), torch.full_like(y, float("nan"))
+        B.laplex_decay_attention(q, k, v, dev(rates), z, ws, 0.3, b, starts, same, same)
+        assert torch.equal(z, y) and torch.equal(same, last)
+    # and with the stretches against the oracle, a head of the longest sequence
+    i = int(np.argmax(lengths)); at = sum(lengths[:i])
+    hq, hk, hv = (p[1][at:at + lengths[i], 1] for p in parts)
+    wy, ws_, sy, ss = O.attention_sequence(hq, hk, hv, rates[1], 0.3, host(state[i, 1]))
+    within("y", host(y[at:at + lengths[i], 1]), wy, attention_bound(sy, lengths[i], dk, dtype, wy))
+    within("state", host(last[i, 1]), ws_, attention_bound(ss, lengths[i], dk, F32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_attention_rates_at_their_ends(dtype):
     """Rate 0: plain causal sums.  Infinite and huge rates: every token sees only itself, and 0 * inf is no NaN."""
     r = seeded("rates")
