@@ -429,6 +429,51 @@ def test_logprob_empty_vocabulary():
     assert (out["lse"] == -float("inf")).all() and (out["entropy"] == 0).all() and (out["logp"] == 0).all()
 
 
+# --- offsets beyond 32 bits ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("ld", [1 << 21, (1 << 24) + 40])
+def test_attention_and_rotary_rows_far_apart(ld):
+    """Rows so far apart that the last one lies beyond 2^31 elements, and (the second) a chunk's rows beyond 2^31 bytes."""
+    r = seeded("far", ld)
+    n, heads, d = (1 << 31) // ld + 70, 1, 64
+    m = torch.empty(n * ld, device="cuda", dtype=BF16).view(n, ld)
+    rows = [m[:, i * d:(i + 1) * d].unflatten(1, (heads, d)) for i in range(5)]
+    near = [rounded(r, (n, heads, d), BF16)[0] for _ in range(4)]
+    for far, t in zip(rows, near):
+        far.copy_(t)
+    (q, k, v, gy), rates = near, dev(np.array([0.05], np.float32))
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(BF16, n, 1, heads, d, d), dtype=torch.uint8, device="cuda")
+    y = torch.empty_like(v)
+    B.laplex_decay_attention(q, k, v, rates, y, ws, 0.125)
+    B.laplex_decay_attention(*rows[:3], rates, rows[4], ws, 0.125)
+    assert torch.equal(rows[4], y)
+    grads = [torch.empty_like(q) for _ in range(3)]
+    B.laplex_decay_attention_backward(q, k, v, rates, gy, *grads, ws, 0.125)
+    for i in range(3):
+        one = [rows[4] if j == i else None for j in range(3)]
+        B.laplex_decay_attention_backward(*rows[:3], rates, rows[3], *one, ws, 0.125)
+        assert torch.equal(rows[4], grads[i])
+    positions, freq = dev(np.arange(n), torch.int64), dev((100.0 ** -np.linspace(0, 1, d // 2)).astype(np.float32))
+    B.laplex_rotary(q, positions, freq, y)
+    B.laplex_rotary(rows[0], positions, freq, rows[4])
+    assert torch.equal(rows[4], y)
+
+
+def test_logprob_logits_beyond_32_bits():
+    r = seeded("far logits")
+    k, ld = 70001, 32000
+    m = torch.empty(k * ld, device="cuda", dtype=BF16).view(k, ld)
+    y, targets = m[:, 40:45], np.array([k - 1, 0, 5, k - 2, -1])
+    y.copy_(rounded(r, (k, 5), BF16)[0] * 3)
+    near = y.contiguous()
+    out = check_logprob(y, host(near), targets, 1.0, 9)
+    ones, dt = torch.ones(5, device="cuda"), dev(targets, torch.int64)
+    want = torch.empty_like(near)
+    B.laplex_logprob_backward(near, dt, out["lse"], out["entropy"], ones, ones, None, want)
+    B.laplex_logprob_backward(y, dt, out["lse"], out["entropy"], ones, ones, None, y)
+    assert torch.equal(y, want)
+
+
 # --- streams and graphs ----------------------------------------------------------------------------------------------------
 
 def test_calls_run_on_the_stream_they_are_given_and_in_graphs():
