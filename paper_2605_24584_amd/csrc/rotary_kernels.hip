@@ -63,8 +63,7 @@ __device__ __forceinline__ void store_vec(T* p, const float* in)
     *reinterpret_cast<typename Vec<T, VEC>::type*>(p) = v;
 }
 
-// A unit of the first half of a head is VEC pairs: VEC numbers from either half, or (INTERLEAVED) VEC pairs side by side, in two
-// pieces of VEC numbers.
+// A unit is VEC pairs, VEC numbers from either half of what is turned; INTERLEAVED: the pairs of VEC numbers side by side (of two, if VEC is one).
 template <typename T, int VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRotaryThreads)
 k_rotary(RotaryTiles R)
@@ -86,29 +85,38 @@ k_rotary(RotaryTiles R)
             const T* x = static_cast<const T*>(A.x) + (token0 + t) * A.ldx + h * A.dim;
             T* y = static_cast<T*>(A.y) + (token0 + t) * A.ldy + h * A.dim;
             if (unit < (uint32_t)R.pairs) {
-                const float2* turns = table + t * A.half + unit * VEC;
-                const int first = INTERLEAVED ? 2 * unit * VEC : unit * VEC, second = INTERLEAVED ? first + VEC : first + A.half;
-                float u[VEC], v[VEC];
-                load_vec<T, VEC>(u, x + first);
-                load_vec<T, VEC>(v, x + second);
-                float nu[VEC], nv[VEC];
+                if constexpr (INTERLEAVED) {
+                    constexpr int PAIRS = VEC > 1 ? VEC / 2 : 1, PIECE = VEC > 1 ? VEC : 1;
+                    const float2* turns = table + t * A.half + unit * PAIRS;
+                    const int first = 2 * unit * PAIRS;
+                    float u[2 * PAIRS];
+                    load_vec<T, PIECE>(u, x + first);
+                    if (VEC == 1) load_vec<T, PIECE>(u + 1, x + first + 1);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float2 w = turns[j];
-                    // the j-th pair of the unit: numbers j of both pieces, or numbers 2 j and 2 j + 1 of the two pieces as one
-                    const float p = INTERLEAVED ? (2 * j < VEC ? u[(2 * j) % VEC] : v[(2 * j) % VEC]) : u[j];
-                    const float q = INTERLEAVED ? (2 * j + 1 < VEC ? u[(2 * j + 1) % VEC] : v[(2 * j + 1) % VEC]) : v[j];
-                    const float a = p * w.x - q * w.y, b = q * w.x + p * w.y;
-                    if (INTERLEAVED) {
-                        (2 * j < VEC ? nu : nv)[(2 * j) % VEC] = a;
-                        (2 * j + 1 < VEC ? nu : nv)[(2 * j + 1) % VEC] = b;
-                    } else {
-                        nu[j] = a;
-                        nv[j] = b;
+                    for (int j = 0; j < PAIRS; ++j) {
+                        const float2 w = turns[j];
+                        const float p = u[2 * j], q = u[2 * j + 1];
+                        u[2 * j] = p * w.x - q * w.y;
+                        u[2 * j + 1] = q * w.x + p * w.y;
                     }
+                    store_vec<T, PIECE>(y + first, u);
+                    if (VEC == 1) store_vec<T, PIECE>(y + first + 1, u + 1);
+                } else {
+                    const float2* turns = table + t * A.half + unit * VEC;
+                    const int first = unit * VEC, second = first + A.half;
+                    float u[VEC], v[VEC];
+                    load_vec<T, VEC>(u, x + first);
+                    load_vec<T, VEC>(v, x + second);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float2 w = turns[j];
+                        const float p = u[j], q = v[j];
+                        u[j] = p * w.x - q * w.y;
+                        v[j] = q * w.x + p * w.y;
+                    }
+                    store_vec<T, VEC>(y + first, u);
+                    store_vec<T, VEC>(y + second, v);
                 }
-                store_vec<T, VEC>(y + first, nu);
-                store_vec<T, VEC>(y + second, nv);
             } else {
                 const int at = 2 * A.half + (unit - R.pairs) * VEC;
                 *reinterpret_cast<typename Vec<T, VEC>::type*>(y + at) = *reinterpret_cast<const typename Vec<T, VEC>::type*>(x + at);
@@ -169,13 +177,13 @@ hipError_t launch_rotary(const RotaryArgs& A, hipStream_t st)
     const auto fits = [&](int v) {
         const int64_t bytes = (int64_t)v * size;
         return reinterpret_cast<uintptr_t>(A.x) % bytes == 0 && reinterpret_cast<uintptr_t>(A.y) % bytes == 0 && A.ldx * size % bytes == 0 &&
-               A.ldy * size % bytes == 0 && A.dim % v == 0 && A.half % v == 0;
+               A.ldy * size % bytes == 0 && A.dim % v == 0 && (A.interleaved ? 2 * A.half : A.half) % v == 0;
     };
     if (!fits(vec)) vec /= 2;
     if (!fits(vec)) vec = 1;
     RotaryTiles R{};
     R.A = A;
-    R.pairs = A.half / vec;
+    R.pairs = A.interleaved && vec > 1 ? 2 * A.half / vec : A.half / vec;
     R.rest = copies ? rest / vec : 0;
     const int64_t units = (int64_t)(R.pairs + R.rest) * A.heads;
     R.head = Divisor((uint32_t)(R.pairs + R.rest));
