@@ -305,6 +305,13 @@ __device__ __forceinline__ float state_value(const Walk& W, int64_t at, int row,
     return W.in_scale * W.state_in[at + (W.transposed ? (int64_t)col * W.dk + row : (int64_t)row * W.dv + col)];
 }
 
+// Where a set's state has row `row` and column `col`, in numbers from its first: pieces of four rows, as the accumulators hold them.
+template <int DK, int COLS>
+__device__ __forceinline__ int set_place(int row, int col)
+{
+    return (col / COLS) * DK * COLS + ((((col % COLS) / 16) * (DK / 16) + row / 16) * 64 + (row % 16) / 4 * 16 + col % 16) * 4 + row % 4;
+}
+
 // Sizes of a walk's kernel: DK the padded rows of the state; every wavefront has NT tiles of 16 columns.
 template <typename T, int DK, int WAVES, int NT>
 struct Geometry {
@@ -319,7 +326,7 @@ struct Geometry {
 
 // STATES: only what a stretch adds to the state, for the stretches behind it (U below).
 template <typename T, int DK, int WAVES, int NT, bool STATES>
-__global__ void __launch_bounds__(64 * WAVES, (NT > 1 || DK > 128 ? 2 : DK > 96 ? 4 : DK > 64 && sizeof(T) == 4 ? 5 : 3))      // as many as LDS and the state leave room for
+__global__ void __launch_bounds__(64 * WAVES, (STATES && sizeof(T) == 4 ? (DK > 128 ? 4 : DK > 96 ? 5 : 6) : NT > 1 || DK > 128 ? 2 : DK > 96 ? 4 : DK > 64 && sizeof(T) == 4 ? 5 : 3))      // as many as LDS and the state leave room for
 k_attention_walk(AttentionArgs A)
 {
     typedef Geometry<T, DK, WAVES, NT> G;
@@ -336,9 +343,9 @@ k_attention_walk(AttentionArgs A)
     char* const Ps = Ks + G::kBytesRows;               // [C][C]
 
     // heads side by side: the slots that have nothing to do are then spread over the chiplets, which take workgroups in turn
-    const int walk = blockIdx.z % A.walks, slice = blockIdx.x % A.slices, h = blockIdx.x / A.slices, col0 = slice * G::COLS;
-    const int64_t slot = (int64_t)(blockIdx.z / A.walks) * kSlotRows + blockIdx.y;
-    const Walk W = A.walk[walk];
+    const int walks = STATES ? A.sets : A.walks, walk = blockIdx.z % walks, slice = blockIdx.x % A.slices, h = blockIdx.x / A.slices, col0 = slice * G::COLS;
+    const int64_t slot = (int64_t)(blockIdx.z / walks) * kSlotRows + blockIdx.y;
+    const Walk W = STATES ? A.states[walk] : A.walk[walk];
     if (slot >= A.slots || col0 >= W.dv) return;
     const Stretch s = find_stretch(A, slot);
     if (!s.there || (STATES && s.last)) return;
@@ -360,15 +367,17 @@ k_attention_walk(AttentionArgs A)
     const int64_t first_row = s.begin + (W.reverse ? s.count - 1 - s.lo : s.lo);
     const int64_t sq = back * W.ldq, sk = back * W.ldk, sv = back * W.ldv;
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;      // rows further apart need 64-bit places
-    const bool wide = (A.wide[walk] & 7) == 7 && W.ldq < near && W.ldk < near && W.ldv < near, wo = A.wide[walk] & 8;
+    const int flags = STATES ? A.states_wide[walk] : A.wide[walk];
+    const bool wide = (flags & 7) == 7 && W.ldq < near && W.ldk < near && W.ldv < near, wo = flags & 8;
     const bool whole = wide && W.dk == DK && col0 + G::COLS <= W.dv, whole_out = W.out && wo && col0 + G::COLS <= W.dv;
 
     // the state: rows 16 t + 4 g .. + 3, columns col0 + 16 (wave NT + c) + r16
     f32x4 S[DT][NT];
     const int col = col0 + 16 * wave * NT + r16;
     const int64_t state_at = (s.b * A.heads + h) * (int64_t)W.dk * W.dv;
-    f32x4* const U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)walk * A.slots + slot) * A.heads + h) * A.slices + slice) * (DK * G::COLS / 4) +
-                     wave * NT * DT * 64 + lane;
+    constexpr int kPieces = DK * G::COLS / 4;
+    f32x4* const set = reinterpret_cast<f32x4*>(A.ws) + (((int64_t)(STATES ? walk : W.set) * A.slots + slot) * A.heads + h) * A.slices * kPieces;
+    f32x4* const U = set + (int64_t)slice * kPieces + wave * NT * DT * 64 + lane;
 #pragma unroll
     for (int c = 0; c < NT; ++c)
 #pragma unroll
@@ -376,7 +385,17 @@ k_attention_walk(AttentionArgs A)
             f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
             if (!STATES) {
                 // (of sequences that are cut the initial state, too, comes from U: another workgroup may already write the last state, in its place)
-                if (A.cut ? s.index > 0 || W.state_in : 0) v4 = U[(c * DT + t) * 64];
+                if (A.cut && (s.index > 0 || W.state_in)) {
+                    if (!W.set_transposed) v4 = U[(c * DT + t) * 64];
+                    else {
+                        // row `from` and columns 16 t + 4 g .. + 3 of the set
+                        const int from = col + 16 * c, to = 16 * t + 4 * g;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (from < W.dv && to + r < W.dk)
+                                v4[r] = reinterpret_cast<const float*>(set)[set_place<DK, G::COLS>(from, to + r)];
+                    }
+                }
                 else if (W.state_in) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
@@ -662,7 +681,7 @@ __global__ void __launch_bounds__(256)
 k_attention_carry(AttentionArgs A)
 {
     constexpr int kPieces = DK * COLS / 4, kBlocks = (kPieces + 255) / 256;
-    const Walk W = A.walk[blockIdx.z];
+    const Walk W = A.states[blockIdx.z];
     for (int64_t block = blockIdx.x; block < A.sequences * A.slices * kBlocks; block += gridDim.x) {
         const int64_t b = block / (A.slices * kBlocks);
         const int rest = (int)(block % (A.slices * kBlocks)), slice = rest / kBlocks, piece = (rest % kBlocks) * 256 + threadIdx.x;
@@ -766,7 +785,8 @@ struct Plan {
     bool cut;                          // some sequence may have more than one stretch
 };
 
-// By the sizes alone.
+// By the sizes alone.  walks: 1 for the forward call, 3 for the backward one, also where not all gradients are wanted (what one of them is must not
+// depend on the others).
 Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv, int walks, bool equal)
 {
     Plan P;
@@ -791,9 +811,9 @@ Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv, int w
     return P;
 }
 
-size_t plan_bytes(const Plan& P, int heads, int walks)
+size_t plan_bytes(const Plan& P, int heads, int sets)
 {
-    return P.cut ? (size_t)walks * P.slots * heads * P.slices * P.dk * P.cols * sizeof(float) : 0;
+    return P.cut ? (size_t)sets * P.slots * heads * P.slices * P.dk * P.cols * sizeof(float) : 0;
 }
 
 bool allows(const void* p, int64_t ld, int d, int size, int bytes)
@@ -806,13 +826,14 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
     const int64_t deep = (P.slots + kSlotRows - 1) / kSlotRows;
     const dim3 grid((unsigned)(A.heads * P.slices), (unsigned)(deep > 1 ? kSlotRows : P.slots), (unsigned)(deep * A.walks));
+    const dim3 sets_grid(grid.x, grid.y, (unsigned)(deep * A.sets));
     if (P.cut) {
         profile_before("attention_states", st);
-        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, NT, true>), grid, dim3(64 * WAVES), 0, st, A);
+        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, NT, true>), sets_grid, dim3(64 * WAVES), 0, st, A);
         profile_after("attention_states", st);
         profile_before("attention_carry", st);
         const int64_t blocks = A.sequences * P.slices * ((DK * 16 * NT * WAVES / 4 + 255) / 256), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
-        hipLaunchKernelGGL((k_attention_carry<DK, 16 * NT * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.walks),
+        hipLaunchKernelGGL((k_attention_carry<DK, 16 * NT * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.sets),
                            dim3(256), 0, st, A);
         profile_after("attention_carry", st);
     }
@@ -838,10 +859,10 @@ size_t attention_workspace(bool, int64_t tokens, int64_t sequences, int heads, i
 {
     // the forward and the backward call, with lengths that are equal or not
     size_t most = 0;
-    for (int walks = 1; walks <= 3; ++walks)
+    for (int walks = 1; walks <= 3; walks += 2)
         for (int equal = 0; equal < 2; ++equal) {
             if (equal && (sequences == 0 || tokens % sequences != 0)) continue;
-            const size_t bytes = plan_bytes(plan_of(tokens, sequences, heads, dk, dv, walks, equal != 0), heads, walks);
+            const size_t bytes = plan_bytes(plan_of(tokens, sequences, heads, dk, dv, walks, equal != 0), heads, walks > 1 ? 2 : 1);
             most = bytes > most ? bytes : most;
         }
     return sequences > 0 && heads > 0 ? most : 0;
@@ -850,14 +871,15 @@ size_t attention_workspace(bool, int64_t tokens, int64_t sequences, int heads, i
 hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
 {
     AttentionArgs A = given;
-    const Plan P = plan_of(A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv, A.walks, A.starts == nullptr);
+    const Plan P = plan_of(A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv, A.backward ? 3 : 1, A.starts == nullptr);
     A.cut = P.cut; A.stretch = P.stretch; A.per_sequence = P.per_sequence; A.slots = P.slots; A.slices = P.slices;
     const int size = A.bf16 ? 2 : 4;
-    for (int w = 0; w < A.walks; ++w) {
-        const Walk& W = A.walk[w];
-        A.wide[w] = (allows(W.q, W.ldq, W.dk, size, 4 * size) ? 1 : 0) | (allows(W.k, W.ldk, W.dk, size, 4 * size) ? 2 : 0) |
-                    (allows(W.v, W.ldv, W.dv, size, 4 * size) ? 4 : 0) | (allows(W.out, W.ldo, W.dv, size, 4 * size) ? 8 : 0);
-    }
+    const auto flags = [&](const Walk& W) {
+        return (allows(W.q, W.ldq, W.dk, size, 4 * size) ? 1 : 0) | (allows(W.k, W.ldk, W.dk, size, 4 * size) ? 2 : 0) |
+               (allows(W.v, W.ldv, W.dv, size, 4 * size) ? 4 : 0) | (allows(W.out, W.ldo, W.dv, size, 4 * size) ? 8 : 0);
+    };
+    for (int w = 0; w < A.walks; ++w) A.wide[w] = flags(A.walk[w]);
+    for (int w = 0; w < A.sets; ++w) A.states_wide[w] = flags(A.states[w]);
     return A.bf16 ? walk_of<__bf16>(A, P, st) : walk_of<float>(A, P, st);
 }
 

@@ -142,6 +142,7 @@ int laplex_decay_attention(const void* q, int64_t ldq, const void* k, int64_t ld
     W.state_in = state_in; W.in_scale = 1.0f;
     W.state_out = state_out; W.last_scale = 1.0f;
     W.out_scale = scale;
+    A.states[A.sets++] = W;
     LAPLEX_HIP(launch_attention(A, stream));
     return LAPLEX_OK;
 }
@@ -171,24 +172,30 @@ int laplex_decay_attention_backward(const void* q, int64_t ldq, const void* k, i
     AttentionArgs A{};
     A.starts = starts; A.tokens = tokens; A.sequences = sequences; A.heads = (int)heads; A.rates = rates;
     A.bf16 = type == LAPLEX_BF16; A.ws = static_cast<char*>(ws);
+    A.backward = true;
+    // back: queries k, keys q, values gy.  The states of both walks back are these, whichever of the two is wanted, so that neither depends on the other.
+    Walk B{};
+    B.q = k; B.ldq = ldk; B.k = q; B.ldk = ldq; B.v = gy; B.ldv = ldgy; B.out = gv; B.ldo = ldgv;
+    B.dk = (int)dk; B.dv = (int)dv; B.reverse = 1; B.exact = 1;
+    B.state_in = gstate_out; B.in_scale = 1.0f / scale; B.out_scale = scale;
+    B.state_out = gstate_in; B.last_scale = scale;
+    B.set = A.sets;
+    if (gk || gv || gstate_in) A.states[A.sets++] = B;
     if (gk) {        // back: queries v, keys gy, values q, the transposed state
         Walk& W = A.walk[A.walks++];
+        W.set = B.set; W.set_transposed = 1;
         W.q = v; W.ldq = ldv; W.k = gy; W.ldk = ldgy; W.v = q; W.ldv = ldq; W.out = gk; W.ldo = ldgk;
         W.dk = (int)dv; W.dv = (int)dk; W.reverse = 1; W.transposed = 1;
         W.state_in = gstate_out; W.in_scale = 1.0f / scale; W.out_scale = scale;
     }
-    if (gv || gstate_in) {      // back: queries k, keys q, values gy
-        Walk& W = A.walk[A.walks++];
-        W.q = k; W.ldq = ldk; W.k = q; W.ldk = ldq; W.v = gy; W.ldv = ldgy; W.out = gv; W.ldo = ldgv;
-        W.dk = (int)dk; W.dv = (int)dv; W.reverse = 1; W.exact = 1;
-        W.state_in = gstate_out; W.in_scale = 1.0f / scale; W.out_scale = scale;
-        W.state_out = gstate_in; W.last_scale = scale;
-    }
+    if (gv || gstate_in) A.walk[A.walks++] = B;
     if (gq) {        // ahead: queries gy, keys v, values k, the transposed state
         Walk& W = A.walk[A.walks++];
         W.q = gy; W.ldq = ldgy; W.k = v; W.ldk = ldv; W.v = k; W.ldv = ldk; W.out = gq; W.ldo = ldgq;
         W.dk = (int)dv; W.dv = (int)dk; W.lead = 1; W.transposed = 1;
         W.state_in = state_in; W.in_scale = 1.0f; W.out_scale = scale;
+        W.set = A.sets;
+        A.states[A.sets++] = W;
     }
     LAPLEX_HIP(launch_attention(A, stream));
     return LAPLEX_OK;

@@ -43,22 +43,25 @@ struct Walk {
     const float* state_in;           // [sequences][heads][dk][dv] (or [dv][dk]) or null
     float* state_out;                // the same, never transposed, or null
     float in_scale, out_scale, last_scale;
+    int set, set_transposed;         // which of the state sets below holds the states that enter its stretches, and whether with its sides swapped
 };
 
 struct AttentionArgs {
     Walk walk[3];
     int walks;
+    Walk states[2];                  // state sets: walks whose states alone are formed, where sequences are cut into stretches.  gk and gv share one
+    int sets;
     const int64_t* starts;           // [sequences + 1] or null: equal lengths
     int64_t tokens, sequences;
     int heads;
     const float* rates;
-    bool bf16;
+    bool bf16, backward;
     char* ws;
     // filled in by launch_attention
     int cut;                         // some sequence may have more than one stretch
     int64_t stretch, per_sequence, slots;   // tokens of a stretch that one workgroup walks; stretches of a sequence (equal lengths), of all, at most
     int slices;                      // workgroups side by side over the columns
-    int wide[3];                     // per walk, a bit each for q, k, v, out: its rows may be accessed four numbers at a time
+    int wide[3], states_wide[2];     // per walk, a bit each for q, k, v, out: its rows may be accessed four numbers at a time
 };
 size_t attention_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv);
 hipError_t launch_attention(const AttentionArgs& A, hipStream_t st);

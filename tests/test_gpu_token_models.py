@@ -245,6 +245,36 @@ def test_attention_state_in_place_of_sequences_in_stretches(dtype, lengths):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths,heads,dk,dv", [([2600], 2, 64, 64), ([1, 2000, 0, 900], 3, 96, 80), ([1500, 1500], 2, 20, 130), ([2300], 1, 200, 256)])
+def test_attention_backward_of_sequences_in_stretches(dtype, lengths, heads, dk, dv):
+    """Gradients where sequences are cut, one at a time and all together: the same bits, and the oracle's."""
+    r = seeded("stretches backward", lengths, heads, dk, dv)
+    parts, rates, (state, hstate) = attention_inputs(r, lengths, heads, dk, dv, dtype, True)
+    (q, hq), (k, hk), (v, hv) = parts
+    n, b, scale = sum(lengths), len(lengths), float(np.float32(dk ** -0.5))
+    gy, hgy = rounded(r, (n, heads, dv), dtype)
+    gs, hgs = rounded(r, (b, heads, dk, dv), F32)
+    starts = dev(np.concatenate([[0], np.cumsum(lengths)]), torch.int64)
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(dtype, n, b, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    new = lambda: [torch.full(s, float("nan"), device="cuda", dtype=t)
+                   for s, t in (((n, heads, dk), dtype), ((n, heads, dk), dtype), ((n, heads, dv), dtype), ((b, heads, dk, dv), F32))]
+    call = lambda g: B.laplex_decay_attention_backward(q, k, v, dev(rates), gy, *g[:3], ws, scale, b, starts, state, gs, g[3])
+    every = new()
+    call(every)
+    for only in range(4):
+        some = [t if i == only else None for i, t in enumerate(new())]
+        call(some)
+        assert torch.equal(some[only], every[only])
+    i = int(np.argmax(lengths)); at, m = sum(lengths[:i]), lengths[i]
+    for h in range(heads):
+        cut = lambda t: t[at:at + m, h]
+        want, size = O.attention_sequence_backward(cut(hq), cut(hk), cut(hv), rates[h], scale, hstate[i, h], cut(hgy), hgs[i, h])
+        for name, got, w, s, d in zip(("gq", "gk", "gv"), every, want, size, (dv, dv, dk)):
+            within(f"{name}[{h}]", host(cut(got)), w, attention_bound(s, m, d, dtype, w))
+        within(f"g0[{h}]", host(every[3][i, h]), want[3], attention_bound(size[3], m, dk, F32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_attention_rates_at_their_ends(dtype):
     """Rate 0: plain causal sums.  Infinite and huge rates: every token sees only itself, and 0 * inf is no NaN."""
     r = seeded("rates")
