@@ -312,12 +312,12 @@ __device__ __forceinline__ int set_place(int row, int col)
     return (col / COLS) * DK * COLS + ((((col % COLS) / 16) * (DK / 16) + row / 16) * 64 + (row % 16) / 4 * 16 + col % 16) * 4 + row % 4;
 }
 
-// Sizes of a walk's kernel: DK the padded rows of the state; every wavefront has NT tiles of 16 columns.
-template <typename T, int DK, int WAVES, int NT>
+// Sizes of a walk's kernel: DK the padded rows of the state; every wavefront has a tile of 16 columns.
+template <typename T, int DK, int WAVES>
 struct Geometry {
     static constexpr int E = Num<T>::E, K = Num<T>::K, R = Patch<T>::R, THREADS = 64 * WAVES;
     static constexpr int C = (DK > 128 ? 32 : 64) * 2 / (int)sizeof(T);      // tokens of a chunk
-    static constexpr int COLS = 16 * NT * WAVES;                                  // columns of a workgroup
+    static constexpr int COLS = 16 * WAVES;                                      // columns of a workgroup
     static constexpr int ROW = (DK * (int)sizeof(T) / 16 + 7) / 8 * 8, SEQ = C * (int)sizeof(T) / 16;   // slots of a row of numbers (a multiple of 8: they are permuted by eights), of tokens
     static constexpr int CT = C / 16, DT = DK / 16, KD = DK / K, KC = C / K;
     static constexpr int kBytesRows = C * ROW * 16, kBytesK = DK * SEQ * 16, kBytesV = COLS * SEQ * 16, kBytesP = C * SEQ * 16;
@@ -325,11 +325,11 @@ struct Geometry {
 };
 
 // STATES: only what a stretch adds to the state, for the stretches behind it (U below).
-template <typename T, int DK, int WAVES, int NT, bool STATES>
-__global__ void __launch_bounds__(64 * WAVES, (STATES && sizeof(T) == 4 ? (DK > 128 ? 4 : DK > 96 ? 5 : 6) : NT > 1 || DK > 128 ? 2 : DK > 96 ? 4 : DK > 64 && sizeof(T) == 4 ? 5 : 3))      // as many as LDS and the state leave room for
+template <typename T, int DK, int WAVES, bool STATES>
+__global__ void __launch_bounds__(64 * WAVES, (STATES && sizeof(T) == 4 ? (DK > 128 ? 4 : DK > 96 ? 5 : 6) : DK > 128 ? 2 : DK > 96 ? 4 : DK > 64 && sizeof(T) == 4 ? 5 : 3))      // as many as LDS and the state leave room for
 k_attention_walk(AttentionArgs A)
 {
-    typedef Geometry<T, DK, WAVES, NT> G;
+    typedef Geometry<T, DK, WAVES> G;
     typedef typename Num<T>::frag frag;
     typedef typename Num<T>::quad quad;
     constexpr int E = G::E, C = G::C, R = G::R, ROW = G::ROW, SEQ = G::SEQ, CT = G::CT, DT = G::DT, KD = G::KD, KC = G::KC, THREADS = G::THREADS;
@@ -371,39 +371,37 @@ k_attention_walk(AttentionArgs A)
     const bool wide = (flags & 7) == 7 && W.ldq < near && W.ldk < near && W.ldv < near, wo = flags & 8;
     const bool whole = wide && W.dk == DK && col0 + G::COLS <= W.dv, whole_out = W.out && wo && col0 + G::COLS <= W.dv;
 
-    // the state: rows 16 t + 4 g .. + 3, columns col0 + 16 (wave NT + c) + r16
-    f32x4 S[DT][NT];
-    const int col = col0 + 16 * wave * NT + r16;
+    // the state: rows 16 t + 4 g .. + 3, columns col0 + 16 wave + r16
+    f32x4 S[DT];
+    const int col = col0 + 16 * wave + r16;
     const int64_t state_at = (s.b * A.heads + h) * (int64_t)W.dk * W.dv;
     constexpr int kPieces = DK * G::COLS / 4;
     f32x4* const set = reinterpret_cast<f32x4*>(A.ws) + (((int64_t)(STATES ? walk : W.set) * A.slots + slot) * A.heads + h) * A.slices * kPieces;
-    f32x4* const U = set + (int64_t)slice * kPieces + wave * NT * DT * 64 + lane;
+    f32x4* const U = set + (int64_t)slice * kPieces + wave * DT * 64 + lane;
 #pragma unroll
-    for (int c = 0; c < NT; ++c)
-#pragma unroll
-        for (int t = 0; t < DT; ++t) {
-            f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (!STATES) {
-                // (of sequences that are cut the initial state, too, comes from U: another workgroup may already write the last state, in its place)
-                if (A.cut && (s.index > 0 || W.state_in)) {
-                    if (!W.set_transposed) v4 = U[(c * DT + t) * 64];
-                    else {
-                        // row `from` and columns 16 t + 4 g .. + 3 of the set
-                        const int from = col + 16 * c, to = 16 * t + 4 * g;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (from < W.dv && to + r < W.dk)
-                                v4[r] = reinterpret_cast<const float*>(set)[set_place<DK, G::COLS>(from, to + r)];
-                    }
-                }
-                else if (W.state_in) {
+    for (int t = 0; t < DT; ++t) {
+        f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (!STATES) {
+            // (of sequences that are cut the initial state, too, comes from U: another workgroup may already write the last state, in its place)
+            if (A.cut && (s.index > 0 || W.state_in)) {
+                if (!W.set_transposed) v4 = U[t * 64];
+                else {
+                    // row `from` and columns 16 t + 4 g .. + 3 of the set
+                    const int from = col, to = 16 * t + 4 * g;
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (col + 16 * c < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col + 16 * c);
+                        if (from < W.dv && to + r < W.dk)
+                            v4[r] = reinterpret_cast<const float*>(set)[set_place<DK, G::COLS>(from, to + r)];
                 }
             }
-            S[t][c] = v4;
+            else if (W.state_in) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (col < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col);
+            }
         }
+        S[t] = v4;
+    }
 
     // a chunk's patches
     constexpr int kRowPatches = (C / R) * (DK / 4), kColPatches = (C / R) * (G::COLS / 4);
@@ -449,7 +447,7 @@ k_attention_walk(AttentionArgs A)
     };
     if (s.lo < s.hi) load(s.lo);
     __syncthreads();                                   // the powers are there
-    T* out = static_cast<T*>(W.out) + first_row * W.ldo + (int64_t)h * W.dv + col0 + 16 * wave * NT;      // the chunk's first row
+    T* out = static_cast<T*>(W.out) + first_row * W.ldo + (int64_t)h * W.dv + col0 + 16 * wave;      // the chunk's first row
     const int64_t so = back * W.ldo;
 
     int turn = 0;
@@ -489,9 +487,9 @@ k_attention_walk(AttentionArgs A)
         const int l = here(lane), r16 = l & 15, g = l >> 4;
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
-        Reader<SEQ> values(r16, g);                    // the columns of this wavefront: tiles wave NT + c
-        values.base += wave * NT * 16 * SEQ * 16;
-        values.low ^= ((2 * wave * NT) & Reader<SEQ>::kMask) * 16;
+        Reader<SEQ> values(r16, g);                    // the columns of this wavefront
+        values.base += wave * 16 * SEQ * 16;
+        values.low ^= ((2 * wave) & Reader<SEQ>::kMask) * 16;
         if (!STATES) {
             // P: tiles on and below the diagonal, dealt to the wavefronts; as it leaves the accumulator a lane holds P[i][j .. j + 3]
 #pragma unroll
@@ -514,105 +512,89 @@ k_attention_walk(AttentionArgs A)
                 }
             }
             // q S, weighted by the rows
-            f32x4 O[CT][NT];
+            f32x4 O[CT];
 #pragma unroll
             for (int t = 0; t < CT; ++t)
-#pragma unroll
-                for (int c = 0; c < NT; ++c) O[t][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                O[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int m = 0; m < KD; ++m) {
                 if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);     // (all steps' fragments at once do not fit the registers)
-                frag sf[NT];
+                frag sf;
+                if constexpr (sizeof(T) == 2) {
+                    // rounded for this product alone, as P is for its own: the result is rounded as much again
 #pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    if constexpr (sizeof(T) == 2) {
-                        // rounded for this product alone, as P is for its own: the result is rounded as much again
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sf[c][e] = (__bf16)S[2 * m + (e >> 2)][c][e & 3];
-                    } else {
-                        sf[c] = S[m][c];
-                    }
+                    for (int e = 0; e < 8; ++e) sf[e] = (__bf16)S[2 * m + (e >> 2)][e & 3];
+                } else {
+                    sf = S[m];
                 }
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
                     const frag qf = get<T>(Qs, rows.at(t, m));
-#pragma unroll
-                    for (int c = 0; c < NT; ++c) O[t][c] = mma(sf[c], qf, O[t][c]);
+                    O[t] = mma(sf, qf, O[t]);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < CT; ++t) {
                 const float ahead = power[16 * t + r16 + W.lead];
-#pragma unroll
-                for (int c = 0; c < NT; ++c) O[t][c] *= ahead;
+                O[t] *= ahead;
             }
             __syncthreads();                           // P is there
             const bool slow = odd[turn] != 0;          // a value of v is not finite: 0 * v of the tokens behind a row must not reach it
             if (x == 0) odd[turn ^ 1] = 0;
 #pragma unroll
             for (int m = 0; m < KC; ++m) {
-                frag vf[NT];
+                frag vf = get<T>(Vt, values.at(0, m));
+                if (slow)
 #pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    vf[c] = get<T>(Vt, values.at(c, m));
-                    if (slow)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) vf[c][e] = finite_bits((float)vf[c][e]) ? vf[c][e] : (T)0.0f;
-                }
+                    for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
 #pragma unroll
                 for (int t = 0; t < CT; ++t)
                     if (16 * t + 15 >= m * G::K) {
                         const frag pf = get<T>(Ps, columns.at(t, m));
-#pragma unroll
-                        for (int c = 0; c < NT; ++c) O[t][c] = mma(vf[c], pf, O[t][c]);
+                        O[t] = mma(vf, pf, O[t]);
                     }
             }
             if (slow)
                 for (int j = 0; j < C; ++j) {
-                    const int i0 = here(r16), n0 = here(wave * NT * 16 + 4 * g);
+                    const int i0 = here(r16), n0 = here(wave * 16 + 4 * g);
                     float p[CT];
 #pragma unroll
                     for (int t = 0; t < CT; ++t)
                         p[t] = (float)*reinterpret_cast<const T*>(Ps + 16 * slot_at<SEQ>(16 * t + i0, j / E) + (j % E) * (int)sizeof(T));
 #pragma unroll
-                    for (int c = 0; c < NT; ++c)
+                    for (int r = 0; r < 4; ++r) {
+                        const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n0 + r, j / E) + (j % E) * (int)sizeof(T));
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float vj = (float)*reinterpret_cast<const T*>(Vt + 16 * slot_at<SEQ>(n0 + 16 * c + r, j / E) + (j % E) * (int)sizeof(T));
-#pragma unroll
-                            for (int t = 0; t < CT; ++t)
-                                if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][c][r] += vj * p[t];
-                        }
+                        for (int t = 0; t < CT; ++t)
+                            if (!finite_bits(vj) && 16 * t + i0 >= j) O[t][r] += vj * p[t];
+                    }
                 }
-            const auto result = [&](int t, int c) {
+            const auto result = [&](int t) {
                 quad w;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][c][r] * W.out_scale);
+                for (int r = 0; r < 4; ++r) w[r] = (T)(O[t][r] * W.out_scale);
                 return w;
             };
             if (whole_out && valid == C) {
 #pragma unroll
                 for (int t = 0; t < CT; ++t)
-#pragma unroll
-                    for (int c = 0; c < NT; ++c) *reinterpret_cast<quad*>(out + (16 * t + r16) * so + 4 * g + 16 * c) = result(t, c);
+                    *reinterpret_cast<quad*>(out + (16 * t + r16) * so + 4 * g) = result(t);
             } else if (W.out) {
 #pragma unroll
                 for (int t = 0; t < CT; ++t)
-                    if (16 * t + r16 < valid)
+                    if (16 * t + r16 < valid) {
+                        const int n = col0 + 16 * wave + 4 * g;
+                        T* const at = out + (16 * t + r16) * so + 4 * g;
+                        const quad w = result(t);
+                        if (wo) {
+                            if (n < W.dv) *reinterpret_cast<quad*>(at) = w;
+                        } else {
 #pragma unroll
-                        for (int c = 0; c < NT; ++c) {
-                            const int n = col0 + 16 * (wave * NT + c) + 4 * g;
-                            T* const at = out + (16 * t + r16) * so + 4 * g + 16 * c;
-                            const quad w = result(t, c);
-                            if (wo) {
-                                if (n < W.dv) *reinterpret_cast<quad*>(at) = w;
-                            } else {
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (n + r < W.dv) at[r] = w[r];
-                            }
+                            for (int r = 0; r < 4; ++r)
+                                if (n + r < W.dv) at[r] = w[r];
                         }
+                    }
             }
             out += C * so;
         }
@@ -624,8 +606,7 @@ k_attention_walk(AttentionArgs A)
         if (valid < C) d = end_decay;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int c = 0; c < NT; ++c) S[t][c] *= d;
+            S[t] *= d;
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
             __builtin_amdgcn_sched_barrier(0);
@@ -633,45 +614,39 @@ k_attention_walk(AttentionArgs A)
 #pragma unroll
             for (int e = 0; e < E; ++e) w[e] = weight[(4 * m + g) * E + e];
             constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
-            frag part[TERMS][NT];
+            frag part[TERMS];
+            const frag vf = get<T>(Vt, values.at(0, m));
+            float xs[E];
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                const frag vf = get<T>(Vt, values.at(c, m));
-                float xs[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) xs[e] = w[e] * (float)vf[e];
-                if constexpr (sizeof(T) == 2) {
-                    // all 24 bits where the state can be asked for, 16 where it only goes on into results of 8
-                    if (W.exact) split3(xs, part[0][c], part[1][c], part[2][c]);
-                    else split2(xs, part[0][c], part[1][c]);
-                } else part[0][c] = f32x4{xs[0], xs[1], xs[2], xs[3]};
-            }
+            for (int e = 0; e < E; ++e) xs[e] = w[e] * (float)vf[e];
+            if constexpr (sizeof(T) == 2) {
+                // all 24 bits where the state can be asked for, 16 where it only goes on into results of 8
+                if (W.exact) split3(xs, part[0], part[1], part[2]);
+                else split2(xs, part[0], part[1]);
+            } else part[0] = f32x4{xs[0], xs[1], xs[2], xs[3]};
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
                 const frag kf = get<T>(Kt, columns.at(t, m));
 #pragma unroll
                 for (int p = 0; p < TERMS; ++p)
                     if (p < 2 || W.exact)
-#pragma unroll
-                        for (int c = 0; c < NT; ++c) S[t][c] = mma(kf, part[p][c], S[t][c]);
+                        S[t] = mma(kf, part[p], S[t]);
             }
         }
         __syncthreads();                               // the tiles may be written again
     }
 
 #pragma unroll
-    for (int c = 0; c < NT; ++c)
+    for (int t = 0; t < DT; ++t) {
+        if (STATES) U[t * 64] = S[t];
+        else if (W.state_out && s.last) {
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
-            if (STATES) U[(c * DT + t) * 64] = S[t][c];
-            else if (W.state_out && s.last) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * t + 4 * g + r, column = col + 16 * c;
-                    if (column < W.dv && row < W.dk) W.state_out[state_at + (int64_t)row * W.dv + column] = W.last_scale * S[t][c][r];
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * t + 4 * g + r;
+                if (col < W.dv && row < W.dk) W.state_out[state_at + (int64_t)row * W.dv + col] = W.last_scale * S[t][r];
             }
         }
+    }
 }
 
 // What enters the stretches: carry_n = l^stretch carry_(n-1) + U_(n-1), carry_0 = the initial state, in the places of the U.
@@ -787,7 +762,7 @@ struct Plan {
 
 // By the sizes alone.  walks: 1 for the forward call, 3 for the backward one, also where not all gradients are wanted (what one of them is must not
 // depend on the others).
-Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv, int walks, bool equal)
+Plan plan_of(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv, int walks, bool equal)
 {
     Plan P;
     const int most = dk > dv ? dk : dv;
@@ -802,8 +777,15 @@ Plan plan_of(int64_t tokens, int64_t sequences, int heads, int dk, int dv, int w
     // 1250 tokens on average, 6 heads, fp32 277 / 286 / 530 / 604 / 641, their gradients 694 / 699 / 902 / 1050 / 1061.
     const int64_t work = tokens * heads * P.slices * walks, workgroups = equal ? 512 : 2048;
     P.stretch = (work / workgroups + 63) / 64 * 64;
-    if (P.stretch < 256) P.stretch = 256;
-    P.cut = longest > 2 * P.stretch;
+    // At least 256 tokens, or the states that pass through memory cost more than the walks.  Where even those leave compute units without a workgroup the
+    // time is that of one workgroup's stretch, twice, and of the chain of states over the stretches: shorter ones, the more so the shorter the sequence.
+    // us, stretches of 256 / 128 / 64, one sequence, bf16, a head of 128: 384 tokens 32 / 26 / 21; 1024 40 / 28 / 24; 4096 44 / 36 / 37; 16384 58 / 62 / 92;
+    // fp32 77 / 48 / 32; 83 / 50 / 34; 88 / 58 / 48; 101 / 84 / 103.  Sequences of a few tokens on average need none of it.
+    int64_t least = 256;
+    if (work < 256 * 256 && tokens >= 64 * sequences) least = longest <= 2048 ? 64 : longest <= 8192 ? 128 : 256;
+    if (P.stretch < least) P.stretch = least;
+    // (192 tokens whole / in stretches of 64: bf16 18 / 19 us, their gradients 18 / 22; fp32 41 / 31 and 41 / 34)
+    P.cut = longest > 2 * P.stretch && longest > (bf16 ? 256 : 128);
     if (!P.cut) P.stretch = longest < 64 ? 64 : (longest + 63) / 64 * 64;
     P.per_sequence = equal ? (longest + P.stretch - 1) / P.stretch : 0;
     if (equal && P.per_sequence < 1) P.per_sequence = 1;
@@ -821,7 +803,7 @@ bool allows(const void* p, int64_t ld, int d, int size, int bytes)
     return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0 && d * size % bytes == 0;
 }
 
-template <typename T, int DK, int WAVES, int NT>
+template <typename T, int DK, int WAVES>
 hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
     const int64_t deep = (P.slots + kSlotRows - 1) / kSlotRows;
@@ -829,16 +811,16 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
     const dim3 sets_grid(grid.x, grid.y, (unsigned)(deep * A.sets));
     if (P.cut) {
         profile_before("attention_states", st);
-        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, NT, true>), sets_grid, dim3(64 * WAVES), 0, st, A);
+        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, true>), sets_grid, dim3(64 * WAVES), 0, st, A);
         profile_after("attention_states", st);
         profile_before("attention_carry", st);
-        const int64_t blocks = A.sequences * P.slices * ((DK * 16 * NT * WAVES / 4 + 255) / 256), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
-        hipLaunchKernelGGL((k_attention_carry<DK, 16 * NT * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.sets),
+        const int64_t blocks = A.sequences * P.slices * ((DK * 16 * WAVES / 4 + 255) / 256), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+        hipLaunchKernelGGL((k_attention_carry<DK, 16 * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.sets),
                            dim3(256), 0, st, A);
         profile_after("attention_carry", st);
     }
     profile_before("attention_walk", st);
-    hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, NT, false>), grid, dim3(64 * WAVES), 0, st, A);
+    hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, false>), grid, dim3(64 * WAVES), 0, st, A);
     profile_after("attention_walk", st);
     return hipGetLastError();
 }
@@ -846,23 +828,23 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 template <typename T>
 hipError_t walk_of(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
-    if (P.dk == 64) return walk_with<T, 64, 4, 1>(A, P, st);
-    if (P.dk == 96) return walk_with<T, 96, 6, 1>(A, P, st);
-    if (P.dk == 128) return walk_with<T, 128, 8, 1>(A, P, st);
-    if (P.dk == 192) return walk_with<T, 192, 6, 1>(A, P, st);
-    return walk_with<T, 256, 8, 1>(A, P, st);
+    if (P.dk == 64) return walk_with<T, 64, 4>(A, P, st);
+    if (P.dk == 96) return walk_with<T, 96, 6>(A, P, st);
+    if (P.dk == 128) return walk_with<T, 128, 8>(A, P, st);
+    if (P.dk == 192) return walk_with<T, 192, 6>(A, P, st);
+    return walk_with<T, 256, 8>(A, P, st);
 }
 
 }  // namespace
 
-size_t attention_workspace(bool, int64_t tokens, int64_t sequences, int heads, int dk, int dv)
+size_t attention_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv)
 {
     // the forward and the backward call, with lengths that are equal or not
     size_t most = 0;
     for (int walks = 1; walks <= 3; walks += 2)
         for (int equal = 0; equal < 2; ++equal) {
             if (equal && (sequences == 0 || tokens % sequences != 0)) continue;
-            const size_t bytes = plan_bytes(plan_of(tokens, sequences, heads, dk, dv, walks, equal != 0), heads, walks > 1 ? 2 : 1);
+            const size_t bytes = plan_bytes(plan_of(bf16, tokens, sequences, heads, dk, dv, walks, equal != 0), heads, walks > 1 ? 2 : 1);
             most = bytes > most ? bytes : most;
         }
     return sequences > 0 && heads > 0 ? most : 0;
@@ -871,7 +853,7 @@ size_t attention_workspace(bool, int64_t tokens, int64_t sequences, int heads, i
 hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
 {
     AttentionArgs A = given;
-    const Plan P = plan_of(A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv, A.backward ? 3 : 1, A.starts == nullptr);
+    const Plan P = plan_of(A.bf16, A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv, A.backward ? 3 : 1, A.starts == nullptr);
     A.cut = P.cut; A.stretch = P.stretch; A.per_sequence = P.per_sequence; A.slots = P.slots; A.slices = P.slices;
     const int size = A.bf16 ? 2 : 4;
     const auto flags = [&](const Walk& W) {
