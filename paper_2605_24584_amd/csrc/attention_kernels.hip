@@ -121,29 +121,43 @@ __device__ __forceinline__ void load_wide(Patch<T>& out, const T* base, int64_t 
         }
     }
 }
-template <typename T>
-__device__ __forceinline__ void keep_patch(Patch<T>& p, int first, int valid, int at, int width)
+__device__ __forceinline__ void keep_patch(Patch<float>& p, int first, int valid, int at, int width)
 {
 #pragma unroll
-    for (int i = 0; i < Patch<T>::R; ++i)
-        if (first + i >= valid || at >= width) p.r[i] = typename Num<T>::quad{};
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (first + i >= valid || at + e >= width) p.r[i][e] = 0.0f;
+}
+__device__ __forceinline__ void keep_patch(Patch<__bf16>& p, int first, int valid, int at, int width)
+{
+    const int n = width - at;                          // numbers that exist
+    const uint32_t m0 = n >= 2 ? 0xFFFFFFFFu : n == 1 ? 0xFFFFu : 0, m1 = n >= 4 ? 0xFFFFFFFFu : n == 3 ? 0xFFFFu : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u32x2 v = __builtin_bit_cast(u32x2, p.r[i]);
+        p.r[i] = __builtin_bit_cast(bf16x4, first + i < valid ? u32x2{v[0] & m0, v[1] & m1} : u32x2{0, 0});
+    }
 }
 
-// Rows of any alignment and width.
+// Rows of any alignment, width and distance, a number at a time; as above, others in the place of those that do not exist.
 template <typename T>
 __device__ __forceinline__ void load_some(Patch<T>& out, const T* base, int64_t stride, int first, int valid, int at, int width)
 {
-    const T* p = base + first * stride + at;
 #pragma unroll
     for (int i = 0; i < Patch<T>::R; ++i) {
-        typename Num<T>::quad v = {};
-        if (first + i < valid) {
+        const T* const p = base + (first + i < valid ? first + i : valid - 1) * stride;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (at + e < width) v[e] = p[e];
+        for (int e = 0; e < 4; ++e) out.r[i][e] = p[at + e < width ? at + e : width - 1];
+    }
+    if constexpr (sizeof(T) == 2) {
+        // Put together here, where that waits for the loads of a patch: 16-bit numbers take a register each until then.
+#pragma unroll
+        for (int i = 0; i < Patch<T>::R; ++i) {
+            u32x2 v = __builtin_bit_cast(u32x2, out.r[i]);
+            v[0] = here(v[0]); v[1] = here(v[1]);
+            out.r[i] = __builtin_bit_cast(typename Num<T>::quad, v);
         }
-        out.r[i] = v;
-        p += stride;
     }
 }
 
@@ -300,9 +314,11 @@ __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& A, int64_t 
     return s;
 }
 
+// A number of the initial state, not yet scaled; of one that does not exist, another one.
 __device__ __forceinline__ float state_value(const Walk& W, int64_t at, int row, int col)
 {
-    return W.in_scale * W.state_in[at + (W.transposed ? (int64_t)col * W.dk + row : (int64_t)row * W.dv + col)];
+    const int down = W.transposed ? 1 : W.dv, along = W.transposed ? W.dk : 1;
+    return W.state_in[at + (row < W.dk ? row : W.dk - 1) * down + (col < W.dv ? col : W.dv - 1) * along];
 }
 
 // Where a set's state has row `row` and column `col`, in numbers from its first: pieces of four rows, as the accumulators hold them.
@@ -378,30 +394,33 @@ k_attention_walk(AttentionArgs A)
     constexpr int kPieces = DK * G::COLS / 4;
     f32x4* const set = reinterpret_cast<f32x4*>(A.ws) + (((int64_t)(STATES ? walk : W.set) * A.slots + slot) * A.heads + h) * A.slices * kPieces;
     f32x4* const U = set + (int64_t)slice * kPieces + wave * DT * 64 + lane;
+    // (of sequences that are cut the initial state, too, comes from U: another workgroup may already write the last state, in its place)
+    const bool from_set = !STATES && A.cut && (s.index > 0 || W.state_in), from_given = !STATES && !A.cut && W.state_in;
+    // One branch for all loads of a kind, and others in the place of what does not exist: nothing waits for one of them before the next is asked for.
+    if (from_set && !W.set_transposed) {
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-        f32x4 v4 = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (!STATES) {
-            // (of sequences that are cut the initial state, too, comes from U: another workgroup may already write the last state, in its place)
-            if (A.cut && (s.index > 0 || W.state_in)) {
-                if (!W.set_transposed) v4 = U[t * 64];
-                else {
-                    // row `from` and columns 16 t + 4 g .. + 3 of the set
-                    const int from = col, to = 16 * t + 4 * g;
+        for (int t = 0; t < DT; ++t) S[t] = U[t * 64];
+    } else if (from_set) {
+        // row `col` and columns 16 t + 4 g .. + 3 of the set
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (from < W.dv && to + r < W.dk)
-                            v4[r] = reinterpret_cast<const float*>(set)[set_place<DK, G::COLS>(from, to + r)];
-                }
-            }
-            else if (W.state_in) {
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (col < W.dv && 16 * t + 4 * g + r < W.dk) v4[r] = state_value(W, state_at, 16 * t + 4 * g + r, col);
-            }
-        }
-        S[t] = v4;
+            for (int r = 0; r < 4; ++r) S[t][r] = reinterpret_cast<const float*>(set)[set_place<DK, G::COLS>(col, 16 * t + 4 * g + r)];
+    } else if (from_given) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = state_value(W, state_at, 16 * t + 4 * g + r, col);
+    } else {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) S[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
+    const float scale = from_given ? W.in_scale : 1.0f;
+    if ((from_set && W.set_transposed) || from_given)
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = col < W.dv && 16 * t + 4 * g + r < W.dk ? scale * S[t][r] : 0.0f;
 
     // a chunk's patches
     constexpr int kRowPatches = (C / R) * (DK / 4), kColPatches = (C / R) * (G::COLS / 4);
@@ -613,12 +632,12 @@ k_attention_walk(AttentionArgs A)
             float w[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) w[e] = weight[(4 * m + g) * E + e];
-            constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
-            frag part[TERMS];
             const frag vf = get<T>(Vt, values.at(0, m));
             float xs[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) xs[e] = w[e] * (float)vf[e];
+            constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
+            frag part[TERMS];
             if constexpr (sizeof(T) == 2) {
                 // all 24 bits where the state can be asked for, 16 where it only goes on into results of 8
                 if (W.exact) split3(xs, part[0], part[1], part[2]);
@@ -629,8 +648,7 @@ k_attention_walk(AttentionArgs A)
                 const frag kf = get<T>(Kt, columns.at(t, m));
 #pragma unroll
                 for (int p = 0; p < TERMS; ++p)
-                    if (p < 2 || W.exact)
-                        S[t] = mma(kf, part[p], S[t]);
+                    if (p < 2 || W.exact) S[t] = mma(kf, part[p], S[t]);
             }
         }
         __syncthreads();                               // the tiles may be written again
@@ -676,7 +694,8 @@ k_attention_carry(AttentionArgs A)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * t + 4 * (lane >> 4) + r;
-                if (col < W.dv && row < W.dk) carry[r] = state_value(W, (b * A.heads + h) * (int64_t)W.dk * W.dv, row, col);
+                const float v = state_value(W, (b * A.heads + h) * (int64_t)W.dk * W.dv, row, col);
+                carry[r] = col < W.dv && row < W.dk ? W.in_scale * v : 0.0f;
             }
         }
         const int64_t step = (int64_t)A.heads * A.slices * kPieces;
