@@ -504,6 +504,54 @@ def test_logprob_logits_beyond_32_bits():
     assert torch.equal(y, want)
 
 
+# --- attention: where sequences begin to be cut, and where they are not -------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths,dk,dv", [([128], 33, 64), ([129], 64, 31), ([256], 35, 160), ([257], 101, 90), ([193, 320], 200, 130), ([700, 64, 65], 79, 79),
+                                           ([63] * 9, 48, 48), ([2049], 17, 96), ([400], 130, 256)])
+def test_attention_of_few_sequences(dtype, lengths, dk, dv):
+    """One head, rows of no particular alignment, states: lengths beside those at which the stretches become shorter or none."""
+    r = seeded("few", lengths, dk, dv)
+    parts, rates, (state, hstate) = attention_inputs(r, lengths, 1, dk, dv, dtype, True)
+    (q, hq), (k, hk), (v, hv) = parts
+    n, b, scale = sum(lengths), len(lengths), float(np.float32(dk ** -0.5))
+    y, last = run_forward(parts, rates, state, lengths, dv, scale, True)
+    gy, hgy = rounded(r, (n, 1, dv), dtype)
+    gs, hgs = rounded(r, (b, 1, dk, dv), F32)
+    got = [torch.full(s, float("nan"), device="cuda", dtype=t) for s, t in (((n, 1, dk), dtype), ((n, 1, dk), dtype), ((n, 1, dv), dtype), ((b, 1, dk, dv), F32))]
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(dtype, n, b, 1, dk, dv), dtype=torch.uint8, device="cuda")
+    starts = dev(np.concatenate([[0], np.cumsum(lengths)]), torch.int64)
+    # what the workspace holds before does not matter
+    ws.fill_(0xFF)
+    B.laplex_decay_attention_backward(q, k, v, dev(rates), gy, *got[:3], ws, scale, b, starts, state, gs, got[3])
+    at = 0
+    for i, m in enumerate(lengths):
+        cut = lambda t: t[at:at + m, 0]
+        wy, wl, sy, sl = O.attention_sequence(cut(hq), cut(hk), cut(hv), rates[0], scale, hstate[i, 0])
+        within(f"y[{i}]", host(cut(y)), wy, attention_bound(sy, m, dk, dtype, wy))
+        within(f"state[{i}]", host(last[i, 0]), wl, attention_bound(sl, m, dk, F32))
+        want, size = O.attention_sequence_backward(cut(hq), cut(hk), cut(hv), rates[0], scale, hstate[i, 0], cut(hgy), hgs[i, 0])
+        for name, t, w, s_, d in zip(("gq", "gk", "gv"), got, want, size, (dv, dv, dk)):
+            within(f"{name}[{i}]", host(cut(t)), w, attention_bound(s_, m, d, dtype, w))
+        within(f"g0[{i}]", host(got[3][i, 0]), want[3], attention_bound(size[3], m, dk, F32))
+        at += m
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("sequences,heads,dk,dv", [(40, 16, 64, 64), (24, 24, 36, 96)])
+def test_attention_of_many_sequences_that_are_not_cut(dtype, sequences, heads, dk, dv):
+    """Enough sequences to fill the card: they are walked whole, many chunks long."""
+    r = seeded("many", sequences, heads, dk, dv)
+    m, scale = 450, 0.25
+    parts, rates, (state, hstate) = attention_inputs(r, [m] * sequences, heads, dk, dv, dtype, True)
+    y, last = run_forward(parts, rates, state, [m] * sequences, dv, scale, False)
+    for i, h in ((0, 0), (sequences - 1, heads - 1), (sequences // 2, 3)):
+        cut = lambda t: t[i * m:(i + 1) * m, h]
+        wy, wl, sy, sl = O.attention_sequence(*(cut(p[1]) for p in parts), rates[h], scale, hstate[i, h])
+        within(f"y[{i},{h}]", host(cut(y)), wy, attention_bound(sy, m, dk, dtype, wy))
+        within(f"state[{i},{h}]", host(last[i, h]), wl, attention_bound(sl, m, dk, F32))
+
+
 # --- streams and graphs ----------------------------------------------------------------------------------------------------
 
 def test_calls_run_on_the_stream_they_are_given_and_in_graphs():
