@@ -182,6 +182,8 @@ __device__ __forceinline__ uint32_t order_of(float v)
     const uint32_t bits = __float_as_uint(v + 0.0f);
     return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
+// and back (NaN is some NaN)
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
 // what lanes of the wavefront have written to LDS is there for the others
 __device__ __forceinline__ void wave_sync()
@@ -405,33 +407,37 @@ k_logprob_finish(FinishArgs F)
             const float* const maxima = F.maxima + first / kGroup * A.batch + t;
             const T* const rows = y + first * A.ldy;
             const bool direct = A.k <= kDirect;
-            const auto group_key = [&](int g) { return order_of(maxima[(int64_t)g * A.batch]); };
+            const auto group_value = [&](int g) { return maxima[(int64_t)g * A.batch]; };
+            const auto row_value = [&](int r) { return to_float(rows[(int64_t)r * A.ldy]); };
+            // (all loads below are of places that exist, whether their values are kept or not: none of them waits for the one before)
             const auto super_key = [&](int n) {
+                float v[kSuper];
+#pragma unroll
+                for (int i = 0; i < kSuper; ++i) v[i] = group_value(n * kSuper + i < groups ? n * kSuper + i : (int)groups - 1);
                 uint32_t most = 0;
 #pragma unroll
-                for (int i = 0; i < kSuper; ++i) {
-                    const uint32_t o = n * kSuper + i < groups ? group_key(n * kSuper + i) : 0;
-                    most = o > most ? o : most;
-                }
+                for (int i = 0; i < kSuper; ++i) { const uint32_t o = order_of(v[i]); most = o > most ? o : most; }
                 return most;
             };
-            const auto row_key = [&](int r) { return order_of(to_float(rows[(int64_t)r * A.ldy])); };
-            // sk[n] <- f(n), n < total: eight of a lane's loads at a time
-            const auto gather = [&](int total, auto f) {
+            // sk[n] <- the key of value(number(n)), n < total, or 0 where the number reaches the limit: eight of a lane's loads at a time
+            const auto gather = [&](int total, int64_t limit, auto number, auto value) {
                 for (int n0 = lane; n0 < total; n0 += 64 * 8) {
-                    uint32_t k[8];
+                    int id[8];
+                    float v[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) k[i] = n0 + i * 64 < total ? f(n0 + i * 64) : 0;
+                    for (int i = 0; i < 8; ++i) id[i] = number(n0 + i * 64 < total ? n0 + i * 64 : total - 1);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = value(id[i] < limit ? id[i] : (int)limit - 1);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (n0 + i * 64 < total) sk[n0 + i * 64] = k[i];
+                        if (n0 + i * 64 < total) sk[n0 + i * 64] = id[i] < limit ? order_of(v[i]) : 0;
                 }
                 wave_sync();
             };
             // keys of the groups of groups (the first stretch's are there), or of the rows where they are few
             const int whole = direct ? (int)left : (int)((groups + kSuper - 1) / kSuper);
             if (direct) {
-                gather(whole, row_key);
+                gather(whole, left, [](int n) { return n; }, row_value);
             } else if (first > 0) {
                 for (int n = lane; n < whole; n += 64) sk[n] = super_key(n);
             }
@@ -464,10 +470,7 @@ k_logprob_finish(FinishArgs F)
                 // (all loads of a level at a time, then what of it is kept)
                 for (int n0 = 0; fits && n0 < listed * kSuper; n0 += kDirect) {
                     const int some = listed * kSuper - n0 < kDirect ? listed * kSuper - n0 : kDirect;
-                    gather(some, [&](int n) {
-                        const int g = ol[(n0 + n) >> kSuperBits] * kSuper + (n & (kSuper - 1));
-                        return g < groups ? group_key(g) : 0;
-                    });
+                    gather(some, groups, [&](int n) { return ol[(n0 + n) >> kSuperBits] * kSuper + (n & (kSuper - 1)); }, group_value);
                     for (int n = lane; n < (some + 63) / 64 * 64; n += 64) {
                         const bool in = n < some && sk[n] >= bound;
                         const uint64_t all = __ballot(in);
@@ -480,10 +483,7 @@ k_logprob_finish(FinishArgs F)
                 fits = fits && opened <= kOpen;
                 for (int n0 = 0; fits && n0 < opened * kGroup; n0 += kDirect) {
                     const int some = opened * kGroup - n0 < kDirect ? opened * kGroup - n0 : kDirect;
-                    gather(some, [&](int n) {
-                        const int row = op[(n0 + n) >> kGroupBits] * kGroup + (n & (kGroup - 1));
-                        return row < left ? row_key(row) : 0;
-                    });
+                    gather(some, left, [&](int n) { return op[(n0 + n) >> kGroupBits] * kGroup + (n & (kGroup - 1)); }, row_value);
                     for (int n = lane; n < (some + 63) / 64 * 64; n += 64) {
                         const uint32_t k = n < some ? sk[n] : 0;
                         const uint64_t all = __ballot(k >= bound);
@@ -509,7 +509,7 @@ k_logprob_finish(FinishArgs F)
 #pragma unroll 4
                     for (int n = lane; n < candidates; n += 64) {
                         const int id = number(n);
-                        sk[n] = level == 0 ? super_key(id) : id >= limit ? 0 : level == 1 ? group_key(id) : row_key(id);
+                        sk[n] = level == 0 ? super_key(id) : id >= limit ? 0 : order_of(level == 1 ? group_value(id) : row_value(id));
                     }
                     const int some = (candidates + 63) / 64;
                     for (int n = candidates + lane; n < some * 64; n += 64) sk[n] = 0;
@@ -552,7 +552,7 @@ k_logprob_finish(FinishArgs F)
         }
         if (lane < best) {
             A.top_ids[lane * A.batch + t] = fr[lane];
-            A.top_logp[lane * A.batch + t] = logp_of(to_float(y[fr[lane] * A.ldy]));
+            A.top_logp[lane * A.batch + t] = logp_of(value_of(fk[lane]));
         }
     }
 }
