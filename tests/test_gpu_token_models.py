@@ -537,6 +537,33 @@ def test_attention_of_few_sequences(dtype, lengths, dk, dv):
         at += m
 
 
+@pytest.mark.parametrize("lengths,heads,dk,dv", [([2] * 8, 1, 64, 64), ([1, 31, 32], 2, 128, 128), ([5, 0, 20], 3, 90, 60), ([17, 30], 1, 192, 150), ([32, 3], 2, 256, 256)])
+def test_attention_of_a_few_bf16_tokens_is_rounded_once(lengths, heads, dk, dv):
+    """Results of few terms are those of 64 bits rounded to bf16, and 2^-14 of the sum of the terms' sizes beside that: nothing within is left at bf16."""
+    r = seeded("rounded once", lengths, heads, dk, dv)
+    parts, rates, (state, hstate) = attention_inputs(r, lengths, heads, dk, dv, BF16, True)
+    (q, hq), (k, hk), (v, hv) = parts
+    n, b, scale = sum(lengths), len(lengths), float(np.float32(dk ** -0.5))
+    y, _ = run_forward(parts, rates, state, lengths, dv, scale, True)
+    gy, hgy = rounded(r, (n, heads, dv), BF16)
+    gs, hgs = rounded(r, (b, heads, dk, dv), F32)
+    got = [torch.full((n, heads, d), float("nan"), device="cuda", dtype=BF16) for d in (dk, dk, dv)]
+    ws = torch.empty(B.laplex_decay_attention_workspace_bytes(BF16, n, b, heads, dk, dv), dtype=torch.uint8, device="cuda")
+    starts = dev(np.concatenate([[0], np.cumsum(lengths)]), torch.int64)
+    B.laplex_decay_attention_backward(q, k, v, dev(rates), gy, *got, ws, scale, b, starts, state, gs)
+    bound = lambda size, m, d, want: attention_bound(size, m, d, F32) + 2.0 ** -14 * size + 1.01 * H * np.abs(want)
+    at = 0
+    for i, m in enumerate(lengths):
+        for h in range(heads):
+            cut = lambda t: t[at:at + m, h]
+            wy, _, sy, _ = O.attention_sequence(cut(hq), cut(hk), cut(hv), rates[h], scale, hstate[i, h])
+            within(f"y[{i},{h}]", host(cut(y)), wy, bound(sy, m, dk, wy))
+            want, size = O.attention_sequence_backward(cut(hq), cut(hk), cut(hv), rates[h], scale, hstate[i, h], cut(hgy), hgs[i, h])
+            for name, t, w, s_, d in zip(("gq", "gk", "gv"), got, want, size, (dv, dv, dk)):
+                within(f"{name}[{i},{h}]", host(cut(t)), w, bound(s_, m, d, w))
+        at += m
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("sequences,heads,dk,dv", [(40, 16, 64, 64), (24, 24, 36, 96)])
 def test_attention_of_many_sequences_that_are_not_cut(dtype, sequences, heads, dk, dv):
