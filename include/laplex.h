@@ -363,7 +363,8 @@ int laplex_get_plan_status(const void* ws, size_t ws_bytes, int64_t count, uint3
  * rules above hold, with these differences: matrices are of one of the types below (`type`), a row of one holds what
  * belongs to one TOKEN ([heads][numbers of a head], ld >= their product, so that the parts of a fused projection's result
  * are read where they lie), and floats named `float*` are fp32 whatever the type.  Sums, states and statistics are held
- * in fp32 at least and rounded once, when they are written.
+ * in fp32 at least and rounded once, when they are written.  What goes from one product of bf16 matrices into the next is
+ * carried in 15 bits at least, and in all 24 where it goes into a state that is written.
  * ------------------------------------------------------------------------- */
 enum {
     LAPLEX_F32 = 0,

@@ -13,9 +13,10 @@
 // Sequences that are long and few are cut into stretches: one launch forms what each stretch adds to the state (k_attention_walk<STATES>, which
 // reads k and v alone), one brings these together in order (k_attention_carry), and then all stretches are walked at once.
 //
-// Numbers: bf16 q, k, v and results; sums and states are fp32.  P, and the state for the product q S alone, are rounded to bf16, as the result is (the error of
-// a result against 64 bits is 1.4 times that of rounding it alone; kShort below is for sequences of a few tokens).  What goes into a state that can be asked for is not rounded to bf16: l^d v is the
-// sum of three bf16 numbers, exactly, so a state is an fp32 sum of exact products.  fp32 runs on the fp32 matrix instructions.
+// Numbers: bf16 q, k, v and results; sums and states are fp32.  What goes from one product into the next is not rounded to the type: P, and the state for the
+// product q S, are the sum of two bf16 numbers (16 bits, where the result is rounded to 8: it is rounded once, whatever the lengths), and what goes into a state
+// that can be asked for is not rounded at all: l^d v is the sum of three bf16 numbers, exactly, so a state is an fp32 sum of exact products.  fp32 runs on
+// the fp32 matrix instructions.
 //
 // What bounds it: a chunk of 64 bf16 tokens of a head of 128 takes a compute unit 4.5 to 4.9 us with two workgroups on it; its LDS reads alone would
 // take 1.9, its vector instructions 1.8, its matrix products 1.0: they overlap only as far as sixteen wavefronts alternate.  us of the walk / states / carry:
@@ -244,6 +245,7 @@ __device__ __forceinline__ void split3(const float* x, bf16x8& hi, bf16x8& mid, 
     hi = uppers(x); mid = uppers(r); lo = uppers(q);
 }
 
+// x = hi + mid but for 2^-15 of x
 __device__ __forceinline__ void split2(const float* x, bf16x8& hi, bf16x8& mid)
 {
     float r[8];
@@ -254,14 +256,15 @@ __device__ __forceinline__ void split2(const float* x, bf16x8& hi, bf16x8& mid)
     for (int e = 0; e < 8; ++e) mid[e] = (__bf16)r[e];
 }
 
-__device__ __forceinline__ bool finite_bits(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
-// what rounding x to bf16 leaves out (nothing, where the rounded number is not finite)
-__device__ __forceinline__ __bf16 left_out(float x)
+__device__ __forceinline__ void split2(f32x4 x, bf16x4& hi, bf16x4& mid)
 {
-    const float r = (float)(__bf16)x;
-    return (__bf16)(finite_bits(r) ? x - r : 0.0f);
+    hi = __builtin_bit_cast(bf16x4, u32x2{__builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u),
+                                          __builtin_amdgcn_perm(__float_as_uint(x[3]), __float_as_uint(x[2]), 0x07060302u)});
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mid[e] = (__bf16)(x[e] - upper(x[e]));
 }
 
+__device__ __forceinline__ bool finite_bits(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
 __device__ __forceinline__ bool finite_patch(const Patch<float>& p)
 {
     uint32_t most = 0;
@@ -356,17 +359,14 @@ struct Geometry {
     static constexpr int COLS = 16 * WAVES;                                      // columns of a workgroup
     static constexpr int ROW = (DK * (int)sizeof(T) / 16 + 7) / 8 * 8, SEQ = C * (int)sizeof(T) / 16;   // slots of a row of numbers (a multiple of 8: they are permuted by eights), of tokens
     static constexpr int CT = C / 16, DT = DK / 16, KD = DK / K, KC = C / K;
-    static constexpr int kBytesRows = C * ROW * 16, kBytesK = DK * SEQ * 16, kBytesV = COLS * SEQ * 16, kBytesP = C * SEQ * 16;
-    static constexpr bool kRests = sizeof(T) == 2 && KC == 1;               // what rounding leaves out of P has a tile of its own
+    static constexpr int kBytesRows = C * ROW * 16, kBytesK = DK * SEQ * 16, kBytesV = COLS * SEQ * 16;
+    // bf16: P's second part is kept beside the first.  Of rows below 32 it lies 32 tokens further along where a row has 64 (they see none of those), of the others, and
+    // where a row has 32, 32 rows further down.
+    static constexpr int kBytesP = (C + (sizeof(T) == 2 ? 32 : 0)) * SEQ * 16;
     static constexpr int kLds = 2 * kBytesRows + kBytesK + kBytesV + kBytesP;
 };
 
-enum { kWalk, kStates, kShort };
-// kStates: only what a stretch adds to the state, for the stretches behind it (U below).  kShort: bf16 sequences of at most kShortTokens.  A chunk of at most 32
-// tokens, which a sequence of few tokens is, there has what rounding leaves out of P beside it (in the columns from 32 on where a chunk has more, which are
-// free then), and what it leaves out of the state in the product q S: of sums of few terms the rounding of P would be as much again as that of the
-// result, and would not average out over so few rows.  (In the kernel for all lengths it would take registers that are not there: 48 bytes of scratch a lane.)
-constexpr int64_t kShortTokens = 128;
+enum { kWalk, kStates };      // kStates: only what a stretch adds to the state, for the stretches behind it (U below)
 
 template <typename T, int DK, int WAVES, int MODE>
 __global__ void __launch_bounds__(64 * WAVES, (MODE == kStates && sizeof(T) == 4 ? (DK > 128 ? 4 : DK > 96 ? 5 : 6) : DK > 128 ? 2 : DK > 96 ? 4 : DK > 64 && sizeof(T) == 4 ? 5 : 3))      // as many as LDS and the state leave room for
@@ -374,18 +374,17 @@ k_attention_walk(AttentionArgs A)
 {
     typedef Geometry<T, DK, WAVES> G;
     constexpr bool STATES = MODE == kStates;
-    constexpr int kRestBytes = MODE == kShort && G::kRests ? G::kBytesP : 0;
     typedef typename Num<T>::frag frag;
     typedef typename Num<T>::quad quad;
     constexpr int E = G::E, C = G::C, R = G::R, ROW = G::ROW, SEQ = G::SEQ, CT = G::CT, DT = G::DT, KD = G::KD, KC = G::KC, THREADS = G::THREADS;
-    __shared__ __attribute__((aligned(16))) char lds[STATES ? G::kBytesK + G::kBytesV : G::kLds + kRestBytes];
+    __shared__ __attribute__((aligned(16))) char lds[STATES ? G::kBytesK + G::kBytesV : G::kLds];
     __shared__ float power[C + 1], weight[C];          // l^d, and the weights of the chunk's tokens in the state
     __shared__ int odd[2];
     char* const Kt = lds;                              // [DK][C]
     char* const Vt = Kt + G::kBytesK;                  // [COLS][C]
     char* const Qs = Vt + G::kBytesV;                  // [C][DK], as Ks
     char* const Ks = Qs + G::kBytesRows;
-    char* const Ps = Ks + G::kBytesRows;               // [C][C]
+    char* const Ps = Ks + G::kBytesRows;               // [C][C], and its second part
 
     // heads side by side: the slots that have nothing to do are then spread over the chiplets, which take workgroups in turn
     const int walks = STATES ? A.sets : A.walks, walk = blockIdx.z % walks, slice = blockIdx.x % A.slices, h = blockIdx.x / A.slices, col0 = slice * G::COLS;
@@ -399,7 +398,7 @@ k_attention_walk(AttentionArgs A)
     const double rate = (double)rate_of(A.rates, h);
     for (int d = x; d <= C; d += THREADS) power[d] = (float)exp(-rate * d);
     if (!STATES)
-        for (int i = x; i < (G::kBytesP + kRestBytes) / 16; i += THREADS) reinterpret_cast<f32x4*>(Ps)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = x; i < G::kBytesP / 16; i += THREADS) reinterpret_cast<f32x4*>(Ps)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (x < 2) odd[x] = 0;
     // A chunk's decay as an fp32 number and what its rounding leaves out, in parts of it: the same rounding in every chunk would add up, so the
     // next number up or down is taken whenever what has been left out reaches half of their distance.  The last chunk may be shorter.
@@ -539,7 +538,6 @@ k_attention_walk(AttentionArgs A)
         values.base += wave * 16 * SEQ * 16;
         values.low ^= ((2 * wave) & Reader<SEQ>::kMask) * 16;
         if (!STATES) {
-            const bool rests = MODE == kShort && valid <= 32;
             // P: tiles on and below the diagonal, dealt to the wavefronts; as it leaves the accumulator a lane holds P[i][j .. j + 3]
 #pragma unroll
             for (int n = 0; n < (CT * (CT + 1) / 2 + WAVES - 1) / WAVES; ++n) {
@@ -550,22 +548,24 @@ k_attention_walk(AttentionArgs A)
                     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int m = 0; m < KD; ++m) acc = mma(get<T>(Ks, rows.at(jt, m)), get<T>(Qs, rows.at(it, m)), acc);
-                    quad w;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int d = 16 * (it - jt) + r16 - 4 * g - r;
                         acc[r] = d >= 0 ? acc[r] * power[d < 0 ? 0 : d] : 0.0f;
-                        w[r] = (T)acc[r];
                     }
                     const int j = 16 * jt + 4 * g;
-                    *reinterpret_cast<quad*>(Ps + 16 * slot_at<SEQ>(16 * it + r16, j / E) + (j % E) * (int)sizeof(T)) = w;
-                    if constexpr (MODE == kShort)
-                        if (rests && it < 2) {
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) w[r] = left_out(acc[r]);
-                            const int at = G::kRests ? j : j + 32;
-                            *reinterpret_cast<quad*>(Ps + kRestBytes + 16 * slot_at<SEQ>(16 * it + r16, at / E) + (at % E) * (int)sizeof(T)) = w;
-                        }
+                    const auto put = [&](int row, int j, quad w) {
+                        *reinterpret_cast<quad*>(Ps + 16 * slot_at<SEQ>(row + r16, j / E) + (j % E) * (int)sizeof(T)) = w;
+                    };
+                    if constexpr (sizeof(T) == 2) {
+                        quad hi, mid;
+                        split2(acc, hi, mid);
+                        put(16 * it, j, hi);
+                        const bool along = KC == 2 && it < 2;
+                        put(along ? 16 * it : 16 * it + 32, along ? j + 32 : j, mid);
+                    } else {
+                        put(16 * it, j, acc);
+                    }
                 }
             }
             // q S, weighted by the rows
@@ -576,35 +576,24 @@ k_attention_walk(AttentionArgs A)
 #pragma unroll
             for (int m = 0; m < KD; ++m) {
                 if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);     // (all steps' fragments at once do not fit the registers)
-                frag sf;
+                constexpr int TERMS = sizeof(T) == 2 ? 2 : 1;
+                frag sf[TERMS];
                 if constexpr (sizeof(T) == 2) {
-                    // rounded for this product alone, as P is for its own: the result is rounded as much again
+                    float xs[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sf[e] = (__bf16)S[2 * m + (e >> 2)][e & 3];
+                    for (int e = 0; e < 8; ++e) xs[e] = S[2 * m + (e >> 2)][e & 3];
+                    split2(xs, sf[0], sf[1]);
                 } else {
-                    sf = S[m];
+                    sf[0] = S[m];
                 }
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
                     const frag qf = get<T>(Qs, rows.at(t, m));
-                    O[t] = mma(sf, qf, O[t]);
+#pragma unroll
+                    for (int p = 0; p < TERMS; ++p) O[t] = mma(sf[p], qf, O[t]);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (MODE == kShort)
-                if (rests) {
-                    const Reader<ROW> again(here(r16), here(g));
-#pragma unroll
-                    for (int m = 0; m < KD; ++m) {
-                        __builtin_amdgcn_sched_barrier(0);
-                        frag sf;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sf[e] = left_out(S[2 * m + (e >> 2)][e & 3]);
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) O[t] = mma(sf, get<T>(Qs, again.at(t, m)), O[t]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
 #pragma unroll
             for (int t = 0; t < CT; ++t) {
                 const float ahead = power[16 * t + r16 + W.lead];
@@ -624,18 +613,12 @@ k_attention_walk(AttentionArgs A)
                     if (16 * t + 15 >= m * G::K) {
                         const frag pf = get<T>(Ps, columns.at(t, m));
                         O[t] = mma(vf, pf, O[t]);
+                        if constexpr (sizeof(T) == 2) {
+                            const bool along = KC == 2 && t < 2;
+                            O[t] = mma(vf, get<T>(Ps, columns.at(along ? t : t + 2, along ? 1 : m)), O[t]);
+                        }
                     }
             }
-            if constexpr (MODE == kShort)
-                if (rests) {
-                    const Reader<SEQ> again(here(r16), here(g));
-                    frag vf = get<T>(Vt, values.at(0, 0));
-                    if (slow)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) vf[e] = finite_bits((float)vf[e]) ? vf[e] : (T)0.0f;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) O[t] = mma(vf, get<T>(Ps + kRestBytes, again.at(t, KC - 1)), O[t]);
-                }
             if (slow)
                 for (int j = 0; j < C; ++j) {
                     const int i0 = here(r16), n0 = here(wave * 16 + 4 * g);
@@ -901,11 +884,7 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
         profile_after("attention_carry", st);
     }
     profile_before("attention_walk", st);
-    // (a sequence that is not cut is a stretch)
-    if (sizeof(T) == 2 && !P.cut && P.stretch <= kShortTokens)
-        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, sizeof(T) == 2 ? kShort : kWalk>), grid, dim3(64 * WAVES), 0, st, A);
-    else
-        hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, kWalk>), grid, dim3(64 * WAVES), 0, st, A);
+    hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, kWalk>), grid, dim3(64 * WAVES), 0, st, A);
     profile_after("attention_walk", st);
     return hipGetLastError();
 }

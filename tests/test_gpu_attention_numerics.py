@@ -1,0 +1,140 @@
+"""Numerics of the attention with a decay for each head that per-element bounds on the sum of absolute terms do not show.
+
+Tolerances.  U = 2^-24 and H = 2^-8 are the unit roundings of fp32 and bf16.  A bf16 call's factors between its products are two bf16 numbers, off by at most
+2^-15 of themselves, and a term passes two of them: 2^-14 of the sum of absolute terms, beside the fp32 sums' 16 sqrt(n + d + 64) U of it and the result's one rounding, H.
+In the 2-norm: a result that is off by e before it is rounded is rounded the other way with the probability e / ulp, and is then a whole ulp off: against the exact result
+rounded to bf16 the difference is sqrt(e ulp) on average over many.  With e = 2^-15 of the results' size and an ulp of at most 2^-7 that is 2^-11; 2^-10 is allowed.
+"""
+import numpy as np
+import pytest
+
+from oracle import token_oracle as O
+from paper_2605_24584_amd import binding as B
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U, H = 2.0 ** -24, 2.0 ** -8
+F32, BF16 = torch.float32, torch.bfloat16
+RATES = np.array([0.03, 0.7, 0.0, 0.002, 3.0, 0.25], np.float32)
+
+
+def seeded(*what):
+    import zlib
+    return np.random.default_rng(zlib.crc32(repr(what).encode()))
+
+
+def dev(v, dtype=F32):
+    return torch.from_numpy(np.ascontiguousarray(v)).to("cuda").to(dtype)
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def within(name, got, want, bound):
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (f"{name}: {int(bad.sum())} of {bad.size} off, first at {tuple(np.argwhere(bad)[0])}: "
+                           f"{got[bad][0]} instead of {want[bad][0]}, may be off by {np.broadcast_to(bound, bad.shape)[bad][0]}")
+
+
+class Problem:
+    """Inputs of a forward and a backward call; `starts` is None for equal lengths that are not packed."""
+
+    def __init__(self, lengths, heads, dk, dv, dtype, packed=True, states=True, scale=None, rates=None, what=""):
+        r = seeded(what, lengths, heads, dk, dv)
+        n, b = int(sum(lengths)), len(lengths)
+        self.lengths, self.heads, self.dk, self.dv, self.dtype, self.n, self.b = lengths, heads, dk, dv, dtype, n, b
+        of = lambda *s, t=dtype: dev(r.normal(size=s).astype(np.float32), t)
+        self.q, self.k, self.v, self.gy = of(n, heads, dk), of(n, heads, dk), of(n, heads, dv), of(n, heads, dv)
+        self.state, self.gstate = (of(b, heads, dk, dv, t=F32), of(b, heads, dk, dv, t=F32)) if states else (None, None)
+        self.rates = np.resize(RATES if rates is None else np.asarray(rates, np.float32), heads)
+        self.scale = float(np.float32(dk ** -0.5 if scale is None else scale))
+        self.starts = dev(np.concatenate([[0], np.cumsum(lengths)]), torch.int64) if packed else None
+
+    def workspace(self):
+        """Of exactly the size that is asked for; what it holds does not matter."""
+        size = B.laplex_decay_attention_workspace_bytes(self.dtype, self.n, self.b, self.heads, self.dk, self.dv)
+        return torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def new(self, *s, t=None):
+        return torch.full(s, float("nan"), device="cuda", dtype=t or self.dtype)
+
+    def forward(self):
+        y, last = self.new(self.n, self.heads, self.dv), self.new(self.b, self.heads, self.dk, self.dv, t=F32)
+        B.laplex_decay_attention(self.q, self.k, self.v, dev(self.rates), y, self.workspace(), self.scale, self.b, self.starts, self.state, last)
+        return {"y": y, "state": last}
+
+    def backward(self):
+        gq, gk, gv = (self.new(self.n, self.heads, d) for d in (self.dk, self.dk, self.dv))
+        g0 = self.new(self.b, self.heads, self.dk, self.dv, t=F32)
+        B.laplex_decay_attention_backward(self.q, self.k, self.v, dev(self.rates), self.gy, gq, gk, gv, self.workspace(), self.scale, self.b, self.starts,
+                                          self.state, self.gstate, g0)
+        return {"gq": gq, "gk": gk, "gv": gv, "gstate": g0}
+
+    def each(self, got):
+        """(name, what was got, the definition's result in 64 bits, its sum of absolute terms, tokens) for every sequence and head"""
+        at = 0
+        for i, n in enumerate(self.lengths):
+            for h in range(self.heads):
+                q, k, v, gy = (host(t[at:at + n, h]) for t in (self.q, self.k, self.v, self.gy))
+                S, G = (None if t is None else host(t[i, h]) for t in (self.state, self.gstate))
+                want = dict(zip(("y", "state", "|y|", "|state|"), O.attention_sequence(q, k, v, self.rates[h], self.scale, S))) if "y" in got else {}
+                if "gq" in got:
+                    w, s = O.attention_sequence_backward(q, k, v, self.rates[h], self.scale, S, gy, G)
+                    for name, a, b in zip(("gq", "gk", "gv", "gstate"), w, s):
+                        want[name], want[f"|{name}|"] = a, b
+                for name, t in got.items():
+                    yield f"{name}[{i},{h}]", host(t[i, h] if "state" in name else t[at:at + n, h]), want[name], want[f"|{name}|"], n
+            at += n
+
+
+# --- bf16 results are rounded once, whatever the lengths and however the sequences are passed ---------------------------------------
+
+ONCE = [
+    ([2] * 64, 2, 64, 64, True), ([2] * 70, 1, 128, 128, True), ([3, 1, 4, 2] * 20, 1, 96, 80, True), ([5, 2] * 30, 1, 190, 256, True),      # packed, over 128 tokens in all
+    ([2] * 70, 1, 64, 64, False), ([130, 7], 2, 128, 128, True), ([64], 2, 64, 48, False), ([65, 31, 33], 1, 128, 100, True),
+    ([700, 3, 0, 64, 65], 3, 96, 80, True), ([2000], 3, 128, 128, False), ([900, 900], 3, 64, 128, False), ([1100], 2, 256, 256, False), ([600, 40], 2, 192, 130, True),
+]
+
+
+@pytest.mark.parametrize("lengths,heads,dk,dv,packed", ONCE)
+@pytest.mark.parametrize("states", [False, True])
+def test_bf16_results_are_rounded_once(lengths, heads, dk, dv, packed, states):
+    p = Problem(lengths, heads, dk, dv, BF16, packed, states, what="once")
+    off, size = {}, {}
+    for name, got, want, terms, n in p.each({**p.forward(), **p.backward()}):
+        exact = 16 * np.sqrt(n + max(dk, dv) + 64.0) * U * terms
+        if "state" in name:
+            within(name, got, want, exact)
+            continue
+        within(name, got, want, exact + 2.0 ** -14 * terms + 1.01 * H * np.abs(want))
+        once = host(torch.from_numpy(want).to(BF16))
+        kind = name.split("[")[0], name.split(",")[1]
+        off[kind] = off.get(kind, 0.0) + ((got - once) ** 2).sum()
+        size[kind] = size.get(kind, 0.0) + (want ** 2).sum()
+    for kind in off:
+        assert off[kind] <= (2.0 ** -10) ** 2 * size[kind], f"{kind}: {np.sqrt(off[kind] / size[kind]):.2e} from the rounded result"
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_short_sequence_has_the_same_bits_in_every_pack(dtype):
+    """Alone, of equal lengths, and packed among others."""
+    few = Problem([20] * 3, 2, 64, 48, dtype, False, what="pack")
+    many = Problem([20] * 40, 2, 64, 48, dtype, True, what="pack of more")
+    long = Problem([900, 20, 0, 20, 20, 1500], 2, 64, 48, dtype, True, what="pack with long ones")
+    places = {many: (list(range(0, 60, 20)), [0, 1, 2]), long: ([900, 920, 940], [1, 3, 4])}
+    for p, (rows, sequences) in places.items():
+        for name in ("q", "k", "v", "gy"):
+            for i, at in enumerate(rows):
+                getattr(p, name)[at:at + 20] = getattr(few, name)[20 * i:20 * i + 20]
+        for name in ("state", "gstate"):
+            getattr(p, name)[sequences] = getattr(few, name)
+        p.scale = few.scale
+    want = {**few.forward(), **few.backward()}
+    for p, (rows, sequences) in places.items():
+        got = {**p.forward(), **p.backward()}
+        for name, t in want.items():
+            for i, at in enumerate(rows):
+                one = got[name][sequences[i]] if "state" in name else got[name][at:at + 20]
+                assert torch.equal(one, t[i] if "state" in name else t[20 * i:20 * i + 20]), name
