@@ -429,7 +429,9 @@ int laplex_rotary_frequencies(float* frequencies, int64_t rotary_dim, double bas
  * Rows before a value that is not finite are not touched by it; from its token on everything that it is weighted into is not finite.
  */
 int laplex_decay_attention_workspace_bytes(int type, int64_t tokens, int64_t sequences, int64_t heads, int64_t dk, int64_t dv,
-                                           size_t* out /* host; enough for the forward and the backward call */);
+                                           size_t* out /* host */);
+/* Enough for the forward and the backward call of that type, heads, dk, dv with up to so many tokens and sequences, of equal lengths or packed: one workspace for the
+ * longest prompt and the largest batch serves all smaller ones.  It does not grow with the tokens or the sequences for long (0.54 GB at most). */
 
 int laplex_decay_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
                            int64_t tokens, int64_t sequences, const int64_t* starts, int64_t heads, int64_t dk, int64_t dv,

@@ -289,6 +289,9 @@ __device__ __forceinline__ bool finite_patch(const Patch<__bf16>& p)
 // Which stretch of which sequence: sequences are cut into stretches of `stretch` tokens (a multiple of every C), each with a slot.  Of equal lengths
 // every sequence has its slots; otherwise sequence b has those from start / stretch + b on: at least one, and as many as it has stretches, and a
 // slot beyond those has nothing to do.
+//
+// A sequence of several stretches has a place in the workspace for the state that enters each.  They are numbered like the slots, but for b, where no more than
+// start / (stretch + 1) sequences before this one can have several: however many short sequences are packed, there are at most two places for `stretch` tokens.
 // ----------------------------------------------------------------------------
 constexpr int64_t kSlotRows = 32768;      // slots along a grid's second axis
 
@@ -302,21 +305,31 @@ struct Stretch {
 
 __device__ __forceinline__ int64_t first_slot(const AttentionArgs& A, int64_t b, int64_t begin)
 {
-    return A.starts ? begin / A.stretch + b : b * A.per_sequence;
+    return A.starts ? (uint32_t)begin / (uint32_t)A.stretch + b : b * A.per_sequence;
 }
 
+__device__ __forceinline__ int64_t first_place(const AttentionArgs& A, int64_t b, int64_t begin)
+{
+    if (!A.starts) return b * A.per_sequence;
+    const int64_t several = (uint32_t)begin / (uint32_t)(A.stretch + 1);
+    return (uint32_t)begin / (uint32_t)A.stretch + (b < several ? b : several);
+}
+
+// The stretch with this slot, or (PLACES) the one with this place, if there is one.
+template <bool PLACES>
 __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& A, int64_t slot)
 {
+    const auto first = [&](int64_t b, int64_t begin) { return PLACES ? first_place(A, b, begin) : first_slot(A, b, begin); };
     Stretch s;
     int64_t lo = 0;
     if (A.starts) {
-        // the last sequence whose first slot is at most this one: 64 candidates at a time
+        // the last sequence whose first one is at most this one: 64 candidates at a time
         int64_t hi = A.sequences;                      // in [lo, hi)
         const int lane = threadIdx.x & 63;
         while (hi - lo > 1) {
             const int64_t step = (hi - lo + 63) / 64;
             const int64_t c = lo + lane * step;
-            const bool mine = c < hi && start_of(A.starts, A.tokens, A.sequences, c) / A.stretch + c <= slot;
+            const bool mine = c < hi && first(c, start_of(A.starts, A.tokens, A.sequences, c)) <= slot;
             const uint64_t votes = __ballot(mine);
             const int at = votes ? 63 - __builtin_clzll(votes) : 0;
             lo += at * step;
@@ -329,7 +342,7 @@ __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& A, int64_t 
     s.begin = start_of(A.starts, A.tokens, A.sequences, lo);
     const int64_t end = start_of(A.starts, A.tokens, A.sequences, lo + 1);
     s.count = end > s.begin ? end - s.begin : 0;
-    s.index = slot - first_slot(A, lo, s.begin);
+    s.index = slot - first(lo, s.begin);
     s.lo = s.index * A.stretch;
     s.there = s.index >= 0 && (s.lo < s.count || s.index == 0);
     s.hi = s.lo + A.stretch < s.count ? s.lo + A.stretch : s.count;
@@ -390,8 +403,8 @@ k_attention_walk(AttentionArgs A)
     const int walks = STATES ? A.sets : A.walks, walk = blockIdx.z % walks, slice = blockIdx.x % A.slices, h = blockIdx.x / A.slices, col0 = slice * G::COLS;
     const int64_t slot = (int64_t)(blockIdx.z / walks) * kSlotRows + blockIdx.y;
     const Walk W = STATES ? A.states[walk] : A.walk[walk];
-    if (slot >= A.slots || col0 >= W.dv) return;
-    const Stretch s = find_stretch(A, slot);
+    if (slot >= (STATES ? A.places : A.slots) || col0 >= W.dv) return;
+    const Stretch s = find_stretch<STATES>(A, slot);
     if (!s.there || (STATES && s.last)) return;
 
     const int x = threadIdx.x, lane = x & 63, wave = __builtin_amdgcn_readfirstlane(x >> 6), r16 = lane & 15, g = lane >> 4;
@@ -420,10 +433,12 @@ k_attention_walk(AttentionArgs A)
     const int col = col0 + 16 * wave + r16;
     const int64_t state_at = (s.b * A.heads + h) * (int64_t)W.dk * W.dv;
     constexpr int kPieces = DK * G::COLS / 4;
-    f32x4* const set = reinterpret_cast<f32x4*>(A.ws) + (((int64_t)(STATES ? walk : W.set) * A.slots + slot) * A.heads + h) * A.slices * kPieces;
+    const int64_t place = STATES ? slot : first_place(A, s.b, s.begin) + s.index;
+    f32x4* const set = reinterpret_cast<f32x4*>(A.ws) + (((int64_t)(STATES ? walk : W.set) * A.places + place) * A.heads + h) * A.slices * kPieces;
     f32x4* const U = set + (int64_t)slice * kPieces + wave * DT * 64 + lane;
-    // (of sequences that are cut the initial state, too, comes from U: another workgroup may already write the last state, in its place)
-    const bool from_set = !STATES && A.cut && (s.index > 0 || W.state_in), from_given = !STATES && !A.cut && W.state_in;
+    // (of several stretches the first one's state, too, comes from U: another workgroup may already write the last state, in its place)
+    const bool several = s.count > A.stretch;
+    const bool from_set = !STATES && several && (s.index > 0 || W.state_in), from_given = !STATES && !several && W.state_in;
     // One branch for all loads of a kind, and others in the place of what does not exist: nothing waits for one of them before the next is asked for.
     if (from_set && !W.set_transposed) {
 #pragma unroll
@@ -729,8 +744,8 @@ k_attention_carry(AttentionArgs A)
         const int lane = piece & 63, t = (piece >> 6) % DT, wave = piece / (64 * DT);
         const int64_t begin = start_of(A.starts, A.tokens, A.sequences, b), end = start_of(A.starts, A.tokens, A.sequences, b + 1);
         const int64_t count = end > begin ? end - begin : 0, stretches = (count + A.stretch - 1) / A.stretch;
-        const int64_t slot = first_slot(A, b, begin);
-        if ((stretches < 2 && !W.state_in) || slot >= A.slots || slot + stretches > A.slots) continue;
+        const int64_t place = first_place(A, b, begin);
+        if (stretches < 2 || place + stretches > A.places) continue;
         const double d = exp(-(double)rate_of(A.rates, h) * (double)A.stretch);
         const float hi = (float)d, lo = (float)(d - (double)hi);
         f32x4 carry = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -744,9 +759,8 @@ k_attention_carry(AttentionArgs A)
             }
         }
         const int64_t step = (int64_t)A.heads * A.slices * kPieces;
-        f32x4* U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.slots + slot) * A.heads + h) * A.slices + slice) * kPieces + piece;
-        f32x4 next = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (stretches > 1) next = U[0];
+        f32x4* U = reinterpret_cast<f32x4*>(A.ws) + ((((int64_t)blockIdx.z * A.places + place) * A.heads + h) * A.slices + slice) * kPieces + piece;
+        f32x4 next = U[0];
         if (W.state_in) U[0] = carry;
         for (int64_t n = 1; n < stretches; ++n) {
 #pragma unroll
@@ -820,9 +834,11 @@ k_attention_step(AttentionStepArgs A, int lanes_log2, int slices)
 
 struct Plan {
     int dk, cols, slices;              // padded rows of the state, columns of a workgroup, workgroups side by side
-    int64_t stretch, per_sequence, slots;
+    int64_t stretch, per_sequence, slots, places;
     bool cut;                          // some sequence may have more than one stretch
 };
+
+constexpr int64_t kPackedWorkgroups = 2048, kLeastStretch = 64;
 
 // By the sizes alone.  walks: 1 for the forward call, 3 for the backward one, also where not all gradients are wanted (what one of them is must not
 // depend on the others).
@@ -839,14 +855,14 @@ Plan plan_of(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, in
     // stretch is what the others wait for.  us, stretches of 256 / 512 / 1024 / 2048 / whole sequences: 4 x 2048 tokens, 16 heads 82 / 80 / 128 / - / 164; 65536
     // tokens, 8 heads 369 / 283 / 258 / 318 / 5155; 8 x 4096, 16 heads 294 / 250 / 229 / 264 / 344, their gradients 835 / 698 / 632 / 592 / 492; 24 sequences of
     // 1250 tokens on average, 6 heads, fp32 277 / 286 / 530 / 604 / 641, their gradients 694 / 699 / 902 / 1050 / 1061.
-    const int64_t work = tokens * heads * P.slices * walks, workgroups = equal ? 512 : 2048;
-    P.stretch = (work / workgroups + 63) / 64 * 64;
+    const int64_t work = tokens * heads * P.slices * walks, workgroups = equal ? 512 : kPackedWorkgroups;
+    P.stretch = (work + 64 * workgroups - 1) / (64 * workgroups) * 64;
     // At least 256 tokens, or the states that pass through memory cost more than the walks.  Where even those leave compute units without a workgroup the
     // time is that of one workgroup's stretch, twice, and of the chain of states over the stretches: shorter ones, the more so the shorter the sequence.
     // us, stretches of 256 / 128 / 64, one sequence, bf16, a head of 128: 384 tokens 32 / 26 / 21; 1024 40 / 28 / 24; 4096 44 / 36 / 37; 16384 58 / 62 / 92;
     // fp32 77 / 48 / 32; 83 / 50 / 34; 88 / 58 / 48; 101 / 84 / 103.  Sequences of a few tokens on average need none of it.
     int64_t least = 256;
-    if (work < 256 * 256 && tokens >= 64 * sequences) least = longest <= 2048 ? 64 : longest <= 8192 ? 128 : 256;
+    if (work < 256 * 256 && tokens >= 64 * sequences) least = longest <= 2048 ? kLeastStretch : longest <= 8192 ? 128 : 256;
     if (P.stretch < least) P.stretch = least;
     // (192 tokens whole / in stretches of 64: bf16 18 / 19 us, their gradients 18 / 22; fp32 41 / 31 and 41 / 34)
     P.cut = longest > 2 * P.stretch && longest > (bf16 ? 256 : 128);
@@ -854,12 +870,9 @@ Plan plan_of(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, in
     P.per_sequence = equal ? (longest + P.stretch - 1) / P.stretch : 0;
     if (equal && P.per_sequence < 1) P.per_sequence = 1;
     P.slots = equal ? sequences * P.per_sequence : tokens / P.stretch + sequences;
+    const int64_t several = tokens / (P.stretch + 1);
+    P.places = !P.cut ? 0 : equal ? P.slots : tokens / P.stretch + (sequences < several ? sequences : several);
     return P;
-}
-
-size_t plan_bytes(const Plan& P, int heads, int sets)
-{
-    return P.cut ? (size_t)sets * P.slots * heads * P.slices * P.dk * P.cols * sizeof(float) : 0;
 }
 
 bool allows(const void* p, int64_t ld, int d, int size, int bytes)
@@ -872,8 +885,9 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
 {
     const int64_t deep = (P.slots + kSlotRows - 1) / kSlotRows;
     const dim3 grid((unsigned)(A.heads * P.slices), (unsigned)(deep > 1 ? kSlotRows : P.slots), (unsigned)(deep * A.walks));
-    const dim3 sets_grid(grid.x, grid.y, (unsigned)(deep * A.sets));
     if (P.cut) {
+        const int64_t places_deep = (P.places + kSlotRows - 1) / kSlotRows;
+        const dim3 sets_grid(grid.x, (unsigned)(places_deep > 1 ? kSlotRows : P.places), (unsigned)(places_deep * A.sets));
         profile_before("attention_states", st);
         hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, kStates>), sets_grid, dim3(64 * WAVES), 0, st, A);
         profile_after("attention_states", st);
@@ -901,24 +915,25 @@ hipError_t walk_of(const AttentionArgs& A, const Plan& P, hipStream_t st)
 
 }  // namespace
 
-size_t attention_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv)
+// For any number of tokens and sequences up to these, the forward and the backward call, lengths that are equal or not: a stretch has at least kLeastStretch tokens and
+// at least work / kPackedWorkgroups, so that there are at most `most` whole ones, and a place more for each sequence of several.
+size_t attention_workspace(int64_t tokens, int64_t sequences, int heads, int dk, int dv)
 {
-    // the forward and the backward call, with lengths that are equal or not
-    size_t most = 0;
-    for (int walks = 1; walks <= 3; walks += 2)
-        for (int equal = 0; equal < 2; ++equal) {
-            if (equal && (sequences == 0 || tokens % sequences != 0)) continue;
-            const size_t bytes = plan_bytes(plan_of(bf16, tokens, sequences, heads, dk, dv, walks, equal != 0), heads, walks > 1 ? 2 : 1);
-            most = bytes > most ? bytes : most;
-        }
-    return sequences > 0 && heads > 0 ? most : 0;
+    size_t bytes = 0;
+    for (int walks = 1; walks <= 3 && heads > 0 && tokens > 128; walks += 2) {
+        const Plan P = plan_of(false, tokens, sequences, heads, dk, dv, walks, false);
+        const int64_t by_work = kPackedWorkgroups / ((int64_t)heads * P.slices * walks), most = tokens / kLeastStretch < by_work ? tokens / kLeastStretch : by_work;
+        const size_t here = (size_t)(walks > 1 ? 2 : 1) * (most + (sequences < most ? sequences : most)) * heads * P.slices * P.dk * P.cols * sizeof(float);
+        bytes = here > bytes ? here : bytes;
+    }
+    return bytes;
 }
 
 hipError_t launch_attention(const AttentionArgs& given, hipStream_t st)
 {
     AttentionArgs A = given;
     const Plan P = plan_of(A.bf16, A.tokens, A.sequences, A.heads, A.walk[0].dk, A.walk[0].dv, A.backward ? 3 : 1, A.starts == nullptr);
-    A.cut = P.cut; A.stretch = P.stretch; A.per_sequence = P.per_sequence; A.slots = P.slots; A.slices = P.slices;
+    A.stretch = P.stretch; A.per_sequence = P.per_sequence; A.slots = P.slots; A.places = P.places; A.slices = P.slices;
     const int size = A.bf16 ? 2 : 4;
     const auto flags = [&](const Walk& W) {
         return (allows(W.q, W.ldq, W.dk, size, 4 * size) ? 1 : 0) | (allows(W.k, W.ldk, W.dk, size, 4 * size) ? 2 : 0) |

@@ -112,7 +112,7 @@ int laplex_decay_attention_workspace_bytes(int type, int64_t tokens, int64_t seq
 {
     if (!out) return LAPLEX_ERR_NULL;
     LAPLEX_CHECK(check_attention_sizes(type, tokens, sequences, heads, dk, dv, false));
-    *out = attention_workspace(type == LAPLEX_BF16, tokens, sequences, (int)heads, (int)dk, (int)dv);
+    *out = attention_workspace(tokens, sequences, (int)heads, (int)dk, (int)dv);
     return LAPLEX_OK;
 }
 
@@ -132,7 +132,7 @@ int laplex_decay_attention(const void* q, int64_t ldq, const void* k, int64_t ld
     LAPLEX_CHECK(check_array(state_in, sequences * heads, 4, false));
     LAPLEX_CHECK(check_array(state_out, sequences * heads, 4, false));
     if (sequences == 0 || heads == 0 || (tokens == 0 && !state_out)) return LAPLEX_OK;
-    LAPLEX_CHECK(check_ws(ws, ws_bytes, attention_workspace(type == LAPLEX_BF16, tokens, sequences, (int)heads, (int)dk, (int)dv)));
+    LAPLEX_CHECK(check_ws(ws, ws_bytes, attention_workspace(tokens, sequences, (int)heads, (int)dk, (int)dv)));
     AttentionArgs A{};
     A.starts = starts; A.tokens = tokens; A.sequences = sequences; A.heads = (int)heads; A.rates = rates;
     A.bf16 = type == LAPLEX_BF16; A.ws = static_cast<char*>(ws);
@@ -168,7 +168,7 @@ int laplex_decay_attention_backward(const void* q, int64_t ldq, const void* k, i
     LAPLEX_CHECK(check_array(gstate_out, sequences * heads, 4, false));
     LAPLEX_CHECK(check_array(gstate_in, sequences * heads, 4, false));
     if (sequences == 0 || heads == 0 || (tokens == 0 && !gstate_in) || (!gq && !gk && !gv && !gstate_in)) return LAPLEX_OK;
-    LAPLEX_CHECK(check_ws(ws, ws_bytes, attention_workspace(type == LAPLEX_BF16, tokens, sequences, (int)heads, (int)dk, (int)dv)));
+    LAPLEX_CHECK(check_ws(ws, ws_bytes, attention_workspace(tokens, sequences, (int)heads, (int)dk, (int)dv)));
     AttentionArgs A{};
     A.starts = starts; A.tokens = tokens; A.sequences = sequences; A.heads = (int)heads; A.rates = rates;
     A.bf16 = type == LAPLEX_BF16; A.ws = static_cast<char*>(ws);

@@ -58,12 +58,12 @@ struct AttentionArgs {
     bool bf16, backward;
     char* ws;
     // filled in by launch_attention
-    int cut;                         // some sequence may have more than one stretch
     int64_t stretch, per_sequence, slots;   // tokens of a stretch that one workgroup walks; stretches of a sequence (equal lengths), of all, at most
+    int64_t places;                  // states that enter stretches of sequences that have several, at most
     int slices;                      // workgroups side by side over the columns
     int wide[3], states_wide[2];     // per walk, a bit each for q, k, v, out: its rows may be accessed four numbers at a time
 };
-size_t attention_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv);
+size_t attention_workspace(int64_t tokens, int64_t sequences, int heads, int dk, int dv);
 hipError_t launch_attention(const AttentionArgs& A, hipStream_t st);
 
 struct AttentionStepArgs {

@@ -138,3 +138,45 @@ def test_a_short_sequence_has_the_same_bits_in_every_pack(dtype):
             for i, at in enumerate(rows):
                 one = got[name][sequences[i]] if "state" in name else got[name][at:at + 20]
                 assert torch.equal(one, t[i] if "state" in name else t[20 * i:20 * i + 20]), name
+
+
+# --- many sequences ------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("inside", [[], [(7, 900), (39990, 1300)]])
+def test_attention_of_tens_of_thousands_of_sequences(dtype, inside):
+    """More slots than a grid's second axis takes, empty sequences among them, long ones too or none; states in place."""
+    r = seeded("tens of thousands", len(inside))
+    lengths = r.integers(0, 4, 40000)
+    for i, n in inside:
+        lengths[i] = n
+    p = Problem([int(n) for n in lengths], 1, 8, 8, dtype, True, rates=[0.1], what="many")
+    got = {**p.forward(), **p.backward()}
+    some = [0, 1, 2, 7, 8, 32767, 32768, 32769, 39990, 39991, 39999] + [int(i) for i in r.integers(0, 40000, 40)]
+    at = np.concatenate([[0], np.cumsum(p.lengths)])
+    for i in some:
+        one = Problem([p.lengths[i]], 1, 8, 8, dtype, True, rates=[0.1])
+        for name in ("q", "k", "v", "gy"):
+            setattr(one, name, getattr(p, name)[at[i]:at[i + 1]])
+        one.state, one.gstate, one.scale = p.state[i:i + 1], p.gstate[i:i + 1], p.scale
+        mine = {name: t[i:i + 1] if "state" in name else t[at[i]:at[i + 1]] for name, t in got.items()}
+        for name, g, want, terms, n in one.each(mine):
+            exact = 16 * np.sqrt(n + 72.0) * U * terms
+            within(f"{i}: {name}", g, want, exact if dtype == F32 or "state" in name else exact + 2.0 ** -14 * terms + 1.01 * H * np.abs(want))
+    # in place
+    state, y = p.state.clone(), torch.full_like(got["y"], float("nan"))
+    B.laplex_decay_attention(p.q, p.k, p.v, dev(p.rates), y, p.workspace(), p.scale, p.b, p.starts, state, state)
+    assert torch.equal(y, got["y"]) and torch.equal(state, got["state"])
+    empty = torch.from_numpy(lengths == 0).cuda()
+    assert torch.equal(state[empty], p.state[empty])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_state_in_place_among_sequences_of_one_stretch_and_of_several(dtype):
+    """What several workgroups read and the last of them writes comes through the workspace; what one workgroup does, does not."""
+    p = Problem([1, 900, 0, 64, 65, 2000, 3, 700], 2, 130, 72, dtype, True, what="in place")
+    want = p.forward()
+    for _ in range(3):
+        state, y = p.state.clone(), torch.full_like(want["y"], float("nan"))
+        B.laplex_decay_attention(p.q, p.k, p.v, dev(p.rates), y, p.workspace(), p.scale, p.b, p.starts, state, state)
+        assert torch.equal(y, want["y"]) and torch.equal(state, want["state"])
