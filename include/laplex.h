@@ -423,7 +423,7 @@ int laplex_rotary_frequencies(float* frequencies, int64_t rotary_dim, double bas
  * q, k [tokens][heads][dk], v, y [tokens][heads][dv].  The sequences lie one behind the other: sequence b has the rows
  * starts[b] .. starts[b+1]-1 (int64 device array of sequences + 1 ascending values from 0 to tokens; 8-byte aligned), or, with starts NULL,
  * all have tokens / sequences rows.  Sequences may be empty.  Values in starts that are out of order or of range give wrong values, never a fault.
- * rates[heads] >= 0 in device memory (constants of the layer: they get no gradient; +inf: every token sees only itself).
+ * rates[heads] >= 0 in device memory (constants of the layer: they get no gradient; +inf: every token sees only itself; NaN: its head is NaN).
  * state_in, state_out: fp32 [sequences][heads][dk][dv]; state_in NULL = zeros, state_out NULL = not wanted; they may be the same buffer.
  * An empty sequence hands its state through.  1 <= dk, dv <= LAPLEX_ATTENTION_MAX_DIM; scale positive and finite.
  * Rows before a value that is not finite are not touched by it; from its token on everything that it is weighted into is not finite.

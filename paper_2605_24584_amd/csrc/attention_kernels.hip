@@ -32,7 +32,8 @@ constexpr int kStepThreads = 256;
 
 __device__ __forceinline__ float rate_of(const float* rates, int h)
 {
-    return fminf(rates[h], 1.0e30f);      // an infinite rate: nothing but the token itself, and 0 * rate stays 0
+    const float r = rates[h];
+    return r > 1.0e30f ? 1.0e30f : r;     // an infinite rate: nothing but the token itself, and 0 * rate stays 0.  NaN stays NaN
 }
 
 __device__ __forceinline__ int64_t start_of(const int64_t* starts, int64_t tokens, int64_t sequences, int64_t b)

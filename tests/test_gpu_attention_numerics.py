@@ -180,3 +180,25 @@ def test_a_state_in_place_among_sequences_of_one_stretch_and_of_several(dtype):
         state, y = p.state.clone(), torch.full_like(want["y"], float("nan"))
         B.laplex_decay_attention(p.q, p.k, p.v, dev(p.rates), y, p.workspace(), p.scale, p.b, p.starts, state, state)
         assert torch.equal(y, want["y"]) and torch.equal(state, want["state"])
+
+
+# --- rates ---------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths", [[70, 3], [1000]])
+def test_a_rate_that_is_nan_shows_in_its_head(dtype, lengths):
+    """Everything of that head is NaN, and the other heads are the same bits as without it."""
+    p = Problem(lengths, 3, 40, 64, dtype, True, rates=[0.1, 0.2, 0.3])
+    fine = {**p.forward(), **p.backward()}
+    one = [t[:1].clone() for t in (p.q, p.k, p.v)]
+    fine_state, fine_y = p.state[:1].clone(), p.new(1, 3, 64)
+    B.laplex_decay_attention_step(*one, dev(p.rates), fine_state, fine_y, p.scale)
+    p.rates[1] = np.nan
+    odd = {**p.forward(), **p.backward()}
+    state, y = p.state[:1].clone(), p.new(1, 3, 64)
+    B.laplex_decay_attention_step(*one, dev(p.rates), state, y, p.scale)
+    fine.update(step=fine_y, step_state=fine_state)
+    odd.update(step=y, step_state=state)
+    for name, t in odd.items():
+        assert torch.isnan(t[:, 1]).all(), name
+        assert torch.equal(t[:, [0, 2]], fine[name][:, [0, 2]]), name
