@@ -681,8 +681,8 @@ k_attention_walk(AttentionArgs A)
         // the state at the chunk's end
         float d = decay;
         left += rest;
-        if (left >= 0.5f * ulp) { d = decay + ulp; left -= ulp; }
-        else if (left <= -0.5f * ulp) { d = decay - ulp; left += ulp; }
+        if (left + left >= ulp) { d = decay + ulp; left -= ulp; }            // (half of the smallest distance would be 0)
+        else if (left + left <= -ulp) { d = decay - ulp; left += ulp; }
         if (valid < C) d = end_decay;
 #pragma unroll
         for (int t = 0; t < DT; ++t)

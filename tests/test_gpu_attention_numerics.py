@@ -202,3 +202,15 @@ def test_a_rate_that_is_nan_shows_in_its_head(dtype, lengths):
     for name, t in odd.items():
         assert torch.isnan(t[:, 1]).all(), name
         assert torch.equal(t[:, [0, 2]], fine[name][:, [0, 2]]), name
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("length", [16, 32, 64, 96, 192, 2048])
+def test_nothing_is_left_of_a_state_whose_decay_is_zero(dtype, length):
+    """Rates from which exp(-rate) is 0, and 0 over a chunk: of the largest states nothing reaches the tokens behind the first, or the last state."""
+    p = Problem([length], 3, 64, 64, dtype, False, rates=[np.inf, 200.0, 1e6], what="zero")
+    p.k.zero_(), p.v.zero_()
+    p.q.fill_(1.0 / 128.0)                # (q S0 itself has to fit fp32)
+    p.state.fill_(3e38)
+    got = p.forward()
+    assert (got["y"] == 0).all() and (got["state"] == 0).all()
