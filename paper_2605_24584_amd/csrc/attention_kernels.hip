@@ -418,7 +418,8 @@ k_attention_walk(AttentionArgs A)
     // next number up or down is taken whenever what has been left out reaches half of their distance.  The last chunk may be shorter.
     const double full_decay = exp(-rate * C);
     const float decay = uniform((float)full_decay), end_decay = uniform((float)exp(-rate * (int)((s.hi - s.lo) % C)));
-    const float ulp = uniform(__uint_as_float(__float_as_uint(decay) + 1) - decay), rest = uniform((float)(full_decay - (double)decay));
+    // (twice the smallest number at least: half of that is not 0)
+    const float ulp = uniform(fmaxf(__uint_as_float(__float_as_uint(decay) + 1) - decay, 2.8e-45f)), rest = uniform((float)(full_decay - (double)decay));
     float left = 0.0f;
 
     const int64_t back = W.reverse ? -1 : 1;
@@ -681,8 +682,8 @@ k_attention_walk(AttentionArgs A)
         // the state at the chunk's end
         float d = decay;
         left += rest;
-        if (left + left >= ulp) { d = decay + ulp; left -= ulp; }            // (half of the smallest distance would be 0)
-        else if (left + left <= -ulp) { d = decay - ulp; left += ulp; }
+        if (left >= 0.5f * ulp) { d = decay + ulp; left -= ulp; }
+        else if (left <= -0.5f * ulp) { d = decay - ulp; left += ulp; }
         if (valid < C) d = end_decay;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
