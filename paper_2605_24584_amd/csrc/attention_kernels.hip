@@ -392,7 +392,7 @@ k_attention_walk(AttentionArgs A)
     typedef typename Num<T>::quad quad;
     constexpr int E = G::E, C = G::C, R = G::R, ROW = G::ROW, SEQ = G::SEQ, CT = G::CT, DT = G::DT, KD = G::KD, KC = G::KC, THREADS = G::THREADS;
     __shared__ __attribute__((aligned(16))) char lds[STATES ? G::kBytesK + G::kBytesV : G::kLds];
-    __shared__ float power[C + 1], weight[C];          // l^d, and the weights of the chunk's tokens in the state
+    __shared__ float power[C + 1], weight[C];          // l^d (times inner, where it is used for the weights alone), and the weights of the chunk's tokens in the state
     __shared__ int odd[2];
     char* const Kt = lds;                              // [DK][C]
     char* const Vt = Kt + G::kBytesK;                  // [COLS][C]
@@ -410,7 +410,8 @@ k_attention_walk(AttentionArgs A)
 
     const int x = threadIdx.x, lane = x & 63, wave = __builtin_amdgcn_readfirstlane(x >> 6), r16 = lane & 15, g = lane >> 4;
     const double rate = (double)rate_of(A.rates, h);
-    for (int d = x; d <= C; d += THREADS) power[d] = (float)exp(-rate * d);
+    const float inner = uniform(W.inner);
+    for (int d = x; d <= C; d += THREADS) power[d] = STATES ? (float)exp(-rate * d) * inner : (float)exp(-rate * d);
     if (!STATES)
         for (int i = x; i < G::kBytesP / 16; i += THREADS) reinterpret_cast<f32x4*>(Ps)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (x < 2) odd[x] = 0;
@@ -460,7 +461,7 @@ k_attention_walk(AttentionArgs A)
 #pragma unroll
         for (int t = 0; t < DT; ++t) S[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const float scale = from_given ? W.in_scale : 1.0f;
+    const float scale = from_given ? 1.0f / W.last_scale : 1.0f;
     if ((from_set && W.set_transposed) || from_given)
 #pragma unroll
         for (int t = 0; t < DT; ++t)
@@ -544,7 +545,7 @@ k_attention_walk(AttentionArgs A)
         }
         if (!STATES && !fine) odd[turn] = 1;
         if (u == s.lo || valid < C)
-            if (x < C) weight[x] = power[x < valid ? valid - x - W.lead : 0];
+            if (x < C) weight[x] = STATES ? power[x < valid ? valid - x - W.lead : 0] : power[x < valid ? valid - x - W.lead : 0] * inner;
         if (u + C < s.hi) load(u + C);
         __syncthreads();
 
@@ -568,7 +569,7 @@ k_attention_walk(AttentionArgs A)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int d = 16 * (it - jt) + r16 - 4 * g - r;
-                        acc[r] = d >= 0 ? acc[r] * power[d < 0 ? 0 : d] : 0.0f;
+                        acc[r] = d >= 0 ? acc[r] * power[d < 0 ? 0 : d] * inner : 0.0f;
                     }
                     const int j = 16 * jt + 4 * g;
                     const auto put = [&](int row, int j, quad w) {
@@ -757,7 +758,7 @@ k_attention_carry(AttentionArgs A)
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * t + 4 * (lane >> 4) + r;
                 const float v = state_value(W, (b * A.heads + h) * (int64_t)W.dk * W.dv, row, col);
-                carry[r] = col < W.dv && row < W.dk ? W.in_scale * v : 0.0f;
+                carry[r] = col < W.dv && row < W.dk ? (1.0f / W.last_scale) * v : 0.0f;
             }
         }
         const int64_t step = (int64_t)A.heads * A.slices * kPieces;

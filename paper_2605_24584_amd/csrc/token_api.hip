@@ -139,8 +139,8 @@ int laplex_decay_attention(const void* q, int64_t ldq, const void* k, int64_t ld
     Walk& W = A.walk[A.walks++];
     W.q = q; W.ldq = ldq; W.k = k; W.ldk = ldk; W.v = v; W.ldv = ldv; W.out = y; W.ldo = ldy;
     W.dk = (int)dk; W.dv = (int)dv; W.lead = 1; W.exact = 1;
-    W.state_in = state_in; W.in_scale = 1.0f;
-    W.state_out = state_out; W.last_scale = 1.0f;
+    W.state_in = state_in; W.inner = W.last_scale = 1.0f;
+    W.state_out = state_out;
     W.out_scale = scale;
     A.states[A.sets++] = W;
     LAPLEX_HIP(launch_attention(A, stream));
@@ -173,12 +173,15 @@ int laplex_decay_attention_backward(const void* q, int64_t ldq, const void* k, i
     A.starts = starts; A.tokens = tokens; A.sequences = sequences; A.heads = (int)heads; A.rates = rates;
     A.bf16 = type == LAPLEX_BF16; A.ws = static_cast<char*>(ws);
     A.backward = true;
+    // The walks back weight their sums by the scale, but not the state they begin from: the scale goes into the sums, as far as it leaves their parts room, and what is
+    // left of it around them (gstate_out / scale alone would overflow where neither it nor the gradients do).
+    const float inner = scale < 0x1p-40f ? 0x1p-40f : scale > 0x1p40f ? 0x1p40f : scale, outer = scale / inner;
     // back: queries k, keys q, values gy.  The states of both walks back are these, whichever of the two is wanted, so that neither depends on the other.
     Walk B{};
     B.q = k; B.ldq = ldk; B.k = q; B.ldk = ldq; B.v = gy; B.ldv = ldgy; B.out = gv; B.ldo = ldgv;
     B.dk = (int)dk; B.dv = (int)dv; B.reverse = 1; B.exact = 1;
-    B.state_in = gstate_out; B.in_scale = 1.0f / scale; B.out_scale = scale;
-    B.state_out = gstate_in; B.last_scale = scale;
+    B.state_in = gstate_out; B.inner = inner; B.out_scale = outer;
+    B.state_out = gstate_in; B.last_scale = outer;
     B.set = A.sets;
     if (gk || gv || gstate_in) A.states[A.sets++] = B;
     if (gk) {        // back: queries v, keys gy, values q, the transposed state
@@ -186,14 +189,14 @@ int laplex_decay_attention_backward(const void* q, int64_t ldq, const void* k, i
         W.set = B.set; W.set_transposed = 1;
         W.q = v; W.ldq = ldv; W.k = gy; W.ldk = ldgy; W.v = q; W.ldv = ldq; W.out = gk; W.ldo = ldgk;
         W.dk = (int)dv; W.dv = (int)dk; W.reverse = 1; W.transposed = 1;
-        W.state_in = gstate_out; W.in_scale = 1.0f / scale; W.out_scale = scale;
+        W.state_in = gstate_out; W.inner = inner; W.out_scale = W.last_scale = outer;
     }
     if (gv || gstate_in) A.walk[A.walks++] = B;
     if (gq) {        // ahead: queries gy, keys v, values k, the transposed state
         Walk& W = A.walk[A.walks++];
         W.q = gy; W.ldq = ldgy; W.k = v; W.ldk = ldv; W.v = k; W.ldv = ldk; W.out = gq; W.ldo = ldgq;
         W.dk = (int)dv; W.dv = (int)dk; W.lead = 1; W.transposed = 1;
-        W.state_in = state_in; W.in_scale = 1.0f; W.out_scale = scale;
+        W.state_in = state_in; W.inner = W.last_scale = 1.0f; W.out_scale = scale;
         W.set = A.sets;
         A.states[A.sets++] = W;
     }

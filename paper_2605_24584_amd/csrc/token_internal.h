@@ -28,8 +28,8 @@ hipError_t launch_rotary_frequencies(float* out, int64_t pairs, double base, int
 
 // ----------------------------------------------------------------------------
 // Attention with a decay for each head.  A walk goes over the tokens of every sequence in one direction, u = 0, 1, ...:
-//   out_u = out_scale * ( sum_{w <= u} l^(u - w) (q_u . k_w) v_w + l^(u + lead) q_u X ),      l = exp(-rate of the head)
-//   last  = last_scale * ( l^n X + sum_w l^(n - w - lead) k_w v_w^T ),                        X = in_scale * state_in
+//   out_u = out_scale * ( inner sum_{w <= u} l^(u - w) (q_u . k_w) v_w + l^(u + lead) q_u X ),      l = exp(-rate of the head)
+//   last  = last_scale * ( l^n X + inner sum_w l^(n - w - lead) k_w v_w^T ),                        X = state_in / last_scale
 // The forward call is one walk ahead (lead = 1), the backward call one ahead (gq) and two back (gk, gv: lead = 0), with the
 // parts of q, k, v changed about; a state matrix is read transposed where those swap its two sides.
 // ----------------------------------------------------------------------------
@@ -42,7 +42,7 @@ struct Walk {
     int exact;                       // the walk's state can be asked for: an fp32 sum of fp32 products, whether it is or not (so that `out` has the same bits)
     const float* state_in;           // [sequences][heads][dk][dv] (or [dv][dk]) or null
     float* state_out;                // the same, never transposed, or null
-    float in_scale, out_scale, last_scale;
+    float inner, out_scale, last_scale;
     int set, set_transposed;         // which of the state sets below holds the states that enter its stretches, and whether with its sides swapped
 };
 

@@ -214,3 +214,17 @@ def test_nothing_is_left_of_a_state_whose_decay_is_zero(dtype, length):
     p.state.fill_(3e38)
     got = p.forward()
     assert (got["y"] == 0).all() and (got["state"] == 0).all()
+
+
+# --- scales --------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths", [[50, 9], [700]])
+@pytest.mark.parametrize("scale,size", [(1e-39, 1.0), (1e-38, 1.0), (1e-30, 1e-3), (1e-10, 1e30), (1e-3, 1e35), (2.0 ** -41, 5.0), (1e20, 1e10)])
+def test_gradients_of_states_beside_small_and_large_scales(dtype, lengths, scale, size):
+    """The gradients are sums of a part that is weighted by the scale and one that is not: neither is lost or infinite for the other's sake."""
+    p = Problem(lengths, 2, 48, 40, dtype, True, scale=scale, what="scales")
+    p.gstate *= size
+    for name, got, want, terms, n in p.each(p.backward()):
+        exact = 16 * np.sqrt(n + 112.0) * U * terms + 2.0 ** -126          # (2^-126: results and decayed weights below the smallest normal number have fewer bits)
+        within(name, got, want, exact if dtype == F32 or "state" in name else exact + 2.0 ** -14 * terms + 1.01 * H * np.abs(want))
