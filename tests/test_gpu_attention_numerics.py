@@ -228,3 +228,39 @@ def test_gradients_of_states_beside_small_and_large_scales(dtype, lengths, scale
     for name, got, want, terms, n in p.each(p.backward()):
         exact = 16 * np.sqrt(n + 112.0) * U * terms + 2.0 ** -126          # (2^-126: results and decayed weights below the smallest normal number have fewer bits)
         within(name, got, want, exact if dtype == F32 or "state" in name else exact + 2.0 ** -14 * terms + 1.01 * H * np.abs(want))
+
+
+# --- values that are not finite ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (150, 200), (48, 256), (256, 256)])
+@pytest.mark.parametrize("lengths,at", [([20, 25, 9], 33), ([100, 900, 40], 500), ([100, 900, 40], 999)])
+@pytest.mark.parametrize("value", [float("nan"), float("-inf")])
+def test_attention_values_that_are_not_finite_show_and_stay_where_they_reach(dtype, dk, dv, lengths, at, value):
+    """One number of one token of the middle sequence, a short one or one in several stretches.  What it is weighted into is not finite, everything else the same bits."""
+    p = Problem(lengths, 2, dk, dv, dtype, True, rates=[0.01, 0.03], what="odd")
+    first, end, col = lengths[0], lengths[0] + lengths[1], 21
+    fine = {**p.forward(), **p.backward()}
+    # (result, its rows, its columns) that the number reaches
+    every, before, behind = slice(None), slice(first, at + 1), slice(at, end)
+    reach = {
+        "q": [("y", slice(at, at + 1), every), ("gk", before, col), ("gv", before, every)],
+        "k": [("y", behind, every), ("gq", behind, col), ("gv", slice(at, at + 1), every)],
+        "v": [("y", behind, col), ("gq", behind, every), ("gk", slice(at, at + 1), every)],
+        "gy": [("gq", slice(at, at + 1), every), ("gk", before, every), ("gv", before, col)],
+    }
+    states = {"q": ("gstate", col, every), "k": ("state", col, every), "v": ("state", every, col), "gy": ("gstate", every, col)}
+    for what in reach:
+        t = getattr(p, what)
+        kept = t[at, 1, col].clone()
+        t[at, 1, col] = value
+        odd = {**p.forward(), **p.backward()}
+        t[at, 1, col] = kept
+        for name, rows, columns in reach[what]:
+            assert not torch.isfinite(odd[name][rows, 1, columns]).any(), f"{what}: {name}"
+            odd[name][rows, 1, columns] = fine[name][rows, 1, columns]
+        name, rows, columns = states[what]
+        assert not torch.isfinite(odd[name][1, 1, rows, columns]).any(), f"{what}: {name}"
+        odd[name][1, 1, rows, columns] = fine[name][1, 1, rows, columns]
+        for name, t in odd.items():
+            assert torch.equal(t, fine[name]), f"{what}: {name}"
