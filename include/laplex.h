@@ -483,7 +483,8 @@ int laplex_logprob(const void* y, int64_t ldy, int type, int64_t k, int64_t batc
  *   gy[i,t] = tau * ( glogp[t] (1[i == targets[t]] - p) - gentropy[t] p (log p + entropy[t]) + glse[t] p )
  * glogp, gentropy, glse may each be NULL (= zeros).  lse and, if gentropy is given, entropy are the forward call's; targets are needed with glogp, and
  * a target outside 0 .. k-1 contributes nothing.  gy (same type as y) may be y itself (in place).  No gradient flows through top_logp.
- * A column of -inf alone has gradient 0; a column with a NaN or +inf gets NaN.
+ * A column of -inf alone has gradient 0; a column with a NaN or +inf gets NaN.  The precision does not depend on where the logits lie: columns with |lse| > 64, whose
+ * lse is rounded to less than p needs, are summed up anew (and take several times as long).
  */
 int laplex_logprob_backward(const void* y, int64_t ldy, int type, int64_t k, int64_t batch, const int64_t* targets, float tau,
                             const float* lse, const float* entropy, const float* glogp, const float* gentropy, const float* glse,
