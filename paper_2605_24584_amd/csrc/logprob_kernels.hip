@@ -727,13 +727,14 @@ k_logprob_backward(BackwardArgs F)
 
 constexpr int64_t kFewWorkgroups = 256;      // compute units
 
-// Lanes across the columns, and how often a thread takes rows: about kTarget workgroups, if there are rows for them.
+// Lanes across the columns, and how often a thread takes rows: about `target` workgroups, if there are rows for them.  few: smaller ones, where others would leave compute
+// units without one.
 struct Shape {
     int vec, lanes_log2, turns, threads;
     int64_t slabs, blocks;
 };
 
-Shape shape_of(int64_t k, int64_t batch, int rows, int64_t target)
+Shape shape_of(int64_t k, int64_t batch, int rows, int64_t target, bool few)
 {
     Shape S;
     S.threads = kRowThreads;
@@ -742,7 +743,7 @@ Shape shape_of(int64_t k, int64_t batch, int rows, int64_t target)
     S.lanes_log2 = 0;
     while (S.lanes_log2 < 6 && (int64_t(1) << S.lanes_log2) < wide) ++S.lanes_log2;
     S.slabs = (wide + (int64_t(1) << S.lanes_log2) - 1) >> S.lanes_log2;
-    if (rows == kGroup && S.slabs * ((k * (int64_t(1) << S.lanes_log2)) / (kRowThreads * rows)) < kFewWorkgroups) S.threads = kRowThreadsFew;
+    if (few && S.slabs * ((k * (int64_t(1) << S.lanes_log2)) / (kRowThreads * rows)) < kFewWorkgroups) S.threads = kRowThreadsFew;
     const int64_t row_lanes = S.threads >> S.lanes_log2, turn = row_lanes * rows, all = (k + turn - 1) / turn;
     int64_t blocks = target / S.slabs;
     blocks = blocks < 1 ? 1 : blocks > all ? all : blocks;
@@ -765,7 +766,7 @@ struct Plan {
 Plan plan_of(int64_t k, int64_t batch, int64_t top)
 {
     Plan P;
-    P.rows = shape_of(k, batch, kGroup, kRowsTarget);
+    P.rows = shape_of(k, batch, kGroup, kRowsTarget, true);
     P.groups = top > 0 && k > kDirect ? (k + kGroup - 1) / kGroup : 0;
     P.off_maxima = ((size_t)P.rows.blocks * 3 * batch * sizeof(float) + 255) / 256 * 256;
     P.total = P.off_maxima + (size_t)P.groups * batch * sizeof(float);
@@ -822,7 +823,7 @@ hipError_t launch_logprob(const LogprobArgs& A, hipStream_t st)
 
 hipError_t launch_logprob_backward(const LogprobBackwardArgs& A, hipStream_t st)
 {
-    const Shape S = shape_of(A.k, A.batch, kBackRows, kBackTarget);
+    const Shape S = shape_of(A.k, A.batch, kBackRows, kBackTarget, false);
     BackwardArgs F{};
     F.B = A; F.lanes_log2 = S.lanes_log2; F.turns = S.turns; F.slabs = S.slabs;
     // 64 bytes of fp32 rows side by side, if that leaves every compute unit a workgroup
