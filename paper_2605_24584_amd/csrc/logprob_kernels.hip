@@ -61,6 +61,14 @@ struct Stats { float m, s, w; };      // maximum, sum exp(tau (y - m)), sum (y -
 
 __device__ __forceinline__ float exp_of(float d, float c) { return __builtin_amdgcn_exp2f(d * c); }      // c = tau / log 2
 
+// tau / log 2, or the largest number: with an infinite one the maximum itself would give 0 * inf.  (From tau = 2.3e38 on, where logits that are not equal differ by
+// less than 1e-36 or have probability 0.)
+__host__ __device__ __forceinline__ float rate_of(float tau)
+{
+    const float c = tau * 1.44269504088896340736f;
+    return c < 3.402823466e38f ? c : 3.402823466e38f;
+}
+
 // brings the sums of `a` to the maximum m >= a.m (a maximum of -inf: there is nothing in them)
 __device__ __forceinline__ void rebase(Stats& a, float m, float c)
 {
@@ -654,7 +662,7 @@ __device__ __forceinline__ void far_columns(const BackwardArgs& F, int64_t block
     Columns<VEC> C;
     const bool mine = have > 0 && load_common(A, C, t, have);
     if (!__syncthreads_or(mine)) return;
-    const float c2 = A.tau * 1.44269504088896340736f;
+    const float c2 = rate_of(A.tau);
     Stats st[VEC];
 #pragma unroll
     for (int c = 0; c < VEC; ++c) st[c] = Stats{-INFINITY, 0.0f, 0.0f};
@@ -803,7 +811,7 @@ hipError_t launch_logprob(const LogprobArgs& A, hipStream_t st)
 {
     const Plan P = plan_of(A.k, A.batch, A.top);
     RowsArgs R{};
-    R.y = A.y; R.ldy = A.ldy; R.k = A.k; R.batch = A.batch; R.c = A.tau * 1.44269504088896340736f;
+    R.y = A.y; R.ldy = A.ldy; R.k = A.k; R.batch = A.batch; R.c = rate_of(A.tau);
     R.lanes_log2 = P.rows.lanes_log2; R.turns = P.rows.turns; R.slabs = P.rows.slabs;
     R.parts = reinterpret_cast<float*>(A.ws); R.maxima = reinterpret_cast<float*>(A.ws + P.off_maxima);
     if (A.k > 0) {

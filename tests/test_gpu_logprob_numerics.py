@@ -158,3 +158,26 @@ def test_a_column_of_the_gradient_does_not_depend_on_its_neighbours(dtype):
     assert torch.isnan(got_odd[:, [3, 13, 2]]).all()
     rest = [c for c in range(batch) if c not in (3, 13, 2)]
     assert torch.equal(got_odd[:, rest], got[:, rest])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,batch", [(9, 2), (300, 7), (3000, 5)])
+@pytest.mark.parametrize("tau", [3e38, 3.4e38, 2.5e38, 1e30, 1e-30, 1e-38])
+def test_inverse_temperatures_at_their_ends(dtype, k, batch, tau):
+    """All that is positive and finite is accepted: the largest logits have all of the probability, or all logits have the same."""
+    r = seeded("tau", k, batch)
+    y = dev(np.round(r.normal(size=(k, batch)) * 8.0).astype(np.float32) / 8.0, dtype)
+    y[1:, 0] = -float("inf")
+    hy = host(y)
+    targets = hy.argmax(axis=0)
+    f = forward(y, targets, tau, 3)
+    n = (hy == hy.max(axis=0)).sum(axis=0) if tau > 1 else np.isfinite(hy).sum(axis=0)
+    within("logp", host(f["logp"]), -np.log(n), 64 * U * (1 + np.log(n)))
+    within("entropy", host(f["entropy"]), np.log(n), 64 * U * (1 + np.log(n)))
+    within("top_logp", host(f["top_logp"])[0], -np.log(n), 64 * U * (1 + np.log(n)))
+    gy = torch.full_like(y, float("nan"))
+    ones = torch.ones(batch, device="cuda")
+    B.laplex_logprob_backward(y, dev(targets, torch.int64), f["lse"], f["entropy"], None, None, ones / k * 1e-3, gy, tau)
+    likely = (hy == hy.max(axis=0)) if tau > 1 else np.isfinite(hy)
+    want = float(np.float32(tau)) * np.where(likely, 1.0 / n, 0.0) * float(np.float32(1.0) / np.float32(k) * np.float32(1e-3))
+    within("gy", host(gy), want, (H if dtype == BF16 else 0.0) * want + 128 * U * want + 1e-37)
