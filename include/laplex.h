@@ -470,6 +470,7 @@ int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64
  * logp, lse, entropy may each be NULL; targets (int64 device array) may be NULL if logp is.  A target outside 0 .. k-1 (padding) has
  * logp 0.  Logits of -inf (banned entries) have probability 0 and add nothing to the entropy; a column of nothing else has
  * lse = logp = top_logp = -inf and entropy 0.  A column with a NaN or +inf gives NaN; NaN counts as the largest logit.
+ * Logits further below a column's largest than fp32 reaches (3.4e38) count as -inf.
  * k == 0 gives lse = -inf, entropy 0, logp 0.
  */
 int laplex_logprob_workspace_bytes(int64_t k, int64_t batch, int64_t top, size_t* out /* host */);

@@ -1,8 +1,8 @@
 // Log probabilities, entropy and the likeliest alternatives over logits y[k][batch] (a row per vocabulary entry), and the
 // gradient into the logits.
 //
-// Per column, with m = max y, d = y - m:   s = sum exp(tau d),  w = sum d exp(tau d);
-//   lse = tau m + log s,   entropy = log s - tau w / s,   logp = tau (y - m) - log s.
+// Per column, with m = max y, x = tau (y - m) / log 2:   s = sum 2^x,  w = sum x 2^x;
+//   lse = tau m + log s,   entropy = log s - log 2 w / s,   logp = tau (y - m) - log s.
 // One pass over the logits (k_logprob_rows): a thread holds (m, s, w) of up to four neighbouring columns and takes groups of kGroup consecutive
 // rows; the running maximum and the rescaling cost it one more exponential per group.  A second launch (k_logprob_finish), a
 // wavefront per column, brings the parts together.  All sums are fp32, a few hundred rows to a part.
@@ -57,11 +57,9 @@ __device__ __forceinline__ void load_columns(float* out, const T* p, int have)
     }
 }
 
-struct Stats { float m, s, w; };      // maximum, sum exp(tau (y - m)), sum (y - m) exp(tau (y - m))
+struct Stats { float m, s, w; };      // maximum, sum 2^x, sum x 2^x
 
-__device__ __forceinline__ float exp_of(float d, float c) { return __builtin_amdgcn_exp2f(d * c); }      // c = tau / log 2
-
-// tau / log 2, or the largest number: with an infinite one the maximum itself would give 0 * inf.  (From tau = 2.3e38 on, where logits that are not equal differ by
+// c of x = c (y - m): tau / log 2, or the largest number: with an infinite one the maximum itself would give 0 * inf.  (From tau = 2.3e38 on, where logits that are not equal differ by
 // less than 1e-36 or have probability 0.)
 __host__ __device__ __forceinline__ float rate_of(float tau)
 {
@@ -72,9 +70,9 @@ __host__ __device__ __forceinline__ float rate_of(float tau)
 // brings the sums of `a` to the maximum m >= a.m (a maximum of -inf: there is nothing in them)
 __device__ __forceinline__ void rebase(Stats& a, float m, float c)
 {
-    const float d = a.m == -INFINITY ? 0.0f : a.m - m;
-    const float e = exp_of(d, c);
-    a.w = e > 0.0f ? (a.w + d * a.s) * e : (a.s != a.s ? a.s : 0.0f);
+    const float x = a.m == -INFINITY ? 0.0f : (a.m - m) * c;
+    const float e = __builtin_amdgcn_exp2f(x);
+    a.w = e > 0.0f ? (a.w + x * a.s) * e : (a.s != a.s ? a.s : 0.0f);
     a.s = a.s * e;
     a.m = m;
 }
@@ -147,9 +145,9 @@ k_logprob_rows(RowsArgs A)
                 float s = 0.0f, w = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) {
-                    const float d = v[i][c] - base, e = exp_of(d, A.c);
+                    const float x = (v[i][c] - base) * A.c, e = __builtin_amdgcn_exp2f(x);
                     s += e;
-                    w += e > 0.0f ? d * e : 0.0f;
+                    w += e > 0.0f ? x * e : 0.0f;
                 }
                 st[c].s += s;
                 st[c].w += w;
@@ -393,7 +391,7 @@ k_logprob_finish(FinishArgs F)
     auto logp_of = [&](float v) { return empty ? -INFINITY : (v - st.m) * A.tau - log_sum; };
     if (lane == 0) {
         if (A.lse) A.lse[t] = empty ? -INFINITY : st.m * A.tau + log_sum;
-        if (A.entropy) A.entropy[t] = empty ? 0.0f : log_sum - A.tau * (st.w / st.s);
+        if (A.entropy) A.entropy[t] = empty ? 0.0f : log_sum - 0.69314718055994530942f * (st.w / st.s);
         if (A.logp) {
             const int64_t target = A.targets[t];
             A.logp[t] = target >= 0 && target < A.k ? logp_of(to_float(y[target * A.ldy])) : 0.0f;
@@ -685,7 +683,7 @@ __device__ __forceinline__ void far_columns(const BackwardArgs& F, int64_t block
                 rebase(st[c], fmaxf(st[c].m, m), c2);
                 const float base = st[c].m == -INFINITY ? 0.0f : st[c].m;
 #pragma unroll
-                for (int i = 0; i < kBackRows; ++i) st[c].s += exp_of(v[i][c] - base, c2);
+                for (int i = 0; i < kBackRows; ++i) st[c].s += __builtin_amdgcn_exp2f((v[i][c] - base) * c2);
             }
         }
 #pragma unroll

@@ -181,3 +181,17 @@ def test_inverse_temperatures_at_their_ends(dtype, k, batch, tau):
     likely = (hy == hy.max(axis=0)) if tau > 1 else np.isfinite(hy)
     want = float(np.float32(tau)) * np.where(likely, 1.0 / n, 0.0) * float(np.float32(1.0) / np.float32(k) * np.float32(1e-3))
     within("gy", host(gy), want, (H if dtype == BF16 else 0.0) * want + 128 * U * want + 1e-37)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,batch", [(50, 3), (2000, 6), (40000, 2)])
+def test_entropy_of_logits_as_large_as_the_type_at_a_small_inverse_temperature(dtype, k, batch):
+    """Sums of differences times probabilities beyond the type, whose product with tau is of ordinary size (the differences themselves are within it)."""
+    r = seeded("large logits", k, batch)
+    y = dev((r.normal(size=(k, batch)).clip(-5.0, 5.0) * 3e37).astype(np.float32), dtype)
+    hy, targets, tau = host(y), r.integers(0, k, batch), float(np.float32(2.0 ** -125))
+    f = forward(y, targets, tau)
+    o, _ = oracle(hy, targets, tau)
+    within("logp", host(f["logp"]), o["logp"], U * (64 + 8 * np.abs(o["logp"])))
+    within("entropy", host(f["entropy"]), o["entropy"], U * (64 + 16 * o["entropy"]))
+    within("lse", host(f["lse"]), o["lse"], U * (64 + 4 * np.abs(o["lse"])))
