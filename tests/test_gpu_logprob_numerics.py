@@ -195,3 +195,56 @@ def test_entropy_of_logits_as_large_as_the_type_at_a_small_inverse_temperature(d
     within("logp", host(f["logp"]), o["logp"], U * (64 + 8 * np.abs(o["logp"])))
     within("entropy", host(f["entropy"]), o["entropy"], U * (64 + 16 * o["entropy"]))
     within("lse", host(f["lse"]), o["lse"], U * (64 + 4 * np.abs(o["lse"])))
+
+
+# --- alternatives: several slabs of columns, several stretches of rows, more equal values than there is room for -------------------------
+
+def check_alternatives(y, top):
+    hy = y.float().cpu().numpy()
+    k, t = hy.shape
+    f = forward(y, np.zeros(t, np.int64), 1.0, top)
+    with np.errstate(invalid="ignore"):
+        for c in range(t):
+            # NaN first, then by value, of equal ones the lowest row
+            order = np.lexsort((np.arange(k), -np.nan_to_num(hy[:, c], nan=0.0, posinf=np.inf, neginf=-np.inf), ~np.isnan(hy[:, c])))[:top]
+            assert np.array_equal(f["top_ids"][:, c].cpu().numpy(), order), f"column {c}"
+    logp = torch.gather(y.double(), 0, f["top_ids"]) - f["lse"].double()
+    empty = f["lse"] == -float("inf")
+    logp[:, empty] = -float("inf")
+    got = f["top_logp"].double()
+    assert torch.equal(torch.isnan(got), torch.isnan(logp))
+    some = torch.isfinite(logp)
+    assert torch.equal(got[~some & ~torch.isnan(logp)], logp[~some & ~torch.isnan(logp)])
+    assert ((got - logp).abs()[some] <= U * (128 + 16 * logp.abs()[some] + 4 * f["lse"].double().abs().expand_as(logp)[some])).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,batch", [(1025, 257), (1500, 300), (3000, 700), (20000, 260)])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_alternatives_of_many_columns(dtype, k, batch, top):
+    r = seeded("many columns", k, batch)
+    y = (3.0 * r.normal(size=(k, batch))).astype(np.float32)
+    y[:, 1::7] = r.integers(0, 4, size=y[:, 1::7].shape)                   # many equal values
+    y[r.random((k, batch)) < 0.05] = -np.inf
+    y[:, 256] = -np.inf
+    y[k - 1, 2::9] = 50.0
+    check_alternatives(dev(y, dtype), top)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k", [131072, 131073, 140001, 262147])
+@pytest.mark.parametrize("top", [1, 13, 64])
+def test_alternatives_of_several_stretches_of_rows(dtype, k, top):
+    """131072 rows are looked at at a time: equal values, NaN and -inf on either side of that."""
+    r = seeded("stretches of rows", k)
+    edge = 131072
+    c = [np.full(k, -np.inf), np.zeros(k), r.integers(0, 3, k), r.integers(0, 50, k), 3.0 * r.normal(size=k), np.sort(3.0 * r.normal(size=k)), -np.sort(3.0 * r.normal(size=k))]
+    few = r.normal(size=k); few[max(0, edge - 5):edge + 5] = 9.0; c.append(few)              # equal values across the edge
+    nan = r.integers(0, 3, k).astype(float); nan[[3, edge - 1, min(edge, k - 1), k - 1]] = np.nan; c.append(nan)
+    late = np.full(k, -np.inf); late[-3:] = 1.0; c.append(late)                                # all but a few banned
+    both = np.where(r.random(k) < 0.999, -np.inf, 2.0); both[edge - 1:edge + 1] = 7.0; c.append(both)
+    low = np.full(k, float(torch.finfo(dtype).min)); low[-1] = 0.0; c.append(low)
+    y = dev(np.stack(c, axis=1).astype(np.float32), dtype)
+    check_alternatives(y, top)
+    check_alternatives(y[:, 2:4].contiguous(), top)
+    check_alternatives(y[:, 8:9].contiguous(), top)
