@@ -154,16 +154,16 @@ def _ptr(t):
 
 
 def _ld(t):
-    """leading dimension of a (rows, batch) tensor whose batch axis is contiguous"""
+    """leading dimension of a (rows, batch) tensor whose batch axis is contiguous; of a vector, how far apart its numbers lie"""
     if t is None:
         return 0
     if t.dim() == 1:
-        return 1
+        return t.stride(0) if t.shape[0] > 1 else 1
     assert t.dim() == 2
-    if t.shape[0] <= 1 or t.shape[1] == 0:
+    if t.shape[0] == 0 or t.shape[1] == 0:
         return max(t.shape[1], 1)
     assert t.shape[1] == 1 or t.stride(1) == 1, "batch axis must be contiguous"
-    return t.stride(0)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _batch(t):

@@ -248,3 +248,20 @@ def test_alternatives_of_several_stretches_of_rows(dtype, k, top):
     check_alternatives(y, top)
     check_alternatives(y[:, 2:4].contiguous(), top)
     check_alternatives(y[:, 8:9].contiguous(), top)
+
+
+def test_a_vector_of_logits_whose_numbers_lie_apart():
+    r = seeded("apart")
+    m = dev(r.normal(size=(600, 5)).astype(np.float32))
+    y, target = m[:, 3], dev(np.array([17]), torch.int64)
+    new = lambda: torch.full((1,), float("nan"), device="cuda")
+    logp, lse, entropy = new(), new(), new()
+    ws = torch.empty(B.laplex_logprob_workspace_bytes(600, 1), dtype=torch.uint8, device="cuda")
+    B.laplex_logprob(y, target, logp, lse, entropy, None, None, ws)
+    o = O.logprob(host(y)[:, None], [17])
+    within("logp", host(logp), o["logp"], U * (64 + 8 * np.abs(o["logp"])))
+    g, kept = torch.zeros(600, 5, device="cuda"), m.clone()
+    B.laplex_logprob_backward(y, target, lse, entropy, torch.ones(1, device="cuda"), None, None, g[:, 2])
+    want = O.logprob_backward(host(y)[:, None], [17], [1.0], [0.0], [0.0])
+    within("gy", host(g[:, 2]), want[:, 0], 300 * U * np.maximum(np.abs(want[:, 0]), 1e-3))
+    assert torch.equal(m, kept) and (g[:, [0, 1, 3, 4]] == 0).all()
