@@ -78,9 +78,9 @@ class TokenModel:
     def _logprob(self, logits, targets, top=0):
         t = logits.shape[1]
         new = lambda *s: torch.empty(*s, device="cuda")
-        logp, lse, entropy = new(t), new(t), new(t)
+        logp, lse, entropy = new(t) if targets is not None else None, new(t), new(t)
         ids, alternatives = (torch.empty(top, t, dtype=torch.int64, device="cuda"), new(top, t)) if top else (None, None)
-        B.laplex_logprob(logits, targets, logp if targets is not None else None, lse, entropy, ids, alternatives,
+        B.laplex_logprob(logits, targets, logp, lse, entropy, ids, alternatives,
                          self.workspace("logprob", B.laplex_logprob_workspace_bytes(self.vocabulary, t, top)))
         return logp, lse, entropy, ids, alternatives
 
@@ -95,7 +95,7 @@ class TokenModel:
 
     def read(self, tokens, positions, starts=None, state=None, targets=None, top=0):
         """Reads prompts that lie one behind the other (from row starts[b] on); `state` is carried on in place.
-        (log probabilities of the targets, entropies, ids and log probabilities of the likeliest tokens)"""
+        (log probabilities of the targets, if there are any, entropies, ids and log probabilities of the likeliest tokens)"""
         sequences = 1 if starts is None else len(starts) - 1
         x, q, k, v = self._project(tokens, positions)
         y, _ = self._attend(q, k, v, sequences, starts, state, state)
