@@ -425,7 +425,7 @@ int laplex_rotary_frequencies(float* frequencies, int64_t rotary_dim, double bas
  * all have tokens / sequences rows.  Sequences may be empty.  Values in starts that are out of order or of range give wrong values, never a fault.
  * rates[heads] >= 0 in device memory (constants of the layer: they get no gradient; +inf: every token sees only itself; NaN: its head is NaN).
  * state_in, state_out: fp32 [sequences][heads][dk][dv]; state_in NULL = zeros, state_out NULL = not wanted; they may be the same buffer.
- * An empty sequence hands its state through.  1 <= dk, dv <= LAPLEX_ATTENTION_MAX_DIM; scale positive and finite.
+ * An empty sequence hands its state through.  y may overlap no input.  1 <= dk, dv <= LAPLEX_ATTENTION_MAX_DIM; scale positive and finite.
  * Rows before a value that is not finite are not touched by it; from its token on everything that it is weighted into is not finite.
  */
 int laplex_decay_attention_workspace_bytes(int type, int64_t tokens, int64_t sequences, int64_t heads, int64_t dk, int64_t dv,
@@ -455,7 +455,7 @@ int laplex_decay_attention_backward(const void* q, int64_t ldq, const void* k, i
 
 /*
  * The same for one token of every sequence, as when tokens are written one by one: row b of q, k, v, y belongs to sequence b, and
- *   state[b] <- l state[b] + k v^T,   y = scale * q state[b]          (state fp32 [sequences][heads][dk][dv], updated in place).
+ *   state[b] <- l state[b] + k v^T,   y = scale * q state[b]          (state fp32 [sequences][heads][dk][dv], updated in place; y may overlap no input).
  */
 int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
                                 int64_t sequences, int64_t heads, int64_t dk, int64_t dv, const float* rates, float scale,
