@@ -132,9 +132,9 @@ __global__ void k_rotary_frequencies(float* out, int64_t pairs, double base, int
                                      double high)
 {
     const double kTurn = 6.28318530717958647693;
+    if (scaling == 2 && pairs > 1) base *= pow(factor, (double)pairs / (double)(pairs - 1));
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < pairs; i += (int64_t)gridDim.x * blockDim.x) {
         const double part = (double)i / (double)pairs;
-        if (scaling == 2 && pairs > 1) base *= pow(factor, (double)pairs / (double)(pairs - 1));
         double f = pow(base, -part);
         if (scaling == 1) f /= factor;
         if (scaling == 3) {
@@ -143,7 +143,6 @@ __global__ void k_rotary_frequencies(float* out, int64_t pairs, double base, int
             f = f * keep + f / factor * (1.0 - keep);
         }
         out[i] = (float)f;
-        if (scaling == 2 && pairs > 1) base /= pow(factor, (double)pairs / (double)(pairs - 1));
     }
 }
 
