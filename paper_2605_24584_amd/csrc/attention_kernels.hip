@@ -8,7 +8,7 @@
 // wavefront owns 16 columns of the result and of the state, which stays in its accumulator registers from the first chunk to
 // the last: as it leaves an accumulator a pair of tiles IS a fragment of the product q S (over the state's rows in a
 // permuted order, which the rows of q in LDS share), so the state does not pass through memory.  (32 columns a wavefront, four of them: 249 registers
-// instead of 124 and no faster.)
+// instead of 128 and no faster.)
 //
 // Sequences that are long and few are cut into stretches: one launch forms what each stretch adds to the state (k_attention_walk<STATES>, which
 // reads k and v alone), one brings these together in order (k_attention_carry), and then all stretches are walked at once.
@@ -18,10 +18,11 @@
 // that can be asked for is not rounded at all: l^d v is the sum of three bf16 numbers, exactly, so a state is an fp32 sum of exact products.  fp32 runs on
 // the fp32 matrix instructions.
 //
-// What bounds it: a chunk of 64 bf16 tokens of a head of 128 takes a compute unit 4.5 to 4.9 us with two workgroups on it; its LDS reads alone would
-// take 1.9, its vector instructions 1.8, its matrix products 1.0: they overlap only as far as sixteen wavefronts alternate.  us of the walk / states / carry:
-// 4 x 2048 tokens, 16 heads of 128, bf16 48 / 25 / 13; one of 65536, 8 heads 155 / 80 / 27; 8 x 4096, 16 heads 145 / 67 / 13, its gradients 439 uncut
-// (3.7 TB/s: three walks, each with three matrices read and one written); 24 sequences of 1250 on average, 6 heads of 96 x 80, fp32 157 / 57 / 15, its gradients 366 / 114 / 23.
+// What bounds it: a chunk of 64 bf16 tokens of a head of 128 takes a compute unit 5.1 to 5.3 us with two workgroups on it; its LDS reads alone would
+// take 2.1, its vector instructions 2.1, its matrix products 1.3: as they are, they hardly overlap.  us of the walk / states / carry (on average over calls, between
+// which the walk of a long sequence varies most): 4 x 2048 tokens, 16 heads of 128, bf16 51 / 24 / 11; one of 65536, 8 heads 167 to 189 / 82 / 28; 8 x 4096, 16 heads
+// 163 / 67 / 11, its gradients 501 uncut (3.2 TB/s: three walks, each with three matrices read and one written); 24 sequences of 1250 on average, 6 heads of 96 x 80, fp32
+// 143 / 54 / 13, its gradients 380 to 420 / 120 / 21.
 #include "token_internal.h"
 
 namespace laplex {
@@ -775,7 +776,7 @@ k_attention_carry(AttentionArgs A)
 }
 
 // One token for every sequence: the state is read and written once, everything else is a few hundred numbers.  A workgroup takes `lanes` times VEC columns of one
-// state, a lane VEC of them, the rest of the lanes its rows.  256 sequences of 16 heads of 128 x 128: 87 us for 0.54 GB (6.2 TB/s); one sequence 3.7 us.
+// state, a lane VEC of them, the rest of the lanes its rows.  256 sequences of 16 heads of 128 x 128: 88 us for 0.54 GB (6.1 TB/s); one sequence 4.0 us.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kStepThreads)
 k_attention_step(AttentionStepArgs A, int lanes_log2, int slices)
@@ -855,19 +856,19 @@ Plan plan_of(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, in
     const int64_t longest = equal && sequences > 0 ? tokens / sequences : tokens;
     // Two workgroups for every compute unit, where cutting is worth its two further launches and the second read of k and v: not where whole sequences
     // give every compute unit one or nearly (a stretch would be half a sequence or more).  Of unknown lengths four times as many, since the longest
-    // stretch is what the others wait for.  us, stretches of 256 / 512 / 1024 / 2048 / whole sequences: 4 x 2048 tokens, 16 heads 82 / 80 / 128 / - / 164; 65536
-    // tokens, 8 heads 369 / 283 / 258 / 318 / 5155; 8 x 4096, 16 heads 294 / 250 / 229 / 264 / 344, their gradients 835 / 698 / 632 / 592 / 492; 24 sequences of
-    // 1250 tokens on average, 6 heads, fp32 277 / 286 / 530 / 604 / 641, their gradients 694 / 699 / 902 / 1050 / 1061.
+    // stretch is what the others wait for.  us, stretches of 256 / 512 / 1024 / 2048 / whole sequences: 4 x 2048 tokens, 16 heads 92 / 92 / 142 / - / 186; 65536
+    // tokens, 8 heads 371 / 292 / 253 / 297 / 5810; 8 x 4096, 16 heads 310 / 261 / 230 / 285 / 381, their gradients 749 / 651 / 596 / 564 / 502; 24 sequences of
+    // 1250 tokens on average, 6 heads, fp32 226 / 232 / 355 / 503 / 674, their gradients 473 / 509 / 677 / 940 / 783.
     const int64_t work = tokens * heads * P.slices * walks, workgroups = equal ? 512 : kPackedWorkgroups;
     P.stretch = (work + 64 * workgroups - 1) / (64 * workgroups) * 64;
     // At least 256 tokens, or the states that pass through memory cost more than the walks.  Where even those leave compute units without a workgroup the
     // time is that of one workgroup's stretch, twice, and of the chain of states over the stretches: shorter ones, the more so the shorter the sequence.
-    // us, stretches of 256 / 128 / 64, one sequence, bf16, a head of 128: 384 tokens 32 / 26 / 21; 1024 40 / 28 / 24; 4096 44 / 36 / 37; 16384 58 / 62 / 92;
-    // fp32 77 / 48 / 32; 83 / 50 / 34; 88 / 58 / 48; 101 / 84 / 103.  Sequences of a few tokens on average need none of it.
+    // us, stretches of 256 / 128 / 64, one sequence, bf16, a head of 128: 384 tokens 42 / 29 / 25; 1024 46 / 31 / 26; 4096 50 / 39 / 40; 16384 64 / 67 / 96;
+    // fp32 83 / 50 / 34; 86 / 52 / 37; 90 / 60 / 51; 103 / 87 / 106.  Sequences of a few tokens on average need none of it.
     int64_t least = 256;
     if (work < 256 * 256 && tokens >= 64 * sequences) least = longest <= 2048 ? kLeastStretch : longest <= 8192 ? 128 : 256;
     if (P.stretch < least) P.stretch = least;
-    // (192 tokens whole / in stretches of 64: bf16 18 / 19 us, their gradients 18 / 22; fp32 41 / 31 and 41 / 34)
+    // (192 tokens whole / in stretches of 64: bf16 23 / 22 us, their gradients 21 / 22; fp32 44 / 33 and 42 / 33)
     P.cut = longest > 2 * P.stretch && longest > (bf16 ? 256 : 128);
     if (!P.cut) P.stretch = longest < 64 ? 64 : (longest + 63) / 64 * 64;
     P.per_sequence = equal ? (longest + P.stretch - 1) / P.stretch : 0;

@@ -14,9 +14,9 @@
 // is room for; then the first `top` of each level are chosen, one level after the other: a value among the `top` largest lies in one of the `top`
 // groups with the largest maxima (ties: the first ones), since otherwise each of those holds a value before it.
 //
-// The pass and the gradient are bound by memory: 32000 x 4099 fp32 95 to 105 us for 0.52 GB read (5.2 TB/s), the gradient 200 to 210 us for 1.05 GB.  The second
-// launch is bound by latency, three or four dependent rounds of loads: 32000 x 1 with the 8 likeliest 8.2 us (the pass 4.6), 32000 x 256 with 20 18 us (12), none
-// asked for 6.5 us.  (A form that extracted the alternatives level by level took 40 and 59 us.)
+// The pass and the gradient are bound by memory: 32000 x 4099 fp32 95 to 105 us for 0.52 GB read (5.2 TB/s), the gradient 200 to 220 us for 1.05 GB.  The second
+// launch is bound by latency, three or four dependent rounds of loads: 32000 x 1 with the 8 likeliest 8.4 us (the pass 4.7), 32000 x 256 with 20 18.5 us (12), none
+// asked for 7.4 us.  (A form that extracted the alternatives level by level took 40 and 59 us.)
 #include "token_internal.h"
 
 namespace laplex {
