@@ -732,15 +732,22 @@ k_attention_walk(AttentionArgs A)
 }
 
 // What enters the stretches: carry_n = l^stretch carry_(n-1) + U_(n-1), carry_0 = the initial state, in the places of the U.
-// A thread per four rows of a column of the state.
+// A thread per four rows of a column of the state, for every sequence; or, where there are fewer places than sequences, for every place, of which a sequence's first
+// one has something to do (4096 sequences of 16 tokens, 16 heads: 1.3 ms to look at each).
 template <int DK, int COLS>
 __global__ void __launch_bounds__(256)
 k_attention_carry(AttentionArgs A)
 {
     constexpr int kPieces = DK * COLS / 4, kBlocks = (kPieces + 255) / 256;
     const Walk W = A.states[blockIdx.z];
-    for (int64_t block = blockIdx.x; block < A.sequences * A.slices * kBlocks; block += gridDim.x) {
-        const int64_t b = block / (A.slices * kBlocks);
+    const bool by_place = A.places < A.sequences;
+    for (int64_t block = blockIdx.x; block < (by_place ? A.places : A.sequences) * A.slices * kBlocks; block += gridDim.x) {
+        int64_t b = block / (A.slices * kBlocks);
+        if (by_place) {
+            const Stretch s = find_stretch<true>(A, b);
+            if (s.index != 0 || s.count <= A.stretch) continue;
+            b = s.b;
+        }
         const int rest = (int)(block % (A.slices * kBlocks)), slice = rest / kBlocks, piece = (rest % kBlocks) * 256 + threadIdx.x;
         const int h = blockIdx.y, col0 = slice * COLS;
         if (col0 >= W.dv || piece >= kPieces) continue;
@@ -896,7 +903,7 @@ hipError_t walk_with(const AttentionArgs& A, const Plan& P, hipStream_t st)
         hipLaunchKernelGGL((k_attention_walk<T, DK, WAVES, kStates>), sets_grid, dim3(64 * WAVES), 0, st, A);
         profile_after("attention_states", st);
         profile_before("attention_carry", st);
-        const int64_t blocks = A.sequences * P.slices * ((DK * 16 * WAVES / 4 + 255) / 256), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+        const int64_t blocks = (P.places < A.sequences ? P.places : A.sequences) * P.slices * ((DK * 16 * WAVES / 4 + 255) / 256), most = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
         hipLaunchKernelGGL((k_attention_carry<DK, 16 * WAVES>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)A.heads, (unsigned)A.sets),
                            dim3(256), 0, st, A);
         profile_after("attention_carry", st);
