@@ -121,6 +121,20 @@ def test_the_gradient_does_not_depend_on_where_the_logits_lie(dtype, k, batch, i
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,batch", [(37, 4096), (300, 4099), (1100, 5000)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_the_gradient_of_thousands_of_columns(dtype, k, batch, in_place):
+    """Enough columns that those far from zero are taken sixteen at a time, some of them in every sixteen, and stretches with none and with nothing else."""
+    r = seeded("thousands", k, batch)
+    y = shifted(r, k, batch, dtype)
+    y[:, 1000:1500] = dev((3.0 * r.normal(size=(k, 500))).astype(np.float32), dtype)
+    y[:, 2000:2500] = dev((3.0 * r.normal(size=(k, 500)) + 300.0).astype(np.float32), dtype)
+    y[:, 3001:3040] = -float("inf")
+    targets = r.integers(0, k, batch); targets[::6] = -1
+    check_gradient(y, targets, 1.0, in_place=in_place)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("k,batch", [(8, 3), (500, 9), (5001, 17)])
 @pytest.mark.parametrize("tau", [1.0, 1.3, 0.5])
 @pytest.mark.parametrize("which", [(True, True, True), (True, False, False), (False, True, False), (False, False, True)])
