@@ -376,6 +376,10 @@ enum {
     LAPLEX_ROTARY_INVERSE = 32u        /* turn the other way: what carries gradients back */
 };
 
+enum {
+    LAPLEX_VERIFY_GREEDY = 64u         /* a draft is kept where it is the likeliest token */
+};
+
 enum { /* laplex_rotary_frequencies */
     LAPLEX_ROTARY_PLAIN = 0,
     LAPLEX_ROTARY_LINEAR = 1,
@@ -389,6 +393,8 @@ enum { /* laplex_rotary_frequencies */
 #define LAPLEX_ROTARY_MAX_DIM 4096LL        /* numbers of a head */
 #define LAPLEX_ATTENTION_MAX_DIM 256LL      /* numbers of a head in q and k, and in v */
 #define LAPLEX_LOGPROB_MAX_TOP 64LL         /* alternatives of a token */
+#define LAPLEX_NORM_MAX_ROWS 2147483647LL
+#define LAPLEX_NORM_MAX_WIDTH 1048576LL
 
 /*
  * Rotary positions: the first rotary_dim numbers of every head of x[tokens][heads][head_dim] are r/2 pairs, and pair i of
@@ -490,6 +496,54 @@ int laplex_logprob(const void* y, int64_t ldy, int type, int64_t k, int64_t batc
 int laplex_logprob_backward(const void* y, int64_t ldy, int type, int64_t k, int64_t batch, const int64_t* targets, float tau,
                             const float* lse, const float* entropy, const float* glogp, const float* gentropy, const float* glse,
                             void* gy, int64_t ldgy, laplex_stream_t stream);
+
+/*
+ * Layer norm of rows x[rows][width]:
+ *   mean = sum x / width,  rstd = (sum (x - mean)^2 / width + eps)^(-1/2),  y = (x - mean) rstd weight + bias
+ * weight[width] and bias[width] may each be NULL (1, 0); mean[rows] and rstd[rows] (what the backward call needs) may each be NULL.  A row may be a
+ * head of a token: with weight = width^(-1/2) queries and keys become (centred) vectors of length 1.  y may be x (in place, the same ld), else they must
+ * not overlap.  eps positive and finite; 1 <= width <= LAPLEX_NORM_MAX_WIDTH; rows <= LAPLEX_NORM_MAX_ROWS.  The squares are summed in fp32: numbers from
+ * 1e18 in magnitude on may give rows of zeros.  A row with a NaN or an infinity is NaN; others are not touched by it.
+ */
+int laplex_layer_norm(const void* x, int64_t ldx, int type, int64_t rows, int64_t width, const float* weight, const float* bias, float eps,
+                      void* y, int64_t ldy, float* mean, float* rstd, laplex_stream_t stream);
+
+/*
+ * Gradients of sum(gy * y), with the forward call's mean and rstd, hat = (x - mean) rstd and g = gy weight:
+ *   gx = rstd (g - sum g / width - hat sum (g hat) / width),   gweight = sum over rows of gy hat,   gbias = sum over rows of gy
+ * gx, gweight, gbias may each be NULL; gx may be gy or x (in place, the same ld).  rows == 0 gives gweight = gbias = 0.  The workspace (for gweight and gbias alone)
+ * serves either type and all smaller numbers of rows.
+ */
+int laplex_layer_norm_workspace_bytes(int64_t rows, int64_t width, size_t* out /* host */);
+
+int laplex_layer_norm_backward(const void* x, int64_t ldx, const void* gy, int64_t ldgy, int type, int64_t rows, int64_t width,
+                               const float* weight, const float* mean, const float* rstd, void* gx, int64_t ldgx, float* gweight, float* gbias,
+                               void* ws, size_t ws_bytes, laplex_stream_t stream);
+
+/*
+ * Verification of drafted tokens: which of the tokens that something cheaper has proposed are kept, and the next token of every sequence, so that what is written
+ * has the target's distribution.  y[k][batch] are the target's logits in the layout of this library's products, draft_y[k][batch] those that the drafts were drawn
+ * from, p = softmax(tau y) and q = softmax(draft_tau draft_y) of a column (draft_y NULL: the drafts are certain, q = 1 for the draft and 0 beside it).
+ * Sequence b has the columns starts[b] .. starts[b+1]-1 (int64 device array of sequences + 1 ascending values from 0 to batch), or, with starts NULL, batch / sequences
+ * of them.  Column c of a sequence belongs to the token before its c-th draft: that draft is drafts[.] of the same column, and is kept while
+ *   chances[.] * q(draft) < p(draft);
+ * the last column of a sequence has no draft.  At the first draft that is not kept the next token is drawn from max(p - q, 0), at the last column from p:
+ *   next[b] = the lowest row whose running sum of weights, in ascending order of rows, is above next_chances[b] * (the sum of all).
+ * accepted[b] = number of drafts kept; next[b] = -1 for a sequence without columns.  chances[batch] and next_chances[sequences] are random numbers from [0, 1) in fp64, everything
+ * compared is formed in fp64.  logp[batch] (may be NULL): log p(draft), 0 where there is no draft; next_logp[sequences] (may be NULL): log p(next), 0 for none.
+ * A draft outside 0 .. k-1 (padding) ends the drafts: the token there is drawn from p.  So it is where q is undefined (a NaN, +inf or nothing but -inf among the
+ * draft's logits).  A column whose target logits hold a NaN or +inf, or nothing but -inf, has no distribution: its draft is not kept, logp is NaN, and next is -1 if
+ * it has to be drawn there.  Logits of -inf (banned entries) are never kept or drawn.
+ * LAPLEX_VERIFY_GREEDY: a draft is kept where it is the row of the column's largest logit (of equal ones the lowest), and next is that row; chances, next_chances and
+ * draft_y are not looked at and may be NULL (tau still scales logp and next_logp).
+ * 1 <= k.  The workspace serves all smaller calls.
+ */
+int laplex_verify_workspace_bytes(int64_t k, int64_t batch, int64_t sequences, size_t* out /* host */);
+
+int laplex_verify_drafts(const void* y, int64_t ldy, const void* draft_y, int64_t ld_draft, int type, int64_t k, int64_t batch, const int64_t* drafts,
+                         int64_t sequences, const int64_t* starts, float tau, float draft_tau, const double* chances, const double* next_chances,
+                         int64_t* accepted, int64_t* next, float* logp, float* next_logp, void* ws, size_t ws_bytes, uint32_t flags,
+                         laplex_stream_t stream);
 
 /* Host: static text for a status code. */
 const char* laplex_status_string(int status);

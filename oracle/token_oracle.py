@@ -131,3 +131,73 @@ def logprob_backward(y, targets, glogp, gentropy, glse, tau=1.0):
         g[some, c] -= gentropy[c] * (p[some] * (logp[some] + f["entropy"][c]))
         g[:, c] += glse[c] * p
     return tau * g
+
+
+def layer_norm(x, weight, bias, eps):
+    """(y, mean, rstd) over the last axis."""
+    x = np.asarray(x, np.float64)
+    mean = x.mean(-1, keepdims=True)
+    rstd = 1.0 / np.sqrt(((x - mean) ** 2).mean(-1, keepdims=True) + eps)
+    y = (x - mean) * rstd
+    y = y * (1.0 if weight is None else weight) + (0.0 if bias is None else bias)
+    return y, mean[..., 0], rstd[..., 0]
+
+
+def layer_norm_backward(x, gy, weight, eps):
+    """(gx, gweight, gbias) of sum(gy y), rows x (rows, width)."""
+    x, gy = np.asarray(x, np.float64), np.asarray(gy, np.float64)
+    mean = x.mean(-1, keepdims=True)
+    rstd = 1.0 / np.sqrt(((x - mean) ** 2).mean(-1, keepdims=True) + eps)
+    hat = (x - mean) * rstd
+    g = gy * (1.0 if weight is None else weight)
+    gx = rstd * (g - g.mean(-1, keepdims=True) - hat * (g * hat).mean(-1, keepdims=True))
+    return gx, (gy * hat).sum(0), gy.sum(0)
+
+
+def _softmax(z):
+    z = np.asarray(z, np.float64)
+    top = z.max() if len(z) else -np.inf
+    if np.isnan(z).any() or not np.isfinite(top):
+        return None, None
+    e = np.exp(z - top)
+    return e / e.sum(), z - top - np.log(e.sum())
+
+
+def verify_drafts(y, z, drafts, starts, tau, draft_tau, chances, next_chances, greedy=False):
+    """(accepted, next, logp, next_logp) sequence by sequence, column by column."""
+    k, t = y.shape
+    b = len(starts) - 1
+    accepted, following = np.zeros(b, np.int64), np.full(b, -1, np.int64)
+    logp, next_logp = np.zeros(t), np.zeros(b)
+    for i in range(b):
+        going = True
+        for c in range(starts[i], starts[i + 1]):
+            p, log = _softmax(tau * y[:, c])
+            x = int(drafts[c]) if c + 1 < starts[i + 1] and 0 <= drafts[c] < k else None
+            if x is not None:
+                logp[c] = np.nan if p is None else log[x]
+            if not going:
+                continue
+            if p is None:
+                going = False
+                continue
+            if greedy:
+                best = int(np.argmax(y[:, c]))
+                if x == best:
+                    accepted[i] += 1
+                    continue
+                following[i], next_logp[i], going = best, log[best], False
+                continue
+            q = None
+            if x is not None:
+                q = (np.arange(k) == x) * 1.0 if z is None else _softmax(draft_tau * z[:, c])[0]
+            if q is not None and chances[c] * q[x] < p[x]:
+                accepted[i] += 1
+                continue
+            left = p if q is None else np.maximum(p - q, 0.0)
+            left = left if left.sum() > 0.0 else p
+            run = np.cumsum(left)
+            past = np.nonzero((run > next_chances[i] * run[-1]) & (left > 0.0))[0]
+            at = int(past[0]) if len(past) else int(np.nonzero(left > 0.0)[0][-1])
+            following[i], next_logp[i], going = at, log[at], False
+    return accepted, following, logp, next_logp

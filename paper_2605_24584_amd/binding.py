@@ -44,6 +44,10 @@ LAPLEX_TOKEN_MAX_SEQUENCES = 1048576
 LAPLEX_ROTARY_MAX_DIM = 4096
 LAPLEX_ATTENTION_MAX_DIM = 256
 LAPLEX_LOGPROB_MAX_TOP = 64
+LAPLEX_NORM_MAX_ROWS = 2147483647
+LAPLEX_NORM_MAX_WIDTH = 1048576
+
+LAPLEX_VERIFY_GREEDY = 64
 
 EXPORTS = (
     "laplex_workspace_bytes", "laplex_apply", "laplex_apply_backward", "laplex_gram",
@@ -58,6 +62,8 @@ EXPORTS = (
     "laplex_decay_attention_workspace_bytes", "laplex_decay_attention", "laplex_decay_attention_backward",
     "laplex_decay_attention_step",
     "laplex_logprob_workspace_bytes", "laplex_logprob", "laplex_logprob_backward",
+    "laplex_layer_norm", "laplex_layer_norm_workspace_bytes", "laplex_layer_norm_backward",
+    "laplex_verify_workspace_bytes", "laplex_verify_drafts",
 )
 
 # include/laplex_diag.h: hooks for benchmarks and tests
@@ -137,6 +143,11 @@ def lib() -> ctypes.CDLL:
         L.laplex_logprob_workspace_bytes.argtypes = [_I, _I, _I, ctypes.POINTER(_Z)]
         L.laplex_logprob.argtypes = [_P, _I, _C, _I, _I, _P, _F, _P, _P, _P, _I, _P, _P, _P, _Z, _P]
         L.laplex_logprob_backward.argtypes = [_P, _I, _C, _I, _I, _P, _F, _P, _P, _P, _P, _P, _P, _I, _P]
+        L.laplex_layer_norm.argtypes = [_P, _I, _C, _I, _I, _P, _P, _F, _P, _I, _P, _P, _P]
+        L.laplex_layer_norm_workspace_bytes.argtypes = [_I, _I, ctypes.POINTER(_Z)]
+        L.laplex_layer_norm_backward.argtypes = [_P, _I, _P, _I, _C, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P, _Z, _P]
+        L.laplex_verify_workspace_bytes.argtypes = [_I, _I, _I, ctypes.POINTER(_Z)]
+        L.laplex_verify_drafts.argtypes = [_P, _I, _P, _I, _C, _I, _I, _P, _I, _P, _F, _F, _P, _P, _P, _P, _P, _P, _P, _Z, _U, _P]
         for name in EXPORTS + DIAG_EXPORTS:
             if name not in ("laplex_status_string", "laplex_last_hip_error"):
                 getattr(L, name).restype = ctypes.c_int
@@ -513,3 +524,75 @@ def laplex_logprob_backward(y, targets, lse, entropy, glogp, gentropy, glse, gy,
     f = lambda x: _whole(x, (t,), torch.float32)
     _check(lib().laplex_logprob_backward(_ptr(y), _ld(y), _same_type(y, gy), k, t, _whole(targets, (t,), torch.int64), tau, f(lse), f(entropy),
                                          f(glogp), f(gentropy), f(glse), _ptr(gy), _ld(gy), _stream(stream)))
+
+
+def _rows(x):
+    """(rows, width, row stride) of a tensor whose last axis is a row and whose other axes are rows that lie equally far apart."""
+    width = x.shape[-1]
+    rows = x.numel() // width if width else 0
+    assert x.dim() >= 1 and (width <= 1 or x.numel() == 0 or x.stride(-1) == 1), "a row's numbers must be contiguous"
+    ld = None
+    for size, stride in zip(reversed(x.shape[:-1]), reversed(x.stride()[:-1])):
+        if size == 1 or rows == 0:
+            continue
+        if ld is None:
+            ld, reach = stride, stride * size
+        else:
+            assert stride == reach, "rows must lie equally far apart"
+            reach = stride * size
+    return rows, width, max(width, 1) if ld is None else ld
+
+
+def _ld_rows(t, like):
+    if t is None:
+        return 0
+    assert t.shape == like.shape, f"shape {tuple(t.shape)}, not {tuple(like.shape)}"
+    return _rows(t)[2]
+
+
+def laplex_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
+    """y <- layer norm over the last axis of x, times weight (width,) plus bias (width,), fp32; either may be None.  mean, rstd: one for each
+    row, fp32."""
+    import torch
+    rows, width, ld = _rows(x)
+    f = lambda t, shape: _whole(t, shape, torch.float32)
+    _check(lib().laplex_layer_norm(_ptr(x), ld, _same_type(x, y), rows, width, f(weight, (width,)), f(bias, (width,)), eps, _ptr(y), _ld_rows(y, x),
+                                   f(mean, x.shape[:-1]), f(rstd, x.shape[:-1]), _stream(stream)))
+
+
+def laplex_layer_norm_workspace_bytes(rows: int, width: int) -> int:
+    out = _Z(0)
+    _check(lib().laplex_layer_norm_workspace_bytes(rows, width, ctypes.byref(out)))
+    return out.value
+
+
+def laplex_layer_norm_backward(x, gy, weight, mean, rstd, gx, gweight, gbias, ws, stream=None) -> None:
+    """gx, gweight, gbias (any may be None) <- gradients of sum(gy * y), with the forward call's mean and rstd."""
+    import torch
+    rows, width, ld = _rows(x)
+    f = lambda t, shape: _whole(t, shape, torch.float32)
+    _check(lib().laplex_layer_norm_backward(
+        _ptr(x), ld, _ptr(gy), _ld_rows(gy, x), _same_type(x, gy, gx), rows, width, f(weight, (width,)), f(mean, x.shape[:-1]), f(rstd, x.shape[:-1]),
+        _ptr(gx), _ld_rows(gx, x), f(gweight, (width,)), f(gbias, (width,)), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def laplex_verify_workspace_bytes(k: int, batch: int, sequences: int) -> int:
+    out = _Z(0)
+    _check(lib().laplex_verify_workspace_bytes(k, batch, sequences, ctypes.byref(out)))
+    return out.value
+
+
+def laplex_verify_drafts(y, draft_y, drafts, chances, next_chances, accepted, following, ws, logp=None, following_logp=None, tau: float = 1.0,
+                         draft_tau: float = 1.0, sequences: int = 1, starts=None, flags: int = 0, stream=None) -> None:
+    """accepted, following (sequences,) int64 <- how many of each sequence's drafts are kept, and its next token; y and draft_y (None: the drafts are
+    certain) are logits (k, batch), one column for each draft and one more; drafts (batch,) int64, chances (batch,) and next_chances (sequences,)
+    fp64 in [0, 1); logp (batch,), following_logp (sequences,): log probabilities under the target, fp32."""
+    import torch
+    k, t = y.shape[0], _batch(y)
+    assert draft_y is None or draft_y.shape == y.shape
+    b, at = _sequences(sequences, starts)
+    _check(lib().laplex_verify_drafts(
+        _ptr(y), _ld(y), _ptr(draft_y), _ld(draft_y), _same_type(y, draft_y), k, t, _whole(drafts, (t,), torch.int64), b, at, tau, draft_tau,
+        _whole(chances, (t,), torch.float64), _whole(next_chances, (b,), torch.float64), _whole(accepted, (b,), torch.int64),
+        _whole(following, (b,), torch.int64), _whole(logp, (t,), torch.float32), _whole(following_logp, (b,), torch.float32),
+        _ptr(ws), 0 if ws is None else ws.numel(), flags, _stream(stream)))

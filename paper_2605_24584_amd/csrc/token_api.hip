@@ -61,6 +61,11 @@ int check_attention_sizes(int type, int64_t tokens, int64_t sequences, int64_t h
     return LAPLEX_OK;
 }
 
+int check_norm_sizes(int64_t rows, int64_t width)
+{
+    return rows < 0 || rows > LAPLEX_NORM_MAX_ROWS || width < 1 || width > LAPLEX_NORM_MAX_WIDTH ? LAPLEX_ERR_SIZE : LAPLEX_OK;
+}
+
 bool positive(float v) { return v > 0.0f && std::isfinite(v); }
 
 }  // namespace
@@ -279,6 +284,102 @@ int laplex_logprob_backward(const void* y, int64_t ldy, int type, int64_t k, int
     A.y = y; A.ldy = ldy; A.k = k; A.batch = batch; A.bf16 = type == LAPLEX_BF16; A.targets = targets; A.tau = tau;
     A.lse = lse; A.entropy = entropy; A.glogp = glogp; A.gentropy = gentropy; A.glse = glse; A.gy = gy; A.ldgy = ldgy;
     LAPLEX_HIP(launch_logprob_backward(A, stream));
+    return LAPLEX_OK;
+}
+
+int laplex_layer_norm(const void* x, int64_t ldx, int type, int64_t rows, int64_t width, const float* weight, const float* bias, float eps,
+                      void* y, int64_t ldy, float* mean, float* rstd, laplex_stream_t stream)
+{
+    LAPLEX_CHECK(check_type(type));
+    LAPLEX_CHECK(check_norm_sizes(rows, width));
+    if (!positive(eps)) return LAPLEX_ERR_VALUE;
+    LAPLEX_CHECK(check_rows(x, type, rows, width, ldx, true));
+    LAPLEX_CHECK(check_rows(y, type, rows, width, ldy, true));
+    LAPLEX_CHECK(check_array(weight, width, 4, false));
+    LAPLEX_CHECK(check_array(bias, width, 4, false));
+    LAPLEX_CHECK(check_array(mean, rows, 4, false));
+    LAPLEX_CHECK(check_array(rstd, rows, 4, false));
+    if (rows == 0) return LAPLEX_OK;
+    NormArgs A{};
+    A.x = x; A.y = y; A.ldx = ldx; A.ldy = ldy; A.rows = rows; A.width = width; A.bf16 = type == LAPLEX_BF16;
+    A.weight = weight; A.bias = bias; A.eps = eps; A.mean_out = mean; A.rstd_out = rstd;
+    LAPLEX_HIP(launch_norm(A, stream));
+    return LAPLEX_OK;
+}
+
+int laplex_layer_norm_workspace_bytes(int64_t rows, int64_t width, size_t* out)
+{
+    if (!out) return LAPLEX_ERR_NULL;
+    LAPLEX_CHECK(check_norm_sizes(rows, width));
+    *out = norm_workspace(rows, width);
+    return LAPLEX_OK;
+}
+
+int laplex_layer_norm_backward(const void* x, int64_t ldx, const void* gy, int64_t ldgy, int type, int64_t rows, int64_t width,
+                               const float* weight, const float* mean, const float* rstd, void* gx, int64_t ldgx, float* gweight, float* gbias,
+                               void* ws, size_t ws_bytes, laplex_stream_t stream)
+{
+    LAPLEX_CHECK(check_type(type));
+    LAPLEX_CHECK(check_norm_sizes(rows, width));
+    LAPLEX_CHECK(check_rows(x, type, rows, width, ldx, true));
+    LAPLEX_CHECK(check_rows(gy, type, rows, width, ldgy, true));
+    LAPLEX_CHECK(check_rows(gx, type, rows, width, ldgx, false));
+    LAPLEX_CHECK(check_array(weight, width, 4, false));
+    LAPLEX_CHECK(check_array(mean, rows, 4, true));
+    LAPLEX_CHECK(check_array(rstd, rows, 4, true));
+    LAPLEX_CHECK(check_array(gweight, width, 4, false));
+    LAPLEX_CHECK(check_array(gbias, width, 4, false));
+    if (!gx && !gweight && !gbias) return LAPLEX_OK;
+    NormBackwardArgs A{};
+    if (gweight || gbias) {
+        LAPLEX_CHECK(check_ws(ws, ws_bytes, norm_workspace(rows, width)));
+        A.parts = static_cast<float*>(ws);
+    }
+    A.x = x; A.gy = gy; A.gx = gx; A.ldx = ldx; A.ldgy = ldgy; A.ldgx = ldgx; A.rows = rows; A.width = width; A.bf16 = type == LAPLEX_BF16;
+    A.weight = weight; A.mean = mean; A.rstd = rstd; A.gweight = gweight; A.gbias = gbias;
+    LAPLEX_HIP(launch_norm_backward(A, stream));
+    return LAPLEX_OK;
+}
+
+int laplex_verify_workspace_bytes(int64_t k, int64_t batch, int64_t sequences, size_t* out)
+{
+    if (!out) return LAPLEX_ERR_NULL;
+    if (k < 1 || k > kLogprobMaxRows || batch < 0 || batch > LAPLEX_TOKEN_MAX_TOKENS || sequences < 0 || sequences > LAPLEX_TOKEN_MAX_SEQUENCES)
+        return LAPLEX_ERR_SIZE;
+    *out = verify_workspace(k, batch, sequences);
+    return LAPLEX_OK;
+}
+
+int laplex_verify_drafts(const void* y, int64_t ldy, const void* draft_y, int64_t ld_draft, int type, int64_t k, int64_t batch, const int64_t* drafts,
+                         int64_t sequences, const int64_t* starts, float tau, float draft_tau, const double* chances, const double* next_chances,
+                         int64_t* accepted, int64_t* next, float* logp, float* next_logp, void* ws, size_t ws_bytes, uint32_t flags,
+                         laplex_stream_t stream)
+{
+    LAPLEX_CHECK(check_type(type));
+    if (flags & ~LAPLEX_VERIFY_GREEDY) return LAPLEX_ERR_FLAGS;
+    const bool greedy = (flags & LAPLEX_VERIFY_GREEDY) != 0;
+    size_t need = 0;
+    LAPLEX_CHECK(laplex_verify_workspace_bytes(k, batch, sequences, &need));
+    if (!starts && (sequences == 0 ? batch != 0 : batch % sequences != 0)) return LAPLEX_ERR_SIZE;
+    if (!positive(tau) || (draft_y && !greedy && !positive(draft_tau))) return LAPLEX_ERR_VALUE;
+    LAPLEX_CHECK(check_rows(y, type, k, batch, ldy, true));
+    if (!greedy) LAPLEX_CHECK(check_rows(draft_y, type, k, batch, ld_draft, false));
+    LAPLEX_CHECK(check_array(drafts, batch, 8, true));
+    LAPLEX_CHECK(check_array(starts, sequences, 8, false));
+    LAPLEX_CHECK(check_array(chances, batch, 8, !greedy));
+    LAPLEX_CHECK(check_array(next_chances, sequences, 8, !greedy));
+    LAPLEX_CHECK(check_array(accepted, sequences, 8, true));
+    LAPLEX_CHECK(check_array(next, sequences, 8, true));
+    LAPLEX_CHECK(check_array(logp, batch, 4, false));
+    LAPLEX_CHECK(check_array(next_logp, sequences, 4, false));
+    if (sequences == 0) return LAPLEX_OK;
+    LAPLEX_CHECK(check_ws(ws, ws_bytes, need));
+    VerifyArgs A{};
+    A.y = y; A.z = greedy ? nullptr : draft_y; A.ldy = ldy; A.ldz = ld_draft; A.k = k; A.batch = batch; A.sequences = sequences;
+    A.bf16 = type == LAPLEX_BF16; A.greedy = greedy; A.drafts = drafts; A.starts = starts; A.chances = chances; A.next_chances = next_chances;
+    A.tau = (double)tau; A.c = (double)tau * 1.4426950408889634074; A.draft_c = (double)draft_tau * 1.4426950408889634074;
+    A.accepted = accepted; A.next = next; A.logp = logp; A.next_logp = next_logp; A.ws = static_cast<char*>(ws);
+    LAPLEX_HIP(launch_verify(A, stream));
     return LAPLEX_OK;
 }
 

@@ -1,5 +1,6 @@
 // Internal declarations of the operators for token models: rotary positions, attention with a decay for each head, log
-// probabilities (rotary_kernels.hip, attention_kernels.hip, logprob_kernels.hip; host side in token_api.hip).
+// probabilities, layer norm, verification of drafts (rotary_kernels.hip, attention_kernels.hip, logprob_kernels.hip, norm_kernels.hip, verify_kernels.hip; host
+// side in token_api.hip).
 #pragma once
 
 #include "laplex_internal.h"
@@ -106,6 +107,64 @@ struct LogprobBackwardArgs {
     int64_t ldgy;
 };
 hipError_t launch_logprob_backward(const LogprobBackwardArgs& A, hipStream_t st);
+
+// ----------------------------------------------------------------------------
+// Layer norm.
+// ----------------------------------------------------------------------------
+struct NormArgs {
+    const void* x;
+    void* y;
+    int64_t ldx, ldy, rows, width;
+    bool bf16;
+    const float *weight, *bias;      // either may be null
+    float eps;
+    float *mean_out, *rstd_out;      // either may be null
+};
+hipError_t launch_norm(const NormArgs& A, hipStream_t st);
+
+struct NormBackwardArgs {
+    const void *x, *gy;
+    void* gx;                        // may be null
+    int64_t ldx, ldgy, ldgx, rows, width;
+    bool bf16;
+    const float *weight, *mean, *rstd;
+    float *gweight, *gbias;          // either may be null
+    float* parts;                    // [workgroups][2][width], null if neither is wanted
+};
+size_t norm_workspace(int64_t rows, int64_t width);
+hipError_t launch_norm_backward(const NormBackwardArgs& A, hipStream_t st);
+
+// ----------------------------------------------------------------------------
+// Verification of drafted tokens.
+// ----------------------------------------------------------------------------
+enum { kVerifyNone, kVerifyPlace, kVerifyAll, kVerifyLeft, kVerifyOthers };      // the next token: none, the likeliest, from p, from max(p - q, 0), from p without the draft
+
+struct VerifyColumn {
+    double s, draft_s;               // sums of 2^(c (y - m)) of the two matrices
+    int64_t place;                   // of the maximum, for the greedy rule
+    float m, draft_m;
+    int kept, mode;
+};
+
+struct VerifyArgs {
+    const void *y, *z;               // z: the drafts' logits, or null
+    int64_t ldy, ldz, k, batch, sequences;
+    bool bf16, greedy;
+    const int64_t *drafts, *starts;
+    const double *chances, *next_chances;
+    double tau, c, draft_c;          // c: tau / log 2
+    int64_t *accepted, *next;
+    float *logp, *next_logp;         // either may be null
+    char* ws;
+    // filled in by launch_verify
+    int lanes_log2, seq_log2;
+    int64_t part_rows, parts;
+    double* part_sum; float* part_max; int64_t* part_place;      // [matrix][part][column]
+    VerifyColumn* columns;
+    double* left;                    // [part][sequence]
+};
+size_t verify_workspace(int64_t k, int64_t batch, int64_t sequences);
+hipError_t launch_verify(const VerifyArgs& A, hipStream_t st);
 
 #ifdef __HIPCC__
 __device__ __forceinline__ float to_float(float v) { return v; }
