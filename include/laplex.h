@@ -468,6 +468,51 @@ int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64
                                 float* state, void* y, int64_t ldy, laplex_stream_t stream);
 
 /*
+ * Linear attention by the gated delta rule: the state forgets by a decay for each token and head, and a token corrects what the state holds for its key instead of
+ * adding to it.  Per head of a sequence, with l_t = exp(-rates[t][head]), b_t = beta[t][head] and the state S (dk x dv; S0 = state_in, or zeros):
+ *   S <- l_t S,   u_t = b_t (v_t - S^T k_t),   S <- S + k_t u_t^T,   y_t = scale S^T q_t,        t = 0 .. n-1
+ * q, k [tokens][key_heads][dk], v, y [tokens][heads][dv]; head h of values uses head h / (heads / key_heads) of queries and keys (key_heads divides heads).
+ * rates and beta: fp32 [tokens][heads], rows ldr and ldb floats apart, in device memory.  Sequences, starts and states as for laplex_decay_attention;
+ * lengths (int64 device array of `sequences` numbers, or NULL): only the first lengths[b] rows of sequence b are read (all of them where it has fewer, none where that is
+ * negative), and the rows behind them are left as they were, in y and in the gradients: what a batch with padding, or drafted tokens of which some were accepted, needs.
+ * Keys are usually of length 1 and b_t from 0 to 1: then the state cannot grow from what it holds.  Rates >= 0 (+inf: nothing is left of the state;
+ * from 1e5 on so too); other rates are carried as they are as long as exp(-sum of 64 of them) is a number.
+ * Rows before a value that is not finite (in k, v, beta, or a NaN or -inf in rates) are not touched by it; from its token on the results and the state of its head may be NaN.  In q it reaches
+ * its own row.  state_out may be state_in; nothing else may overlap.  1 <= dk, dv <= LAPLEX_ATTENTION_MAX_DIM; scale positive and finite.
+ * Flags: LAPLEX_SAVE_SCANS (needs a workspace for training): what the gradients need stays in the workspace for laplex_delta_attention_backward with the same flag
+ * and the same arguments.
+ */
+int laplex_delta_attention_workspace_bytes(int type, int64_t tokens, int64_t sequences, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv,
+                                           int training /* 0: the forward call without LAPLEX_SAVE_SCANS; else all calls */, size_t* out /* host */);
+/* Enough for up to so many tokens and sequences.  It grows with tokens + 64 sequences: about 0.18 KB, and for training 3.2 KB, for each of them and each head of 128. */
+
+int laplex_delta_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                           int64_t tokens, int64_t sequences, const int64_t* starts, const int64_t* lengths, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv,
+                           const float* rates, int64_t ldr, const float* beta, int64_t ldb, float scale, const float* state_in, void* y, int64_t ldy, float* state_out,
+                           void* ws, size_t ws_bytes, uint32_t flags, laplex_stream_t stream);
+
+/*
+ * Gradients of sum(gy * y) + sum(gstate_out * Sn) with respect to q, k, v, rates, beta and S0; those of q and k are summed over the heads that share them.  Any of
+ * gq, gk, gv, grates, gbeta (the last two fp32 [tokens][heads], rows ldgr and ldgb apart) and gstate_in may be NULL; gstate_out NULL = zeros; state_in, starts, lengths as in the
+ * forward call.  No output may overlap an input or another output.  Flags: LAPLEX_SAVE_SCANS (the workspace holds what the forward call with that flag has left); without it
+ * the call stands alone.  The workspace is the one for training.  A head of a sequence that holds a value that is not finite may have gradients that are NaN everywhere.
+ */
+int laplex_delta_attention_backward(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                                    int64_t tokens, int64_t sequences, const int64_t* starts, const int64_t* lengths, int64_t heads, int64_t key_heads, int64_t dk,
+                                    int64_t dv, const float* rates, int64_t ldr, const float* beta, int64_t ldb, float scale, const float* state_in,
+                                    const void* gy, int64_t ldgy, const float* gstate_out, void* gq, int64_t ldgq, void* gk, int64_t ldgk, void* gv, int64_t ldgv,
+                                    float* grates, int64_t ldgr, float* gbeta, int64_t ldgb, float* gstate_in, void* ws, size_t ws_bytes, uint32_t flags,
+                                    laplex_stream_t stream);
+
+/*
+ * The same for one token of every sequence: row b of q, k, v, rates, beta, y belongs to sequence b, and state[sequences][heads][dk][dv] (fp32) is updated in place.
+ * y may overlap no input.
+ */
+int laplex_delta_attention_step(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                                int64_t sequences, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv, const float* rates, int64_t ldr, const float* beta,
+                                int64_t ldb, float scale, float* state, void* y, int64_t ldy, laplex_stream_t stream);
+
+/*
  * Log probabilities over logits y[k][batch] in the layout of this library's products (row = vocabulary entry, column = token),
  * z = tau * y (tau an inverse temperature as above):
  *   lse[t] = log sum_i exp z[i,t],  logp[t] = z[targets[t], t] - lse[t],  entropy[t] = -sum_i p log p,  p = exp(z - lse)

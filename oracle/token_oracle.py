@@ -201,3 +201,48 @@ def verify_drafts(y, z, drafts, starts, tau, draft_tau, chances, next_chances, g
             at = int(past[0]) if len(past) else int(np.nonzero(left > 0.0)[0][-1])
             following[i], next_logp[i], going = at, log[at], False
     return accepted, following, logp, next_logp
+
+
+def delta_sequence(q, k, v, rates, beta, scale, state=None):
+    """One head of one sequence by the gated delta rule, token by token: (y, last state, sizes).  The update is a contraction for keys up to length 1 and beta from 0 to 2:
+    errors do not grow, and are measured against sizes = the largest length of a column of the state, the largest |u|, of each column."""
+    q, k, v, rates, beta = (np.asarray(t, np.float64) for t in (q, k, v, rates, beta))
+    S = np.zeros((q.shape[1], v.shape[1])) if state is None else np.asarray(state, np.float64).copy()
+    y, length, most = np.zeros(v.shape), np.sqrt((S ** 2).sum(0)), np.zeros(v.shape[1])
+    for t in range(q.shape[0]):
+        S = np.exp(-rates[t]) * S
+        u = beta[t] * (v[t] - k[t] @ S)
+        S = S + np.outer(k[t], u)
+        y[t] = scale * (q[t] @ S)
+        length = np.maximum(length, np.sqrt((S ** 2).sum(0)))
+        most = np.maximum(most, np.abs(u) + np.abs(beta[t] * v[t]))
+    return y, S, length + most
+
+
+def delta_sequence_backward(q, k, v, rates, beta, scale, state, gy, gstate):
+    """Gradients of sum(gy y) + sum(gstate last): (gq, gk, gv, grates, gbeta, g0), and the largest length of a column of the state's gradient."""
+    q, k, v, rates, beta, gy = (np.asarray(t, np.float64) for t in (q, k, v, rates, beta, gy))
+    n = q.shape[0]
+    S = np.zeros((q.shape[1], v.shape[1])) if state is None else np.asarray(state, np.float64).copy()
+    steps = []
+    for t in range(n):
+        before = np.exp(-rates[t]) * S
+        miss = v[t] - k[t] @ before
+        S = before + np.outer(k[t], beta[t] * miss)
+        steps.append((before, miss, S))
+    G = np.zeros_like(S) if gstate is None else np.asarray(gstate, np.float64).copy()
+    gq, gk, gv, gr, gb = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape), np.zeros(n), np.zeros(n)
+    length = np.sqrt((G ** 2).sum(0))
+    for t in range(n - 1, -1, -1):
+        before, miss, after = steps[t]
+        gq[t] = scale * (after @ gy[t])
+        G = G + scale * np.outer(q[t], gy[t])
+        length = np.maximum(length, np.sqrt((G ** 2).sum(0)))
+        gu = k[t] @ G
+        gb[t] = gu @ miss
+        gv[t] = beta[t] * gu
+        gk[t] = G @ (beta[t] * miss) - before @ gv[t]
+        G = G - np.outer(k[t], gv[t])
+        gr[t] = -(G * before).sum()
+        G = np.exp(-rates[t]) * G
+    return (gq, gk, gv, gr, gb, G), length

@@ -62,6 +62,7 @@ EXPORTS = (
     "laplex_decay_attention_workspace_bytes", "laplex_decay_attention", "laplex_decay_attention_backward",
     "laplex_decay_attention_step",
     "laplex_logprob_workspace_bytes", "laplex_logprob", "laplex_logprob_backward",
+    "laplex_delta_attention_workspace_bytes", "laplex_delta_attention", "laplex_delta_attention_backward", "laplex_delta_attention_step",
     "laplex_layer_norm", "laplex_layer_norm_workspace_bytes", "laplex_layer_norm_backward",
     "laplex_verify_workspace_bytes", "laplex_verify_drafts",
 )
@@ -143,6 +144,11 @@ def lib() -> ctypes.CDLL:
         L.laplex_logprob_workspace_bytes.argtypes = [_I, _I, _I, ctypes.POINTER(_Z)]
         L.laplex_logprob.argtypes = [_P, _I, _C, _I, _I, _P, _F, _P, _P, _P, _I, _P, _P, _P, _Z, _P]
         L.laplex_logprob_backward.argtypes = [_P, _I, _C, _I, _I, _P, _F, _P, _P, _P, _P, _P, _P, _I, _P]
+        L.laplex_delta_attention_workspace_bytes.argtypes = [_C, _I, _I, _I, _I, _I, _I, _C, ctypes.POINTER(_Z)]
+        L.laplex_delta_attention.argtypes = [_P, _I, _P, _I, _P, _I, _C, _I, _I, _P, _P, _I, _I, _I, _I, _P, _I, _P, _I, _F, _P, _P, _I, _P, _P, _Z, _U, _P]
+        L.laplex_delta_attention_backward.argtypes = [_P, _I, _P, _I, _P, _I, _C, _I, _I, _P, _P, _I, _I, _I, _I, _P, _I, _P, _I, _F, _P, _P, _I, _P,
+                                                      _P, _I, _P, _I, _P, _I, _P, _I, _P, _I, _P, _P, _Z, _U, _P]
+        L.laplex_delta_attention_step.argtypes = [_P, _I, _P, _I, _P, _I, _C, _I, _I, _I, _I, _I, _P, _I, _P, _I, _F, _P, _P, _I, _P]
         L.laplex_layer_norm.argtypes = [_P, _I, _C, _I, _I, _P, _P, _F, _P, _I, _P, _P, _P]
         L.laplex_layer_norm_workspace_bytes.argtypes = [_I, _I, ctypes.POINTER(_Z)]
         L.laplex_layer_norm_backward.argtypes = [_P, _I, _P, _I, _C, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P, _Z, _P]
@@ -524,6 +530,73 @@ def laplex_logprob_backward(y, targets, lse, entropy, glogp, gentropy, glse, gy,
     f = lambda x: _whole(x, (t,), torch.float32)
     _check(lib().laplex_logprob_backward(_ptr(y), _ld(y), _same_type(y, gy), k, t, _whole(targets, (t,), torch.int64), tau, f(lse), f(entropy),
                                          f(glogp), f(gentropy), f(glse), _ptr(gy), _ld(gy), _stream(stream)))
+
+
+def laplex_delta_attention_workspace_bytes(dtype, tokens: int, sequences: int, heads: int, key_heads: int, dk: int, dv: int,
+                                           training: bool = False) -> int:
+    out = _Z(0)
+    _check(lib().laplex_delta_attention_workspace_bytes(_type(dtype), tokens, sequences, heads, key_heads, dk, dv, int(training), ctypes.byref(out)))
+    return out.value
+
+
+def _numbers(t, shape):
+    """(address, row stride) of fp32 numbers (tokens, heads) whose rows are contiguous."""
+    import torch
+    if t is None:
+        return None, 0
+    assert t.shape == shape, f"shape {tuple(t.shape)}, not {tuple(shape)}"
+    assert t.dtype == torch.float32, f"type {t.dtype}, not {torch.float32}"
+    n, h = shape
+    assert h <= 1 or n == 0 or t.stride(1) == 1, "a token's numbers must be contiguous"
+    return t.data_ptr(), t.stride(0) if n > 1 else max(h, 1)
+
+
+def _each(lengths, sequences):
+    import torch
+    return _whole(lengths, (sequences,), torch.int64)
+
+
+def laplex_delta_attention(q, k, v, rates, beta, y, ws, scale: float = 1.0, sequences: int = 1, starts=None, lengths=None, state_in=None,
+                           state_out=None, flags: int = 0, stream=None) -> None:
+    """y (tokens, heads, dv) <- linear attention by the gated delta rule of q, k (tokens, key_heads, dk) and v with the decays exp(-rates) and the
+    weights beta, both (tokens, heads) fp32.  Sequences and states as for laplex_decay_attention; of sequence b the first lengths[b] tokens are read."""
+    import torch
+    n, kh, dk = q.shape
+    h, dv = v.shape[1:]
+    b, at = _sequences(sequences, starts)
+    state = (b, h, dk, dv)
+    _check(lib().laplex_delta_attention(
+        _ptr(q), _ld_tokens(q, (n, kh, dk)), _ptr(k), _ld_tokens(k, (n, kh, dk)), _ptr(v), _ld_tokens(v, (n, h, dv)), _same_type(q, k, v, y),
+        n, b, at, _each(lengths, b), h, kh, dk, dv, *_numbers(rates, (n, h)), *_numbers(beta, (n, h)), scale, _whole(state_in, state, torch.float32),
+        _ptr(y), _ld_tokens(y, (n, h, dv)), _whole(state_out, state, torch.float32), _ptr(ws), 0 if ws is None else ws.numel(), flags, _stream(stream)))
+
+
+def laplex_delta_attention_backward(q, k, v, rates, beta, gy, gq, gk, gv, grates, gbeta, ws, scale: float = 1.0, sequences: int = 1, starts=None,
+                                    lengths=None, state_in=None, gstate_out=None, gstate_in=None, flags: int = 0, stream=None) -> None:
+    """gq, gk, gv, grates, gbeta, gstate_in (any may be None) <- gradients of sum(gy * y) + sum(gstate_out * state_out)."""
+    import torch
+    n, kh, dk = q.shape
+    h, dv = v.shape[1:]
+    b, at = _sequences(sequences, starts)
+    state = (b, h, dk, dv)
+    _check(lib().laplex_delta_attention_backward(
+        _ptr(q), _ld_tokens(q, (n, kh, dk)), _ptr(k), _ld_tokens(k, (n, kh, dk)), _ptr(v), _ld_tokens(v, (n, h, dv)),
+        _same_type(q, k, v, gy, gq, gk, gv), n, b, at, _each(lengths, b), h, kh, dk, dv, *_numbers(rates, (n, h)), *_numbers(beta, (n, h)), scale,
+        _whole(state_in, state, torch.float32), _ptr(gy), _ld_tokens(gy, (n, h, dv)), _whole(gstate_out, state, torch.float32),
+        _ptr(gq), _ld_tokens(gq, (n, kh, dk)), _ptr(gk), _ld_tokens(gk, (n, kh, dk)), _ptr(gv), _ld_tokens(gv, (n, h, dv)),
+        *_numbers(grates, (n, h)), *_numbers(gbeta, (n, h)), _whole(gstate_in, state, torch.float32), _ptr(ws), 0 if ws is None else ws.numel(), flags,
+        _stream(stream)))
+
+
+def laplex_delta_attention_step(q, k, v, rates, beta, state, y, scale: float = 1.0, stream=None) -> None:
+    """One token of every sequence: state (sequences, heads, dk, dv) is updated in place, y (sequences, heads, dv) written."""
+    import torch
+    b, kh, dk = q.shape
+    h, dv = v.shape[1:]
+    _check(lib().laplex_delta_attention_step(
+        _ptr(q), _ld_tokens(q, (b, kh, dk)), _ptr(k), _ld_tokens(k, (b, kh, dk)), _ptr(v), _ld_tokens(v, (b, h, dv)), _same_type(q, k, v, y),
+        b, h, kh, dk, dv, *_numbers(rates, (b, h)), *_numbers(beta, (b, h)), scale, _whole(state, (b, h, dk, dv), torch.float32),
+        _ptr(y), _ld_tokens(y, (b, h, dv)), _stream(stream)))
 
 
 def _rows(x):

@@ -66,6 +66,18 @@ int check_norm_sizes(int64_t rows, int64_t width)
     return rows < 0 || rows > LAPLEX_NORM_MAX_ROWS || width < 1 || width > LAPLEX_NORM_MAX_WIDTH ? LAPLEX_ERR_SIZE : LAPLEX_OK;
 }
 
+// what the calls of the delta rule have in common
+struct DeltaSizes { int64_t tokens, sequences, heads, key_heads, dk, dv; };
+
+int check_delta_sizes(int type, const DeltaSizes& s, bool equal)
+{
+    LAPLEX_CHECK(check_attention_sizes(type, s.tokens, s.sequences, s.heads, s.dk, s.dv, equal));
+    return s.key_heads < 0 || (s.heads > 0 && (s.key_heads == 0 || s.heads % s.key_heads != 0)) ? LAPLEX_ERR_SIZE : LAPLEX_OK;
+}
+
+// float rows [tokens][heads]
+int check_numbers(const float* p, const DeltaSizes& s, int64_t ld, bool required) { return check_rows(p, LAPLEX_F32, s.tokens, s.heads, ld, required); }
+
 bool positive(float v) { return v > 0.0f && std::isfinite(v); }
 
 }  // namespace
@@ -227,6 +239,110 @@ int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64
     A.heads = (int)heads; A.dk = (int)dk; A.dv = (int)dv; A.rates = rates; A.scale = scale; A.state = state;
     A.bf16 = type == LAPLEX_BF16;
     LAPLEX_HIP(launch_attention_step(A, stream));
+    return LAPLEX_OK;
+}
+
+int laplex_delta_attention_workspace_bytes(int type, int64_t tokens, int64_t sequences, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv, int training,
+                                           size_t* out)
+{
+    if (!out) return LAPLEX_ERR_NULL;
+    LAPLEX_CHECK(check_delta_sizes(type, {tokens, sequences, heads, key_heads, dk, dv}, false));
+    *out = delta_workspace(type == LAPLEX_BF16, tokens, sequences, (int)heads, (int)dk, (int)dv, training != 0);
+    return LAPLEX_OK;
+}
+
+int laplex_delta_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                           int64_t tokens, int64_t sequences, const int64_t* starts, const int64_t* lengths, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv,
+                           const float* rates, int64_t ldr, const float* beta, int64_t ldb, float scale, const float* state_in, void* y, int64_t ldy, float* state_out,
+                           void* ws, size_t ws_bytes, uint32_t flags, laplex_stream_t stream)
+{
+    const DeltaSizes s{tokens, sequences, heads, key_heads, dk, dv};
+    LAPLEX_CHECK(check_delta_sizes(type, s, starts == nullptr));
+    if (flags & ~LAPLEX_SAVE_SCANS) return LAPLEX_ERR_FLAGS;
+    if (!positive(scale)) return LAPLEX_ERR_VALUE;
+    LAPLEX_CHECK(check_rows(q, type, tokens, key_heads * dk, ldq, true));
+    LAPLEX_CHECK(check_rows(k, type, tokens, key_heads * dk, ldk, true));
+    LAPLEX_CHECK(check_rows(v, type, tokens, heads * dv, ldv, true));
+    LAPLEX_CHECK(check_rows(y, type, tokens, heads * dv, ldy, true));
+    LAPLEX_CHECK(check_array(starts, sequences, 8, false));
+    LAPLEX_CHECK(check_array(lengths, sequences, 8, false));
+    LAPLEX_CHECK(check_numbers(rates, s, ldr, true));
+    LAPLEX_CHECK(check_numbers(beta, s, ldb, true));
+    LAPLEX_CHECK(check_array(state_in, sequences * heads, 4, false));
+    LAPLEX_CHECK(check_array(state_out, sequences * heads, 4, false));
+    if (sequences == 0 || heads == 0 || (tokens == 0 && !state_out)) return LAPLEX_OK;
+    const bool save = (flags & LAPLEX_SAVE_SCANS) != 0;
+    LAPLEX_CHECK(check_ws(ws, ws_bytes, delta_workspace(type == LAPLEX_BF16, tokens, sequences, (int)heads, (int)dk, (int)dv, save)));
+    DeltaArgs A{};
+    A.q = q; A.ldq = ldq; A.k = k; A.ldk = ldk; A.v = v; A.ldv = ldv; A.y = y; A.ldy = ldy; A.bf16 = type == LAPLEX_BF16;
+    A.tokens = tokens; A.sequences = sequences; A.starts = starts; A.lengths = lengths;
+    A.heads = (int)heads; A.key_heads = (int)key_heads; A.dk = (int)dk; A.dv = (int)dv;
+    A.rates = rates; A.ldr = ldr; A.beta = beta; A.ldb = ldb; A.scale = scale; A.state_in = state_in; A.state_out = state_out;
+    A.forward = true; A.saved = save; A.ws = static_cast<char*>(ws);
+    LAPLEX_HIP(launch_delta(A, stream));
+    return LAPLEX_OK;
+}
+
+int laplex_delta_attention_backward(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                                    int64_t tokens, int64_t sequences, const int64_t* starts, const int64_t* lengths, int64_t heads, int64_t key_heads, int64_t dk,
+                                    int64_t dv, const float* rates, int64_t ldr, const float* beta, int64_t ldb, float scale, const float* state_in,
+                                    const void* gy, int64_t ldgy, const float* gstate_out, void* gq, int64_t ldgq, void* gk, int64_t ldgk, void* gv, int64_t ldgv,
+                                    float* grates, int64_t ldgr, float* gbeta, int64_t ldgb, float* gstate_in, void* ws, size_t ws_bytes, uint32_t flags,
+                                    laplex_stream_t stream)
+{
+    const DeltaSizes s{tokens, sequences, heads, key_heads, dk, dv};
+    LAPLEX_CHECK(check_delta_sizes(type, s, starts == nullptr));
+    if (flags & ~LAPLEX_SAVE_SCANS) return LAPLEX_ERR_FLAGS;
+    if (!positive(scale)) return LAPLEX_ERR_VALUE;
+    LAPLEX_CHECK(check_rows(q, type, tokens, key_heads * dk, ldq, true));
+    LAPLEX_CHECK(check_rows(k, type, tokens, key_heads * dk, ldk, true));
+    LAPLEX_CHECK(check_rows(v, type, tokens, heads * dv, ldv, true));
+    LAPLEX_CHECK(check_rows(gy, type, tokens, heads * dv, ldgy, true));
+    LAPLEX_CHECK(check_rows(gq, type, tokens, key_heads * dk, ldgq, false));
+    LAPLEX_CHECK(check_rows(gk, type, tokens, key_heads * dk, ldgk, false));
+    LAPLEX_CHECK(check_rows(gv, type, tokens, heads * dv, ldgv, false));
+    LAPLEX_CHECK(check_array(starts, sequences, 8, false));
+    LAPLEX_CHECK(check_array(lengths, sequences, 8, false));
+    LAPLEX_CHECK(check_numbers(rates, s, ldr, true));
+    LAPLEX_CHECK(check_numbers(beta, s, ldb, true));
+    LAPLEX_CHECK(check_numbers(grates, s, ldgr, false));
+    LAPLEX_CHECK(check_numbers(gbeta, s, ldgb, false));
+    LAPLEX_CHECK(check_array(state_in, sequences * heads, 4, false));
+    LAPLEX_CHECK(check_array(gstate_out, sequences * heads, 4, false));
+    LAPLEX_CHECK(check_array(gstate_in, sequences * heads, 4, false));
+    if (sequences == 0 || heads == 0 || (tokens == 0 && !gstate_in) || (!gq && !gk && !gv && !grates && !gbeta && !gstate_in)) return LAPLEX_OK;
+    LAPLEX_CHECK(check_ws(ws, ws_bytes, delta_workspace(type == LAPLEX_BF16, tokens, sequences, (int)heads, (int)dk, (int)dv, true)));
+    DeltaArgs A{};
+    A.q = q; A.ldq = ldq; A.k = k; A.ldk = ldk; A.v = v; A.ldv = ldv; A.gy = gy; A.ldgy = ldgy; A.bf16 = type == LAPLEX_BF16;
+    A.gq = gq; A.ldgq = ldgq; A.gk = gk; A.ldgk = ldgk; A.gv = gv; A.ldgv = ldgv; A.grates = grates; A.ldgr = ldgr; A.gbeta = gbeta; A.ldgb = ldgb;
+    A.tokens = tokens; A.sequences = sequences; A.starts = starts; A.lengths = lengths;
+    A.heads = (int)heads; A.key_heads = (int)key_heads; A.dk = (int)dk; A.dv = (int)dv;
+    A.rates = rates; A.ldr = ldr; A.beta = beta; A.ldb = ldb; A.scale = scale; A.state_in = state_in; A.gstate_out = gstate_out; A.gstate_in = gstate_in;
+    A.saved = (flags & LAPLEX_SAVE_SCANS) != 0; A.ws = static_cast<char*>(ws);
+    LAPLEX_HIP(launch_delta(A, stream));
+    return LAPLEX_OK;
+}
+
+int laplex_delta_attention_step(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
+                                int64_t sequences, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv, const float* rates, int64_t ldr, const float* beta,
+                                int64_t ldb, float scale, float* state, void* y, int64_t ldy, laplex_stream_t stream)
+{
+    const DeltaSizes s{sequences, sequences, heads, key_heads, dk, dv};
+    LAPLEX_CHECK(check_delta_sizes(type, s, true));
+    if (!positive(scale)) return LAPLEX_ERR_VALUE;
+    LAPLEX_CHECK(check_rows(q, type, sequences, key_heads * dk, ldq, true));
+    LAPLEX_CHECK(check_rows(k, type, sequences, key_heads * dk, ldk, true));
+    LAPLEX_CHECK(check_rows(v, type, sequences, heads * dv, ldv, true));
+    LAPLEX_CHECK(check_rows(y, type, sequences, heads * dv, ldy, true));
+    LAPLEX_CHECK(check_numbers(rates, s, ldr, true));
+    LAPLEX_CHECK(check_numbers(beta, s, ldb, true));
+    LAPLEX_CHECK(check_array(state, sequences * heads, 4, true));
+    if (sequences == 0 || heads == 0) return LAPLEX_OK;
+    DeltaArgs A{};
+    A.q = q; A.ldq = ldq; A.k = k; A.ldk = ldk; A.v = v; A.ldv = ldv; A.y = y; A.ldy = ldy; A.bf16 = type == LAPLEX_BF16;
+    A.tokens = A.sequences = sequences; A.heads = (int)heads; A.key_heads = (int)key_heads; A.dk = (int)dk; A.dv = (int)dv;
+    A.rates = rates; A.ldr = ldr; A.beta = beta; A.ldb = ldb; A.scale = scale; A.state_in = A.state_out = state; A.forward = true;
+    LAPLEX_HIP(launch_delta_tokens(A, stream));
     return LAPLEX_OK;
 }
 

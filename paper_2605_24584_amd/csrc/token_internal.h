@@ -1,5 +1,5 @@
 // Internal declarations of the operators for token models: rotary positions, attention with a decay for each head, log
-// probabilities, layer norm, verification of drafts (rotary_kernels.hip, attention_kernels.hip, logprob_kernels.hip, norm_kernels.hip, verify_kernels.hip; host
+// probabilities, the gated delta rule, layer norm, verification of drafts (rotary_kernels.hip, attention_kernels.hip, logprob_kernels.hip, delta_kernels.hip, norm_kernels.hip, verify_kernels.hip; host
 // side in token_api.hip).
 #pragma once
 
@@ -78,6 +78,33 @@ struct AttentionStepArgs {
     bool bf16;
 };
 hipError_t launch_attention_step(const AttentionStepArgs& A, hipStream_t st);
+
+// ----------------------------------------------------------------------------
+// Attention by the gated delta rule.
+// ----------------------------------------------------------------------------
+struct DeltaArgs {
+    const void *q, *k, *v, *gy;
+    void *y, *gq, *gk, *gv;          // gq, gk, gv: any may be null
+    int64_t ldq, ldk, ldv, ldy, ldgy, ldgq, ldgk, ldgv;
+    const float *rates, *beta;       // [tokens][heads], rows ldr and ldb apart
+    float *grates, *gbeta;           // the same, either may be null
+    int64_t ldr, ldb, ldgr, ldgb;
+    int64_t tokens, sequences;
+    const int64_t *starts, *lengths; // either may be null
+    int heads, key_heads, dk, dv;
+    float scale;
+    const float *state_in, *gstate_out;      // [sequences][heads][dk][dv], any of the four may be null
+    float *state_out, *gstate_in;
+    bool bf16, forward, saved;       // saved: the forward call leaves, and the backward call finds, what the gradients need
+    char* ws;
+    // filled in by launch_delta
+    int slices, wide;                // workgroups side by side over the columns; a bit each for q, k, v, y, gy, gq, gk: four numbers at a time
+    int64_t per_sequence, chunks;    // chunks of a sequence (equal lengths), of all, at most
+    float *maps, *states_out, *u_out, *gstates, *r_out;
+};
+size_t delta_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv, bool training);
+hipError_t launch_delta(const DeltaArgs& A, hipStream_t st);
+hipError_t launch_delta_tokens(const DeltaArgs& A, hipStream_t st);      // forward, for sequences of a few tokens
 
 // ----------------------------------------------------------------------------
 // Log probabilities over logits y[k][batch].
