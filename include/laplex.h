@@ -484,7 +484,7 @@ int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64
  */
 int laplex_delta_attention_workspace_bytes(int type, int64_t tokens, int64_t sequences, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv,
                                            int training /* 0: the forward call without LAPLEX_SAVE_SCANS; else all calls */, size_t* out /* host */);
-/* Enough for up to so many tokens and sequences.  It grows with tokens + 64 sequences: about 0.18 KB, and for training 3.2 KB, for each of them and each head of 128. */
+/* Enough for up to so many tokens and sequences.  It grows with tokens + 64 sequences: about 0.4 KB, and for training 3.5 KB, for each of them and each head of 128. */
 
 int laplex_delta_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int type,
                            int64_t tokens, int64_t sequences, const int64_t* starts, const int64_t* lengths, int64_t heads, int64_t key_heads, int64_t dk, int64_t dv,

@@ -47,34 +47,78 @@ __device__ __forceinline__ int64_t count_of(const DeltaArgs& A, int64_t b, int64
     return n < 0 ? 0 : n < count ? n : count;
 }
 
-template <int C>
-__device__ __forceinline__ int64_t first_chunk(const DeltaArgs& A, int64_t b, int64_t begin)
+// Sequences are cut into units of so many tokens (chunks, or stretches of chunks): sequence b has those from first_unit(b) on, at least as many as its rows need.
+__device__ __forceinline__ int64_t first_unit(const DeltaArgs& A, int64_t b, int64_t begin, int64_t size, int64_t per_sequence)
 {
-    return A.starts ? begin / C + b : b * A.per_sequence;
+    return A.starts ? begin / size + b : b * per_sequence;
 }
 
-// The chunk with this number: its first row and how many rows it has (0: there is none).  By a wavefront.
 template <int C>
-__device__ __forceinline__ void find_chunk(const DeltaArgs& A, int64_t chunk, int64_t& row, int& valid)
+__device__ __forceinline__ int64_t first_chunk(const DeltaArgs& A, int64_t b, int64_t begin) { return first_unit(A, b, begin, C, A.per_sequence); }
+
+// The unit with this number: its sequence and its number there.  By a wavefront.
+struct Unit { int64_t b, index, begin, count; };      // begin, count: the sequence's rows
+__device__ __forceinline__ Unit find_unit(const DeltaArgs& A, int64_t unit, int64_t size, int64_t per_sequence)
 {
     int64_t lo = 0;
     if (A.starts) {
-        // the last sequence whose first chunk is at most this one: 64 candidates at a time
+        // the last sequence whose first unit is at most this one: 64 candidates at a time
         int64_t hi = A.sequences;
         const int lane = threadIdx.x & 63;
         while (hi - lo > 1) {
             const int64_t step = (hi - lo + 63) / 64, c = lo + lane * step;
-            const uint64_t votes = __ballot(c < hi && first_chunk<C>(A, c, start_of(A, c)) <= chunk);
+            const uint64_t votes = __ballot(c < hi && first_unit(A, c, start_of(A, c), size, per_sequence) <= unit);
             const int at = votes ? 63 - __builtin_clzll(votes) : 0;
             lo += at * step;
             hi = lo + step < hi ? lo + step : hi;
         }
     } else {
-        lo = chunk / A.per_sequence;
+        lo = unit / per_sequence;
     }
-    const int64_t begin = start_of(A, lo), count = count_of(A, lo, begin), at = (chunk - first_chunk<C>(A, lo, begin)) * C;
-    row = begin + at;
-    valid = at >= 0 && at < count ? (count - at < C ? (int)(count - at) : C) : 0;
+    Unit u;
+    u.b = lo;
+    u.begin = start_of(A, lo);
+    u.count = count_of(A, lo, u.begin);
+    u.index = unit - first_unit(A, lo, u.begin, size, per_sequence);
+    return u;
+}
+
+// The chunk with this number: its first row and how many rows it has (0: there is none).
+template <int C>
+__device__ __forceinline__ void find_chunk(const DeltaArgs& A, int64_t chunk, int64_t& row, int& valid)
+{
+    const Unit u = find_unit(A, chunk, C, A.per_sequence);
+    const int64_t at = u.index * C;
+    row = u.begin + at;
+    valid = at >= 0 && at < u.count ? (u.count - at < C ? (int)(u.count - at) : C) : 0;
+}
+
+// Of sequences with several stretches each has a place in the workspace.  They are numbered like the stretches, but for b, where no more than
+// begin / (stretch + 1) sequences before this one can have several: however many short sequences are packed, there are at most two places for `stretch` tokens.
+__device__ __forceinline__ int64_t first_place(const DeltaArgs& A, int64_t b, int64_t begin)
+{
+    if (!A.starts) return b * A.stretches;
+    const int64_t several = begin / (A.stretch + 1);
+    return begin / A.stretch + (b < several ? b : several);
+}
+
+// The stretch with this number, [lo, hi) of its sequence's tokens.
+struct Stretch {
+    int64_t b, begin, lo, hi, index, place;
+    bool there, last, several;        // several: its sequence has more than one
+};
+__device__ __forceinline__ Stretch find_stretch(const DeltaArgs& A, int64_t slot)
+{
+    const Unit u = find_unit(A, slot, A.stretch, A.stretches);
+    Stretch s;
+    s.b = u.b; s.begin = u.begin; s.index = u.index;
+    s.lo = u.index * A.stretch;
+    s.there = u.index >= 0 && (s.lo < u.count || u.index == 0);
+    s.hi = s.lo + A.stretch < u.count ? s.lo + A.stretch : u.count;
+    s.last = s.hi == u.count;
+    s.several = u.count > A.stretch;
+    s.place = first_place(A, s.b, s.begin) + s.index;
+    return s;
 }
 
 // ----------------------------------------------------------------------------
@@ -89,9 +133,9 @@ struct Sizes {
     static constexpr int kBytesRows = C * ROW * 16, kBytesTurned = DK * SEQ * 16, kBytesMap = C * SEQ * 16;
     static constexpr int PARTS = sizeof(T) == 2 ? 3 : 1, SOME = sizeof(T) == 2 ? 2 : 1;                    // of an fp32 number: all 24 bits, 16
     static constexpr int TILES = CT * (CT + 1) / 2;
-    // numbers of a chunk and head: T (tiles on and below the diagonal, rows of 16), then what follows
-    static constexpr int kT = TILES * 256;
-    static constexpr int kBeta = kT, kGamma = kT + C, kTail = kT + 2 * C, kHigh = kT + 3 * C, kLow = kT + 4 * C, kWhole = kT + 5 * C, kBad = kWhole + 2, kNumbers = kT + 5 * C + 4;
+    // numbers of a chunk and head: T and scale P (tiles on and below the diagonal, rows of 16), then what follows
+    static constexpr int kP = TILES * 256, kBeta = 2 * kP, kGamma = kBeta + C, kTail = kGamma + C, kHigh = kTail + C, kLow = kHigh + C, kWhole = kLow + C, kBad = kWhole + 2,
+                         kNumbers = kWhole + 4;
 };
 
 __device__ __forceinline__ int tile_at(int i, int j) { return i * (i + 1) / 2 + j; }
@@ -176,14 +220,19 @@ __device__ __forceinline__ void put_parts(char* at, int size, f32x4 v)
     }
 }
 
+// How a matrix is read: kSome a number at a time, kWide four at a time, kWhole so where all of them exist.
+enum { kSome, kWide, kWhole };
+__device__ __forceinline__ int how(bool wide, bool whole) { return !wide ? kSome : whole ? kWhole : kWide; }
+
 template <typename T>
 __device__ __forceinline__ void put_number(char* at, T v) { *reinterpret_cast<T*>(at) = v; }
 
-// A patch of R rows of four numbers, whatever their alignment; zeros in the place of those that do not exist.
+// A patch of R rows of four numbers, whatever their alignment; others in the place of those that do not exist (keep_patch makes zeros of them).
 template <typename T>
-__device__ __forceinline__ void load_patch(Patch<T>& p, const T* base, int64_t stride, int first, int valid, int at, int width, bool wide)
+__device__ __forceinline__ void load_patch(Patch<T>& p, const T* base, int64_t stride, int first, int valid, int at, int width, int how)
 {
-    if (wide) load_wide<T, true>(p, base, stride, first, valid, at, width);
+    if (how == kWhole) load_wide<T, false>(p, base, stride, first, valid, at, width);
+    else if (how == kWide) load_wide<T, true>(p, base, stride, first, valid, at, width);
     else load_some(p, base, stride, first, valid, at, width);
 }
 
@@ -226,7 +275,7 @@ k_delta_prepare(DeltaArgs A)
 {
     typedef Sizes<T, DK> Z;
     constexpr int C = Z::C, CT = Z::CT, R = Z::R, WAVES = kPrepareThreads / 64, PAD = C + 4;
-    __shared__ __attribute__((aligned(16))) char Ks[Z::kBytesRows];
+    __shared__ __attribute__((aligned(16))) char Ks[Z::kBytesRows], Qs[Z::kBytesRows];
     __shared__ __attribute__((aligned(16))) float map[C * PAD], diagonal[CT][16][20];
     __shared__ double G[C];
     __shared__ float beta[C];
@@ -243,11 +292,15 @@ k_delta_prepare(DeltaArgs A)
     __syncthreads();
     const T* const k = static_cast<const T*>(A.k) + row * A.ldk + (int64_t)kh * A.dk;
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;
-    const bool wide = (A.wide & 2) && A.ldk < near;
+    const bool wide = (A.wide & 2) && A.ldk < near, wide_q = (A.wide & 1) && A.ldq < near;
+    const T* const q = static_cast<const T*>(A.q) + row * A.ldq + (int64_t)kh * A.dk;
     for (int p = x; p < (C / R) * (DK / 4); p += kPrepareThreads) {
         const int piece = p % (DK / 4), first = (p / (DK / 4)) * R;
-        Patch<T> patch;
+        Patch<T> patch, query;
         load_patch(patch, k, A.ldk, first, valid, piece * 4, A.dk, wide);
+        load_patch(query, q, A.ldq, first, valid, piece * 4, A.dk, wide_q);
+        keep_patch(query, first, valid, piece * 4, A.dk);
+        put_rows<Z::ROW>(Qs, query, first, piece);
         keep_patch(patch, first, valid, piece * 4, A.dk);
         if (!finite_patch(patch)) {
             atomicMin(&odd_key, first + odd_row(patch));
@@ -256,19 +309,23 @@ k_delta_prepare(DeltaArgs A)
         put_rows<Z::ROW>(Ks, patch, first, piece);
     }
     __syncthreads();
-    // k_i . k_j: a lane holds rows 4 g .. + 3 and column r16 of a tile
+    // k_i . k_j and q_i . k_j: a lane holds rows 4 g .. + 3 and column r16 of a tile
     constexpr int NT = (Z::TILES + WAVES - 1) / WAVES;
-    f32x4 kk[NT];
+    f32x4 kk[NT], qk[NT];
     const Reader<Z::ROW> rows(r16, g);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int tile = n * WAVES + wave;
         int it = 0, jt = tile;
         while (jt > it) { jt -= it + 1; ++it; }
-        kk[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        kk[n] = qk[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         if (it < CT)
 #pragma unroll
-            for (int m = 0; m < Z::KD; ++m) kk[n] = mma(get<T>(Ks, rows.at(it, m)), get<T>(Ks, rows.at(jt, m)), kk[n]);
+            for (int m = 0; m < Z::KD; ++m) {
+                const typename Num<T>::frag kf = get<T>(Ks, rows.at(jt, m));
+                kk[n] = mma(get<T>(Ks, rows.at(it, m)), kf, kk[n]);
+                qk[n] = mma(get<T>(Qs, rows.at(it, m)), kf, qk[n]);
+            }
     }
     for (int e = 0; e < group; ++e) {
         const int h = kh * group + e;
@@ -320,7 +377,9 @@ k_delta_prepare(DeltaArgs A)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = 16 * it + 4 * g + r, j = 16 * jt + r16;
-                    map[i * PAD + j] = j < i ? beta[i] * expf((float)(G[i] - G[j])) * kk[n][r] : 0.0f;
+                    const float d = j <= i ? expf((float)(G[i] - G[j])) : 0.0f;
+                    map[i * PAD + j] = j < i ? beta[i] * d * kk[n][r] : 0.0f;
+                    out[Z::kP + tile * 256 + (4 * g + r) * 16 + r16] = j <= i ? A.scale * d * qk[n][r] : 0.0f;
                 }
         }
         __syncthreads();
@@ -372,24 +431,30 @@ struct WalkLds {
     static constexpr int kBytes = OUT ? kP + Z::SOME * Z::kBytesMap : kQueries;
 };
 
-template <typename T, int DK, int WAVES, bool OUT>
+enum { kResults, kKeep, kStates };      // with results; what gradients need alone; what a stretch does to the state, for the stretches behind it
+
+template <typename T, int DK, int WAVES, int MODE>
 __global__ void __launch_bounds__(64 * WAVES)
 k_delta_walk(DeltaArgs A)
 {
     typedef Sizes<T, DK> Z;
+    constexpr bool OUT = MODE == kResults, STATES = MODE == kStates;
     typedef WalkLds<T, DK, WAVES, OUT> L;
     typedef typename Num<T>::frag frag;
     typedef typename Num<T>::quad quad;
     constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, COLS = L::COLS;
     __shared__ __attribute__((aligned(16))) char lds[L::kBytes];
-    __shared__ float beta[C], gamma[C], tail[C], high[C], low[C], whole[2];
+    __shared__ float beta[C], gamma[C], tail[C], whole[2];
     __shared__ int odd[2];
     char *const Kt = lds + L::kTurned, *const Ts = lds + L::kMap, *const Ks = lds + L::kKeys, *const Vt = lds + L::kValues, *const Qs = lds + L::kQueries, *const Ps = lds + L::kP;
 
-    const int slice = blockIdx.x % A.slices, h = blockIdx.x / A.slices, col0 = slice * COLS;
-    const int64_t b = (int64_t)blockIdx.z * kRows + blockIdx.y;
-    if (b >= A.sequences || col0 >= A.dv) return;
-    const int64_t begin = start_of(A, b), count = count_of(A, b, begin), chunk0 = first_chunk<C>(A, b, begin);
+    // STATES: the first half of a head's workgroups sum up what the stretch adds to the state, the second half how it turns the state that enters it: the columns of a unit matrix
+    const int parts = STATES ? 2 : 1, slice = blockIdx.x % A.slices, part = blockIdx.x / A.slices % parts, h = blockIdx.x / (A.slices * parts), col0 = slice * COLS;
+    const int64_t slot = (int64_t)blockIdx.z * kRows + blockIdx.y;
+    if (slot >= A.slots || col0 >= (part ? A.dk : (A.dv + Z::K - 1) / Z::K * Z::K)) return;      // (k_delta_gradients reads whole fragments of columns)
+    const Stretch s = find_stretch(A, slot);
+    if (!s.there || (STATES && (!s.several || (s.last && !(part && A.training))))) return;
+    const int64_t b = s.b, begin = s.begin, count = s.hi, chunk0 = first_chunk<C>(A, b, begin);
     const int x = threadIdx.x, lane = x & 63, wave = __builtin_amdgcn_readfirstlane(x >> 6), r16 = lane & 15, g = lane >> 4;
     const int kh = h / (A.heads / A.key_heads), col = col0 + 16 * wave + r16;
     for (int i = x; i < Z::PARTS * Z::kBytesMap / 16; i += THREADS) reinterpret_cast<f32x4*>(Ts)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -399,13 +464,16 @@ k_delta_walk(DeltaArgs A)
 
     // the state: rows 16 t + 4 g .. + 3, column col
     f32x4 S[DT];
+    float* const entering = A.added + (s.place * A.heads + h) * (int64_t)DK * DK + col;      // (of several stretches the first one's, too: another workgroup may already write the last state in its place)
     const int64_t state_at = (b * A.heads + h) * (int64_t)A.dk * A.dv;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * t + 4 * g + r;
-            S[t][r] = A.state_in && row < A.dk && col < A.dv ? A.state_in[state_at + (int64_t)row * A.dv + col] : 0.0f;
+            if (STATES) S[t][r] = part && row == col ? 1.0f : 0.0f;
+            else if (s.several) S[t][r] = col < A.dv ? entering[row * DK] : 0.0f;
+            else S[t][r] = A.state_in && row < A.dk && col < A.dv ? A.state_in[state_at + (int64_t)row * A.dv + col] : 0.0f;
         }
 
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;
@@ -413,12 +481,13 @@ k_delta_walk(DeltaArgs A)
     constexpr int kRowPatches = (C / R) * (DK / 4), kColPatches = (C / R) * (COLS / 4);
     constexpr int NR = (kRowPatches + THREADS - 1) / THREADS, NV = (kColPatches + THREADS - 1) / THREADS, NM = (Z::TILES * 64 + THREADS - 1) / THREADS;
     Patch<T> pq[NR], pk[NR], pv[NV];
-    f32x4 pt[NM];
-    float pn[5], pw = 0.0f;
+    f32x4 pt[NM], pp[NM];
+    float pn[3], pw = 0.0f;
     int pb = C;
     const auto load = [&](int64_t at) {
         const int valid = (int)(count - at < C ? count - at : C);
         const int64_t row = begin + at;
+        const int hq = how(wq, valid == C && A.dk == DK), hk = how(wk, valid == C && A.dk == DK), hv = how(wv, valid == C && col0 + COLS <= A.dv);
         const T* const q = static_cast<const T*>(A.q) + row * A.ldq + (int64_t)kh * A.dk;
         const T* const k = static_cast<const T*>(A.k) + row * A.ldk + (int64_t)kh * A.dk;
         const T* const v = static_cast<const T*>(A.v) + row * A.ldv + (int64_t)h * A.dv;
@@ -427,33 +496,36 @@ k_delta_walk(DeltaArgs A)
         for (int i = 0; i < NR; ++i) {
             const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = (p % (DK / 4)) * 4;
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
-                if (OUT) load_patch(pq[i], q, A.ldq, first, valid, piece, A.dk, wq);
-                load_patch(pk[i], k, A.ldk, first, valid, piece, A.dk, wk);
+                if (OUT) load_patch(pq[i], q, A.ldq, first, valid, piece, A.dk, hq);
+                load_patch(pk[i], k, A.ldk, first, valid, piece, A.dk, hk);
             }
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int p = x + i * THREADS;
-            if (kColPatches % THREADS == 0 || p < kColPatches)
-                load_patch(pv[i], v, A.ldv, (p / (COLS / 4)) * R, valid, col0 + (p % (COLS / 4)) * 4, A.dv, wv);
+            if ((kColPatches % THREADS == 0 || p < kColPatches) && part == 0)
+                load_patch(pv[i], v, A.ldv, (p / (COLS / 4)) * R, valid, col0 + (p % (COLS / 4)) * 4, A.dv, hv);
         }
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
             const int p = x + i * THREADS;
-            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
+            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
+                pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
+                if (OUT) pp[i] = reinterpret_cast<const f32x4*>(numbers + Z::kP)[p];
+            }
         }
         if (x < C) {
 #pragma unroll
-            for (int i = 0; i < 5; ++i) pn[i] = numbers[Z::kBeta + i * C + x];
+            for (int i = 0; i < 3; ++i) pn[i] = numbers[Z::kBeta + i * C + x];
         }
         if (x < 2) pw = numbers[Z::kWhole + x];
         if (x == 0) pb = reinterpret_cast<const int*>(numbers)[Z::kBad];
     };
-    if (count > 0) load(0);
+    if (s.lo < count) load(s.lo);
     __syncthreads();
 
     int turn = 0;
-    for (int64_t at = 0; at < count; at += C, turn ^= 1) {
+    for (int64_t at = s.lo; at < count; at += C, turn ^= 1) {
         const int valid = (int)(count - at < C ? count - at : C);
         const int64_t row = begin + at, chunk = chunk0 + at / C;
 #pragma unroll
@@ -461,10 +533,10 @@ k_delta_walk(DeltaArgs A)
             const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = p % (DK / 4);
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
                 if (OUT) {
-                    keep_patch(pq[i], first, valid, piece * 4, A.dk);
+                    if (!(valid == C && A.dk == DK)) keep_patch(pq[i], first, valid, piece * 4, A.dk);
                     put_rows<ROW>(Qs, pq[i], first, piece);
                 }
-                keep_patch(pk[i], first, valid, piece * 4, A.dk);
+                if (!(valid == C && A.dk == DK)) keep_patch(pk[i], first, valid, piece * 4, A.dk);
                 if (!finite_patch(pk[i])) clean_patch(pk[i]);
                 put_rows<ROW>(Ks, pk[i], first, piece);
                 put_turned<T, SEQ>(Kt, pk[i], first, piece);
@@ -473,8 +545,8 @@ k_delta_walk(DeltaArgs A)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int p = x + i * THREADS, first = (p / (COLS / 4)) * R, piece = p % (COLS / 4);
-            if (kColPatches % THREADS == 0 || p < kColPatches) {
-                keep_patch(pv[i], first, valid, col0 + piece * 4, A.dv);
+            if ((kColPatches % THREADS == 0 || p < kColPatches) && part == 0) {
+                if (!(valid == C && col0 + COLS <= A.dv)) keep_patch(pv[i], first, valid, col0 + piece * 4, A.dv);
                 if (!finite_patch(pv[i])) {
                     atomicMin(&odd[turn], first + odd_row(pv[i]));
                     clean_patch(pv[i]);
@@ -489,42 +561,28 @@ k_delta_walk(DeltaArgs A)
                 const int tile = p >> 6;
                 int it = 0, jt = tile;
                 while (jt > it) { jt -= it + 1; ++it; }
-                put_parts<T, Z::PARTS>(Ts + quad_at<T, SEQ>(16 * it + ((p & 63) >> 2), 4 * jt + (p & 3)), Z::kBytesMap, pt[i]);
+                const int to = quad_at<T, SEQ>(16 * it + ((p & 63) >> 2), 4 * jt + (p & 3));
+                put_parts<T, Z::PARTS>(Ts + to, Z::kBytesMap, pt[i]);
+                if (OUT) put_parts<T, Z::SOME>(Ps + to, Z::kBytesMap, pp[i]);
             }
         }
-        if (x < C) { beta[x] = pn[0]; gamma[x] = pn[1]; tail[x] = pn[2]; high[x] = pn[3]; low[x] = pn[4]; }
+        if (x < C) { beta[x] = pn[0]; gamma[x] = pn[1]; tail[x] = pn[2]; }
         if (x < 2) whole[x] = pw;
         if (x == 0 && pb < C) atomicMin(&odd[turn], pb);
         if (at + C < count) load(at + C);
         __syncthreads();
 
         const int bad = odd[turn];                     // from this token on there is nothing but NaN
+        // (formed anew for each chunk: places kept from before the loop would fill the registers)
+        const int l = here(lane), r16 = l & 15, g = l >> 4;
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
-        if (A.states_out) {
+        if (!STATES && A.states_out) {
             float* const to = A.states_out + (chunk * A.heads + h) * (int64_t)DK * DK + col;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = S[t][r];
-        }
-        if (OUT) {
-            // P, tiles on and below the diagonal dealt to the wavefronts: a lane holds P[i][j .. j + 3]
-#pragma unroll
-            for (int n = 0; n < (Z::TILES + WAVES - 1) / WAVES; ++n) {
-                const int tile = n * WAVES + wave;
-                int it = 0, jt = tile;
-                while (jt > it) { jt -= it + 1; ++it; }
-                if (it < CT) {
-                    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int m = 0; m < KD; ++m) acc = mma(get<T>(Ks, rows.at(jt, m)), get<T>(Qs, rows.at(it, m)), acc);
-                    const int i = 16 * it + r16, j = 16 * jt + 4 * g;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[r] = j + r <= i ? acc[r] * decay_of(high[i], low[i], high[j + r], low[j + r]) : 0.0f;
-                    put_parts<T, Z::SOME>(Ps + quad_at<T, SEQ>(i, j >> 2), Z::kBytesMap, acc);
-                }
-            }
         }
         f32x4 U[CT], O[CT];
 #pragma unroll
@@ -532,6 +590,7 @@ k_delta_walk(DeltaArgs A)
         // K S and Q S: rows of tokens 16 t + 4 g .. + 3, column col, of the one, the other way round of the other
 #pragma unroll
         for (int m = 0; m < KD; ++m) {
+            if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(S, m, xs);
             frag sf[Z::PARTS];
@@ -550,22 +609,29 @@ k_delta_walk(DeltaArgs A)
         frag Rf[KC][Z::PARTS];
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            const quad v = *reinterpret_cast<const quad*>(Vt + quad_at<T, SEQ>(16 * wave + r16, 4 * t + g));
+            quad v;
+            if (STATES && part)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = (T)0.0f;
+            else
+                v = *reinterpret_cast<const quad*>(Vt + quad_at<T, SEQ>(16 * wave + r16, 4 * t + g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = 16 * t + 4 * g + r;
                 U[t][r] = beta[i] * ((float)v[r] - gamma[i] * U[t][r]);
             }
-            if (OUT) O[t] *= gamma[16 * t + r16];
+            if (OUT) O[t] *= A.scale * gamma[16 * t + r16];
         }
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
+            __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(U, m, xs);
             parts_of<T, Z::PARTS>(xs, Rf[m]);
         }
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
+            if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
             U[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int m = 0; m < KC; ++m)
@@ -576,7 +642,7 @@ k_delta_walk(DeltaArgs A)
                     U[t] = mma_parts<Z::PARTS>(tf, Rf[m], U[t]);
                 }
         }
-        if (A.u_out) {
+        if (!STATES && A.u_out) {
             float* const to = A.u_out + (chunk * A.heads + h) * (int64_t)C * DK + col;
 #pragma unroll
             for (int t = 0; t < CT; ++t)
@@ -584,9 +650,9 @@ k_delta_walk(DeltaArgs A)
                 for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = U[t][r];
         }
         if (OUT) {
-            __syncthreads();                           // P is there
 #pragma unroll
             for (int m = 0; m < KC; ++m) {
+                __builtin_amdgcn_sched_barrier(0);
                 float xs[Z::E];
                 numbers_of<T>(U, m, xs);
                 frag uf[Z::SOME];
@@ -608,7 +674,7 @@ k_delta_walk(DeltaArgs A)
                 if (i >= valid) continue;
                 quad w;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[r] = (T)(i < bad ? O[t][r] * A.scale : NAN);
+                for (int r = 0; r < 4; ++r) w[r] = (T)(i < bad ? O[t][r] : NAN);
                 T* const to = out + i * A.ldy + n;
                 if (wo) {
                     if (n < A.dv) *reinterpret_cast<quad*>(to) = w;
@@ -627,6 +693,7 @@ k_delta_walk(DeltaArgs A)
             for (int r = 0; r < 4; ++r) S[t][r] = bad < C ? NAN : fmaf(S[t][r], d, S[t][r] * rest);
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
+            __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(U, m, xs);
 #pragma unroll
@@ -639,7 +706,13 @@ k_delta_walk(DeltaArgs A)
         __syncthreads();                               // the tiles may be written again
         if (x == 0) odd[turn] = C;
     }
-    if (A.state_out)
+    if (STATES) {
+        float* const to = (part ? A.turned : A.added) + (s.place * A.heads + h) * (int64_t)DK * DK + col;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = S[t][r];
+    } else if (A.state_out && s.last)
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -656,11 +729,11 @@ template <typename T, int DK, int WAVES>
 struct BackLds {
     typedef Sizes<T, DK> Z;
     static constexpr int COLS = 16 * WAVES;
-    static constexpr int kKeysTurned = 0, kQueriesTurned = kKeysTurned + Z::kBytesTurned, kKeys = kQueriesTurned + Z::kBytesTurned, kQueries = kKeys + Z::kBytesRows;
-    static constexpr int kValues = kQueries + Z::kBytesRows, kMap = kValues + COLS * Z::SEQ * 16, kP = kMap + Z::PARTS * Z::kBytesMap, kBytes = kP + Z::PARTS * Z::kBytesMap;
+    static constexpr int kKeysTurned = 0, kQueriesTurned = kKeysTurned + Z::kBytesTurned, kKeys = kQueriesTurned + Z::kBytesTurned;
+    static constexpr int kValues = kKeys + Z::kBytesRows, kMap = kValues + COLS * Z::SEQ * 16, kP = kMap + Z::PARTS * Z::kBytesMap, kBytes = kP + Z::PARTS * Z::kBytesMap;
 };
 
-template <typename T, int DK, int WAVES>
+template <typename T, int DK, int WAVES, bool STATES>
 __global__ void __launch_bounds__(64 * WAVES)
 k_delta_back(DeltaArgs A)
 {
@@ -669,37 +742,43 @@ k_delta_back(DeltaArgs A)
     typedef typename Num<T>::frag frag;
     constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, COLS = L::COLS;
     __shared__ __attribute__((aligned(16))) char lds[L::kBytes];
-    __shared__ float beta[C], gamma[C], tail[C], high[C], low[C], whole[2];
-    char *const Kt = lds + L::kKeysTurned, *const Qt = lds + L::kQueriesTurned, *const Ks = lds + L::kKeys, *const Qs = lds + L::kQueries, *const Yt = lds + L::kValues,
+    __shared__ float beta[C], gamma[C], tail[C], whole[2];
+    char *const Kt = lds + L::kKeysTurned, *const Qt = lds + L::kQueriesTurned, *const Ks = lds + L::kKeys, *const Yt = lds + L::kValues,
          *const Ts = lds + L::kMap, *const Ps = lds + L::kP;
 
     const int slice = blockIdx.x % A.slices, h = blockIdx.x / A.slices, col0 = slice * COLS;
-    const int64_t b = (int64_t)blockIdx.z * kRows + blockIdx.y;
-    if (b >= A.sequences || col0 >= A.dv) return;
-    const int64_t begin = start_of(A, b), count = count_of(A, b, begin), chunk0 = first_chunk<C>(A, b, begin);
+    const int64_t slot = (int64_t)blockIdx.z * kRows + blockIdx.y;
+    if (slot >= A.slots || col0 >= (A.dv + Z::K - 1) / Z::K * Z::K) return;
+    const Stretch s = find_stretch(A, slot);
+    if (!s.there || (STATES && (!s.several || s.index == 0))) return;
+    const int64_t b = s.b, begin = s.begin, count = s.hi, chunk0 = first_chunk<C>(A, b, begin);
     const int x = threadIdx.x, lane = x & 63, wave = __builtin_amdgcn_readfirstlane(x >> 6), r16 = lane & 15, g = lane >> 4;
     const int kh = h / (A.heads / A.key_heads), col = col0 + 16 * wave + r16;
     for (int i = x; i < 2 * Z::PARTS * Z::kBytesMap / 16; i += THREADS) reinterpret_cast<f32x4*>(Ts)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     f32x4 S[DT];
+    float* const entering = A.added_back + (s.place * A.heads + h) * (int64_t)DK * DK + col;
     const int64_t state_at = (b * A.heads + h) * (int64_t)A.dk * A.dv;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * t + 4 * g + r;
-            S[t][r] = A.gstate_out && row < A.dk && col < A.dv ? A.gstate_out[state_at + (int64_t)row * A.dv + col] : 0.0f;
+            if (STATES) S[t][r] = 0.0f;
+            else if (s.several) S[t][r] = col < A.dv ? entering[row * DK] : 0.0f;
+            else S[t][r] = A.gstate_out && row < A.dk && col < A.dv ? A.gstate_out[state_at + (int64_t)row * A.dv + col] : 0.0f;
         }
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;
     const bool wq = (A.wide & 1) && A.ldq < near, wk = (A.wide & 2) && A.ldk < near, wy = (A.wide & 16) && A.ldgy < near;
     constexpr int kRowPatches = (C / R) * (DK / 4), kColPatches = (C / R) * (COLS / 4);
     constexpr int NR = (kRowPatches + THREADS - 1) / THREADS, NV = (kColPatches + THREADS - 1) / THREADS, NM = (Z::TILES * 64 + THREADS - 1) / THREADS;
     Patch<T> pq[NR], pk[NR], pv[NV];
-    f32x4 pt[NM];
-    float pn[5], pw = 0.0f;
+    f32x4 pt[NM], pp[NM];
+    float pn[3], pw = 0.0f;
     const auto load = [&](int64_t at) {
         const int valid = (int)(count - at < C ? count - at : C);
         const int64_t row = begin + at;
+        const int hq = how(wq, valid == C && A.dk == DK), hk = how(wk, valid == C && A.dk == DK), hy = how(wy, valid == C && col0 + COLS <= A.dv);
         const T* const q = static_cast<const T*>(A.q) + row * A.ldq + (int64_t)kh * A.dk;
         const T* const k = static_cast<const T*>(A.k) + row * A.ldk + (int64_t)kh * A.dk;
         const T* const gy = static_cast<const T*>(A.gy) + row * A.ldgy + (int64_t)h * A.dv;
@@ -708,40 +787,44 @@ k_delta_back(DeltaArgs A)
         for (int i = 0; i < NR; ++i) {
             const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = (p % (DK / 4)) * 4;
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
-                load_patch(pq[i], q, A.ldq, first, valid, piece, A.dk, wq);
-                load_patch(pk[i], k, A.ldk, first, valid, piece, A.dk, wk);
+                load_patch(pq[i], q, A.ldq, first, valid, piece, A.dk, hq);
+                load_patch(pk[i], k, A.ldk, first, valid, piece, A.dk, hk);
             }
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int p = x + i * THREADS;
             if (kColPatches % THREADS == 0 || p < kColPatches)
-                load_patch(pv[i], gy, A.ldgy, (p / (COLS / 4)) * R, valid, col0 + (p % (COLS / 4)) * 4, A.dv, wy);
+                load_patch(pv[i], gy, A.ldgy, (p / (COLS / 4)) * R, valid, col0 + (p % (COLS / 4)) * 4, A.dv, hy);
         }
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
             const int p = x + i * THREADS;
-            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
+            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
+                pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
+                pp[i] = reinterpret_cast<const f32x4*>(numbers + Z::kP)[p];
+            }
         }
         if (x < C) {
 #pragma unroll
-            for (int i = 0; i < 5; ++i) pn[i] = numbers[Z::kBeta + i * C + x];
+            for (int i = 0; i < 3; ++i) pn[i] = numbers[Z::kBeta + i * C + x];
         }
         if (x < 2) pw = numbers[Z::kWhole + x];
     };
-    const int64_t last = count > 0 ? (count - 1) / C * C : -1;
-    if (count > 0) load(last);
+    const int64_t last = count > s.lo ? s.lo + (count - 1 - s.lo) / C * C : -1;
+    if (last >= 0) load(last);
     __syncthreads();
-    for (int64_t at = last; at >= 0; at -= C) {
+    for (int64_t at = last; at >= s.lo; at -= C) {
         const int valid = (int)(count - at < C ? count - at : C);
         const int64_t chunk = chunk0 + at / C;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = p % (DK / 4);
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
-                keep_patch(pq[i], first, valid, piece * 4, A.dk);
-                keep_patch(pk[i], first, valid, piece * 4, A.dk);
-                put_rows<ROW>(Qs, pq[i], first, piece);
+                if (!(valid == C && A.dk == DK)) {
+                    keep_patch(pq[i], first, valid, piece * 4, A.dk);
+                    keep_patch(pk[i], first, valid, piece * 4, A.dk);
+                }
                 put_rows<ROW>(Ks, pk[i], first, piece);
                 put_turned<T, SEQ>(Qt, pq[i], first, piece);
                 put_turned<T, SEQ>(Kt, pk[i], first, piece);
@@ -751,11 +834,11 @@ k_delta_back(DeltaArgs A)
         for (int i = 0; i < NV; ++i) {
             const int p = x + i * THREADS, first = (p / (COLS / 4)) * R, piece = p % (COLS / 4);
             if (kColPatches % THREADS == 0 || p < kColPatches) {
-                keep_patch(pv[i], first, valid, col0 + piece * 4, A.dv);
+                if (!(valid == C && col0 + COLS <= A.dv)) keep_patch(pv[i], first, valid, col0 + piece * 4, A.dv);
                 put_turned<T, SEQ>(Yt, pv[i], first, piece);
             }
         }
-        // T turned: row j, tokens i along the slots
+        // T and P turned: row j, tokens i along the slots
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
             const int p = x + i * THREADS;
@@ -767,45 +850,35 @@ k_delta_back(DeltaArgs A)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     char* const to = Ts + quad_at<T, SEQ>(16 * jt + 4 * (p & 3) + e, token >> 2) + (token & 3) * (int)sizeof(T);
-                    float v = pt[i][e];
+                    float v = pt[i][e], w = pp[i][e];
 #pragma unroll
                     for (int part = 0; part < Z::PARTS; ++part) {
-                        const float up = sizeof(T) == 2 ? upper(v) : v;
+                        const float up = sizeof(T) == 2 ? upper(v) : v, wp = sizeof(T) == 2 ? upper(w) : w;
                         put_number<T>(to + part * Z::kBytesMap, (T)up);
+                        put_number<T>(to + (Ps - Ts) + part * Z::kBytesMap, (T)wp);
                         v -= up;
+                        w -= wp;
                     }
                 }
             }
         }
-        if (x < C) { beta[x] = pn[0]; gamma[x] = pn[1]; tail[x] = pn[2]; high[x] = pn[3]; low[x] = pn[4]; }
+        if (x < C) { beta[x] = pn[0]; gamma[x] = pn[1]; tail[x] = pn[2]; }
         if (x < 2) whole[x] = pw;
-        if (at >= C) load(at - C);
+        if (at - C >= s.lo) load(at - C);
         __syncthreads();
+        // (formed anew for each chunk: places kept from before the loop would fill the registers)
+        const int l = here(lane), r16 = l & 15, g = l >> 4;
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
         Reader<SEQ> values(r16, g);
         values.base += wave * 16 * SEQ * 16;
         values.low ^= ((2 * wave) & Reader<SEQ>::kMask) * 16;
-        float* const to_state = A.gstates + (chunk * A.heads + h) * (int64_t)DK * DK + col;
+        if (!STATES) {
+            float* const to = A.gstates + (chunk * A.heads + h) * (int64_t)DK * DK + col;
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+            for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) to_state[(16 * t + 4 * g + r) * DK] = S[t][r];
-        // P turned: row j, four tokens i
-#pragma unroll
-        for (int n = 0; n < (Z::TILES + WAVES - 1) / WAVES; ++n) {
-            const int tile = n * WAVES + wave;
-            int it = 0, jt = tile;
-            while (jt > it) { jt -= it + 1; ++it; }
-            if (it < CT) {
-                f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int m = 0; m < KD; ++m) acc = mma(get<T>(Qs, rows.at(it, m)), get<T>(Ks, rows.at(jt, m)), acc);
-                const int i = 16 * it + 4 * g, j = 16 * jt + r16;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[r] = j <= i + r ? acc[r] * A.scale * decay_of(high[i + r], low[i + r], high[j], low[j]) : 0.0f;
-                put_parts<T, Z::PARTS>(Ps + quad_at<T, SEQ>(j, i >> 2), Z::kBytesMap, acc);
-            }
+                for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = S[t][r];
         }
         // tail K G
         f32x4 U[CT];
@@ -813,6 +886,7 @@ k_delta_back(DeltaArgs A)
         for (int t = 0; t < CT; ++t) U[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int m = 0; m < KD; ++m) {
+            if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(S, m, xs);
             frag sf[Z::PARTS];
@@ -824,9 +898,9 @@ k_delta_back(DeltaArgs A)
         for (int t = 0; t < CT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) U[t][r] *= tail[16 * t + 4 * g + r];
-        __syncthreads();                               // P is there
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
+            __builtin_amdgcn_sched_barrier(0);
             const frag yf = get<T>(Yt, values.at(0, m));
 #pragma unroll
             for (int t = 0; t < CT; ++t)
@@ -838,12 +912,14 @@ k_delta_back(DeltaArgs A)
         frag Uf[KC][Z::PARTS];
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
+            __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(U, m, xs);
             parts_of<T, Z::PARTS>(xs, Uf[m]);
         }
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
+            if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
             U[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int m = 0; m < KC; ++m)
@@ -854,11 +930,13 @@ k_delta_back(DeltaArgs A)
                     U[t] = mma_parts<Z::PARTS>(tf, Uf[m], U[t]);
                 }
         }
-        float* const to_r = A.r_out + (chunk * A.heads + h) * (int64_t)C * DK + col;
+        if (!STATES) {
+            float* const to = A.r_out + (chunk * A.heads + h) * (int64_t)C * DK + col;
 #pragma unroll
-        for (int t = 0; t < CT; ++t)
+            for (int t = 0; t < CT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) to_r[(16 * t + 4 * g + r) * DK] = U[t][r];
+                for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = U[t][r];
+        }
         const float d = whole[0], rest = whole[1];
 #pragma unroll
         for (int t = 0; t < DT; ++t)
@@ -866,6 +944,7 @@ k_delta_back(DeltaArgs A)
             for (int r = 0; r < 4; ++r) S[t][r] = fmaf(S[t][r], d, S[t][r] * rest);
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
+            __builtin_amdgcn_sched_barrier(0);
             const frag yf = get<T>(Yt, values.at(0, m));
             float xs[Z::E], ys[Z::E];
             numbers_of<T>(U, m, xs);
@@ -886,7 +965,12 @@ k_delta_back(DeltaArgs A)
         }
         __syncthreads();
     }
-    if (A.gstate_in)
+    if (STATES) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) entering[(16 * t + 4 * g + r) * DK] = S[t][r];
+    } else if (A.gstate_in && s.index == 0)
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -897,13 +981,108 @@ k_delta_back(DeltaArgs A)
 }
 
 // ----------------------------------------------------------------------------
-// What is left of the gradients: a workgroup takes a chunk and a head of keys, a wavefront 16 numbers of a head of keys (or twice 16), and the heads of values
+// The states that enter the stretches of a sequence that has several, in the places of what the stretches add: S_(n+1) = turned_n S_n + added_n from state_in on, or, back,
+// G_(n-1) = turned_n^T G_n + added_n from gstate_out on.  A wavefront to 16 columns, on the fp32 matrix instructions whatever the type.
+// ----------------------------------------------------------------------------
+constexpr int kCarryWaves = 4;
+
+template <int DK, bool BACK>
+__global__ void __launch_bounds__(64 * kCarryWaves)
+k_delta_carry(DeltaArgs A)
+{
+    constexpr int DT = DK / 16, SLICES = (DT + kCarryWaves - 1) / kCarryWaves, THREADS = 64 * kCarryWaves, PAD = DK + 4;
+    constexpr int ROWS = DK > 192 ? 64 : DK > 128 ? 80 : DK, BLOCKS = (DK + ROWS - 1) / ROWS, N = (ROWS * DK / 4 + THREADS - 1) / THREADS;
+    __shared__ __attribute__((aligned(16))) float M[ROWS * PAD];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x / SLICES, col = ((blockIdx.x % SLICES) * kCarryWaves + wave) * 16 + r16;
+    const int64_t b = (int64_t)blockIdx.z * kRows + blockIdx.y;
+    if (b >= A.sequences) return;
+    const int64_t begin = start_of(A, b), count = count_of(A, b, begin);
+    if (count <= A.stretch || (int)(blockIdx.x % SLICES) * kCarryWaves * 16 >= A.dv) return;
+    const bool live = (col & ~15) < A.dv;
+    const int64_t stretches = (count + A.stretch - 1) / A.stretch, place = first_place(A, b, begin), step = (int64_t)A.heads * DK * DK;
+    const float* const given = BACK ? A.gstate_out : A.state_in;
+    float* const added = (BACK ? A.added_back : A.added) + (place * A.heads + h) * (int64_t)DK * DK;
+    const float* const turned = A.turned + (place * A.heads + h) * (int64_t)DK * DK;
+    f32x4 S[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * t + 4 * g + r;
+            S[t][r] = given && row < A.dk && col < A.dv ? given[(b * A.heads + h) * (int64_t)A.dk * A.dv + (int64_t)row * A.dv + col] : 0.0f;
+        }
+    // blocks of rows of `turned` go through LDS; the next one is on its way meanwhile
+    f32x4 ahead[N];
+    const auto ask = [&](int64_t n, int block) {
+        const f32x4* const from = reinterpret_cast<const f32x4*>(turned + n * step + block * ROWS * DK);
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            const int at = c * THREADS + threadIdx.x, row = at / (DK / 4), column = at % (DK / 4) * 4;
+            ahead[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // (no workgroup has written the columns behind dk)
+            if (at < ROWS * DK / 4 && block * ROWS + row < DK && column < (A.dk + 15) / 16 * 16) ahead[c] = from[at];
+        }
+    };
+    const auto number = [&](int64_t i) { return BACK ? stretches - 1 - i : i; };
+    ask(number(0), 0);
+    for (int64_t i = 0; i < stretches; ++i) {
+        const int64_t n = number(i);
+        float* const here = added + n * step + col;
+        const bool last = i + 1 == stretches;
+        f32x4 next[DT];
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) next[t][r] = live && !last ? here[(16 * t + 4 * g + r) * DK] : 0.0f;
+        if (live)
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) here[(16 * t + 4 * g + r) * DK] = S[t][r];
+        if (last) break;
+#pragma unroll
+        for (int block = 0; block < BLOCKS; ++block) {
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                const int at = c * THREADS + threadIdx.x, row = at / (DK / 4), column = at % (DK / 4) * 4;
+                if (at < ROWS * DK / 4) *reinterpret_cast<f32x4*>(&M[row * PAD + column]) = ahead[c];
+            }
+            __syncthreads();
+            if (block + 1 < BLOCKS) ask(n, block + 1);
+            else if (i + 2 < stretches) ask(number(i + 1), 0);
+            // rows of the block are results ahead, what is summed over back
+#pragma unroll
+            for (int a = 0; a < ROWS / 16; ++a) {
+                const int mine = block * (ROWS / 16) + a;
+                if (mine >= DT) continue;
+#pragma unroll
+                for (int c = 0; c < DT; ++c) {
+                    f32x4 f;
+                    if (BACK)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) f[r] = M[(16 * a + 4 * g + r) * PAD + 16 * c + r16];
+                    else
+                        f = *reinterpret_cast<const f32x4*>(&M[(16 * a + r16) * PAD + 16 * c + 4 * g]);
+                    if (BACK) next[c] = mma(f, S[mine], next[c]);
+                    else next[mine] = mma(f, S[c], next[mine]);
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) S[t] = next[t];
+    }
+}
+
+// ----------------------------------------------------------------------------
+// What is left of the gradients: a workgroup takes a chunk and a head of keys, a wavefront 16 numbers of a head of keys (or twice 16) for half of
+// the tokens, and the heads of values
 // that share them one after the other, so that their gradients are summed in its registers.
 // With X1 = S0 gY^T, X2 = S0 dR^T, X3 = G U^T (numbers of a key x tokens) and the rows and columns of the maps:
 //   dG_i = sum_j (in_ij) - sum_j (in_ji) + scale gamma_i q_i.X1_i - beta_i gamma_i k_i.X2_i - tail_i k_i.X3_i,     in = N (q k) + M (k k)
 //   and, of the chunk's whole decay,  sum_i tail_i k_i.X3_i + gamma_C <S0, G>;   grates_t = -(sum_{i >= t} dG_i + that).
 // ----------------------------------------------------------------------------
-template <typename T, int DK, int WAVES>
+template <typename T, int DK>
 struct GradientLds {
     typedef Sizes<T, DK> Z;
     static constexpr int kKeys = 0, kQueries = kKeys + Z::kBytesRows, kY = kQueries + Z::kBytesRows, kU = kY + Z::kBytesRows, kR = kU + Z::PARTS * Z::kBytesRows,
@@ -914,20 +1093,21 @@ struct GradientLds {
     static constexpr int kAll = kBytes > kEnd ? kBytes : kEnd;
 };
 
-template <typename T, int DK, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES)
+template <typename T, int DK, int ACROSS, int HALVES>
+__global__ void __launch_bounds__(64 * ACROSS * HALVES)
 k_delta_gradients(DeltaArgs A)
 {
     typedef Sizes<T, DK> Z;
-    typedef GradientLds<T, DK, WAVES> L;
+    typedef GradientLds<T, DK> L;
+    constexpr int WAVES = ACROSS * HALVES;
     typedef typename Num<T>::frag frag;
     typedef typename Num<T>::quad quad;
-    constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, NT = DT / WAVES;
-    static_assert(DT % WAVES == 0, "every wavefront has as many tiles");
+    constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, NT = DT / ACROSS, CH = CT / HALVES;
+    static_assert(DT % ACROSS == 0 && CT % HALVES == 0, "every wavefront has as many tiles");
     constexpr int NM = (Z::TILES + WAVES - 1) / WAVES;
     __shared__ __attribute__((aligned(16))) char lds[L::kAll];
     __shared__ float beta[C], gamma[C], tail[C], high[C], low[C], whole;
-    __shared__ float row_in[CT][C], col_in[CT][C], row_kk[CT][C], dots[WAVES][3][C], rv[C], state_dot[WAVES];
+    __shared__ float row_in[CT][C], col_in[CT][C], row_kk[CT][C], dots[ACROSS][3][C], rv[C], state_dot[ACROSS];
     char *const Ks = lds + L::kKeys, *const Qs = lds + L::kQueries, *const Ys = lds + L::kY, *const Us = lds + L::kU, *const Rs = lds + L::kR;
     char *const Kt = lds + L::kKeysTurned, *const Qt = lds + L::kQueriesTurned, *const Ns = lds + L::kN, *const Nt = lds + L::kNt, *const Ms = lds + L::kM;
 
@@ -938,9 +1118,10 @@ k_delta_gradients(DeltaArgs A)
     find_chunk<C>(A, chunk, row, valid);
     if (valid == 0) return;
     const int x = threadIdx.x, lane = x & 63, wave = __builtin_amdgcn_readfirstlane(x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int across = wave % ACROSS, half = wave / ACROSS;
     const int kh = blockIdx.x, group = A.heads / A.key_heads, kdv = (A.dv + Z::K - 1) / Z::K;
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;
-    const bool wq = (A.wide & 1) && A.ldq < near, wk = (A.wide & 2) && A.ldk < near, wy = (A.wide & 16) && A.ldgy < near;
+    const bool wq = (A.wide & 1) && A.ldq < near, wk = (A.wide & 2) && A.ldk < near, wy = (A.wide & 16) && A.ldgy < near, wv = A.wide & 4, wg = A.wide & 128;
     const T* const q = static_cast<const T*>(A.q) + row * A.ldq + (int64_t)kh * A.dk;
     const T* const k = static_cast<const T*>(A.k) + row * A.ldk + (int64_t)kh * A.dk;
     constexpr int kPatches = (C / R) * (DK / 4);
@@ -954,13 +1135,11 @@ k_delta_gradients(DeltaArgs A)
         put_rows<ROW>(Qs, a, first, piece);
         put_rows<ROW>(Ks, c, first, piece);
     }
-    const Reader<ROW> rows(r16, g);
-    const Reader<SEQ> columns(r16, g);
-    f32x4 gq[NT][CT], gk[NT][CT];          // numbers 16 t + 4 g .. + 3 of the key, token 16 tt + r16
+    f32x4 gq[NT][CH], gk[NT][CH];          // numbers 16 t + 4 g .. + 3 of the key, token 16 (half CH + tt) + r16
 #pragma unroll
     for (int a = 0; a < NT; ++a)
 #pragma unroll
-        for (int t = 0; t < CT; ++t) gq[a][t] = gk[a][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < CH; ++t) gq[a][t] = gk[a][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     for (int e = 0; e < group; ++e) {
         const int h = kh * group + e;
@@ -977,11 +1156,42 @@ k_delta_gradients(DeltaArgs A)
             keep_patch(a, first, valid, piece * 4, A.dv);
             put_rows<ROW>(Ys, a, first, piece);
         }
-        for (int p = x; p < C * DK / 4; p += THREADS) {
-            const int piece = p % (DK / 4), i = p / (DK / 4);
-            if (piece * 4 >= kdv * Z::K) continue;     // (columns that no workgroup of the walks has written)
-            put_parts<T, Z::PARTS>(Us + quad_at<T, ROW>(i, piece), Z::kBytesRows, *reinterpret_cast<const f32x4*>(u + i * DK + piece * 4));
-            put_parts<T, Z::PARTS>(Rs + quad_at<T, ROW>(i, piece), Z::kBytesRows, *reinterpret_cast<const f32x4*>(dr + i * DK + piece * 4));
+        // U and dR; gv, and dR . v of every token, on the way.  (PIECES threads of a wavefront have a token)
+        constexpr int PIECES = DK <= 64 ? 16 : DK <= 128 ? 32 : 64;
+        for (int p = x; p < C * PIECES; p += THREADS) {
+            const int piece = p % PIECES, i = p / PIECES, at = 4 * piece;
+            float s = 0.0f;
+            if (at < kdv * Z::K) {                     // (behind those no workgroup of the walks has written)
+                const f32x4 u4 = *reinterpret_cast<const f32x4*>(u + i * DK + at), r4 = *reinterpret_cast<const f32x4*>(dr + i * DK + at);
+                if (i < valid && at < A.dv) {
+                    const T* const v = static_cast<const T*>(A.v) + (row + i) * A.ldv + (int64_t)h * A.dv + at;
+                    T* const gv = static_cast<T*>(A.gv) + (row + i) * A.ldgv + (int64_t)h * A.dv + at;
+                    const float bi = numbers[Z::kBeta + i];
+                    quad v4, g4;
+                    if (wv) {
+                        v4 = *reinterpret_cast<const quad*>(v);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) v4[c] = at + c < A.dv ? v[c] : (T)0.0f;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        s = fmaf(r4[c], (float)v4[c], s);
+                        g4[c] = (T)(bi * r4[c]);
+                    }
+                    if (A.gv && wg) {
+                        *reinterpret_cast<quad*>(gv) = g4;
+                    } else if (A.gv) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (at + c < A.dv) gv[c] = g4[c];
+                    }
+                }
+                put_parts<T, Z::PARTS>(Us + quad_at<T, ROW>(i, piece), Z::kBytesRows, u4);
+                put_parts<T, Z::PARTS>(Rs + quad_at<T, ROW>(i, piece), Z::kBytesRows, r4);
+            }
+            for (int step = 1; step < PIECES; step <<= 1) s += __shfl_xor(s, step);
+            if (piece == 0) rv[i] = s;
         }
         if (x < C) {
             beta[x] = numbers[Z::kBeta + x]; gamma[x] = numbers[Z::kGamma + x]; tail[x] = numbers[Z::kTail + x];
@@ -989,22 +1199,12 @@ k_delta_gradients(DeltaArgs A)
         }
         if (x == 0) whole = numbers[Z::kWhole];
         for (int i = x; i < CT * C; i += THREADS) (&row_in[0][0])[i] = (&col_in[0][0])[i] = (&row_kk[0][0])[i] = 0.0f;
-        // gv, and dR . v of every token
-        for (int i = wave; i < valid; i += WAVES) {
-            const T* const v = static_cast<const T*>(A.v) + (row + i) * A.ldv + (int64_t)h * A.dv;
-            T* const gv = A.gv ? static_cast<T*>(A.gv) + (row + i) * A.ldgv + (int64_t)h * A.dv : nullptr;
-            const float bi = numbers[Z::kBeta + i];
-            float s = 0.0f;
-            for (int c = lane; c < A.dv; c += 64) {
-                const float r = dr[i * DK + c];
-                s = fmaf(r, to_float(v[c]), s);
-                if (gv) gv[c] = (T)(bi * r);
-            }
-            for (int step = 1; step < 64; step <<= 1) s += __shfl_xor(s, step);
-            if (lane == 0) rv[i] = s;
-        }
         __syncthreads();
 
+        // (formed anew for each head: places kept from before the loop would fill the registers)
+        const int l = here(lane), r16 = l & 15, g = l >> 4;
+        const Reader<ROW> rows(r16, g);
+        const Reader<SEQ> columns(r16, g);
         // the maps: a lane holds rows i = 16 it + 4 g .. + 3 and column j = 16 jt + r16 of a tile
         f32x4 N[NM], M[NM];
 #pragma unroll
@@ -1015,6 +1215,7 @@ k_delta_gradients(DeltaArgs A)
             N[n] = M[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if (it >= CT) continue;
             f32x4 qk = {0.0f, 0.0f, 0.0f, 0.0f}, kk = qk;
+#pragma unroll 1
             for (int m = 0; m < kdv; ++m) {
                 frag uf[Z::PARTS], rf[Z::PARTS];
 #pragma unroll
@@ -1051,52 +1252,71 @@ k_delta_gradients(DeltaArgs A)
             if (g == 0) col_in[it][j] = col;
         }
 
-        // X1, X2, X3 of the wavefront's numbers of a key, one tile after the other
-        float state_sum = 0.0f, q1[CT], k2[CT], k3[CT];
+        // X1, X2, X3 of the wavefront's numbers of a key and half of the tokens, one tile of numbers after the other
+        float state_sum = 0.0f, q1[CH], k2[CH], k3[CH];
 #pragma unroll
-        for (int t = 0; t < CT; ++t) q1[t] = k2[t] = k3[t] = 0.0f;
+        for (int t = 0; t < CH; ++t) q1[t] = k2[t] = k3[t] = 0.0f;
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
-            const int t0 = a * WAVES + wave;
-            f32x4 X1[CT], X2[CT], X3[CT];
+            const int t0 = a * ACROSS + across;
+            f32x4 X1[CH], X2[CH], X3[CH];
 #pragma unroll
-            for (int t = 0; t < CT; ++t) X1[t] = X2[t] = X3[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            const float* const s0 = A.states_out + of * (int64_t)DK * DK + (16 * t0 + r16) * DK;
-            const float* const gs = A.gstates + of * (int64_t)DK * DK + (16 * t0 + r16) * DK;
+            for (int t = 0; t < CH; ++t) X1[t] = X2[t] = X3[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            const float* const s0 = A.states_out + of * (int64_t)DK * DK + (16 * t0 + r16) * DK + 4 * g;
+            const float* const gs = A.gstates + of * (int64_t)DK * DK + (16 * t0 + r16) * DK + 4 * g;
+            // (G apart from S0: the parts of both at once do not fit the registers)
+            const auto ask = [&](f32x4* to, const float* from, int m) {
+#pragma unroll
+                for (int c = 0; c < Z::E / 4; ++c) to[c] = *reinterpret_cast<const f32x4*>(from + m * Z::K + 16 * c);
+            };
+            f32x4 s4[Z::E / 4], g4[Z::E / 4];          // what is asked for next
+            ask(s4, s0, 0);
+            ask(g4, gs, 0);
+#pragma unroll 1
             for (int m = 0; m < kdv; ++m) {
-                float xs[Z::E], ys[Z::E];
+                float xs[Z::E];
 #pragma unroll
-                for (int c = 0; c < Z::E; c += 4) {
-                    const int at = m * Z::K + 4 * c + 4 * g;
-                    const f32x4 a4 = *reinterpret_cast<const f32x4*>(s0 + at), b4 = *reinterpret_cast<const f32x4*>(gs + at);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        xs[c + r] = a4[r];
-                        ys[c + r] = b4[r];
-                        state_sum = fmaf(a4[r], b4[r], state_sum);
-                    }
+                for (int c = 0; c < Z::E; ++c) {
+                    xs[c] = s4[c >> 2][c & 3];
+                    state_sum = fmaf(xs[c], g4[c >> 2][c & 3], state_sum);
                 }
-                frag sf[Z::PARTS], gf[Z::PARTS];
+                frag sf[Z::PARTS];
                 parts_of<T, Z::PARTS>(xs, sf);
-                parts_of<T, Z::PARTS>(ys, gf);
+                ask(g4, gs, m + 1 < kdv ? m + 1 : 0);
+                if (m + 1 < kdv) ask(s4, s0, m + 1);
 #pragma unroll
-                for (int t = 0; t < CT; ++t) {
-                    const frag yf = get<T>(Ys, rows.at(t, m));
+                for (int t = 0; t < CH; ++t) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int tt = half * CH + t;
+                    const frag yf = get<T>(Ys, rows.at(tt, m));
 #pragma unroll
                     for (int p = Z::PARTS - 1; p >= 0; --p) X1[t] = mma(sf[p], yf, X1[t]);
-                    frag uf[Z::PARTS], rf[Z::PARTS];
+                    frag rf[Z::PARTS];
 #pragma unroll
-                    for (int p = 0; p < Z::PARTS; ++p) {
-                        uf[p] = get<T>(Us + p * Z::kBytesRows, rows.at(t, m));
-                        rf[p] = get<T>(Rs + p * Z::kBytesRows, rows.at(t, m));
-                    }
+                    for (int p = 0; p < Z::PARTS; ++p) rf[p] = get<T>(Rs + p * Z::kBytesRows, rows.at(tt, m));
                     X2[t] = mma_parts<Z::PARTS>(sf, rf, X2[t]);
+                }
+            }
+#pragma unroll 1
+            for (int m = 0; m < kdv; ++m) {
+                float xs[Z::E];
+#pragma unroll
+                for (int c = 0; c < Z::E; ++c) xs[c] = g4[c >> 2][c & 3];
+                frag gf[Z::PARTS];
+                parts_of<T, Z::PARTS>(xs, gf);
+                if (m + 1 < kdv) ask(g4, gs, m + 1);
+#pragma unroll
+                for (int t = 0; t < CH; ++t) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    frag uf[Z::PARTS];
+#pragma unroll
+                    for (int p = 0; p < Z::PARTS; ++p) uf[p] = get<T>(Us + p * Z::kBytesRows, rows.at(half * CH + t, m));
                     X3[t] = mma_parts<Z::PARTS>(gf, uf, X3[t]);
                 }
             }
 #pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                const int i = 16 * t + r16;
+            for (int t = 0; t < CH; ++t) {
+                const int i = 16 * (half * CH + t) + r16;
                 const quad q4 = *reinterpret_cast<const quad*>(Qs + quad_at<T, ROW>(i, 4 * t0 + g)), k4 = *reinterpret_cast<const quad*>(Ks + quad_at<T, ROW>(i, 4 * t0 + g));
                 const float c1 = A.scale * gamma[i], c2 = beta[i] * gamma[i], c3 = tail[i];
 #pragma unroll
@@ -1110,17 +1330,18 @@ k_delta_gradients(DeltaArgs A)
             }
         }
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
+        for (int t = 0; t < CH; ++t) {
+            const int i = 16 * (half * CH + t) + r16;
 #pragma unroll
             for (int step = 16; step < 64; step <<= 1) {
                 q1[t] += __shfl_xor(q1[t], step);
                 k2[t] += __shfl_xor(k2[t], step);
                 k3[t] += __shfl_xor(k3[t], step);
             }
-            if (g == 0) { dots[wave][0][16 * t + r16] = q1[t]; dots[wave][1][16 * t + r16] = k2[t]; dots[wave][2][16 * t + r16] = k3[t]; }
+            if (g == 0) { dots[across][0][i] = q1[t]; dots[across][1][i] = k2[t]; dots[across][2][i] = k3[t]; }
         }
         for (int step = 1; step < 64; step <<= 1) state_sum += __shfl_xor(state_sum, step);
-        if (lane == 0) state_dot[wave] = state_sum;
+        if (lane == 0 && half == 0) state_dot[across] = state_sum;
         __syncthreads();                               // U and dR are done with
 
         for (int p = x; p < kPatches; p += THREADS) {
@@ -1174,7 +1395,7 @@ k_delta_gradients(DeltaArgs A)
                 kk_sum += row_kk[t][i];
             }
             for (int t = 0; t < CT; ++t) in -= col_in[t][i];
-            for (int w = 0; w < WAVES; ++w) {
+            for (int w = 0; w < ACROSS; ++w) {
                 d1 += dots[w][0][i];
                 d2 += dots[w][1][i];
                 d3 += dots[w][2][i];
@@ -1195,27 +1416,29 @@ k_delta_gradients(DeltaArgs A)
         __syncthreads();
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
-            const int t0 = a * WAVES + wave;
+            const int t0 = a * ACROSS + across;
 #pragma unroll
             for (int m = 0; m < KC; ++m) {
                 const frag kf = get<T>(Kt, columns.at(t0, m)), qf = get<T>(Qt, columns.at(t0, m));
 #pragma unroll
-                for (int t = 0; t < CT; ++t)
+                for (int t = 0; t < CH; ++t) {
+                    const int tt = half * CH + t;
 #pragma unroll
                     for (int p = Z::SOME - 1; p >= 0; --p) {
-                        if (16 * t + 15 >= m * Z::K) gq[a][t] = mma(kf, get<T>(Ns + p * Z::kBytesMap, columns.at(t, m)), gq[a][t]);
-                        if (m * Z::K + Z::K > 16 * t) gk[a][t] = mma(qf, get<T>(Nt + p * Z::kBytesMap, columns.at(t, m)), gk[a][t]);
-                        gk[a][t] = mma(kf, get<T>(Ms + p * Z::kBytesMap, columns.at(t, m)), gk[a][t]);
+                        if (16 * tt + 15 >= m * Z::K) gq[a][t] = mma(kf, get<T>(Ns + p * Z::kBytesMap, columns.at(tt, m)), gq[a][t]);
+                        if (m * Z::K + Z::K > 16 * tt) gk[a][t] = mma(qf, get<T>(Nt + p * Z::kBytesMap, columns.at(tt, m)), gk[a][t]);
+                        gk[a][t] = mma(kf, get<T>(Ms + p * Z::kBytesMap, columns.at(tt, m)), gk[a][t]);
                     }
+                }
             }
         }
     }
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
-        const int n = 16 * (a * WAVES + wave) + 4 * g;
+        const int n = 16 * (a * ACROSS + across) + 4 * g;
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            const int i = 16 * t + r16;
+        for (int t = 0; t < CH; ++t) {
+            const int i = 16 * (half * CH + t) + r16;
             if (i >= valid) continue;
             const auto write = [&](void* base, int64_t ld, bool wide, f32x4 v) {
                 if (!base) return;
@@ -1355,23 +1578,49 @@ int64_t chunks_of(int64_t tokens, int64_t sequences, int c, bool equal)
 
 size_t aligned(size_t v) { return (v + 255) / 256 * 256; }
 
-struct Parts { size_t maps, states, u, gstates, r, all; };
+struct Parts { size_t maps, states, u, gstates, r, added, turned, added_back, all; };
 
-Parts layout_of(bool bf16, int64_t chunks, int heads, int dk, int dv, bool training)
+Parts layout_of(bool bf16, int64_t chunks, int64_t places, int heads, int dk, int dv, bool training)
 {
     const int d = padded_of(dk, dv), c = tokens_of_chunk(bf16, d), ct = c / 16;
-    const size_t each = (size_t)chunks * heads * sizeof(float), numbers = (size_t)(ct * (ct + 1) / 2 * 256 + 5 * c + 4);
+    const size_t each = (size_t)chunks * heads * sizeof(float), numbers = (size_t)(ct * (ct + 1) * 256 + 5 * c + 4), state = (size_t)places * heads * d * d * sizeof(float);
     Parts L{};
-    L.maps = 0;
-    L.all = aligned(each * numbers);
+    const auto take = [&](size_t bytes) { const size_t at = L.all; L.all += aligned(bytes); return at; };
+    L.maps = take(each * numbers);
+    L.added = take(state);
+    L.turned = take(state);
     if (training) {
-        const auto take = [&](size_t bytes) { const size_t at = L.all; L.all += aligned(bytes); return at; };
+        L.added_back = take(state);
         L.states = take(each * d * d);
         L.u = take(each * c * d);
         L.gstates = take(each * d * d);
         L.r = take(each * c * d);
     }
     return L;
+}
+
+// How sequences are cut into stretches.
+struct Cut { bool cut; int64_t stretch, per_sequence, slots, places; };
+
+constexpr int64_t kWorkgroups = 256, kPackedWorkgroups = 512, kLeastChunks = 4;      // a workgroup of a walk takes most of a compute unit's LDS
+
+// By the sizes alone.
+Cut cut_of(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv, bool equal)
+{
+    const int d = padded_of(dk, dv), c = tokens_of_chunk(bf16, d), slices = d > 128 ? 2 : 1;
+    const int64_t longest = equal ? (sequences > 0 ? tokens / sequences : 0) : tokens, wanted = equal ? kWorkgroups : kPackedWorkgroups;
+    const int64_t units = (int64_t)heads * slices * tokens;
+    Cut P;
+    P.stretch = ((units + wanted - 1) / wanted + c - 1) / c * c;
+    if (P.stretch < kLeastChunks * c) P.stretch = kLeastChunks * c;
+    P.cut = longest > 3 * P.stretch;
+    if (!P.cut) P.stretch = longest < 1 ? 1 : longest;
+    P.per_sequence = 1;
+    if (equal && P.cut) P.per_sequence = (longest + P.stretch - 1) / P.stretch;
+    P.slots = !P.cut ? sequences : equal ? sequences * P.per_sequence : tokens / P.stretch + sequences;
+    const int64_t several = tokens / (P.stretch + 1);
+    P.places = !P.cut ? 0 : equal ? P.slots : tokens / P.stretch + (sequences < several ? sequences : several);
+    return P;
 }
 
 bool allows(const void* p, int64_t ld, int d, int size, int bytes)
@@ -1385,42 +1634,76 @@ dim3 grid_of(int64_t across, int64_t rows)
     return dim3((unsigned)across, (unsigned)(deep > 1 ? kRows : rows), (unsigned)deep);
 }
 
+enum { kRunResults, kRunKeep, kRunStates, kRunBack, kRunBackStates };
+
+// WAVES: wavefronts of a walk's workgroup, 16 columns of the state each
 template <typename T, int DK, int WAVES>
-hipError_t run_with(DeltaArgs A, hipStream_t st)
+hipError_t walks_with(const DeltaArgs& A, int what, hipStream_t st)
 {
-    const dim3 sequences = grid_of((int64_t)A.heads * A.slices, A.sequences), chunks = grid_of(A.key_heads, A.chunks), block(64 * WAVES);
+    const dim3 grid = grid_of((int64_t)A.heads * A.slices, A.slots), twice = grid_of((int64_t)A.heads * A.slices * 2, A.slots), block(64 * WAVES);
+    const char* const names[] = {"delta_walk", "delta_walk", "delta_states", "delta_back", "delta_back_states"};
+    profile_before(names[what], st);
+    if (what == kRunResults) hipLaunchKernelGGL((k_delta_walk<T, DK, WAVES, kResults>), grid, block, 0, st, A);
+    else if (what == kRunKeep) hipLaunchKernelGGL((k_delta_walk<T, DK, WAVES, kKeep>), grid, block, 0, st, A);
+    else if (what == kRunStates) hipLaunchKernelGGL((k_delta_walk<T, DK, WAVES, kStates>), twice, block, 0, st, A);
+    else if (what == kRunBack) hipLaunchKernelGGL((k_delta_back<T, DK, WAVES, false>), grid, block, 0, st, A);
+    else hipLaunchKernelGGL((k_delta_back<T, DK, WAVES, true>), grid, block, 0, st, A);
+    profile_after(names[what], st);
+    return hipGetLastError();
+}
+
+template <int DK>
+hipError_t carry_with(const DeltaArgs& A, bool back, hipStream_t st)
+{
+    const dim3 grid = grid_of((int64_t)A.heads * ((DK / 16 + kCarryWaves - 1) / kCarryWaves), A.sequences), block(64 * kCarryWaves);
+    profile_before("delta_carry", st);
+    if (back) hipLaunchKernelGGL((k_delta_carry<DK, true>), grid, block, 0, st, A);
+    else hipLaunchKernelGGL((k_delta_carry<DK, false>), grid, block, 0, st, A);
+    profile_after("delta_carry", st);
+    return hipGetLastError();
+}
+
+template <typename T, int DK, int ACROSS>
+hipError_t run_with(DeltaArgs A, bool cut, hipStream_t st)
+{
+    const dim3 chunks = grid_of(A.key_heads, A.chunks);
+    // Half as many columns of a workgroup, where whole ones would leave compute units without one: a workgroup takes most of one's LDS.
+    const bool narrow = A.slots * A.heads * (DK / (16 * ACROSS)) < 256;
+    A.slices = DK / (16 * ACROSS) * (narrow ? 2 : 1);
+    const auto walks = [&](int what) { return narrow ? walks_with<T, DK, ACROSS / 2>(A, what, st) : walks_with<T, DK, ACROSS>(A, what, st); };
+    hipError_t e = hipSuccess;
     if (A.forward || !A.saved) {
         if (A.chunks > 0) {
             profile_before("delta_prepare", st);
             hipLaunchKernelGGL((k_delta_prepare<T, DK>), chunks, dim3(kPrepareThreads), 0, st, A);
             profile_after("delta_prepare", st);
         }
-        profile_before("delta_walk", st);
-        if (A.forward) hipLaunchKernelGGL((k_delta_walk<T, DK, WAVES, true>), sequences, block, 0, st, A);
-        else hipLaunchKernelGGL((k_delta_walk<T, DK, WAVES, false>), sequences, block, 0, st, A);
-        profile_after("delta_walk", st);
+        if (cut) e = walks(kRunStates);
+        if (cut && e == hipSuccess) e = carry_with<DK>(A, false, st);
+        if (e == hipSuccess) e = walks(A.forward ? kRunResults : kRunKeep);
     }
-    if (!A.forward) {
-        profile_before("delta_back", st);
-        hipLaunchKernelGGL((k_delta_back<T, DK, WAVES>), sequences, block, 0, st, A);
-        profile_after("delta_back", st);
-        if (A.chunks > 0 && (A.gq || A.gk || A.gv || A.grates || A.gbeta)) {
-            profile_before("delta_gradients", st);
-            hipLaunchKernelGGL((k_delta_gradients<T, DK, WAVES>), chunks, block, 0, st, A);
-            profile_after("delta_gradients", st);
-        }
+    if (A.forward || e != hipSuccess) return e;
+    if (cut) e = walks(kRunBackStates);
+    if (cut && e == hipSuccess) e = carry_with<DK>(A, true, st);
+    if (e == hipSuccess) e = walks(kRunBack);
+    if (e == hipSuccess && A.chunks > 0 && (A.gq || A.gk || A.gv || A.grates || A.gbeta)) {
+        constexpr int HALVES = Sizes<T, DK>::CT > 1 ? 2 : 1;
+        profile_before("delta_gradients", st);
+        hipLaunchKernelGGL((k_delta_gradients<T, DK, ACROSS, HALVES>), chunks, dim3(64 * ACROSS * HALVES), 0, st, A);
+        profile_after("delta_gradients", st);
+        e = hipGetLastError();
     }
-    return hipGetLastError();
+    return e;
 }
 
 template <typename T>
-hipError_t run_of(const DeltaArgs& A, int padded, hipStream_t st)
+hipError_t run_of(const DeltaArgs& A, bool cut, int padded, hipStream_t st)
 {
-    if (padded == 64) return run_with<T, 64, 4>(A, st);
-    if (padded == 96) return run_with<T, 96, 6>(A, st);
-    if (padded == 128) return run_with<T, 128, 8>(A, st);
-    if (padded == 192) return run_with<T, 192, 6>(A, st);
-    return run_with<T, 256, 8>(A, st);
+    if (padded == 64) return run_with<T, 64, 4>(A, cut, st);
+    if (padded == 96) return run_with<T, 96, 6>(A, cut, st);
+    if (padded == 128) return run_with<T, 128, 8>(A, cut, st);
+    if (padded == 192) return run_with<T, 192, 6>(A, cut, st);
+    return run_with<T, 256, 8>(A, cut, st);
 }
 
 template <typename T, int VEC>
@@ -1440,8 +1723,11 @@ hipError_t tokens_with(const DeltaArgs& A, int lanes_log2, int slices, hipStream
 // For up to so many tokens and sequences, of equal lengths or not, of heads and sizes like these.
 size_t delta_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv, bool training)
 {
-    const int c = tokens_of_chunk(bf16, padded_of(dk, dv));
-    return layout_of(bf16, tokens / c + sequences, heads, dk, dv, training).all;
+    if (heads == 0) return 0;
+    // of equal lengths or packed, and cut into stretches of no fewer than so many tokens
+    const int d = padded_of(dk, dv), c = tokens_of_chunk(bf16, d);
+    const int64_t by_size = tokens / (kLeastChunks * c), by_work = kPackedWorkgroups / ((int64_t)heads * (d > 128 ? 2 : 1)) + 1, several = by_size < by_work ? by_size : by_work;
+    return layout_of(bf16, tokens / c + sequences, several > 0 ? several + (sequences < several ? sequences : several) : 0, heads, dk, dv, training).all;
 }
 
 hipError_t launch_delta_tokens(const DeltaArgs& A, hipStream_t st)
@@ -1462,12 +1748,16 @@ hipError_t launch_delta(const DeltaArgs& given, hipStream_t st)
     DeltaArgs A = given;
     const int padded = padded_of(A.dk, A.dv), c = tokens_of_chunk(A.bf16, padded), size = A.bf16 ? 2 : 4;
     const bool training = !A.forward || A.saved;
-    A.slices = padded > 128 ? 2 : 1;
     A.per_sequence = !A.starts && A.sequences > 0 ? (A.tokens / A.sequences + c - 1) / c : 0;
     A.chunks = chunks_of(A.tokens, A.sequences, c, A.starts == nullptr);
-    const Parts L = layout_of(A.bf16, A.chunks, A.heads, A.dk, A.dv, training);
+    const Cut P = cut_of(A.bf16, A.tokens, A.sequences, A.heads, A.dk, A.dv, A.starts == nullptr);
+    A.stretch = P.stretch; A.stretches = P.per_sequence; A.slots = P.slots; A.training = training;
+    const Parts L = layout_of(A.bf16, A.chunks, P.places, A.heads, A.dk, A.dv, training);
     A.maps = reinterpret_cast<float*>(A.ws + L.maps);
+    A.added = reinterpret_cast<float*>(A.ws + L.added);
+    A.turned = reinterpret_cast<float*>(A.ws + L.turned);
     if (training) {
+        A.added_back = reinterpret_cast<float*>(A.ws + L.added_back);
         A.states_out = reinterpret_cast<float*>(A.ws + L.states);
         A.u_out = reinterpret_cast<float*>(A.ws + L.u);
         A.gstates = reinterpret_cast<float*>(A.ws + L.gstates);
@@ -1475,8 +1765,9 @@ hipError_t launch_delta(const DeltaArgs& given, hipStream_t st)
     }
     A.wide = (allows(A.q, A.ldq, A.dk, size, 4 * size) ? 1 : 0) | (allows(A.k, A.ldk, A.dk, size, 4 * size) ? 2 : 0) | (allows(A.v, A.ldv, A.dv, size, 4 * size) ? 4 : 0) |
              (allows(A.y, A.ldy, A.dv, size, 4 * size) ? 8 : 0) | (allows(A.gy, A.ldgy, A.dv, size, 4 * size) ? 16 : 0) |
-             (allows(A.gq, A.ldgq, A.dk, size, 4 * size) ? 32 : 0) | (allows(A.gk, A.ldgk, A.dk, size, 4 * size) ? 64 : 0);
-    return A.bf16 ? run_of<__bf16>(A, padded, st) : run_of<float>(A, padded, st);
+             (allows(A.gq, A.ldgq, A.dk, size, 4 * size) ? 32 : 0) | (allows(A.gk, A.ldgk, A.dk, size, 4 * size) ? 64 : 0) |
+             (allows(A.gv, A.ldgv, A.dv, size, 4 * size) ? 128 : 0);
+    return A.bf16 ? run_of<__bf16>(A, P.cut, padded, st) : run_of<float>(A, P.cut, padded, st);
 }
 
 }  // namespace laplex

@@ -91,6 +91,12 @@ k_norm(NormArgs A)
     __shared__ float side[2][kThreads / 64][1];
     const int lane = threadIdx.x % LANES;
     const float width = (float)A.width;
+    float w[COUNT][N], b[COUNT][N];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        load_weight<N>(w[i], A.weight, (int64_t)(i * LANES + lane) * N, A.width, 1.0f);
+        load_weight<N>(b[i], A.bias, (int64_t)(i * LANES + lane) * N, A.width, 0.0f);
+    }
     for (int64_t first = (int64_t)blockIdx.x * ROWS; first < A.rows; first += (int64_t)gridDim.x * ROWS) {
         const int64_t row = first + threadIdx.x / LANES;
         const bool live = row < A.rows;
@@ -125,12 +131,9 @@ k_norm(NormArgs A)
         for (int i = 0; i < COUNT; ++i) {
             const int64_t at = (int64_t)(i * LANES + lane) * N;
             if (at >= A.width) continue;
-            float w[N], b[N];
-            load_weight<N>(w, A.weight, at, A.width, 1.0f);
-            load_weight<N>(b, A.bias, at, A.width, 0.0f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) w[e] = fmaf(v[i][e] * rstd, w[e], b[e]);
-            store_piece<T>(y, at, A.width, w);
+            for (int e = 0; e < N; ++e) v[i][e] = fmaf(v[i][e] * rstd, w[i][e], b[i][e]);
+            store_piece<T>(y, at, A.width, v[i]);
         }
     }
 }
@@ -374,7 +377,7 @@ Plan plan_of(int64_t pieces, int wavefront_most)
     return {0, 0};
 }
 
-constexpr int64_t kPartWorkgroups = 1024, kMostWorkgroups = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+constexpr int64_t kForwardWorkgroups = 2048, kPartWorkgroups = 1024, kMostWorkgroups = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
 
 unsigned workgroups(int64_t wanted) { return (unsigned)(wanted < kMostWorkgroups ? wanted : kMostWorkgroups); }
 
@@ -390,7 +393,7 @@ template <typename T, int LANES, int COUNT>
 hipError_t forward_with(const NormArgs& A, hipStream_t st)
 {
     constexpr int ROWS = kThreads / LANES;
-    hipLaunchKernelGGL((k_norm<T, LANES, COUNT>), dim3(workgroups((A.rows + ROWS - 1) / ROWS)), dim3(kThreads), 0, st, A);
+    hipLaunchKernelGGL((k_norm<T, LANES, COUNT>), dim3((unsigned)((A.rows + ROWS - 1) / ROWS < kForwardWorkgroups ? (A.rows + ROWS - 1) / ROWS : kForwardWorkgroups)), dim3(kThreads), 0, st, A);
     return hipGetLastError();
 }
 
@@ -452,7 +455,7 @@ size_t norm_workspace(int64_t rows, int64_t width)
 hipError_t launch_norm(const NormArgs& A, hipStream_t st)
 {
     // A wavefront for a row where there are rows for all of them (no barrier), else the workgroup.
-    const Plan P = plan_of(pieces_of(A.bf16, A.width), A.rows >= 2048 ? kMost : 1);
+    const Plan P = plan_of(pieces_of(A.bf16, A.width), A.rows >= 2048 ? 2 : 1);
     profile_before("norm", st);
     const hipError_t e = A.bf16 ? forward_of<__bf16>(A, P, st) : forward_of<float>(A, P, st);
     profile_after("norm", st);

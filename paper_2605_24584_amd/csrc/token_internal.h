@@ -100,7 +100,10 @@ struct DeltaArgs {
     // filled in by launch_delta
     int slices, wide;                // workgroups side by side over the columns; a bit each for q, k, v, y, gy, gq, gk: four numbers at a time
     int64_t per_sequence, chunks;    // chunks of a sequence (equal lengths), of all, at most
+    int64_t stretch, stretches, slots;       // tokens of a stretch that one workgroup walks; stretches of a sequence (equal lengths), of all, at most
+    bool training;
     float *maps, *states_out, *u_out, *gstates, *r_out;
+    float *added, *turned, *added_back;      // [place][head]: what a stretch adds to the state (then: the state that enters it), how it turns it, what it adds to the state's gradient
 };
 size_t delta_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv, bool training);
 hipError_t launch_delta(const DeltaArgs& A, hipStream_t st);

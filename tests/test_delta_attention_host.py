@@ -93,8 +93,8 @@ def test_workspace(L):
             assert sizes == sorted(sizes)
     # what the header says it grows by
     more = need(L, 1, type=B.LAPLEX_BF16, tokens=1 << 20, sequences=1, heads=1, key_heads=1, dk=128, dv=128) / (1 << 20)
-    assert 3.0 * 1024 < more < 3.4 * 1024
-    assert need(L, 0, type=B.LAPLEX_BF16, tokens=1 << 20, sequences=1, heads=1, key_heads=1, dk=128, dv=128) / (1 << 20) < 200
+    assert 3.2 * 1024 < more < 3.6 * 1024
+    assert need(L, 0, type=B.LAPLEX_BF16, tokens=1 << 20, sequences=1, heads=1, key_heads=1, dk=128, dv=128) / (1 << 20) < 500
 
 
 @pytest.mark.parametrize("which", range(6))

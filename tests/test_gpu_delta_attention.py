@@ -380,3 +380,24 @@ def test_two_calls_at_once():
     for g, w in zip(got, want):
         for a, b in zip(g, w):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths,heads,key_heads,dk,dv,packed,read", [
+    ([2600], 2, 1, 64, 64, False, None), ([1, 2000, 0, 900], 4, 2, 96, 80, True, None), ([1500, 1500], 2, 2, 20, 130, False, None), ([1300], 1, 1, 200, 256, False, None),
+    ([1100, 1100, 1100], 2, 2, 48, 48, False, [1100, 77, 1027]), ([40, 1500, 30, 2000], 2, 2, 128, 128, True, [40, 1501, 7, 1025]), ([769, 5, 1025], 1, 1, 256, 64, True, None)])
+def test_sequences_in_stretches(dtype, lengths, heads, key_heads, dk, dv, packed, read):
+    """Sequences that are cut, with lengths that end inside, at and behind the edges of stretches; the state in place."""
+    c = Case(seeded("stretches", lengths, heads, dk, dv), lengths, heads, key_heads, dk, dv, dtype, True, packed, read)
+    y, last = c.forward()
+    c.check_forward(y, last, [heads - 1])
+    ws = c.workspace()
+    z, last2 = c.forward(ws, B.LAPLEX_SAVE_SCANS)
+    assert torch.equal(z.nan_to_num(), y.nan_to_num()) and torch.equal(last2, last)
+    g = c.backward(ws, B.LAPLEX_SAVE_SCANS)
+    c.check_backward(g)
+    for a, b in zip(c.backward(), g):
+        assert torch.equal(a.nan_to_num(), b.nan_to_num())
+    same = c.state.clone()
+    B.laplex_delta_attention(c.q, c.k, c.v, c.rates, c.beta, z, c.workspace(False), c.scale, c.b, c.starts, c.read, same, same)
+    assert torch.equal(z.nan_to_num(), y.nan_to_num()) and torch.equal(same, last)
