@@ -34,7 +34,7 @@ constexpr int64_t kRows = 32768;          // sequences or chunks along a grid's 
 // ----------------------------------------------------------------------------
 __device__ __forceinline__ int64_t start_of(const DeltaArgs& A, int64_t b)
 {
-    if (!A.starts) return A.sequences > 0 ? A.tokens / A.sequences * b : 0;
+    if (!A.starts) return A.each * b;
     const int64_t v = A.starts[b];                     // whatever it holds, no row outside the matrices is touched
     return v < 0 ? 0 : v > A.tokens ? A.tokens : v;
 }
@@ -50,7 +50,7 @@ __device__ __forceinline__ int64_t count_of(const DeltaArgs& A, int64_t b, int64
 // Sequences are cut into units of so many tokens (chunks, or stretches of chunks): sequence b has those from first_unit(b) on, at least as many as its rows need.
 __device__ __forceinline__ int64_t first_unit(const DeltaArgs& A, int64_t b, int64_t begin, int64_t size, int64_t per_sequence)
 {
-    return A.starts ? begin / size + b : b * per_sequence;
+    return A.starts ? (uint32_t)begin / (uint32_t)size + b : b * per_sequence;
 }
 
 template <int C>
@@ -66,14 +66,14 @@ __device__ __forceinline__ Unit find_unit(const DeltaArgs& A, int64_t unit, int6
         int64_t hi = A.sequences;
         const int lane = threadIdx.x & 63;
         while (hi - lo > 1) {
-            const int64_t step = (hi - lo + 63) / 64, c = lo + lane * step;
+            const int64_t step = (uint32_t)(hi - lo + 63) / 64u, c = lo + lane * step;
             const uint64_t votes = __ballot(c < hi && first_unit(A, c, start_of(A, c), size, per_sequence) <= unit);
             const int at = votes ? 63 - __builtin_clzll(votes) : 0;
             lo += at * step;
             hi = lo + step < hi ? lo + step : hi;
         }
     } else {
-        lo = unit / per_sequence;
+        lo = (uint32_t)unit / (uint32_t)per_sequence;
     }
     Unit u;
     u.b = lo;
@@ -98,8 +98,8 @@ __device__ __forceinline__ void find_chunk(const DeltaArgs& A, int64_t chunk, in
 __device__ __forceinline__ int64_t first_place(const DeltaArgs& A, int64_t b, int64_t begin)
 {
     if (!A.starts) return b * A.stretches;
-    const int64_t several = begin / (A.stretch + 1);
-    return begin / A.stretch + (b < several ? b : several);
+    const int64_t several = (uint32_t)begin / (uint32_t)(A.stretch + 1);
+    return (uint32_t)begin / (uint32_t)A.stretch + (b < several ? b : several);
 }
 
 // The stretch with this number, [lo, hi) of its sequence's tokens.
@@ -485,6 +485,7 @@ k_delta_walk(DeltaArgs A)
     float pn[3], pw = 0.0f;
     int pb = C;
     const auto load = [&](int64_t at) {
+        const int y = here(x);                         // (formed anew for each chunk, as everything below: places kept from before the loop would fill the registers)
         const int valid = (int)(count - at < C ? count - at : C);
         const int64_t row = begin + at;
         const int hq = how(wq, valid == C && A.dk == DK), hk = how(wk, valid == C && A.dk == DK), hv = how(wv, valid == C && col0 + COLS <= A.dv);
@@ -494,7 +495,7 @@ k_delta_walk(DeltaArgs A)
         const float* const numbers = A.maps + ((chunk0 + at / C) * A.heads + h) * Z::kNumbers;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = (p % (DK / 4)) * 4;
+            const int p = y + i * THREADS, first = (p / (DK / 4)) * R, piece = (p % (DK / 4)) * 4;
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
                 if (OUT) load_patch(pq[i], q, A.ldq, first, valid, piece, A.dk, hq);
                 load_patch(pk[i], k, A.ldk, first, valid, piece, A.dk, hk);
@@ -502,23 +503,23 @@ k_delta_walk(DeltaArgs A)
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int p = x + i * THREADS;
+            const int p = y + i * THREADS;
             if ((kColPatches % THREADS == 0 || p < kColPatches) && part == 0)
                 load_patch(pv[i], v, A.ldv, (p / (COLS / 4)) * R, valid, col0 + (p % (COLS / 4)) * 4, A.dv, hv);
         }
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
-            const int p = x + i * THREADS;
+            const int p = y + i * THREADS;
             if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
                 pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
                 if (OUT) pp[i] = reinterpret_cast<const f32x4*>(numbers + Z::kP)[p];
             }
         }
-        if (x < C) {
+        if (y < C) {
 #pragma unroll
-            for (int i = 0; i < 3; ++i) pn[i] = numbers[Z::kBeta + i * C + x];
+            for (int i = 0; i < 3; ++i) pn[i] = numbers[Z::kBeta + i * C + y];
         }
-        if (x < 2) pw = numbers[Z::kWhole + x];
+        if (y < 2) pw = numbers[Z::kWhole + y];
         if (x == 0) pb = reinterpret_cast<const int*>(numbers)[Z::kBad];
     };
     if (s.lo < count) load(s.lo);
@@ -527,10 +528,11 @@ k_delta_walk(DeltaArgs A)
     int turn = 0;
     for (int64_t at = s.lo; at < count; at += C, turn ^= 1) {
         const int valid = (int)(count - at < C ? count - at : C);
+        const int y = here(x), l = here(lane), r16 = l & 15, g = l >> 4;
         const int64_t row = begin + at, chunk = chunk0 + at / C;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = p % (DK / 4);
+            const int p = y + i * THREADS, first = (p / (DK / 4)) * R, piece = p % (DK / 4);
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
                 if (OUT) {
                     if (!(valid == C && A.dk == DK)) keep_patch(pq[i], first, valid, piece * 4, A.dk);
@@ -544,7 +546,7 @@ k_delta_walk(DeltaArgs A)
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int p = x + i * THREADS, first = (p / (COLS / 4)) * R, piece = p % (COLS / 4);
+            const int p = y + i * THREADS, first = (p / (COLS / 4)) * R, piece = p % (COLS / 4);
             if ((kColPatches % THREADS == 0 || p < kColPatches) && part == 0) {
                 if (!(valid == C && col0 + COLS <= A.dv)) keep_patch(pv[i], first, valid, col0 + piece * 4, A.dv);
                 if (!finite_patch(pv[i])) {
@@ -556,7 +558,7 @@ k_delta_walk(DeltaArgs A)
         }
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
-            const int p = x + i * THREADS;
+            const int p = y + i * THREADS;
             if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
                 const int tile = p >> 6;
                 int it = 0, jt = tile;
@@ -566,15 +568,12 @@ k_delta_walk(DeltaArgs A)
                 if (OUT) put_parts<T, Z::SOME>(Ps + to, Z::kBytesMap, pp[i]);
             }
         }
-        if (x < C) { beta[x] = pn[0]; gamma[x] = pn[1]; tail[x] = pn[2]; }
-        if (x < 2) whole[x] = pw;
+        if (y < C) { beta[y] = pn[0]; gamma[y] = pn[1]; tail[y] = pn[2]; }
+        if (y < 2) whole[y] = pw;
         if (x == 0 && pb < C) atomicMin(&odd[turn], pb);
-        if (at + C < count) load(at + C);
         __syncthreads();
 
         const int bad = odd[turn];                     // from this token on there is nothing but NaN
-        // (formed anew for each chunk: places kept from before the loop would fill the registers)
-        const int l = here(lane), r16 = l & 15, g = l >> 4;
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
         if (!STATES && A.states_out) {
@@ -605,6 +604,7 @@ k_delta_walk(DeltaArgs A)
                 }
             }
         }
+        if (at + C < count) load(at + C);
         // R = beta (V - gamma K S), U = T R
         frag Rf[KC][Z::PARTS];
 #pragma unroll
@@ -776,6 +776,7 @@ k_delta_back(DeltaArgs A)
     f32x4 pt[NM], pp[NM];
     float pn[3], pw = 0.0f;
     const auto load = [&](int64_t at) {
+        const int y = here(x);                         // (formed anew for each chunk, as everything below: places kept from before the loop would fill the registers)
         const int valid = (int)(count - at < C ? count - at : C);
         const int64_t row = begin + at;
         const int hq = how(wq, valid == C && A.dk == DK), hk = how(wk, valid == C && A.dk == DK), hy = how(wy, valid == C && col0 + COLS <= A.dv);
@@ -785,7 +786,7 @@ k_delta_back(DeltaArgs A)
         const float* const numbers = A.maps + ((chunk0 + at / C) * A.heads + h) * Z::kNumbers;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = (p % (DK / 4)) * 4;
+            const int p = y + i * THREADS, first = (p / (DK / 4)) * R, piece = (p % (DK / 4)) * 4;
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
                 load_patch(pq[i], q, A.ldq, first, valid, piece, A.dk, hq);
                 load_patch(pk[i], k, A.ldk, first, valid, piece, A.dk, hk);
@@ -793,33 +794,34 @@ k_delta_back(DeltaArgs A)
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int p = x + i * THREADS;
+            const int p = y + i * THREADS;
             if (kColPatches % THREADS == 0 || p < kColPatches)
                 load_patch(pv[i], gy, A.ldgy, (p / (COLS / 4)) * R, valid, col0 + (p % (COLS / 4)) * 4, A.dv, hy);
         }
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
-            const int p = x + i * THREADS;
+            const int p = y + i * THREADS;
             if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
                 pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
                 pp[i] = reinterpret_cast<const f32x4*>(numbers + Z::kP)[p];
             }
         }
-        if (x < C) {
+        if (y < C) {
 #pragma unroll
-            for (int i = 0; i < 3; ++i) pn[i] = numbers[Z::kBeta + i * C + x];
+            for (int i = 0; i < 3; ++i) pn[i] = numbers[Z::kBeta + i * C + y];
         }
-        if (x < 2) pw = numbers[Z::kWhole + x];
+        if (y < 2) pw = numbers[Z::kWhole + y];
     };
     const int64_t last = count > s.lo ? s.lo + (count - 1 - s.lo) / C * C : -1;
     if (last >= 0) load(last);
     __syncthreads();
     for (int64_t at = last; at >= s.lo; at -= C) {
         const int valid = (int)(count - at < C ? count - at : C);
+        const int y = here(x), l = here(lane), r16 = l & 15, g = l >> 4;
         const int64_t chunk = chunk0 + at / C;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int p = x + i * THREADS, first = (p / (DK / 4)) * R, piece = p % (DK / 4);
+            const int p = y + i * THREADS, first = (p / (DK / 4)) * R, piece = p % (DK / 4);
             if (kRowPatches % THREADS == 0 || p < kRowPatches) {
                 if (!(valid == C && A.dk == DK)) {
                     keep_patch(pq[i], first, valid, piece * 4, A.dk);
@@ -832,7 +834,7 @@ k_delta_back(DeltaArgs A)
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int p = x + i * THREADS, first = (p / (COLS / 4)) * R, piece = p % (COLS / 4);
+            const int p = y + i * THREADS, first = (p / (COLS / 4)) * R, piece = p % (COLS / 4);
             if (kColPatches % THREADS == 0 || p < kColPatches) {
                 if (!(valid == C && col0 + COLS <= A.dv)) keep_patch(pv[i], first, valid, col0 + piece * 4, A.dv);
                 put_turned<T, SEQ>(Yt, pv[i], first, piece);
@@ -841,7 +843,7 @@ k_delta_back(DeltaArgs A)
         // T and P turned: row j, tokens i along the slots
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
-            const int p = x + i * THREADS;
+            const int p = y + i * THREADS;
             if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
                 const int tile = p >> 6;
                 int it = 0, jt = tile;
@@ -862,12 +864,9 @@ k_delta_back(DeltaArgs A)
                 }
             }
         }
-        if (x < C) { beta[x] = pn[0]; gamma[x] = pn[1]; tail[x] = pn[2]; }
-        if (x < 2) whole[x] = pw;
-        if (at - C >= s.lo) load(at - C);
+        if (y < C) { beta[y] = pn[0]; gamma[y] = pn[1]; tail[y] = pn[2]; }
+        if (y < 2) whole[y] = pw;
         __syncthreads();
-        // (formed anew for each chunk: places kept from before the loop would fill the registers)
-        const int l = here(lane), r16 = l & 15, g = l >> 4;
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
         Reader<SEQ> values(r16, g);
@@ -894,6 +893,7 @@ k_delta_back(DeltaArgs A)
 #pragma unroll
             for (int t = 0; t < CT; ++t) U[t] = mma_exact<Z::PARTS>(get<T>(Ks, rows.at(t, m)), sf, U[t]);
         }
+        if (at - C >= s.lo) load(at - C);
 #pragma unroll
         for (int t = 0; t < CT; ++t)
 #pragma unroll
@@ -1124,12 +1124,13 @@ k_delta_gradients(DeltaArgs A)
     const bool wq = (A.wide & 1) && A.ldq < near, wk = (A.wide & 2) && A.ldk < near, wy = (A.wide & 16) && A.ldgy < near, wv = A.wide & 4, wg = A.wide & 128;
     const T* const q = static_cast<const T*>(A.q) + row * A.ldq + (int64_t)kh * A.dk;
     const T* const k = static_cast<const T*>(A.k) + row * A.ldk + (int64_t)kh * A.dk;
+    const int hy = how(wy, valid == C && A.dv == DK), hq = how(wq, valid == C && A.dk == DK), hk = how(wk, valid == C && A.dk == DK);
     constexpr int kPatches = (C / R) * (DK / 4);
     for (int p = x; p < kPatches; p += THREADS) {
         const int piece = p % (DK / 4), first = (p / (DK / 4)) * R;
         Patch<T> a, c;
-        load_patch(a, q, A.ldq, first, valid, piece * 4, A.dk, wq);
-        load_patch(c, k, A.ldk, first, valid, piece * 4, A.dk, wk);
+        load_patch(a, q, A.ldq, first, valid, piece * 4, A.dk, hq);
+        load_patch(c, k, A.ldk, first, valid, piece * 4, A.dk, hk);
         keep_patch(a, first, valid, piece * 4, A.dk);
         keep_patch(c, first, valid, piece * 4, A.dk);
         put_rows<ROW>(Qs, a, first, piece);
@@ -1141,43 +1142,78 @@ k_delta_gradients(DeltaArgs A)
 #pragma unroll
         for (int t = 0; t < CH; ++t) gq[a][t] = gk[a][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+    // What a head reads, all asked for at once: the rows of its chunk, and (as far as the registers reach) the wavefront's rows of the state.
+    constexpr int PIECES = DK <= 64 ? 16 : DK <= 128 ? 32 : 64, NP = (kPatches + THREADS - 1) / THREADS, NU = (C * PIECES + THREADS - 1) / THREADS;      // (PIECES threads of a wavefront have a token)
+    constexpr int AHEAD = DK <= 128 ? DK / Z::K : 4;   // fragments of a row of the states
+    Patch<T> py[NP];
+    f32x4 pu[NU], pr[NU], s4[AHEAD][Z::E / 4], g4[AHEAD][Z::E / 4];
+    quad pv[NU];
+    const auto ask_state = [&](f32x4 (&to)[AHEAD][Z::E / 4], const float* states, int64_t of, int a, int m0) {
+        const float* const from = states + of * (int64_t)DK * DK + (16 * (a * ACROSS + across) + r16) * DK + 4 * g;
+#pragma unroll
+        for (int m = 0; m < AHEAD; ++m)
+            if (m0 + m < kdv)
+#pragma unroll
+                for (int c = 0; c < Z::E / 4; ++c) to[m][c] = *reinterpret_cast<const f32x4*>(from + (m0 + m) * Z::K + 16 * c);
+    };
+    const auto ask = [&](int h) {
+        const int64_t of = chunk * A.heads + h;
+        const T* const gy = static_cast<const T*>(A.gy) + row * A.ldgy + (int64_t)h * A.dv;
+        const T* const v = static_cast<const T*>(A.v) + row * A.ldv + (int64_t)h * A.dv;
+        const float* const u = A.u_out + of * (int64_t)C * DK;
+        const float* const dr = A.r_out + of * (int64_t)C * DK;
+        const int y = here(x);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+            const int p = y + n * THREADS;
+            if (kPatches % THREADS == 0 || p < kPatches) load_patch(py[n], gy, A.ldgy, (p / (DK / 4)) * R, valid, p % (DK / 4) * 4, A.dv, hy);
+        }
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+            const int p = y + n * THREADS, at = p % PIECES * 4, i = p / PIECES;
+            if (i >= C || at >= kdv * Z::K) continue;  // (behind those no workgroup of the walks has written)
+            pu[n] = *reinterpret_cast<const f32x4*>(u + i * DK + at);
+            pr[n] = *reinterpret_cast<const f32x4*>(dr + i * DK + at);
+            if (i >= valid || at >= A.dv) continue;
+            if (wv) {
+                pv[n] = *reinterpret_cast<const quad*>(v + i * A.ldv + at);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) pv[n][c] = v[i * A.ldv + (at + c < A.dv ? at + c : A.dv - 1)];
+            }
+        }
+        ask_state(s4, A.states_out, of, 0, 0);
+    };
+    ask(kh * group);
     for (int e = 0; e < group; ++e) {
         const int h = kh * group + e;
         const int64_t of = chunk * A.heads + h;
-        const T* const gy = static_cast<const T*>(A.gy) + row * A.ldgy + (int64_t)h * A.dv;
         const float* const numbers = A.maps + of * Z::kNumbers;
-        const float* const u = A.u_out + of * (int64_t)C * DK;
-        const float* const dr = A.r_out + of * (int64_t)C * DK;
+        // (formed anew for each head: places kept from before the loop would fill the registers)
+        const int x = here(threadIdx.x), lane = x & 63, r16 = lane & 15, g = lane >> 4;
         __syncthreads();
-        for (int p = x; p < kPatches; p += THREADS) {
-            const int piece = p % (DK / 4), first = (p / (DK / 4)) * R;
-            Patch<T> a;
-            load_patch(a, gy, A.ldgy, first, valid, piece * 4, A.dv, wy);
-            keep_patch(a, first, valid, piece * 4, A.dv);
-            put_rows<ROW>(Ys, a, first, piece);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+            const int p = x + n * THREADS, piece = p % (DK / 4), first = (p / (DK / 4)) * R;
+            if (kPatches % THREADS == 0 || p < kPatches) {
+                keep_patch(py[n], first, valid, piece * 4, A.dv);
+                put_rows<ROW>(Ys, py[n], first, piece);
+            }
         }
-        // U and dR; gv, and dR . v of every token, on the way.  (PIECES threads of a wavefront have a token)
-        constexpr int PIECES = DK <= 64 ? 16 : DK <= 128 ? 32 : 64;
-        for (int p = x; p < C * PIECES; p += THREADS) {
-            const int piece = p % PIECES, i = p / PIECES, at = 4 * piece;
+        // U and dR; gv, and dR . v of every token, on the way
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+            const int p = x + n * THREADS, piece = p % PIECES, i = p / PIECES, at = 4 * piece;
             float s = 0.0f;
-            if (at < kdv * Z::K) {                     // (behind those no workgroup of the walks has written)
-                const f32x4 u4 = *reinterpret_cast<const f32x4*>(u + i * DK + at), r4 = *reinterpret_cast<const f32x4*>(dr + i * DK + at);
+            if (i < C && at < kdv * Z::K) {
                 if (i < valid && at < A.dv) {
-                    const T* const v = static_cast<const T*>(A.v) + (row + i) * A.ldv + (int64_t)h * A.dv + at;
                     T* const gv = static_cast<T*>(A.gv) + (row + i) * A.ldgv + (int64_t)h * A.dv + at;
                     const float bi = numbers[Z::kBeta + i];
-                    quad v4, g4;
-                    if (wv) {
-                        v4 = *reinterpret_cast<const quad*>(v);
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) v4[c] = at + c < A.dv ? v[c] : (T)0.0f;
-                    }
+                    quad g4;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        s = fmaf(r4[c], (float)v4[c], s);
-                        g4[c] = (T)(bi * r4[c]);
+                        s = fmaf(pr[n][c], at + c < A.dv ? (float)pv[n][c] : 0.0f, s);
+                        g4[c] = (T)(bi * pr[n][c]);
                     }
                     if (A.gv && wg) {
                         *reinterpret_cast<quad*>(gv) = g4;
@@ -1187,11 +1223,11 @@ k_delta_gradients(DeltaArgs A)
                             if (at + c < A.dv) gv[c] = g4[c];
                     }
                 }
-                put_parts<T, Z::PARTS>(Us + quad_at<T, ROW>(i, piece), Z::kBytesRows, u4);
-                put_parts<T, Z::PARTS>(Rs + quad_at<T, ROW>(i, piece), Z::kBytesRows, r4);
+                put_parts<T, Z::PARTS>(Us + quad_at<T, ROW>(i, piece), Z::kBytesRows, pu[n]);
+                put_parts<T, Z::PARTS>(Rs + quad_at<T, ROW>(i, piece), Z::kBytesRows, pr[n]);
             }
             for (int step = 1; step < PIECES; step <<= 1) s += __shfl_xor(s, step);
-            if (piece == 0) rv[i] = s;
+            if (piece == 0 && i < C) rv[i] = s;
         }
         if (x < C) {
             beta[x] = numbers[Z::kBeta + x]; gamma[x] = numbers[Z::kGamma + x]; tail[x] = numbers[Z::kTail + x];
@@ -1201,8 +1237,6 @@ k_delta_gradients(DeltaArgs A)
         for (int i = x; i < CT * C; i += THREADS) (&row_in[0][0])[i] = (&col_in[0][0])[i] = (&row_kk[0][0])[i] = 0.0f;
         __syncthreads();
 
-        // (formed anew for each head: places kept from before the loop would fill the registers)
-        const int l = here(lane), r16 = l & 15, g = l >> 4;
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
         // the maps: a lane holds rows i = 16 it + 4 g .. + 3 and column j = 16 jt + r16 of a tile
@@ -1228,6 +1262,7 @@ k_delta_gradients(DeltaArgs A)
             }
 #pragma unroll
             for (int m = 0; m < KD; ++m) {
+                if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
                 const frag kf = get<T>(Ks, rows.at(jt, m));
                 qk = mma(get<T>(Qs, rows.at(it, m)), kf, qk);
                 kk = mma(get<T>(Ks, rows.at(it, m)), kf, kk);
@@ -1259,73 +1294,86 @@ k_delta_gradients(DeltaArgs A)
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
             const int t0 = a * ACROSS + across;
-            f32x4 X1[CH], X2[CH], X3[CH];
+            f32x4 X1[CH], X2[CH];
 #pragma unroll
-            for (int t = 0; t < CH; ++t) X1[t] = X2[t] = X3[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            const float* const s0 = A.states_out + of * (int64_t)DK * DK + (16 * t0 + r16) * DK + 4 * g;
-            const float* const gs = A.gstates + of * (int64_t)DK * DK + (16 * t0 + r16) * DK + 4 * g;
-            // (G apart from S0: the parts of both at once do not fit the registers)
-            const auto ask = [&](f32x4* to, const float* from, int m) {
+            for (int t = 0; t < CH; ++t) X1[t] = X2[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int m0 = 0; m0 < kdv; m0 += AHEAD) {
+                if (a > 0 || m0 > 0) ask_state(s4, A.states_out, of, a, m0);
+                ask_state(g4, A.gstates, of, a, m0);
 #pragma unroll
-                for (int c = 0; c < Z::E / 4; ++c) to[c] = *reinterpret_cast<const f32x4*>(from + m * Z::K + 16 * c);
-            };
-            f32x4 s4[Z::E / 4], g4[Z::E / 4];          // what is asked for next
-            ask(s4, s0, 0);
-            ask(g4, gs, 0);
-#pragma unroll 1
-            for (int m = 0; m < kdv; ++m) {
-                float xs[Z::E];
+                for (int n = 0; n < AHEAD; ++n) {
+                    const int m = m0 + n;
+                    if (m >= kdv) continue;
+                    float xs[Z::E];
 #pragma unroll
-                for (int c = 0; c < Z::E; ++c) {
-                    xs[c] = s4[c >> 2][c & 3];
-                    state_sum = fmaf(xs[c], g4[c >> 2][c & 3], state_sum);
+                    for (int c = 0; c < Z::E; ++c) xs[c] = s4[n][c >> 2][c & 3];
+                    frag sf[Z::PARTS];
+                    parts_of<T, Z::PARTS>(xs, sf);
+#pragma unroll
+                    for (int t = 0; t < CH; ++t) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        const int tt = half * CH + t;
+                        const frag yf = get<T>(Ys, rows.at(tt, m));
+                        frag rf[Z::PARTS];
+#pragma unroll
+                        for (int p = 0; p < Z::PARTS; ++p) rf[p] = get<T>(Rs + p * Z::kBytesRows, rows.at(tt, m));
+#pragma unroll
+                        for (int p = Z::PARTS - 1; p >= 0; --p) X1[t] = mma(sf[p], yf, X1[t]);
+                        X2[t] = mma_parts<Z::PARTS>(sf, rf, X2[t]);
+                    }
                 }
-                frag sf[Z::PARTS];
-                parts_of<T, Z::PARTS>(xs, sf);
-                ask(g4, gs, m + 1 < kdv ? m + 1 : 0);
-                if (m + 1 < kdv) ask(s4, s0, m + 1);
 #pragma unroll
-                for (int t = 0; t < CH; ++t) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    const int tt = half * CH + t;
-                    const frag yf = get<T>(Ys, rows.at(tt, m));
+                for (int n = 0; n < AHEAD; ++n)
+                    if (m0 + n < kdv)
 #pragma unroll
-                    for (int p = Z::PARTS - 1; p >= 0; --p) X1[t] = mma(sf[p], yf, X1[t]);
-                    frag rf[Z::PARTS];
-#pragma unroll
-                    for (int p = 0; p < Z::PARTS; ++p) rf[p] = get<T>(Rs + p * Z::kBytesRows, rows.at(tt, m));
-                    X2[t] = mma_parts<Z::PARTS>(sf, rf, X2[t]);
-                }
-            }
-#pragma unroll 1
-            for (int m = 0; m < kdv; ++m) {
-                float xs[Z::E];
-#pragma unroll
-                for (int c = 0; c < Z::E; ++c) xs[c] = g4[c >> 2][c & 3];
-                frag gf[Z::PARTS];
-                parts_of<T, Z::PARTS>(xs, gf);
-                if (m + 1 < kdv) ask(g4, gs, m + 1);
-#pragma unroll
-                for (int t = 0; t < CH; ++t) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    frag uf[Z::PARTS];
-#pragma unroll
-                    for (int p = 0; p < Z::PARTS; ++p) uf[p] = get<T>(Us + p * Z::kBytesRows, rows.at(half * CH + t, m));
-                    X3[t] = mma_parts<Z::PARTS>(gf, uf, X3[t]);
-                }
+                        for (int c = 0; c < Z::E; ++c) state_sum = fmaf(s4[n][c >> 2][c & 3], g4[n][c >> 2][c & 3], state_sum);
             }
 #pragma unroll
             for (int t = 0; t < CH; ++t) {
                 const int i = 16 * (half * CH + t) + r16;
                 const quad q4 = *reinterpret_cast<const quad*>(Qs + quad_at<T, ROW>(i, 4 * t0 + g)), k4 = *reinterpret_cast<const quad*>(Ks + quad_at<T, ROW>(i, 4 * t0 + g));
-                const float c1 = A.scale * gamma[i], c2 = beta[i] * gamma[i], c3 = tail[i];
+                const float c1 = A.scale * gamma[i], c2 = beta[i] * gamma[i];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     q1[t] = fmaf((float)q4[r], X1[t][r], q1[t]);
                     k2[t] = fmaf((float)k4[r], X2[t][r], k2[t]);
-                    k3[t] = fmaf((float)k4[r], X3[t][r], k3[t]);
                     gq[a][t][r] = fmaf(c1, X1[t][r], gq[a][t][r]);
-                    gk[a][t][r] = fmaf(-c2, X2[t][r], fmaf(c3, X3[t][r], gk[a][t][r]));
+                    gk[a][t][r] = fmaf(-c2, X2[t][r], gk[a][t][r]);
+                }
+            }
+            f32x4 X3[CH];
+#pragma unroll
+            for (int t = 0; t < CH; ++t) X3[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int m0 = 0; m0 < kdv; m0 += AHEAD) {
+                if (kdv > AHEAD) ask_state(g4, A.gstates, of, a, m0);
+#pragma unroll
+                for (int n = 0; n < AHEAD; ++n) {
+                    const int m = m0 + n;
+                    if (m >= kdv) continue;
+                    float xs[Z::E];
+#pragma unroll
+                    for (int c = 0; c < Z::E; ++c) xs[c] = g4[n][c >> 2][c & 3];
+                    frag gf[Z::PARTS];
+                    parts_of<T, Z::PARTS>(xs, gf);
+#pragma unroll
+                    for (int t = 0; t < CH; ++t) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        frag uf[Z::PARTS];
+#pragma unroll
+                        for (int p = 0; p < Z::PARTS; ++p) uf[p] = get<T>(Us + p * Z::kBytesRows, rows.at(half * CH + t, m));
+                        X3[t] = mma_parts<Z::PARTS>(gf, uf, X3[t]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < CH; ++t) {
+                const int i = 16 * (half * CH + t) + r16;
+                const quad k4 = *reinterpret_cast<const quad*>(Ks + quad_at<T, ROW>(i, 4 * t0 + g));
+                const float c3 = tail[i];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    k3[t] = fmaf((float)k4[r], X3[t][r], k3[t]);
+                    gk[a][t][r] = fmaf(c3, X3[t][r], gk[a][t][r]);
                 }
             }
         }
@@ -1344,13 +1392,15 @@ k_delta_gradients(DeltaArgs A)
         if (lane == 0 && half == 0) state_dot[across] = state_sum;
         __syncthreads();                               // U and dR are done with
 
+        if (e + 1 < group) ask(h + 1);
         for (int p = x; p < kPatches; p += THREADS) {
             const int piece = p % (DK / 4), first = (p / (DK / 4)) * R;
             Patch<T> a, c;
-            load_patch(a, q, A.ldq, first, valid, piece * 4, A.dk, wq);
-            load_patch(c, k, A.ldk, first, valid, piece * 4, A.dk, wk);
-            keep_patch(a, first, valid, piece * 4, A.dk);
-            keep_patch(c, first, valid, piece * 4, A.dk);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                a.r[r] = *reinterpret_cast<const quad*>(Qs + quad_at<T, ROW>(first + r, piece));
+                c.r[r] = *reinterpret_cast<const quad*>(Ks + quad_at<T, ROW>(first + r, piece));
+            }
             put_turned<T, SEQ>(Qt, a, first, piece);
             put_turned<T, SEQ>(Kt, c, first, piece);
         }
@@ -1422,6 +1472,7 @@ k_delta_gradients(DeltaArgs A)
                 const frag kf = get<T>(Kt, columns.at(t0, m)), qf = get<T>(Qt, columns.at(t0, m));
 #pragma unroll
                 for (int t = 0; t < CH; ++t) {
+                    __builtin_amdgcn_sched_barrier(0);
                     const int tt = half * CH + t;
 #pragma unroll
                     for (int p = Z::SOME - 1; p >= 0; --p) {
@@ -1634,6 +1685,9 @@ dim3 grid_of(int64_t across, int64_t rows)
     return dim3((unsigned)across, (unsigned)(deep > 1 ? kRows : rows), (unsigned)deep);
 }
 
+// (one half: the registers of eight wavefronts hold the rows of both states that a head needs while it is prepared)
+template <typename T, int DK> constexpr int kHalves = 1;
+
 enum { kRunResults, kRunKeep, kRunStates, kRunBack, kRunBackStates };
 
 // WAVES: wavefronts of a walk's workgroup, 16 columns of the state each
@@ -1687,7 +1741,7 @@ hipError_t run_with(DeltaArgs A, bool cut, hipStream_t st)
     if (cut && e == hipSuccess) e = carry_with<DK>(A, true, st);
     if (e == hipSuccess) e = walks(kRunBack);
     if (e == hipSuccess && A.chunks > 0 && (A.gq || A.gk || A.gv || A.grates || A.gbeta)) {
-        constexpr int HALVES = Sizes<T, DK>::CT > 1 ? 2 : 1;
+        constexpr int HALVES = kHalves<T, DK>;
         profile_before("delta_gradients", st);
         hipLaunchKernelGGL((k_delta_gradients<T, DK, ACROSS, HALVES>), chunks, dim3(64 * ACROSS * HALVES), 0, st, A);
         profile_after("delta_gradients", st);
@@ -1730,8 +1784,10 @@ size_t delta_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, 
     return layout_of(bf16, tokens / c + sequences, several > 0 ? several + (sequences < several ? sequences : several) : 0, heads, dk, dv, training).all;
 }
 
-hipError_t launch_delta_tokens(const DeltaArgs& A, hipStream_t st)
+hipError_t launch_delta_tokens(const DeltaArgs& given, hipStream_t st)
 {
+    DeltaArgs A = given;
+    A.each = !A.starts && A.sequences > 0 ? A.tokens / A.sequences : 0;
     const bool aligned4 = A.dv % 4 == 0 && reinterpret_cast<uintptr_t>(A.state_in) % 16 == 0 && reinterpret_cast<uintptr_t>(A.state_out) % 16 == 0;
     const int vec = aligned4 ? 4 : 1, wide = (A.dv + vec - 1) / vec;
     // at most 16 lanes: 16 rows of the state for every thread then
@@ -1748,7 +1804,8 @@ hipError_t launch_delta(const DeltaArgs& given, hipStream_t st)
     DeltaArgs A = given;
     const int padded = padded_of(A.dk, A.dv), c = tokens_of_chunk(A.bf16, padded), size = A.bf16 ? 2 : 4;
     const bool training = !A.forward || A.saved;
-    A.per_sequence = !A.starts && A.sequences > 0 ? (A.tokens / A.sequences + c - 1) / c : 0;
+    A.each = !A.starts && A.sequences > 0 ? A.tokens / A.sequences : 0;
+    A.per_sequence = (A.each + c - 1) / c;
     A.chunks = chunks_of(A.tokens, A.sequences, c, A.starts == nullptr);
     const Cut P = cut_of(A.bf16, A.tokens, A.sequences, A.heads, A.dk, A.dv, A.starts == nullptr);
     A.stretch = P.stretch; A.stretches = P.per_sequence; A.slots = P.slots; A.training = training;

@@ -99,7 +99,7 @@ struct DeltaArgs {
     char* ws;
     // filled in by launch_delta
     int slices, wide;                // workgroups side by side over the columns; a bit each for q, k, v, y, gy, gq, gk: four numbers at a time
-    int64_t per_sequence, chunks;    // chunks of a sequence (equal lengths), of all, at most
+    int64_t each, per_sequence, chunks;      // tokens of a sequence (equal lengths); chunks of a sequence (equal lengths), of all, at most
     int64_t stretch, stretches, slots;       // tokens of a stretch that one workgroup walks; stretches of a sequence (equal lengths), of all, at most
     bool training;
     float *maps, *states_out, *u_out, *gstates, *r_out;
