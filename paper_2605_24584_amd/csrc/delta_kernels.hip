@@ -1142,24 +1142,24 @@ k_delta_gradients(DeltaArgs A)
 #pragma unroll
         for (int t = 0; t < CH; ++t) gq[a][t] = gk[a][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // What a head reads, all asked for at once: the rows of its chunk, and (as far as the registers reach) the wavefront's rows of the state.
+    // The rows that a head reads, all asked for at once.  (For the next head while this one's last products run they would not fit the registers.)
     constexpr int PIECES = DK <= 64 ? 16 : DK <= 128 ? 32 : 64, NP = (kPatches + THREADS - 1) / THREADS, NU = (C * PIECES + THREADS - 1) / THREADS;      // (PIECES threads of a wavefront have a token)
-    constexpr int AHEAD = DK <= 128 ? DK / Z::K : 4;   // fragments of a row of the states
+    constexpr int AHEAD = DK / Z::K % 4 == 0 ? 4 : DK / Z::K % 3 == 0 ? 3 : 2;   // fragments of a row of the states
     Patch<T> py[NP];
     f32x4 pu[NU], pr[NU], s4[AHEAD][Z::E / 4], g4[AHEAD][Z::E / 4];
-    quad pv[NU];
     const auto ask_state = [&](f32x4 (&to)[AHEAD][Z::E / 4], const float* states, int64_t of, int a, int m0) {
         const float* const from = states + of * (int64_t)DK * DK + (16 * (a * ACROSS + across) + r16) * DK + 4 * g;
 #pragma unroll
         for (int m = 0; m < AHEAD; ++m)
-            if (m0 + m < kdv)
 #pragma unroll
-                for (int c = 0; c < Z::E / 4; ++c) to[m][c] = *reinterpret_cast<const f32x4*>(from + (m0 + m) * Z::K + 16 * c);
+            for (int c = 0; c < Z::E / 4; ++c) {
+                to[m][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};      // (behind those no workgroup of the walks has written)
+                if (m0 + m < kdv) to[m][c] = *reinterpret_cast<const f32x4*>(from + (m0 + m) * Z::K + 16 * c);
+            }
     };
     const auto ask = [&](int h) {
         const int64_t of = chunk * A.heads + h;
         const T* const gy = static_cast<const T*>(A.gy) + row * A.ldgy + (int64_t)h * A.dv;
-        const T* const v = static_cast<const T*>(A.v) + row * A.ldv + (int64_t)h * A.dv;
         const float* const u = A.u_out + of * (int64_t)C * DK;
         const float* const dr = A.r_out + of * (int64_t)C * DK;
         const int y = here(x);
@@ -1171,26 +1171,35 @@ k_delta_gradients(DeltaArgs A)
 #pragma unroll
         for (int n = 0; n < NU; ++n) {
             const int p = y + n * THREADS, at = p % PIECES * 4, i = p / PIECES;
-            if (i >= C || at >= kdv * Z::K) continue;  // (behind those no workgroup of the walks has written)
+            pu[n] = pr[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (i >= C || at >= kdv * Z::K) continue;
             pu[n] = *reinterpret_cast<const f32x4*>(u + i * DK + at);
             pr[n] = *reinterpret_cast<const f32x4*>(dr + i * DK + at);
-            if (i >= valid || at >= A.dv) continue;
-            if (wv) {
-                pv[n] = *reinterpret_cast<const quad*>(v + i * A.ldv + at);
-            } else {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) pv[n][c] = v[i * A.ldv + (at + c < A.dv ? at + c : A.dv - 1)];
-            }
         }
-        ask_state(s4, A.states_out, of, 0, 0);
     };
-    ask(kh * group);
     for (int e = 0; e < group; ++e) {
         const int h = kh * group + e;
         const int64_t of = chunk * A.heads + h;
         const float* const numbers = A.maps + of * Z::kNumbers;
         // (formed anew for each head: places kept from before the loop would fill the registers)
         const int x = here(threadIdx.x), lane = x & 63, r16 = lane & 15, g = lane >> 4;
+        const T* const v = static_cast<const T*>(A.v) + row * A.ldv + (int64_t)h * A.dv;
+        quad pv[NU];
+        ask(h);
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+            const int p = x + n * THREADS, at = p % PIECES * 4, i = p / PIECES;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) pv[n][c] = (T)0.0f;
+            if (i >= valid || at >= A.dv) continue;
+            if (wv) {
+                pv[n] = *reinterpret_cast<const quad*>(v + i * A.ldv + at);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (at + c < A.dv) pv[n][c] = v[i * A.ldv + at + c];
+            }
+        }
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
@@ -1205,14 +1214,14 @@ k_delta_gradients(DeltaArgs A)
         for (int n = 0; n < NU; ++n) {
             const int p = x + n * THREADS, piece = p % PIECES, i = p / PIECES, at = 4 * piece;
             float s = 0.0f;
-            if (i < C && at < kdv * Z::K) {
+            if (i < C && piece < DK / 4) {
                 if (i < valid && at < A.dv) {
                     T* const gv = static_cast<T*>(A.gv) + (row + i) * A.ldgv + (int64_t)h * A.dv + at;
                     const float bi = numbers[Z::kBeta + i];
                     quad g4;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        s = fmaf(pr[n][c], at + c < A.dv ? (float)pv[n][c] : 0.0f, s);
+                        s = fmaf(pr[n][c], (float)pv[n][c], s);
                         g4[c] = (T)(bi * pr[n][c]);
                     }
                     if (A.gv && wg) {
@@ -1229,6 +1238,7 @@ k_delta_gradients(DeltaArgs A)
             for (int step = 1; step < PIECES; step <<= 1) s += __shfl_xor(s, step);
             if (piece == 0 && i < C) rv[i] = s;
         }
+        ask_state(s4, A.states_out, of, 0, 0);         // (on its way while the maps are formed)
         if (x < C) {
             beta[x] = numbers[Z::kBeta + x]; gamma[x] = numbers[Z::kGamma + x]; tail[x] = numbers[Z::kTail + x];
             high[x] = numbers[Z::kHigh + x]; low[x] = numbers[Z::kLow + x];
@@ -1249,8 +1259,8 @@ k_delta_gradients(DeltaArgs A)
             N[n] = M[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if (it >= CT) continue;
             f32x4 qk = {0.0f, 0.0f, 0.0f, 0.0f}, kk = qk;
-#pragma unroll 1
-            for (int m = 0; m < kdv; ++m) {
+#pragma unroll 2
+            for (int m = 0; m < DK / Z::K; ++m) {
                 frag uf[Z::PARTS], rf[Z::PARTS];
 #pragma unroll
                 for (int p = 0; p < Z::PARTS; ++p) {
@@ -1297,13 +1307,13 @@ k_delta_gradients(DeltaArgs A)
             f32x4 X1[CH], X2[CH];
 #pragma unroll
             for (int t = 0; t < CH; ++t) X1[t] = X2[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            for (int m0 = 0; m0 < kdv; m0 += AHEAD) {
+#pragma unroll 1
+            for (int m0 = 0; m0 < DK / Z::K; m0 += AHEAD) {
                 if (a > 0 || m0 > 0) ask_state(s4, A.states_out, of, a, m0);
                 ask_state(g4, A.gstates, of, a, m0);
 #pragma unroll
                 for (int n = 0; n < AHEAD; ++n) {
                     const int m = m0 + n;
-                    if (m >= kdv) continue;
                     float xs[Z::E];
 #pragma unroll
                     for (int c = 0; c < Z::E; ++c) xs[c] = s4[n][c >> 2][c & 3];
@@ -1324,9 +1334,8 @@ k_delta_gradients(DeltaArgs A)
                 }
 #pragma unroll
                 for (int n = 0; n < AHEAD; ++n)
-                    if (m0 + n < kdv)
 #pragma unroll
-                        for (int c = 0; c < Z::E; ++c) state_sum = fmaf(s4[n][c >> 2][c & 3], g4[n][c >> 2][c & 3], state_sum);
+                    for (int c = 0; c < Z::E; ++c) state_sum = fmaf(s4[n][c >> 2][c & 3], g4[n][c >> 2][c & 3], state_sum);
             }
 #pragma unroll
             for (int t = 0; t < CH; ++t) {
@@ -1344,12 +1353,12 @@ k_delta_gradients(DeltaArgs A)
             f32x4 X3[CH];
 #pragma unroll
             for (int t = 0; t < CH; ++t) X3[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            for (int m0 = 0; m0 < kdv; m0 += AHEAD) {
-                if (kdv > AHEAD) ask_state(g4, A.gstates, of, a, m0);
+#pragma unroll 1
+            for (int m0 = 0; m0 < DK / Z::K; m0 += AHEAD) {
+                if (DK / Z::K > AHEAD) ask_state(g4, A.gstates, of, a, m0);
 #pragma unroll
                 for (int n = 0; n < AHEAD; ++n) {
                     const int m = m0 + n;
-                    if (m >= kdv) continue;
                     float xs[Z::E];
 #pragma unroll
                     for (int c = 0; c < Z::E; ++c) xs[c] = g4[n][c >> 2][c & 3];
@@ -1392,7 +1401,6 @@ k_delta_gradients(DeltaArgs A)
         if (lane == 0 && half == 0) state_dot[across] = state_sum;
         __syncthreads();                               // U and dR are done with
 
-        if (e + 1 < group) ask(h + 1);
         for (int p = x; p < kPatches; p += THREADS) {
             const int piece = p % (DK / 4), first = (p / (DK / 4)) * R;
             Patch<T> a, c;
