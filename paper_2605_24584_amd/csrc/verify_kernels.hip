@@ -18,32 +18,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroup = 8;                 // rows that a thread has asked for at a time
-constexpr int kMaxParts = 256, kWorkgroups = 4096, kSlab = 128;      // parts of the rows; workgroups that are enough for a matrix; columns of a workgroup
+constexpr int kMaxParts = 256, kWorkgroups = 4096, kSlab = 64;      // parts of the rows; workgroups that are enough for a matrix; columns of a workgroup
 
-template <typename T, int VEC> struct Lane;
-template <> struct Lane<float, 1> { typedef float type __attribute__((ext_vector_type(1))); };
-template <> struct Lane<__bf16, 1> { typedef __bf16 type __attribute__((ext_vector_type(1))); };
-template <> struct Lane<float, 2> { typedef float type __attribute__((ext_vector_type(2), aligned(4))); };
-template <> struct Lane<__bf16, 2> { typedef __bf16 type __attribute__((ext_vector_type(2), aligned(2))); };
-
-// `have` of the VEC columns at p exist
-template <typename T, int VEC>
-__device__ __forceinline__ void load_columns(float* out, const T* p, int have)
+// 2^t, t <= 0 and finite; 0 below 2^-1074
+__device__ __forceinline__ double power_in_range(double t)
 {
-    if (have >= VEC) {
-        const typename Lane<T, VEC>::type v = *reinterpret_cast<const typename Lane<T, VEC>::type*>(p);
-#pragma unroll
-        for (int c = 0; c < VEC; ++c) out[c] = (float)v[c];
-    } else {
-#pragma unroll
-        for (int c = 0; c < VEC; ++c) out[c] = c < have ? to_float(p[c]) : -INFINITY;
-    }
-}
-
-// 2^t, t <= 0 (NaN for NaN)
-__device__ __forceinline__ double power_of_two(double t)
-{
-    if (t < -1100.0) return 0.0;
     const double n = __builtin_rint(t), f = t - n;
     double s = 0x1.816193166d0f9p-40;                          // log(2)^13 / 13!, then 12, ...
     s = fma(s, f, 0x1.c3bd650fc2986p-36);
@@ -61,6 +40,9 @@ __device__ __forceinline__ double power_of_two(double t)
     s = fma(s, f, 1.0);
     return __builtin_ldexp(s, (int)n);
 }
+
+// 2^t, t <= 0 (NaN for NaN)
+__device__ __forceinline__ double power_of_two(double t) { return t < -1100.0 ? 0.0 : power_in_range(t); }
 
 // 2^(c (y - m)) of a logit below the maximum m, which is finite or -inf (then there is nothing but -inf)
 __device__ __forceinline__ double weight_of(float y, float m, double c)
@@ -87,81 +69,83 @@ __device__ __forceinline__ double shuffle(double v, int step)
 // ----------------------------------------------------------------------------
 // The pass over a matrix: 2^lanes_log2 lanes across the columns, the rest of the workgroup across groups of rows; a part is a range of consecutive rows.
 // ----------------------------------------------------------------------------
-template <typename T, int VEC, bool PLACE>
+template <typename T, bool PLACE>
 __global__ void __launch_bounds__(kThreads)
 k_verify_rows(VerifyArgs A)
 {
-    __shared__ Sum side[kThreads / 64][64][VEC];
-    __shared__ int64_t side_at[kThreads / 64][PLACE ? 64 : 1][VEC];
+    __shared__ Sum side[kThreads / 64][64];
+    __shared__ int64_t side_at[kThreads / 64][PLACE ? 64 : 1];
     const int lanes = 1 << A.lanes_log2, x = threadIdx.x, column_lane = x & (lanes - 1), row_lane = x >> A.lanes_log2, row_lanes = kThreads >> A.lanes_log2;
     const int64_t slab = blockIdx.x, part = blockIdx.y;
     const int which = blockIdx.z;
-    const T* const y = static_cast<const T*>(which ? A.z : A.y);
-    const int64_t ld = which ? A.ldz : A.ldy, t = (slab * lanes + column_lane) * VEC;
+    const int64_t ld = which ? A.ldz : A.ldy, t = slab * lanes + column_lane;
+    const T* const y = static_cast<const T*>(which ? A.z : A.y) + t;
     const double c = which ? A.draft_c : A.c;
-    const int have = A.batch - t >= VEC ? VEC : A.batch > t ? (int)(A.batch - t) : 0;
-    Sum st[VEC];
-    int64_t place[VEC];
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) { st[v] = Sum{-INFINITY, 0.0}; place[v] = INT64_MAX; }
+    const float far = (float)(1200.0 / c);
+    const int64_t first = part * A.part_rows + (int64_t)row_lane * kGroup, step = (int64_t)row_lanes * kGroup;
     const int64_t end = (part + 1) * A.part_rows < A.k ? (part + 1) * A.part_rows : A.k;
-    if (have > 0)
-        for (int64_t row = part * A.part_rows + (int64_t)row_lane * kGroup; row < end; row += (int64_t)row_lanes * kGroup) {
-            const T* const p = y + row * ld + t;
+    Sum st{-INFINITY, 0.0};
+    int64_t place = INT64_MAX;
+    float ahead[kGroup];                               // the next rows are on their way while these are summed
+    const auto ask = [&](int64_t row) {
+        const T* const p = y + row * ld;
+        const int rows = end - row < kGroup ? (int)(end - row) : kGroup;
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) ahead[i] = to_float(p[(i < rows ? i : 0) * ld]);
+    };
+    if (t < A.batch && first < end) {
+        ask(first);
+        for (int64_t row = first; row < end; row += step) {
             const int rows = end - row < kGroup ? (int)(end - row) : kGroup;
-            float v[kGroup][VEC];
+            float v[kGroup], m = -INFINITY;
+            bool bad = false;                          // NaN or +inf
 #pragma unroll
-            for (int i = 0; i < kGroup; ++i) load_columns<T, VEC>(v[i], p + (i < rows ? i : 0) * ld, have);
+            for (int i = 0; i < kGroup; ++i) v[i] = i < rows ? ahead[i] : -INFINITY;
+            if (row + step < end) ask(row + step);
 #pragma unroll
-            for (int q = 0; q < VEC; ++q) {
-                float m = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < kGroup; ++i) {
-                    if (i >= rows) v[i][q] = -INFINITY;
-                    if (v[i][q] < INFINITY) {
-                        if (PLACE && v[i][q] > m && v[i][q] > st[q].m) place[q] = row + i;
-                        m = fmaxf(m, v[i][q]);
-                    }
-                }
-                if (m > st[q].m) {
-                    st[q].s *= weight_of(st[q].m, m, c);
-                    st[q].m = m;
-                }
-#pragma unroll
-                for (int i = 0; i < kGroup; ++i) st[q].s += v[i][q] < INFINITY ? weight_of(v[i][q], st[q].m, c) : (double)NAN;
+            for (int i = 0; i < kGroup; ++i) {
+                bad = bad || !(v[i] < INFINITY);
+                if (PLACE && v[i] > m && v[i] > st.m) place = row + i;
+                m = fmaxf(m, v[i]);
             }
+            if (m > st.m) {
+                st.s *= weight_of(st.m, m, c);
+                st.m = m;
+            }
+            // What is so far below the maximum that its weight is 0 is brought nearer, to where it is still 0: no further test in 64 bits.
+            const float reach = st.m - far;
+            if (reach > -3.4e38f) {
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) st.s += power_in_range(((double)fmaxf(v[i], reach) - (double)st.m) * c);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) st.s += weight_of(v[i], st.m, c);
+            }
+            if (bad) st.s = NAN;
         }
+    }
     const auto both = [&](Sum& a, int64_t& at, Sum b, int64_t bt) {
         if (PLACE) at = b.m > a.m || (b.m == a.m && bt < at) ? bt : at;
         a = join(a, b, c);
     };
-#pragma unroll
-    for (int q = 0; q < VEC; ++q)
-        for (int step = lanes; step < 64; step <<= 1) {
-            const Sum other{__shfl_xor(st[q].m, step), shuffle(st[q].s, step)};
-            int64_t at = 0;
-            if (PLACE) at = __double_as_longlong(shuffle(__longlong_as_double(place[q]), step));
-            both(st[q], place[q], other, at);
-        }
-#pragma unroll
-    for (int q = 0; q < VEC; ++q) {
-        side[x >> 6][x & 63][q] = st[q];
-        if (PLACE) side_at[x >> 6][PLACE ? x & 63 : 0][q] = place[q];
+    for (int step = lanes; step < 64; step <<= 1) {
+        const Sum other{__shfl_xor(st.m, step), shuffle(st.s, step)};
+        int64_t at = 0;
+        if (PLACE) at = __double_as_longlong(shuffle(__longlong_as_double(place), step));
+        both(st, place, other, at);
     }
+    side[x >> 6][x & 63] = st;
+    if (PLACE) side_at[x >> 6][PLACE ? x & 63 : 0] = place;
     __syncthreads();
-    if (x < lanes)
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            Sum all = side[0][x][q];
-            int64_t at = PLACE ? side_at[0][PLACE ? x : 0][q] : 0;
-            for (int w = 1; w < kThreads / 64; ++w) both(all, at, side[w][x][q], PLACE ? side_at[w][PLACE ? x : 0][q] : 0);
-            if (q < have) {
-                const int64_t to = (which * A.parts + part) * A.batch + t + q;
-                A.part_max[to] = all.m;
-                A.part_sum[to] = all.s;
-                if (PLACE) A.part_place[to] = at;
-            }
-        }
+    if (x < lanes && t < A.batch) {
+        Sum all = side[0][x];
+        int64_t at = PLACE ? side_at[0][PLACE ? x : 0] : 0;
+        for (int w = 1; w < kThreads / 64; ++w) both(all, at, side[w][x], PLACE ? side_at[w][PLACE ? x : 0] : 0);
+        const int64_t to = (which * A.parts + part) * A.batch + t;
+        A.part_max[to] = all.m;
+        A.part_sum[to] = all.s;
+        if (PLACE) A.part_place[to] = at;
+    }
 }
 
 __device__ __forceinline__ int64_t start_of(const VerifyArgs& A, int64_t b)
@@ -208,30 +192,45 @@ k_verify_judge(VerifyArgs A)
         }
         return;
     }
-    Sum sum[2] = {{-INFINITY, 0.0}, {-INFINITY, 0.0}};
-    int64_t place = INT64_MAX;
+    // the parts of both matrices: the largest maximum first, then every part's sum once
+    constexpr int N = kMaxParts / 64;
+    float m[2][N];
+    double s[2][N];
+    int64_t at[N];
     const int matrices = A.z ? 2 : 1;
-    for (int which = 0; which < matrices; ++which) {
-        const double c = which ? A.draft_c : A.c;
-        Sum all{-INFINITY, 0.0};
-        for (int64_t p = lane; p < A.parts; p += 64) {
-            const int64_t from = (which * A.parts + p) * A.batch + t;
-            const Sum one{A.part_max[from], A.part_sum[from]};
-            if (PLACE) {
-                const int64_t at = A.part_place[from];
-                place = one.m > all.m || (one.m == all.m && at < place) ? at : place;
-            }
-            all = join(all, one, c);
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int64_t p = n * 64 + lane, from = (which * A.parts + p) * A.batch + t;
+            const bool there = which < matrices && p < A.parts;
+            m[which][n] = there ? A.part_max[from] : -INFINITY;
+            s[which][n] = there ? A.part_sum[from] : 0.0;
+            if (PLACE && which == 0) at[n] = there ? A.part_place[from] : INT64_MAX;
         }
+    Sum sum[2];
+    int64_t place = INT64_MAX;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float most = m[which][0];
+#pragma unroll
+        for (int n = 1; n < N; ++n) most = fmaxf(most, m[which][n]);
+        for (int step = 1; step < 64; step <<= 1) most = fmaxf(most, __shfl_xor(most, step));
+        double all = 0.0;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (m[which][n] > -INFINITY || s[which][n] != 0.0) all += s[which][n] * weight_of(m[which][n], most, which ? A.draft_c : A.c);
+        for (int step = 1; step < 64; step <<= 1) all += shuffle(all, step);
+        sum[which] = Sum{most, all};
+    }
+    if (PLACE) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (m[0][n] == sum[0].m && at[n] < place) place = at[n];
         for (int step = 1; step < 64; step <<= 1) {
-            const Sum other{__shfl_xor(all.m, step), shuffle(all.s, step)};
-            if (PLACE) {
-                const int64_t at = __double_as_longlong(shuffle(__longlong_as_double(place), step));
-                place = other.m > all.m || (other.m == all.m && at < place) ? at : place;
-            }
-            all = join(all, other, c);
+            const int64_t other = __double_as_longlong(shuffle(__longlong_as_double(place), step));
+            place = other < place ? other : place;
         }
-        sum[which] = all;
     }
     if (lane != 0) return;
     const bool fine = sum[0].s > 0.0, draft_fine = !A.z || sum[1].s > 0.0;      // not of a NaN, +inf or nothing but -inf
@@ -280,9 +279,10 @@ __device__ __forceinline__ void find_drawn(const VerifyArgs& A, int64_t b0, int 
     __syncthreads();
 }
 
-__device__ __forceinline__ double left_of(const VerifyArgs& A, const VerifyColumn& C, float y, float z)
+// share, draft_share: one over the columns' sums
+__device__ __forceinline__ double left_of(const VerifyArgs& A, const VerifyColumn& C, double share, double draft_share, float y, float z)
 {
-    const double p = weight_of(y, C.m, A.c) / C.s, q = weight_of(z, C.draft_m, A.draft_c) / C.draft_s, d = p - q;
+    const double p = weight_of(y, C.m, A.c) * share, q = weight_of(z, C.draft_m, A.draft_c) * draft_share, d = p - q;
     return d > 0.0 ? d : 0.0;
 }
 
@@ -296,7 +296,7 @@ k_verify_left(VerifyArgs A)
     __shared__ int drawn[16];
     __shared__ double side[kThreads];
     const int width = 1 << A.seq_log2, x = threadIdx.x;
-    const int64_t b0 = (int64_t)blockIdx.x * width, part = blockIdx.y;
+    const int64_t b0 = (int64_t)blockIdx.x * width;
     find_drawn(A, b0, A.seq_log2, drawn);
     const int mine = x & (width - 1), rows = kThreads >> A.seq_log2;
     if (x < width) {
@@ -304,25 +304,26 @@ k_verify_left(VerifyArgs A)
         if (drawn[x] >= 0 && of[x].mode != kVerifyLeft) drawn[x] = -1;
     }
     __syncthreads();
-    const int64_t t = drawn[mine], end = (part + 1) * A.part_rows < A.k ? (part + 1) * A.part_rows : A.k;
+    const int64_t t = drawn[mine], part = blockIdx.y, end = (part + 1) * A.part_rows < A.k ? (part + 1) * A.part_rows : A.k;
+    VerifyColumn C{};
+    if (t >= 0) C = of[mine];
+    const double share = 1.0 / C.s, draft_share = 1.0 / C.draft_s;
+    const T* const y = static_cast<const T*>(A.y) + (t >= 0 ? t : 0);
+    const T* const z = static_cast<const T*>(A.z) + (t >= 0 ? t : 0);
     double sum = 0.0;
-    if (t >= 0) {
-        const VerifyColumn C = of[mine];
-        const T* const y = static_cast<const T*>(A.y) + t;
-        const T* const z = static_cast<const T*>(A.z) + t;
-        for (int64_t r0 = part * A.part_rows + (x >> A.seq_log2); r0 < end; r0 += 4 * rows) {
-            float p[4], q[4];
+    if (t >= 0)
+        for (int64_t r0 = part * A.part_rows + (x >> A.seq_log2); r0 < end; r0 += 8 * rows) {
+            float p[8], q[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 const int64_t r = r0 + i * rows < end ? r0 + i * rows : r0;
                 p[i] = to_float(y[r * A.ldy]);
                 q[i] = to_float(z[r * A.ldz]);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (r0 + i * rows < end) sum += left_of(A, C, p[i], q[i]);
+            for (int i = 0; i < 8; ++i)
+                if (r0 + i * rows < end) sum += left_of(A, C, share, draft_share, p[i], q[i]);
         }
-    }
     side[x] = sum;
     __syncthreads();
     if (x < width && t >= 0) {
@@ -378,15 +379,16 @@ k_verify_draw(VerifyArgs A)
         return;
     }
     const int64_t draft = C.mode == kVerifyOthers ? A.drafts[t] : -1;
+    const double share = 1.0 / C.s, draft_share = 1.0 / C.draft_s;
     const double chance = A.next_chances[b];
     // the weights of the parts of the rows: a thread each
     const auto part_weight = [&](int mode) {
         if (x >= A.parts) return 0.0;
         if (mode == kVerifyLeft) return A.left[x * A.sequences + b];
         const float m = A.part_max[x * A.batch + t];
-        double w = A.part_sum[x * A.batch + t] * weight_of(m, C.m, A.c) / C.s;
+        double w = A.part_sum[x * A.batch + t] * weight_of(m, C.m, A.c) * share;
         if (mode == kVerifyOthers && draft / A.part_rows == x) {
-            w -= weight_of(to_float(static_cast<const T*>(A.y)[draft * A.ldy + t]), C.m, A.c) / C.s;
+            w -= weight_of(to_float(static_cast<const T*>(A.y)[draft * A.ldy + t]), C.m, A.c) * share;
             w = w > 0.0 ? w : 0.0;
         }
         return w;
@@ -418,8 +420,8 @@ k_verify_draw(VerifyArgs A)
     const int64_t each = (end - begin + kThreads - 1) / kThreads, r0 = begin + x * each, r1 = r0 + each < end ? r0 + each : end;
     const auto row_weight = [&](int64_t r) {
         const float y = to_float(static_cast<const T*>(A.y)[r * A.ldy + t]);
-        if (mode == kVerifyLeft) return left_of(A, C, y, to_float(static_cast<const T*>(A.z)[r * A.ldz + t]));
-        return mode == kVerifyOthers && r == draft ? 0.0 : weight_of(y, C.m, A.c) / C.s;
+        if (mode == kVerifyLeft) return left_of(A, C, share, draft_share, y, to_float(static_cast<const T*>(A.z)[r * A.ldz + t]));
+        return mode == kVerifyOthers && r == draft ? 0.0 : weight_of(y, C.m, A.c) * share;
     };
     double rows = 0.0;
     for (int64_t r = r0; r < r1; ++r) rows += row_weight(r);
@@ -442,15 +444,14 @@ k_verify_draw(VerifyArgs A)
     }
 }
 
-struct Plan { int lanes_log2, vec; int64_t slabs, part_rows, parts; };
+struct Plan { int lanes_log2; int64_t slabs, part_rows, parts; };
 
 Plan plan_of(int64_t k, int64_t batch)
 {
     Plan P;
-    P.vec = batch >= 64 ? 2 : 1;
     P.lanes_log2 = 0;
-    while (P.lanes_log2 < 6 && (int64_t(P.vec) << P.lanes_log2) < batch) ++P.lanes_log2;
-    P.slabs = (batch + (int64_t(P.vec) << P.lanes_log2) - 1) / (int64_t(P.vec) << P.lanes_log2);
+    while (P.lanes_log2 < 6 && (1 << P.lanes_log2) < batch) ++P.lanes_log2;
+    P.slabs = (batch + (1 << P.lanes_log2) - 1) >> P.lanes_log2;
     const int64_t at_once = (int64_t)(kThreads >> P.lanes_log2) * kGroup;
     int64_t parts = (k + at_once - 1) / at_once;
     if (parts > kMaxParts) parts = kMaxParts;
@@ -490,13 +491,8 @@ static hipError_t launch_verify_of(const VerifyArgs& A, const Plan& P, hipStream
     const dim3 grid((unsigned)P.slabs, (unsigned)P.parts, A.z ? 2 : 1), block(kThreads);
     const bool place = A.part_place != nullptr;
     profile_before("verify_rows", st);
-    if (P.vec == 2) {
-        if (place) hipLaunchKernelGGL((k_verify_rows<T, 2, true>), grid, block, 0, st, A);
-        else hipLaunchKernelGGL((k_verify_rows<T, 2, false>), grid, block, 0, st, A);
-    } else {
-        if (place) hipLaunchKernelGGL((k_verify_rows<T, 1, true>), grid, block, 0, st, A);
-        else hipLaunchKernelGGL((k_verify_rows<T, 1, false>), grid, block, 0, st, A);
-    }
+    if (place) hipLaunchKernelGGL((k_verify_rows<T, true>), grid, block, 0, st, A);
+    else hipLaunchKernelGGL((k_verify_rows<T, false>), grid, block, 0, st, A);
     profile_after("verify_rows", st);
     const dim3 columns((unsigned)((A.batch + kThreads / 64 - 1) / (kThreads / 64)));
     profile_before("verify_judge", st);
