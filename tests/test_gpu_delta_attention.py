@@ -150,7 +150,8 @@ SHAPES = [
     ([1], 1, 1, 1, 1, False), ([1, 1, 1], 2, 1, 16, 16, False), ([5], 3, 3, 7, 9, False), ([16], 1, 1, 32, 32, False), ([17, 0, 1, 64, 65], 2, 2, 20, 33, True),
     ([63], 2, 1, 64, 64, False), ([64, 64], 2, 2, 64, 64, False), ([130], 1, 1, 128, 128, False), ([200, 3, 0, 0, 129], 4, 2, 96, 80, True),
     ([150], 1, 1, 256, 256, False), ([70], 2, 1, 256, 40, False), ([95], 1, 1, 40, 256, False), ([0, 0], 2, 2, 8, 8, True), ([400, 213], 1, 1, 48, 100, True),
-    ([97, 65], 2, 2, 129, 65, True), ([33, 100], 3, 1, 192, 150, True), ([32, 31, 15, 16, 48], 2, 2, 128, 96, True), ([700], 2, 1, 64, 128, False),
+    ([97, 65], 2, 2, 129, 65, True), ([33, 100], 3, 1, 192, 150, True), ([32, 31, 15, 16, 48], 2, 2, 128, 96, True), ([700], 2, 1, 64, 128, False), ([12, 12, 12], 4, 2, 128, 128, False), ([13, 13], 2, 2, 128, 128, False), ([9] * 3, 2, 1, 256, 33, False), ([11], 1, 1, 100, 256, False),
+    ([10] * 70, 4, 4, 64, 64, False),
 ]
 
 
