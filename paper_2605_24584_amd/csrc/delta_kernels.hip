@@ -56,6 +56,13 @@ __device__ __forceinline__ int64_t first_unit(const DeltaArgs& A, int64_t b, int
 template <int C>
 __device__ __forceinline__ int64_t first_chunk(const DeltaArgs& A, int64_t b, int64_t begin) { return first_unit(A, b, begin, C, A.per_sequence); }
 
+// a whole number that all lanes hold
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
 // The unit with this number: its sequence and its number there.  By a wavefront.
 struct Unit { int64_t b, index, begin, count; };      // begin, count: the sequence's rows
 __device__ __forceinline__ Unit find_unit(const DeltaArgs& A, int64_t unit, int64_t size, int64_t per_sequence)
@@ -76,10 +83,10 @@ __device__ __forceinline__ Unit find_unit(const DeltaArgs& A, int64_t unit, int6
         lo = (uint32_t)unit / (uint32_t)per_sequence;
     }
     Unit u;
-    u.b = lo;
-    u.begin = start_of(A, lo);
-    u.count = count_of(A, lo, u.begin);
-    u.index = unit - first_unit(A, lo, u.begin, size, per_sequence);
+    u.b = uniform(lo);
+    u.begin = uniform(start_of(A, u.b));
+    u.count = uniform(count_of(A, u.b, u.begin));
+    u.index = uniform(unit - first_unit(A, u.b, u.begin, size, per_sequence));
     return u;
 }
 
@@ -186,15 +193,17 @@ __device__ __forceinline__ int quad_at(int row, int p)
     return 16 * slot_at<SLOTS>(row, p);
 }
 
-// The patch's columns as rows, tokens along the slots in that order.
+// The patch's columns as rows, tokens along the slots in that order.  (The permutation of row 4 piece + e is that of row 4 piece, changed by e alone.)
 template <typename T, int SLOTS>
 __device__ __forceinline__ void put_turned(char* tile, const Patch<T>& p, int first, int piece)
 {
+    const int quad = first >> 2, slot = sizeof(T) == 2 ? (quad >> 3) * 4 + (quad & 3) : quad, low = slot ^ twist<SLOTS>(piece * 4);
+    char* const at = tile + piece * 4 * SLOTS * 16 + (sizeof(T) == 2 ? 8 * ((quad >> 2) & 1) : (first & 2) * 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        char* const at = tile + quad_at<T, SLOTS>(piece * 4 + e, first >> 2);
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4*>(at) = bf16x4{p.r[0][e], p.r[1][e], p.r[2][e], p.r[3][e]};
-        else *reinterpret_cast<f32x2*>(at + (first & 2) * 4) = f32x2{p.r[0][e], p.r[1][e]};
+        char* const to = at + e * SLOTS * 16 + 16 * (low ^ (SLOTS >= 8 ? e : (e >> 1)));
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4*>(to) = bf16x4{p.r[0][e], p.r[1][e], p.r[2][e], p.r[3][e]};
+        else *reinterpret_cast<f32x2*>(to) = f32x2{p.r[0][e], p.r[1][e]};
     }
 }
 
@@ -223,6 +232,17 @@ __device__ __forceinline__ void put_parts(char* at, int size, f32x4 v)
 // How a matrix is read: kSome a number at a time, kWide four at a time, kWhole so where all of them exist.
 enum { kSome, kWide, kWhole };
 __device__ __forceinline__ int how(bool wide, bool whole) { return !wide ? kSome : whole ? kWhole : kWide; }
+
+// Accumulators to rows of `stride` numbers from base on, which all lanes share: rows 16 t + 4 g + r, column col.
+template <int TILES>
+__device__ __forceinline__ void store_tiles(float* base, const f32x4* acc, int stride, int g, int col)
+{
+    const uint32_t at = 4 * g * stride + col;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) *reinterpret_cast<float*>(reinterpret_cast<char*>(base) + (at + (16 * t + r) * stride) * 4u) = acc[t][r];
+}
 
 template <typename T>
 __device__ __forceinline__ void put_number(char* at, T v) { *reinterpret_cast<T*>(at) = v; }
@@ -270,13 +290,17 @@ __device__ __forceinline__ float decay_of(float high_i, float low_i, float high_
 // T by blocks of 16: those on the diagonal by substitution, a lane to a column; T_ij = -T_ii sum_{j <= m < i} A_im T_mj, a wavefront to a column of blocks.
 // ----------------------------------------------------------------------------
 template <typename T, int DK>
-__global__ void __launch_bounds__(kPrepareThreads)
+__global__ void __launch_bounds__(kPrepareThreads, 4)
 k_delta_prepare(DeltaArgs A)
 {
     typedef Sizes<T, DK> Z;
     constexpr int C = Z::C, CT = Z::CT, R = Z::R, WAVES = kPrepareThreads / 64, PAD = C + 4;
-    __shared__ __attribute__((aligned(16))) char Ks[Z::kBytesRows], Qs[Z::kBytesRows];
-    __shared__ __attribute__((aligned(16))) float map[C * PAD], diagonal[CT][16][20];
+    // the keys and queries, and in their place, when their products are formed, A and the inverses of its blocks
+    constexpr int kMap = C * PAD * 4, kDiagonal = CT * 16 * 20 * 4, kBytes = 2 * Z::kBytesRows > kMap + kDiagonal ? 2 * Z::kBytesRows : kMap + kDiagonal;
+    __shared__ __attribute__((aligned(16))) char lds[kBytes];
+    char *const Ks = lds, *const Qs = lds + Z::kBytesRows;
+    float* const map = reinterpret_cast<float*>(lds);
+    float (*const diagonal)[16][20] = reinterpret_cast<float (*)[16][20]>(lds + kMap);
     __shared__ double G[C];
     __shared__ float beta[C];
     __shared__ int odd_key, odd;
@@ -444,7 +468,7 @@ k_delta_walk(DeltaArgs A)
     typedef typename Num<T>::quad quad;
     constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, COLS = L::COLS;
     __shared__ __attribute__((aligned(16))) char lds[L::kBytes];
-    __shared__ float beta[C], gamma[C], tail[C], whole[2];
+    __shared__ __attribute__((aligned(16))) float beta[C], gamma[C], tail[C], whole[2];
     __shared__ int odd[2];
     char *const Kt = lds + L::kTurned, *const Ts = lds + L::kMap, *const Ks = lds + L::kKeys, *const Vt = lds + L::kValues, *const Qs = lds + L::kQueries, *const Ps = lds + L::kP;
 
@@ -510,7 +534,7 @@ k_delta_walk(DeltaArgs A)
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
             const int p = y + i * THREADS;
-            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
+            if (Z::TILES % WAVES == 0 || i * WAVES + wave < Z::TILES) {
                 pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
                 if (OUT) pp[i] = reinterpret_cast<const f32x4*>(numbers + Z::kP)[p];
             }
@@ -558,12 +582,11 @@ k_delta_walk(DeltaArgs A)
         }
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
-            const int p = y + i * THREADS;
-            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
-                const int tile = p >> 6;
+            const int tile = i * WAVES + wave;         // (a wavefront takes a tile)
+            if (Z::TILES % WAVES == 0 || tile < Z::TILES) {
                 int it = 0, jt = tile;
                 while (jt > it) { jt -= it + 1; ++it; }
-                const int to = quad_at<T, SEQ>(16 * it + ((p & 63) >> 2), 4 * jt + (p & 3));
+                const int to = quad_at<T, SEQ>(16 * it + (l >> 2), 4 * jt + (l & 3));
                 put_parts<T, Z::PARTS>(Ts + to, Z::kBytesMap, pt[i]);
                 if (OUT) put_parts<T, Z::SOME>(Ps + to, Z::kBytesMap, pp[i]);
             }
@@ -576,34 +599,47 @@ k_delta_walk(DeltaArgs A)
         const int bad = odd[turn];                     // from this token on there is nothing but NaN
         const Reader<ROW> rows(r16, g);
         const Reader<SEQ> columns(r16, g);
-        if (!STATES && A.states_out) {
-            float* const to = A.states_out + (chunk * A.heads + h) * (int64_t)DK * DK + col;
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = S[t][r];
-        }
+        if (!STATES && A.states_out) store_tiles<DT>(A.states_out + (chunk * A.heads + h) * (int64_t)DK * DK, S, DK, g, col);
         f32x4 U[CT], O[CT];
 #pragma unroll
         for (int t = 0; t < CT; ++t) U[t] = O[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         // K S and Q S: rows of tokens 16 t + 4 g .. + 3, column col, of the one, the other way round of the other
+        // (fragments are asked for a step ahead of their products, here and below: the compiler would ask for each where it is needed, and wait)
+        frag kf[2][CT], qf[2][CT];
+        const auto ask_rows = [&](int m) {
+#pragma unroll
+            for (int t = 0; t < CT; ++t) {
+                kf[m & 1][t] = get<T>(Ks, rows.at(t, m));
+                if (OUT) qf[m & 1][t] = get<T>(Qs, rows.at(t, m));
+            }
+        };
+        ask_rows(0);
 #pragma unroll
         for (int m = 0; m < KD; ++m) {
-            if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            if (m + 1 < KD) ask_rows(m + 1);
+            __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(S, m, xs);
             frag sf[Z::PARTS];
             parts_of<T, Z::PARTS>(xs, sf);
 #pragma unroll
             for (int t = 0; t < CT; ++t) {
-                U[t] = mma_exact<Z::PARTS>(get<T>(Ks, rows.at(t, m)), sf, U[t]);
-                if (OUT) {
-                    const frag qf = get<T>(Qs, rows.at(t, m));
+                U[t] = mma_exact<Z::PARTS>(kf[m & 1][t], sf, U[t]);
+                if (OUT)
 #pragma unroll
-                    for (int p = Z::SOME - 1; p >= 0; --p) O[t] = mma(sf[p], qf, O[t]);
-                }
+                    for (int p = Z::SOME - 1; p >= 0; --p) O[t] = mma(sf[p], qf[m & 1][t], O[t]);
             }
         }
+        frag tf[2][KC][Z::PARTS];
+        const auto ask_map = [&](int t) {
+#pragma unroll
+            for (int m = 0; m < KC; ++m)
+#pragma unroll
+                for (int p = 0; p < Z::PARTS; ++p)
+                    if (16 * t + 15 >= m * Z::K) tf[t & 1][m][p] = get<T>(Ts + p * Z::kBytesMap, columns.at(t, m));
+        };
+        ask_map(0);
+        __builtin_amdgcn_sched_barrier(0);
         if (at + C < count) load(at + C);
         // R = beta (V - gamma K S), U = T R
         frag Rf[KC][Z::PARTS];
@@ -631,40 +667,34 @@ k_delta_walk(DeltaArgs A)
         }
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            if (t + 1 < CT) ask_map(t + 1);
+            __builtin_amdgcn_sched_barrier(0);
             U[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int m = 0; m < KC; ++m)
-                if (16 * t + 15 >= m * Z::K) {
-                    frag tf[Z::PARTS];
-#pragma unroll
-                    for (int p = 0; p < Z::PARTS; ++p) tf[p] = get<T>(Ts + p * Z::kBytesMap, columns.at(t, m));
-                    U[t] = mma_parts<Z::PARTS>(tf, Rf[m], U[t]);
-                }
+                if (16 * t + 15 >= m * Z::K) U[t] = mma_parts<Z::PARTS>(tf[t & 1][m], Rf[m], U[t]);
         }
-        if (!STATES && A.u_out) {
-            float* const to = A.u_out + (chunk * A.heads + h) * (int64_t)C * DK + col;
-#pragma unroll
-            for (int t = 0; t < CT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = U[t][r];
-        }
+        if (!STATES && A.u_out) store_tiles<CT>(A.u_out + (chunk * A.heads + h) * (int64_t)C * DK, U, DK, g, col);
         if (OUT) {
 #pragma unroll
             for (int m = 0; m < KC; ++m) {
+                frag pf[2][Z::SOME];
+                const int t0 = m * Z::K / 16;          // rows above this block see none of it
+#pragma unroll
+                for (int p = 0; p < Z::SOME; ++p) pf[0][p] = get<T>(Ps + p * Z::kBytesMap, columns.at(t0, m));
                 __builtin_amdgcn_sched_barrier(0);
                 float xs[Z::E];
                 numbers_of<T>(U, m, xs);
                 frag uf[Z::SOME];
                 parts_of<T, Z::SOME>(xs, uf);
 #pragma unroll
-                for (int t = 0; t < CT; ++t)
-                    if (16 * t + 15 >= m * Z::K) {
-                        frag pf[Z::SOME];
+                for (int t = t0; t < CT; ++t) {
+                    if (t + 1 < CT)
 #pragma unroll
-                        for (int p = 0; p < Z::SOME; ++p) pf[p] = get<T>(Ps + p * Z::kBytesMap, columns.at(t, m));
-                        O[t] = mma_parts<Z::SOME>(uf, pf, O[t]);
-                    }
+                        for (int p = 0; p < Z::SOME; ++p) pf[(t + 1 - t0) & 1][p] = get<T>(Ps + p * Z::kBytesMap, columns.at(t + 1, m));
+                    __builtin_amdgcn_sched_barrier(0);
+                    O[t] = mma_parts<Z::SOME>(uf, pf[(t - t0) & 1], O[t]);
+                }
             }
             T* const out = static_cast<T*>(A.y) + row * A.ldy + (int64_t)h * A.dv;
             const int n = col0 + 16 * wave + 4 * g;
@@ -686,13 +716,16 @@ k_delta_walk(DeltaArgs A)
             }
         }
         // the state at the chunk's end; its decay in two numbers, since the same rounding in every chunk would add up
-        const float d = whole[0], rest = whole[1];
+        const float d = bad < C ? NAN : whole[0], rest = whole[1];
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] = bad < C ? NAN : fmaf(S[t][r], d, S[t][r] * rest);
+            for (int r = 0; r < 4; ++r) S[t][r] = fmaf(S[t][r], d, S[t][r] * rest);
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
+            frag cf[2];
+            cf[0] = get<T>(Kt, columns.at(0, m));
+            cf[1] = get<T>(Kt, columns.at(1, m));
             __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(U, m, xs);
@@ -701,7 +734,12 @@ k_delta_walk(DeltaArgs A)
             frag part[Z::PARTS];
             parts_of<T, Z::PARTS>(xs, part);
 #pragma unroll
-            for (int t = 0; t < DT; ++t) S[t] = mma_exact<Z::PARTS>(get<T>(Kt, columns.at(t, m)), part, S[t]);
+            for (int t = 0; t < DT; ++t) {
+                const frag k = cf[t & 1];
+                if (t + 2 < DT) cf[t & 1] = get<T>(Kt, columns.at(t + 2, m));
+                __builtin_amdgcn_sched_barrier(0);
+                S[t] = mma_exact<Z::PARTS>(k, part, S[t]);
+            }
         }
         __syncthreads();                               // the tiles may be written again
         if (x == 0) odd[turn] = C;
@@ -742,7 +780,7 @@ k_delta_back(DeltaArgs A)
     typedef typename Num<T>::frag frag;
     constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, COLS = L::COLS;
     __shared__ __attribute__((aligned(16))) char lds[L::kBytes];
-    __shared__ float beta[C], gamma[C], tail[C], whole[2];
+    __shared__ __attribute__((aligned(16))) float beta[C], gamma[C], tail[C], whole[2];
     char *const Kt = lds + L::kKeysTurned, *const Qt = lds + L::kQueriesTurned, *const Ks = lds + L::kKeys, *const Yt = lds + L::kValues,
          *const Ts = lds + L::kMap, *const Ps = lds + L::kP;
 
@@ -801,7 +839,7 @@ k_delta_back(DeltaArgs A)
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
             const int p = y + i * THREADS;
-            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
+            if (Z::TILES % WAVES == 0 || i * WAVES + wave < Z::TILES) {
                 pt[i] = reinterpret_cast<const f32x4*>(numbers)[p];
                 pp[i] = reinterpret_cast<const f32x4*>(numbers + Z::kP)[p];
             }
@@ -843,15 +881,14 @@ k_delta_back(DeltaArgs A)
         // T and P turned: row j, tokens i along the slots
 #pragma unroll
         for (int i = 0; i < NM; ++i) {
-            const int p = y + i * THREADS;
-            if ((Z::TILES * 64) % THREADS == 0 || p < Z::TILES * 64) {
-                const int tile = p >> 6;
+            const int tile = i * WAVES + wave;         // (a wavefront takes a tile)
+            if (Z::TILES % WAVES == 0 || tile < Z::TILES) {
                 int it = 0, jt = tile;
                 while (jt > it) { jt -= it + 1; ++it; }
-                const int token = 16 * it + ((p & 63) >> 2);
+                const int token = 16 * it + (l >> 2);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    char* const to = Ts + quad_at<T, SEQ>(16 * jt + 4 * (p & 3) + e, token >> 2) + (token & 3) * (int)sizeof(T);
+                    char* const to = Ts + quad_at<T, SEQ>(16 * jt + 4 * (l & 3) + e, token >> 2) + (token & 3) * (int)sizeof(T);
                     float v = pt[i][e], w = pp[i][e];
 #pragma unroll
                     for (int part = 0; part < Z::PARTS; ++part) {
@@ -872,42 +909,58 @@ k_delta_back(DeltaArgs A)
         Reader<SEQ> values(r16, g);
         values.base += wave * 16 * SEQ * 16;
         values.low ^= ((2 * wave) & Reader<SEQ>::kMask) * 16;
-        if (!STATES) {
-            float* const to = A.gstates + (chunk * A.heads + h) * (int64_t)DK * DK + col;
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = S[t][r];
-        }
+        if (!STATES) store_tiles<DT>(A.gstates + (chunk * A.heads + h) * (int64_t)DK * DK, S, DK, g, col);
         // tail K G
         f32x4 U[CT];
 #pragma unroll
         for (int t = 0; t < CT; ++t) U[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        frag kf[2][CT];
+        const auto ask_rows = [&](int m) {
+#pragma unroll
+            for (int t = 0; t < CT; ++t) kf[m & 1][t] = get<T>(Ks, rows.at(t, m));
+        };
+        ask_rows(0);
 #pragma unroll
         for (int m = 0; m < KD; ++m) {
-            if (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            if (m + 1 < KD) ask_rows(m + 1);
+            __builtin_amdgcn_sched_barrier(0);
             float xs[Z::E];
             numbers_of<T>(S, m, xs);
             frag sf[Z::PARTS];
             parts_of<T, Z::PARTS>(xs, sf);
 #pragma unroll
-            for (int t = 0; t < CT; ++t) U[t] = mma_exact<Z::PARTS>(get<T>(Ks, rows.at(t, m)), sf, U[t]);
+            for (int t = 0; t < CT; ++t) U[t] = mma_exact<Z::PARTS>(kf[m & 1][t], sf, U[t]);
         }
+        // a map's fragments of row t, from the blocks that hold tokens behind it
+        frag tf[2][KC][Z::PARTS];
+        const auto ask_map = [&](const char* map, int t) {
+#pragma unroll
+            for (int m = 0; m < KC; ++m)
+#pragma unroll
+                for (int p = 0; p < Z::PARTS; ++p)
+                    if (m * Z::K + Z::K > 16 * t) tf[t & 1][m][p] = get<T>(map + p * Z::kBytesMap, columns.at(t, m));
+        };
+        frag yf[KC];
+#pragma unroll
+        for (int m = 0; m < KC; ++m) yf[m] = get<T>(Yt, values.at(0, m));
+        ask_map(Ps, 0);
+        __builtin_amdgcn_sched_barrier(0);
         if (at - C >= s.lo) load(at - C);
 #pragma unroll
         for (int t = 0; t < CT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) U[t][r] *= tail[16 * t + 4 * g + r];
 #pragma unroll
-        for (int m = 0; m < KC; ++m) {
+        for (int t = 0; t < CT; ++t) {
+            if (t + 1 < CT) ask_map(Ps, t + 1);
             __builtin_amdgcn_sched_barrier(0);
-            const frag yf = get<T>(Yt, values.at(0, m));
 #pragma unroll
-            for (int t = 0; t < CT; ++t)
+            for (int m = 0; m < KC; ++m)
                 if (m * Z::K + Z::K > 16 * t)
 #pragma unroll
-                    for (int p = Z::PARTS - 1; p >= 0; --p) U[t] = mma(get<T>(Ps + p * Z::kBytesMap, columns.at(t, m)), yf, U[t]);
+                    for (int p = Z::PARTS - 1; p >= 0; --p) U[t] = mma(tf[t & 1][m][p], yf[m], U[t]);
         }
+        ask_map(Ts, 0);
         // dR = T^T dU
         frag Uf[KC][Z::PARTS];
 #pragma unroll
@@ -919,24 +972,14 @@ k_delta_back(DeltaArgs A)
         }
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-            if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            if (t + 1 < CT) ask_map(Ts, t + 1);
+            __builtin_amdgcn_sched_barrier(0);
             U[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int m = 0; m < KC; ++m)
-                if (m * Z::K + Z::K > 16 * t) {
-                    frag tf[Z::PARTS];
-#pragma unroll
-                    for (int p = 0; p < Z::PARTS; ++p) tf[p] = get<T>(Ts + p * Z::kBytesMap, columns.at(t, m));
-                    U[t] = mma_parts<Z::PARTS>(tf, Uf[m], U[t]);
-                }
+                if (m * Z::K + Z::K > 16 * t) U[t] = mma_parts<Z::PARTS>(tf[t & 1][m], Uf[m], U[t]);
         }
-        if (!STATES) {
-            float* const to = A.r_out + (chunk * A.heads + h) * (int64_t)C * DK + col;
-#pragma unroll
-            for (int t = 0; t < CT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) to[(16 * t + 4 * g + r) * DK] = U[t][r];
-        }
+        if (!STATES) store_tiles<CT>(A.r_out + (chunk * A.heads + h) * (int64_t)C * DK, U, DK, g, col);
         const float d = whole[0], rest = whole[1];
 #pragma unroll
         for (int t = 0; t < DT; ++t)
@@ -944,23 +987,31 @@ k_delta_back(DeltaArgs A)
             for (int r = 0; r < 4; ++r) S[t][r] = fmaf(S[t][r], d, S[t][r] * rest);
 #pragma unroll
         for (int m = 0; m < KC; ++m) {
+            frag cf[2];
+            cf[0] = get<T>(Qt, columns.at(0, m));
+            cf[1] = get<T>(Kt, columns.at(0, m));
             __builtin_amdgcn_sched_barrier(0);
-            const frag yf = get<T>(Yt, values.at(0, m));
             float xs[Z::E], ys[Z::E];
             numbers_of<T>(U, m, xs);
 #pragma unroll
             for (int e = 0; e < Z::E; ++e) {
                 const int i = m * Z::K + (sizeof(T) == 2 ? 16 * (e >> 2) + 4 * g + (e & 3) : 4 * g + e);
                 xs[e] *= -beta[i] * gamma[i];
-                ys[e] = (float)yf[e] * (A.scale * gamma[i]);
+                ys[e] = (float)yf[m][e] * (A.scale * gamma[i]);
             }
             frag rf[Z::PARTS], gf[Z::PARTS];
             parts_of<T, Z::PARTS>(xs, rf);
             parts_of<T, Z::PARTS>(ys, gf);
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
-                S[t] = mma_exact<Z::PARTS>(get<T>(Qt, columns.at(t, m)), gf, S[t]);
-                S[t] = mma_exact<Z::PARTS>(get<T>(Kt, columns.at(t, m)), rf, S[t]);
+                const frag q = cf[0], k = cf[1];
+                if (t + 1 < DT) {
+                    cf[0] = get<T>(Qt, columns.at(t + 1, m));
+                    cf[1] = get<T>(Kt, columns.at(t + 1, m));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                S[t] = mma_exact<Z::PARTS>(q, gf, S[t]);
+                S[t] = mma_exact<Z::PARTS>(k, rf, S[t]);
             }
         }
         __syncthreads();
@@ -1106,7 +1157,7 @@ k_delta_gradients(DeltaArgs A)
     static_assert(DT % ACROSS == 0 && CT % HALVES == 0, "every wavefront has as many tiles");
     constexpr int NM = (Z::TILES + WAVES - 1) / WAVES;
     __shared__ __attribute__((aligned(16))) char lds[L::kAll];
-    __shared__ float beta[C], gamma[C], tail[C], high[C], low[C], whole;
+    __shared__ __attribute__((aligned(16))) float beta[C], gamma[C], tail[C], high[C], low[C], whole;
     __shared__ float row_in[CT][C], col_in[CT][C], row_kk[CT][C], dots[ACROSS][3][C], rv[C], state_dot[ACROSS];
     char *const Ks = lds + L::kKeys, *const Qs = lds + L::kQueries, *const Ys = lds + L::kY, *const Us = lds + L::kU, *const Rs = lds + L::kR;
     char *const Kt = lds + L::kKeysTurned, *const Qt = lds + L::kQueriesTurned, *const Ns = lds + L::kN, *const Nt = lds + L::kNt, *const Ms = lds + L::kM;
