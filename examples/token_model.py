@@ -1,8 +1,8 @@
 """A small token model with a LAPLEX^(r) vocabulary head, through the library's entry points: embedding, rotary positions,
 attention with a decay for each head, the head, log probabilities.  Trains on a synthetic text, reads a prompt, and writes on
-from it token by token.
+from it token by token.  With --delta: layer norms, attention by the gated delta rule, and several drafted tokens checked at once.
 
-    python examples/token_model.py [--vocabulary 500] [--width 128] [--heads 4] [--steps 60] [--dtype bf16]
+    python examples/token_model.py [--vocabulary 500] [--width 128] [--heads 4] [--steps 60] [--dtype bf16] [--delta]
 """
 from __future__ import annotations
 
@@ -114,13 +114,9 @@ class TokenModel:
 
     # --- training -----------------------------------------------------------------------------------------------------
 
-    def gradients(self, tokens, positions, targets, starts=None, entropy_bonus=0.0):
-        """(mean of -logp - entropy_bonus * entropy over the tokens that have a target, gradients of all weights)"""
-        sequences = 1 if starts is None else len(starts) - 1
+    def _head_gradients(self, hidden, logits, head_ws, targets, entropy_bonus):
+        """(loss, its gradient with respect to what the head reads, gradients of the head's weights)"""
         W = self.weights
-        x, q, k, v = self._project(tokens, positions)
-        y, attention_ws = self._attend(q, k, v, sequences, starts, None, None)
-        hidden, logits, head_ws = self._head(x, y, save=True)
         logp, lse, entropy, _, _ = self._logprob(logits, targets)
         given = (targets >= 0) & (targets < self.vocabulary)
         share = given.float() / given.sum().clamp(min=1)
@@ -132,7 +128,16 @@ class TokenModel:
         ghidden = torch.empty_like(hidden)
         B.laplex_mix_apply_backward(W["a"], W["b"], W["w"], hidden, logits, ghidden, g["a"], g["b"], g["w"], head_ws,
                                     B.LAPLEX_SAVE_SCANS | B.LAPLEX_REUSE_PLAN)
-        gx = ghidden.T
+        return loss, ghidden.T, g
+
+    def gradients(self, tokens, positions, targets, starts=None, entropy_bonus=0.0):
+        """(mean of -logp - entropy_bonus * entropy over the tokens that have a target, gradients of all weights)"""
+        sequences = 1 if starts is None else len(starts) - 1
+        W = self.weights
+        x, q, k, v = self._project(tokens, positions)
+        y, attention_ws = self._attend(q, k, v, sequences, starts, None, None)
+        hidden, logits, head_ws = self._head(x, y, save=True)
+        loss, gx, g = self._head_gradients(hidden, logits, head_ws, targets, entropy_bonus)
         flat = y.float().reshape(x.shape)
         g["out"] = flat.T @ gx
         gy = (gx @ W["out"].T).to(self.dtype).view(y.shape)
@@ -151,6 +156,101 @@ class TokenModel:
             self.weights[name].sub_(g, alpha=rate)
 
 
+class DeltaTokenModel(TokenModel):
+    """The same around the gated delta rule: a layer norm before the projections, queries and keys of length 1 by a norm of each head, a decay and a
+    weight for every token and head, and drafts checked against the model, with the tokens that are kept read on from the kept state."""
+
+    def __init__(self, vocabulary, width, heads, operators=4, dtype=torch.float32, seed=0):
+        super().__init__(vocabulary, width, heads, operators, dtype, seed=seed)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(seed + 1)
+        self.weights["norm"] = torch.ones(width, device="cuda")
+        self.weights["norm_bias"] = torch.zeros(width, device="cuda")
+        # rates and weights of a token's heads: rate exp(.) of the decay length, sigmoid(.)
+        self.weights["small"] = torch.randn(width, 2 * heads, generator=gen, device="cuda") / math.sqrt(width)
+        self.unit = torch.full((self.dim,), self.dim ** -0.5, device="cuda")
+        self.scale = 1.0
+
+    def _forward(self, tokens, positions, save=False):
+        """Everything before the attention: queries and keys are parts of one matrix, and what the gradients need."""
+        n, h, width = len(tokens), self.heads, self.width
+        new = lambda *s: torch.empty(*s, device="cuda")
+        x = self.weights["embedding"][tokens]
+        normed, mean, rstd = torch.empty_like(x), new(n), new(n)
+        B.laplex_layer_norm(x, self.weights["norm"], self.weights["norm_bias"], normed, mean, rstd)
+        projected = (normed @ self.weights["qkv"][:, :2 * width]).to(self.dtype).view(n, 2 * h, self.dim)
+        v = (normed @ self.weights["qkv"][:, 2 * width:]).to(self.dtype).view(n, h, self.dim)
+        qk = torch.empty_like(projected) if save else projected
+        head_mean, head_rstd = (new(n, 2 * h), new(n, 2 * h)) if save else (None, None)
+        B.laplex_layer_norm(projected, self.unit, None, qk, head_mean, head_rstd)
+        B.laplex_rotary(qk, positions, self.frequencies, qk, self.magnitude)
+        small = normed @ self.weights["small"]
+        rates, beta = (self.rates * torch.exp(small[:, :h])).contiguous(), torch.sigmoid(small[:, h:]).contiguous()
+        return x, normed, mean, rstd, projected, head_mean, head_rstd, qk[:, :h], qk[:, h:], v, rates, beta
+
+    def _delta(self, q, k, v, rates, beta, sequences, starts=None, lengths=None, state_in=None, state_out=None, save=False):
+        y = torch.empty(v.shape, device="cuda", dtype=self.dtype)
+        ws = self.workspace("attention", B.laplex_delta_attention_workspace_bytes(self.dtype, len(q), sequences, self.heads, self.heads, self.dim, self.dim, save))
+        B.laplex_delta_attention(q, k, v, rates, beta, y, ws, self.scale, sequences, starts, lengths, state_in, state_out, B.LAPLEX_SAVE_SCANS if save else 0)
+        return y, ws
+
+    def read(self, tokens, positions, starts=None, state=None, targets=None, top=0):
+        sequences = 1 if starts is None else len(starts) - 1
+        x, *_, q, k, v, rates, beta = self._forward(tokens, positions)
+        y, _ = self._delta(q, k, v, rates, beta, sequences, starts, None, state, state)
+        _, logits, _ = self._head(x, y)
+        logp, _, entropy, ids, alternatives = self._logprob(logits, targets, top)
+        return logp, entropy, ids, alternatives
+
+    def write(self, tokens, positions, state, top=1):
+        x, *_, q, k, v, rates, beta = self._forward(tokens, positions)
+        y = torch.empty(v.shape, device="cuda", dtype=self.dtype)
+        B.laplex_delta_attention_step(q, k, v, rates, beta, state, y, self.scale)
+        _, logits, _ = self._head(x, y)
+        _, _, entropy, ids, alternatives = self._logprob(logits, None, top)
+        return ids, alternatives, entropy
+
+    def check(self, tokens, positions, state, drafts, chances=None, next_chances=None):
+        """Drafts of every sequence's next tokens, all at once.  tokens, positions and drafts are (sequences, columns): tokens the last written token and the drafts behind
+        it, drafts those moved up by one (the last of a row is not looked at).  Without chances the likeliest tokens are kept.  The state is carried on over
+        the last written token and the kept drafts.  (number of kept drafts, the token after them)"""
+        sequences, columns = tokens.shape
+        x, *_, q, k, v, rates, beta = self._forward(tokens.flatten(), positions.flatten())
+        y, _ = self._delta(q, k, v, rates, beta, sequences, state_in=state)
+        _, logits, _ = self._head(x, y)
+        accepted, following = (torch.empty(sequences, dtype=torch.int64, device="cuda") for _ in range(2))
+        ws = self.workspace("verify", B.laplex_verify_workspace_bytes(self.vocabulary, sequences * columns, sequences))
+        B.laplex_verify_drafts(logits, None, drafts.flatten(), chances, next_chances, accepted, following, ws, sequences=sequences,
+                               flags=B.LAPLEX_VERIFY_GREEDY if chances is None else 0)
+        self._delta(q, k, v, rates, beta, sequences, None, accepted + 1, state, state)
+        return accepted, following
+
+    def gradients(self, tokens, positions, targets, starts=None, entropy_bonus=0.0):
+        sequences, W, h, width = 1 if starts is None else len(starts) - 1, self.weights, self.heads, self.width
+        x, normed, mean, rstd, projected, head_mean, head_rstd, q, k, v, rates, beta = self._forward(tokens, positions, save=True)
+        y, attention_ws = self._delta(q, k, v, rates, beta, sequences, starts, save=True)
+        hidden, logits, head_ws = self._head(x, y, save=True)
+        loss, gx, g = self._head_gradients(hidden, logits, head_ws, targets, entropy_bonus)
+        g["out"] = y.float().reshape(x.shape).T @ gx
+        gy = (gx @ W["out"].T).to(self.dtype).view(y.shape)
+        n = len(tokens)
+        gqk = torch.empty(n, 2 * h, self.dim, device="cuda", dtype=self.dtype)
+        gv, grates, gbeta = torch.empty_like(v), torch.empty_like(rates), torch.empty_like(beta)
+        B.laplex_delta_attention_backward(q, k, v, rates, beta, gy, gqk[:, :h], gqk[:, h:], gv, grates, gbeta, attention_ws, self.scale, sequences, starts,
+                                          flags=B.LAPLEX_SAVE_SCANS)
+        B.laplex_rotary(gqk, positions, self.frequencies, gqk, self.magnitude, B.LAPLEX_ROTARY_INVERSE)
+        B.laplex_layer_norm_backward(projected, gqk, self.unit, head_mean, head_rstd, gqk, None, None, None)
+        gqkv = torch.cat([gqk.float().view(n, -1), gv.float().view(n, -1)], 1)
+        gsmall = torch.cat([grates * rates, gbeta * beta * (1 - beta)], 1)
+        g["qkv"], g["small"] = normed.T @ gqkv, normed.T @ gsmall
+        gnormed = gqkv @ W["qkv"].T + gsmall @ W["small"].T
+        g["norm"], g["norm_bias"] = torch.empty_like(W["norm"]), torch.empty_like(W["norm_bias"])
+        B.laplex_layer_norm_backward(x, gnormed, W["norm"], mean, rstd, gnormed, g["norm"], g["norm_bias"],
+                                     self.workspace("norm", B.laplex_layer_norm_workspace_bytes(n, width)))
+        g["embedding"] = torch.zeros_like(W["embedding"]).index_add_(0, tokens, gx + gnormed)
+        return loss, g
+
+
 def text(vocabulary, length, seed=1):
     """A synthetic text: a few phrases over and over."""
     gen = torch.Generator().manual_seed(seed)
@@ -167,8 +267,9 @@ def main():
     p.add_argument("--steps", type=int, default=60)
     p.add_argument("--length", type=int, default=512)
     p.add_argument("--dtype", choices=("f32", "bf16"), default="bf16")
+    p.add_argument("--delta", action="store_true")
     a = p.parse_args()
-    model = TokenModel(a.vocabulary, a.width, a.heads, dtype=torch.bfloat16 if a.dtype == "bf16" else torch.float32)
+    model = (DeltaTokenModel if a.delta else TokenModel)(a.vocabulary, a.width, a.heads, dtype=torch.bfloat16 if a.dtype == "bf16" else torch.float32)
     tokens = text(a.vocabulary, a.length + 1)
     inputs, targets = tokens[:-1], tokens[1:].clone()
     positions = torch.arange(a.length, device="cuda")
@@ -195,6 +296,13 @@ def main():
         following = ids[0]
     print("written:", written)
     print("text:   ", inputs[50:62].tolist())
+    if a.delta:
+        # the same tokens again, drafted and checked at once
+        state = model.new_state(1)
+        model.read(prompt, positions[:50], state=state)
+        drafted = torch.tensor(written, device="cuda")[None]
+        accepted, following = model.check(drafted, torch.arange(50, 62, device="cuda")[None], state, drafted.roll(-1, 1))
+        print(f"checked at once: {int(accepted)} of 11 drafts kept, then {int(following)}")
 
 
 if __name__ == "__main__":

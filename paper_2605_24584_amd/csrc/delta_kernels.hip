@@ -28,6 +28,7 @@ namespace {
 
 constexpr int kPrepareThreads = 256;
 constexpr int64_t kRows = 32768;          // sequences or chunks along a grid's second axis
+constexpr int64_t kPays = 3;              // sequences of more stretches are cut into them (see cut_of)
 
 // ----------------------------------------------------------------------------
 // Sequences, and the chunks of sequences: sequence b has the chunks first_chunk(b), ...: at least as many as its rows need, whatever its length.
@@ -109,7 +110,7 @@ __device__ __forceinline__ int64_t first_place(const DeltaArgs& A, int64_t b, in
     return (uint32_t)begin / (uint32_t)A.stretch + (b < several ? b : several);
 }
 
-// The stretch with this number, [lo, hi) of its sequence's tokens.
+// The stretch with this number, [lo, hi) of its sequence's tokens; a sequence of up to kPays of them is one.
 struct Stretch {
     int64_t b, begin, lo, hi, index, place;
     bool there, last, several;        // several: its sequence has more than one
@@ -119,11 +120,11 @@ __device__ __forceinline__ Stretch find_stretch(const DeltaArgs& A, int64_t slot
     const Unit u = find_unit(A, slot, A.stretch, A.stretches);
     Stretch s;
     s.b = u.b; s.begin = u.begin; s.index = u.index;
-    s.lo = u.index * A.stretch;
-    s.there = u.index >= 0 && (s.lo < u.count || u.index == 0);
-    s.hi = s.lo + A.stretch < u.count ? s.lo + A.stretch : u.count;
+    s.several = u.count > kPays * A.stretch;
+    s.lo = s.several ? u.index * A.stretch : 0;
+    s.there = u.index == 0 || (s.several && u.index > 0 && s.lo < u.count);
+    s.hi = s.several && s.lo + A.stretch < u.count ? s.lo + A.stretch : u.count;
     s.last = s.hi == u.count;
-    s.several = u.count > A.stretch;
     s.place = first_place(A, s.b, s.begin) + s.index;
     return s;
 }
@@ -1049,7 +1050,7 @@ k_delta_carry(DeltaArgs A)
     const int64_t b = (int64_t)blockIdx.z * kRows + blockIdx.y;
     if (b >= A.sequences) return;
     const int64_t begin = start_of(A, b), count = count_of(A, b, begin);
-    if (count <= A.stretch || (int)(blockIdx.x % SLICES) * kCarryWaves * 16 >= A.dv) return;
+    if (count <= kPays * A.stretch || (int)(blockIdx.x % SLICES) * kCarryWaves * 16 >= A.dv) return;
     const bool live = (col & ~15) < A.dv;
     const int64_t stretches = (count + A.stretch - 1) / A.stretch, place = first_place(A, b, begin), step = (int64_t)A.heads * DK * DK;
     const float* const given = BACK ? A.gstate_out : A.state_in;
@@ -1126,9 +1127,8 @@ k_delta_carry(DeltaArgs A)
 }
 
 // ----------------------------------------------------------------------------
-// What is left of the gradients: a workgroup takes a chunk and a head of keys, a wavefront 16 numbers of a head of keys (or twice 16) for half of
-// the tokens, and the heads of values
-// that share them one after the other, so that their gradients are summed in its registers.
+// What is left of the gradients: a workgroup takes a chunk and a head of keys, a wavefront 16 numbers of a head of keys (or twice 16), and the
+// heads of values that share them one after the other, so that their gradients are summed in its registers.
 // With X1 = S0 gY^T, X2 = S0 dR^T, X3 = G U^T (numbers of a key x tokens) and the rows and columns of the maps:
 //   dG_i = sum_j (in_ij) - sum_j (in_ji) + scale gamma_i q_i.X1_i - beta_i gamma_i k_i.X2_i - tail_i k_i.X3_i,     in = N (q k) + M (k k)
 //   and, of the chunk's whole decay,  sum_i tail_i k_i.X3_i + gamma_C <S0, G>;   grates_t = -(sum_{i >= t} dG_i + that).
@@ -1144,21 +1144,20 @@ struct GradientLds {
     static constexpr int kAll = kBytes > kEnd ? kBytes : kEnd;
 };
 
-template <typename T, int DK, int ACROSS, int HALVES>
-__global__ void __launch_bounds__(64 * ACROSS * HALVES)
+template <typename T, int DK, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
 k_delta_gradients(DeltaArgs A)
 {
     typedef Sizes<T, DK> Z;
     typedef GradientLds<T, DK> L;
-    constexpr int WAVES = ACROSS * HALVES;
     typedef typename Num<T>::frag frag;
     typedef typename Num<T>::quad quad;
-    constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, NT = DT / ACROSS, CH = CT / HALVES;
-    static_assert(DT % ACROSS == 0 && CT % HALVES == 0, "every wavefront has as many tiles");
+    constexpr int C = Z::C, R = Z::R, ROW = Z::ROW, SEQ = Z::SEQ, CT = Z::CT, DT = Z::DT, KD = Z::KD, KC = Z::KC, THREADS = 64 * WAVES, NT = DT / WAVES;
+    static_assert(DT % WAVES == 0, "every wavefront has as many tiles");
     constexpr int NM = (Z::TILES + WAVES - 1) / WAVES;
     __shared__ __attribute__((aligned(16))) char lds[L::kAll];
     __shared__ __attribute__((aligned(16))) float beta[C], gamma[C], tail[C], high[C], low[C], whole;
-    __shared__ float row_in[CT][C], col_in[CT][C], row_kk[CT][C], dots[ACROSS][3][C], rv[C], state_dot[ACROSS];
+    __shared__ float row_in[CT][C], col_in[CT][C], row_kk[CT][C], dots[WAVES][3][C], rv[C], state_dot[WAVES];
     char *const Ks = lds + L::kKeys, *const Qs = lds + L::kQueries, *const Ys = lds + L::kY, *const Us = lds + L::kU, *const Rs = lds + L::kR;
     char *const Kt = lds + L::kKeysTurned, *const Qt = lds + L::kQueriesTurned, *const Ns = lds + L::kN, *const Nt = lds + L::kNt, *const Ms = lds + L::kM;
 
@@ -1169,7 +1168,6 @@ k_delta_gradients(DeltaArgs A)
     find_chunk<C>(A, chunk, row, valid);
     if (valid == 0) return;
     const int x = threadIdx.x, lane = x & 63, wave = __builtin_amdgcn_readfirstlane(x >> 6), r16 = lane & 15, g = lane >> 4;
-    const int across = wave % ACROSS, half = wave / ACROSS;
     const int kh = blockIdx.x, group = A.heads / A.key_heads, kdv = (A.dv + Z::K - 1) / Z::K;
     const int64_t near = INT32_MAX / (int64_t)(C * sizeof(T)) - DK;
     const bool wq = (A.wide & 1) && A.ldq < near, wk = (A.wide & 2) && A.ldk < near, wy = (A.wide & 16) && A.ldgy < near, wv = A.wide & 4, wg = A.wide & 128;
@@ -1187,11 +1185,11 @@ k_delta_gradients(DeltaArgs A)
         put_rows<ROW>(Qs, a, first, piece);
         put_rows<ROW>(Ks, c, first, piece);
     }
-    f32x4 gq[NT][CH], gk[NT][CH];          // numbers 16 t + 4 g .. + 3 of the key, token 16 (half CH + tt) + r16
+    f32x4 gq[NT][CT], gk[NT][CT];          // numbers 16 t + 4 g .. + 3 of the key, token 16 t + r16
 #pragma unroll
     for (int a = 0; a < NT; ++a)
 #pragma unroll
-        for (int t = 0; t < CH; ++t) gq[a][t] = gk[a][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < CT; ++t) gq[a][t] = gk[a][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     // The rows that a head reads, all asked for at once.  (For the next head while this one's last products run they would not fit the registers.)
     constexpr int PIECES = DK <= 64 ? 16 : DK <= 128 ? 32 : 64, NP = (kPatches + THREADS - 1) / THREADS, NU = (C * PIECES + THREADS - 1) / THREADS;      // (PIECES threads of a wavefront have a token)
@@ -1199,7 +1197,7 @@ k_delta_gradients(DeltaArgs A)
     Patch<T> py[NP];
     f32x4 pu[NU], pr[NU], s4[AHEAD][Z::E / 4], g4[AHEAD][Z::E / 4];
     const auto ask_state = [&](f32x4 (&to)[AHEAD][Z::E / 4], const float* states, int64_t of, int a, int m0) {
-        const float* const from = states + of * (int64_t)DK * DK + (16 * (a * ACROSS + across) + r16) * DK + 4 * g;
+        const float* const from = states + of * (int64_t)DK * DK + (16 * (a * WAVES + wave) + r16) * DK + 4 * g;
 #pragma unroll
         for (int m = 0; m < AHEAD; ++m)
 #pragma unroll
@@ -1348,16 +1346,16 @@ k_delta_gradients(DeltaArgs A)
             if (g == 0) col_in[it][j] = col;
         }
 
-        // X1, X2, X3 of the wavefront's numbers of a key and half of the tokens, one tile of numbers after the other
-        float state_sum = 0.0f, q1[CH], k2[CH], k3[CH];
+        // X1, X2, X3 of the wavefront's numbers of a key and the tokens, one tile of numbers after the other
+        float state_sum = 0.0f, q1[CT], k2[CT], k3[CT];
 #pragma unroll
-        for (int t = 0; t < CH; ++t) q1[t] = k2[t] = k3[t] = 0.0f;
+        for (int t = 0; t < CT; ++t) q1[t] = k2[t] = k3[t] = 0.0f;
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
-            const int t0 = a * ACROSS + across;
-            f32x4 X1[CH], X2[CH];
+            const int t0 = a * WAVES + wave;
+            f32x4 X1[CT], X2[CT];
 #pragma unroll
-            for (int t = 0; t < CH; ++t) X1[t] = X2[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < CT; ++t) X1[t] = X2[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
             for (int m0 = 0; m0 < DK / Z::K; m0 += AHEAD) {
                 if (a > 0 || m0 > 0) ask_state(s4, A.states_out, of, a, m0);
@@ -1371,13 +1369,12 @@ k_delta_gradients(DeltaArgs A)
                     frag sf[Z::PARTS];
                     parts_of<T, Z::PARTS>(xs, sf);
 #pragma unroll
-                    for (int t = 0; t < CH; ++t) {
+                    for (int t = 0; t < CT; ++t) {
                         __builtin_amdgcn_sched_barrier(0);
-                        const int tt = half * CH + t;
-                        const frag yf = get<T>(Ys, rows.at(tt, m));
+                        const frag yf = get<T>(Ys, rows.at(t, m));
                         frag rf[Z::PARTS];
 #pragma unroll
-                        for (int p = 0; p < Z::PARTS; ++p) rf[p] = get<T>(Rs + p * Z::kBytesRows, rows.at(tt, m));
+                        for (int p = 0; p < Z::PARTS; ++p) rf[p] = get<T>(Rs + p * Z::kBytesRows, rows.at(t, m));
 #pragma unroll
                         for (int p = Z::PARTS - 1; p >= 0; --p) X1[t] = mma(sf[p], yf, X1[t]);
                         X2[t] = mma_parts<Z::PARTS>(sf, rf, X2[t]);
@@ -1389,8 +1386,8 @@ k_delta_gradients(DeltaArgs A)
                     for (int c = 0; c < Z::E; ++c) state_sum = fmaf(s4[n][c >> 2][c & 3], g4[n][c >> 2][c & 3], state_sum);
             }
 #pragma unroll
-            for (int t = 0; t < CH; ++t) {
-                const int i = 16 * (half * CH + t) + r16;
+            for (int t = 0; t < CT; ++t) {
+                const int i = 16 * t + r16;
                 const quad q4 = *reinterpret_cast<const quad*>(Qs + quad_at<T, ROW>(i, 4 * t0 + g)), k4 = *reinterpret_cast<const quad*>(Ks + quad_at<T, ROW>(i, 4 * t0 + g));
                 const float c1 = A.scale * gamma[i], c2 = beta[i] * gamma[i];
 #pragma unroll
@@ -1401,9 +1398,9 @@ k_delta_gradients(DeltaArgs A)
                     gk[a][t][r] = fmaf(-c2, X2[t][r], gk[a][t][r]);
                 }
             }
-            f32x4 X3[CH];
+            f32x4 X3[CT];
 #pragma unroll
-            for (int t = 0; t < CH; ++t) X3[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < CT; ++t) X3[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
             for (int m0 = 0; m0 < DK / Z::K; m0 += AHEAD) {
                 if (DK / Z::K > AHEAD) ask_state(g4, A.gstates, of, a, m0);
@@ -1416,18 +1413,18 @@ k_delta_gradients(DeltaArgs A)
                     frag gf[Z::PARTS];
                     parts_of<T, Z::PARTS>(xs, gf);
 #pragma unroll
-                    for (int t = 0; t < CH; ++t) {
+                    for (int t = 0; t < CT; ++t) {
                         __builtin_amdgcn_sched_barrier(0);
                         frag uf[Z::PARTS];
 #pragma unroll
-                        for (int p = 0; p < Z::PARTS; ++p) uf[p] = get<T>(Us + p * Z::kBytesRows, rows.at(half * CH + t, m));
+                        for (int p = 0; p < Z::PARTS; ++p) uf[p] = get<T>(Us + p * Z::kBytesRows, rows.at(t, m));
                         X3[t] = mma_parts<Z::PARTS>(gf, uf, X3[t]);
                     }
                 }
             }
 #pragma unroll
-            for (int t = 0; t < CH; ++t) {
-                const int i = 16 * (half * CH + t) + r16;
+            for (int t = 0; t < CT; ++t) {
+                const int i = 16 * t + r16;
                 const quad k4 = *reinterpret_cast<const quad*>(Ks + quad_at<T, ROW>(i, 4 * t0 + g));
                 const float c3 = tail[i];
 #pragma unroll
@@ -1438,18 +1435,18 @@ k_delta_gradients(DeltaArgs A)
             }
         }
 #pragma unroll
-        for (int t = 0; t < CH; ++t) {
-            const int i = 16 * (half * CH + t) + r16;
+        for (int t = 0; t < CT; ++t) {
+            const int i = 16 * t + r16;
 #pragma unroll
             for (int step = 16; step < 64; step <<= 1) {
                 q1[t] += __shfl_xor(q1[t], step);
                 k2[t] += __shfl_xor(k2[t], step);
                 k3[t] += __shfl_xor(k3[t], step);
             }
-            if (g == 0) { dots[across][0][i] = q1[t]; dots[across][1][i] = k2[t]; dots[across][2][i] = k3[t]; }
+            if (g == 0) { dots[wave][0][i] = q1[t]; dots[wave][1][i] = k2[t]; dots[wave][2][i] = k3[t]; }
         }
         for (int step = 1; step < 64; step <<= 1) state_sum += __shfl_xor(state_sum, step);
-        if (lane == 0 && half == 0) state_dot[across] = state_sum;
+        if (lane == 0) state_dot[wave] = state_sum;
         __syncthreads();                               // U and dR are done with
 
         for (int p = x; p < kPatches; p += THREADS) {
@@ -1504,7 +1501,7 @@ k_delta_gradients(DeltaArgs A)
                 kk_sum += row_kk[t][i];
             }
             for (int t = 0; t < CT; ++t) in -= col_in[t][i];
-            for (int w = 0; w < ACROSS; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 d1 += dots[w][0][i];
                 d2 += dots[w][1][i];
                 d3 += dots[w][2][i];
@@ -1525,19 +1522,18 @@ k_delta_gradients(DeltaArgs A)
         __syncthreads();
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
-            const int t0 = a * ACROSS + across;
+            const int t0 = a * WAVES + wave;
 #pragma unroll
             for (int m = 0; m < KC; ++m) {
                 const frag kf = get<T>(Kt, columns.at(t0, m)), qf = get<T>(Qt, columns.at(t0, m));
 #pragma unroll
-                for (int t = 0; t < CH; ++t) {
+                for (int t = 0; t < CT; ++t) {
                     __builtin_amdgcn_sched_barrier(0);
-                    const int tt = half * CH + t;
 #pragma unroll
                     for (int p = Z::SOME - 1; p >= 0; --p) {
-                        if (16 * tt + 15 >= m * Z::K) gq[a][t] = mma(kf, get<T>(Ns + p * Z::kBytesMap, columns.at(tt, m)), gq[a][t]);
-                        if (m * Z::K + Z::K > 16 * tt) gk[a][t] = mma(qf, get<T>(Nt + p * Z::kBytesMap, columns.at(tt, m)), gk[a][t]);
-                        gk[a][t] = mma(kf, get<T>(Ms + p * Z::kBytesMap, columns.at(tt, m)), gk[a][t]);
+                        if (16 * t + 15 >= m * Z::K) gq[a][t] = mma(kf, get<T>(Ns + p * Z::kBytesMap, columns.at(t, m)), gq[a][t]);
+                        if (m * Z::K + Z::K > 16 * t) gk[a][t] = mma(qf, get<T>(Nt + p * Z::kBytesMap, columns.at(t, m)), gk[a][t]);
+                        gk[a][t] = mma(kf, get<T>(Ms + p * Z::kBytesMap, columns.at(t, m)), gk[a][t]);
                     }
                 }
             }
@@ -1545,10 +1541,10 @@ k_delta_gradients(DeltaArgs A)
     }
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
-        const int n = 16 * (a * ACROSS + across) + 4 * g;
+        const int n = 16 * (a * WAVES + wave) + 4 * g;
 #pragma unroll
-        for (int t = 0; t < CH; ++t) {
-            const int i = 16 * (half * CH + t) + r16;
+        for (int t = 0; t < CT; ++t) {
+            const int i = 16 * t + r16;
             if (i >= valid) continue;
             const auto write = [&](void* base, int64_t ld, bool wide, f32x4 v) {
                 if (!base) return;
@@ -1728,18 +1724,26 @@ Parts layout_of(bool bf16, int64_t chunks, int64_t places, int heads, int dk, in
 // How sequences are cut into stretches.
 struct Cut { bool cut; int64_t stretch, per_sequence, slots, places; };
 
-constexpr int64_t kWorkgroups = 256, kPackedWorkgroups = 512, kLeastChunks = 4;      // a workgroup of a walk takes most of a compute unit's LDS
+// A workgroup of a walk takes most of a compute unit's LDS, so 256 of them fill the card: us with stretches for 128 / 256 / 512, 16 heads of 128 in bf16: 1 x 65536 tokens of 8
+// heads 1047 / 979 / 1145, 4 x 2048 247 / 227 / 278, 2 x 4096 for training 812 / 730 / 880; in fp32 256 / 512: 4 x 2048 437 / 471, 8 x 4096 for training 3203 / 4085.  Packed sequences of uneven
+// lengths leave places, and two workgroups of fp32 numbers fit a compute unit: 256 / 512 in fp32, 24 sequences of 30011 tokens, 6 heads of 96 and 80, for training 1792 / 1470, their results alone
+// 702 / 540, 16 of 32768 and 16 heads of 128 1656 / 1739; in bf16 16 of 32768 780 / 837, 8 of 32768 for training 2695 / 2737.
+// Stretches of at least 2 / 4 / 8 chunks: 1 x 1024 123 / 112 / 132, 1 x 4096 222 / 222 / 203.
+// A cut costs the maps from state to state besides, about twice the work, and pays for sequences of more than three stretches (kPays).  Cut / whole: 1 x 512 (two stretches) 99 / 82, 8 x 4096 for
+// training (two) 2169 / 1958, 1 x 1024 (four) 112 / 133, 4 x 2048 (four) 231 / 248, 1 x 65536 927 / 6689.
+constexpr int64_t kLeastChunks = 4;
+int64_t workgroups_of(bool bf16, bool equal) { return bf16 || equal ? 256 : 512; }
 
-// By the sizes alone.
+// By the sizes alone: of packed sequences the kernels see which ones are long enough.
 Cut cut_of(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int dv, bool equal)
 {
     const int d = padded_of(dk, dv), c = tokens_of_chunk(bf16, d), slices = d > 128 ? 2 : 1;
-    const int64_t longest = equal ? (sequences > 0 ? tokens / sequences : 0) : tokens, wanted = equal ? kWorkgroups : kPackedWorkgroups;
-    const int64_t units = (int64_t)heads * slices * tokens;
+    const int64_t longest = equal ? (sequences > 0 ? tokens / sequences : 0) : tokens;
+    const int64_t units = (int64_t)heads * slices * tokens, wanted = workgroups_of(bf16, equal);
     Cut P;
     P.stretch = ((units + wanted - 1) / wanted + c - 1) / c * c;
     if (P.stretch < kLeastChunks * c) P.stretch = kLeastChunks * c;
-    P.cut = longest > 3 * P.stretch;
+    P.cut = longest > kPays * P.stretch;
     if (!P.cut) P.stretch = longest < 1 ? 1 : longest;
     P.per_sequence = 1;
     if (equal && P.cut) P.per_sequence = (longest + P.stretch - 1) / P.stretch;
@@ -1759,9 +1763,6 @@ dim3 grid_of(int64_t across, int64_t rows)
     const int64_t deep = (rows + kRows - 1) / kRows;
     return dim3((unsigned)across, (unsigned)(deep > 1 ? kRows : rows), (unsigned)deep);
 }
-
-// (one half: the registers of eight wavefronts hold the rows of both states that a head needs while it is prepared)
-template <typename T, int DK> constexpr int kHalves = 1;
 
 enum { kRunResults, kRunKeep, kRunStates, kRunBack, kRunBackStates };
 
@@ -1796,8 +1797,9 @@ template <typename T, int DK, int ACROSS>
 hipError_t run_with(DeltaArgs A, bool cut, hipStream_t st)
 {
     const dim3 chunks = grid_of(A.key_heads, A.chunks);
-    // Half as many columns of a workgroup, where whole ones would leave compute units without one: a workgroup takes most of one's LDS.
-    const bool narrow = A.slots * A.heads * (DK / (16 * ACROSS)) < 256;
+    // Half as many columns of a workgroup where all compute units have room for twice the workgroups: us, half / whole columns, sequences of 128 tokens and 16 heads of 128: 4 of them
+    // 41 / 49, 8 45 / 50, 12 63 / 51.
+    const bool narrow = A.slots * A.heads * (DK / (16 * ACROSS)) * 2 <= 256;
     A.slices = DK / (16 * ACROSS) * (narrow ? 2 : 1);
     const auto walks = [&](int what) { return narrow ? walks_with<T, DK, ACROSS / 2>(A, what, st) : walks_with<T, DK, ACROSS>(A, what, st); };
     hipError_t e = hipSuccess;
@@ -1816,9 +1818,8 @@ hipError_t run_with(DeltaArgs A, bool cut, hipStream_t st)
     if (cut && e == hipSuccess) e = carry_with<DK>(A, true, st);
     if (e == hipSuccess) e = walks(kRunBack);
     if (e == hipSuccess && A.chunks > 0 && (A.gq || A.gk || A.gv || A.grates || A.gbeta)) {
-        constexpr int HALVES = kHalves<T, DK>;
         profile_before("delta_gradients", st);
-        hipLaunchKernelGGL((k_delta_gradients<T, DK, ACROSS, HALVES>), chunks, dim3(64 * ACROSS * HALVES), 0, st, A);
+        hipLaunchKernelGGL((k_delta_gradients<T, DK, ACROSS>), chunks, dim3(64 * ACROSS), 0, st, A);
         profile_after("delta_gradients", st);
         e = hipGetLastError();
     }
@@ -1856,7 +1857,7 @@ size_t delta_workspace(bool bf16, int64_t tokens, int64_t sequences, int heads, 
     if (heads == 0) return 0;
     // of equal lengths or packed, and cut into stretches of no fewer than so many tokens
     const int d = padded_of(dk, dv), c = tokens_of_chunk(bf16, d);
-    const int64_t by_size = tokens / (kLeastChunks * c), by_work = kPackedWorkgroups / ((int64_t)heads * (d > 128 ? 2 : 1)) + 1, several = by_size < by_work ? by_size : by_work;
+    const int64_t by_size = tokens / (kLeastChunks * c), by_work = workgroups_of(bf16, false) / ((int64_t)heads * (d > 128 ? 2 : 1)) + 1, several = by_size < by_work ? by_size : by_work;
     return layout_of(bf16, tokens / c + sequences, several > 0 ? several + (sequences < several ? sequences : several) : 0, heads, dk, dv, training).all;
 }
 
@@ -1866,7 +1867,7 @@ hipError_t launch_delta_tokens(const DeltaArgs& given, hipStream_t st)
     A.each = !A.starts && A.sequences > 0 ? A.tokens / A.sequences : 0;
     const bool aligned4 = A.dv % 4 == 0 && reinterpret_cast<uintptr_t>(A.state_in) % 16 == 0 && reinterpret_cast<uintptr_t>(A.state_out) % 16 == 0;
     const int vec = aligned4 ? 4 : 1, wide = (A.dv + vec - 1) / vec;
-    // at most 16 lanes: 16 rows of the state for every thread then
+    // at most 16 lanes: 16 rows of the state for every thread then.  us with 8 / 16 lanes, 16 heads of 128: 64 sequences of 1 token 38 / 41, 128 of 1 63 / 64, 256 of 5 210 / 181.
     int lanes_log2 = 0;
     const int most = A.sequences * A.heads >= 1024 ? 4 : 3;
     while (lanes_log2 < most && (1 << lanes_log2) < wide) ++lanes_log2;

@@ -3,7 +3,7 @@
 //   mean = sum x / w,  rstd = (sum (x - mean)^2 / w + eps)^(-1/2),  hat = (x - mean) rstd,  y = hat weight + bias
 //   g = gy weight:  gx = rstd (g - sum g / w - hat sum (g hat) / w),   gweight = sum over rows of gy hat,   gbias = sum over rows of gy
 //
-// Rows of up to kThreads * kMost pieces of 16 bytes are held in registers: x is read once, and the squares are summed about the mean and not as a
+// Rows of up to kThreads * kMost pieces of eight (bf16) or four numbers are held in registers: x is read once, and the squares are summed about the mean and not as a
 // difference of two sums.  A row belongs to `lanes` threads, a power of two: to part of a wavefront, a wavefront, or the workgroup.
 // The gradient's workgroups take a range of rows each and keep the sums of their columns in registers; they are written once for each
 // workgroup (k_norm_parts) and added up in order by a second launch, so that the same call gives the same bits.  Longer rows are read again instead of held
@@ -363,21 +363,23 @@ k_norm_join(const float* parts, int64_t count, int64_t width, float* gweight, fl
     }
 }
 
-// threads of a row and pieces of each, by the width
+// threads of a row and pieces of each, by the width: part of a wavefront, a wavefront with one piece a thread or, if `two`, with two, or the workgroup
 struct Plan { int lanes, count; };
 
-Plan plan_of(int64_t pieces, int wavefront_most)
+Plan plan_of(int64_t pieces, bool two)
 {
     for (int lanes = 1; lanes <= 64; lanes *= 2)
         if (pieces <= lanes) return {lanes, 1};
-    for (int count = 2; count <= wavefront_most; count *= 2)
-        if (pieces <= 64 * count) return {64, count};
+    if (two && pieces <= 128) return {64, 2};
     for (int count = 1; count <= kMost; count *= 2)
         if (pieces <= (int64_t)kThreads * count) return {kThreads, count};
     return {0, 0};
 }
 
-constexpr int64_t kForwardWorkgroups = 2048, kPartWorkgroups = 1024, kMostWorkgroups = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
+// Forward, workgroups that go over the rows with the weights in registers: us with 1024 / 2048 / 4096 / one for each row, bf16: 32768 rows of 4096 130 / 136 / 133 / 150, 524288 of 128
+// 76 / 67 / 66 / 63.  Backward, workgroups that keep sums of columns, 512 / 1024 / 2048: 32768 of 4096 396 / 321 / 349, 524288 of 128 219 / 166 / 177; each has two turns at least where there are
+// more than 256, since it writes as much as a row of sums: 1024 of 8192 in 512 / 1024 parts 63 / 87.
+constexpr int64_t kForwardWorkgroups = 2048, kPartWorkgroups = 1024, kLeastParts = 256, kMostWorkgroups = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
 
 unsigned workgroups(int64_t wanted) { return (unsigned)(wanted < kMostWorkgroups ? wanted : kMostWorkgroups); }
 
@@ -386,7 +388,8 @@ int64_t pieces_of(bool bf16, int64_t width) { return bf16 ? (width + 7) / 8 : (w
 int64_t parts_of(const Plan& P, int64_t rows)
 {
     const int64_t at_once = P.lanes ? kThreads / P.lanes : 1, all = (rows + at_once - 1) / at_once;
-    return all < kPartWorkgroups ? all : kPartWorkgroups;
+    const int64_t some = all / 2 > kLeastParts ? all / 2 : all < kLeastParts ? all : kLeastParts;
+    return some < kPartWorkgroups ? some : kPartWorkgroups;
 }
 
 template <typename T, int LANES, int COUNT>
@@ -408,7 +411,7 @@ hipError_t backward_with(const NormBackwardArgs& A, int64_t parts, hipStream_t s
     do {                                                                                                                          \
         if (P.lanes == kThreads)                                                                                                  \
             return P.count == 1 ? call(kThreads, 1) : P.count == 2 ? call(kThreads, 2) : P.count == 4 ? call(kThreads, 4) : call(kThreads, 8); \
-        if (P.lanes == 64) return P.count == 1 ? call(64, 1) : P.count == 2 ? call(64, 2) : P.count == 4 ? call(64, 4) : call(64, 8);          \
+        if (P.lanes == 64) return P.count == 1 ? call(64, 1) : call(64, 2);                                                       \
         return P.lanes == 32 ? call(32, 1) : P.lanes == 16 ? call(16, 1) : P.lanes == 8 ? call(8, 1) : P.lanes == 4 ? call(4, 1) : P.lanes == 2 ? call(2, 1) : call(1, 1); \
     } while (0)
 
@@ -446,7 +449,7 @@ size_t norm_workspace(int64_t rows, int64_t width)
     // (of either type, and of any number of rows up to these)
     int64_t most = 0;
     for (int bf16 = 0; bf16 < 2; ++bf16) {
-        const int64_t parts = parts_of(plan_of(pieces_of(bf16 != 0, width), 4), rows);
+        const int64_t parts = parts_of(plan_of(pieces_of(bf16 != 0, width), true), rows);
         most = parts > most ? parts : most;
     }
     return (size_t)most * 2 * (size_t)width * sizeof(float);
@@ -454,8 +457,9 @@ size_t norm_workspace(int64_t rows, int64_t width)
 
 hipError_t launch_norm(const NormArgs& A, hipStream_t st)
 {
-    // A wavefront for a row where there are rows for all of them (no barrier), else the workgroup.
-    const Plan P = plan_of(pieces_of(A.bf16, A.width), A.rows >= 2048 ? 2 : 1);
+    // Rows of two pieces a lane: a wavefront for a row where there are rows for all of them (no barrier), else the workgroup.  us, rows of 1024 in bf16, wavefront / workgroup:
+    // 64 rows 7.2 / 6.4, 512 7.4 / 6.5, 1024 7.7 / 7.5, 2048 8.6 / 8.8, 4096 10.2 / 11.7, 32768 41 / 48.
+    const Plan P = plan_of(pieces_of(A.bf16, A.width), A.rows >= 2048);
     profile_before("norm", st);
     const hipError_t e = A.bf16 ? forward_of<__bf16>(A, P, st) : forward_of<float>(A, P, st);
     profile_after("norm", st);
@@ -464,7 +468,8 @@ hipError_t launch_norm(const NormArgs& A, hipStream_t st)
 
 hipError_t launch_norm_backward(const NormBackwardArgs& A, hipStream_t st)
 {
-    const Plan P = plan_of(pieces_of(A.bf16, A.width), 4);
+    // (wavefront / workgroup for rows of two pieces a lane: 8192 of 1024 in bf16 38 / 48 us)
+    const Plan P = plan_of(pieces_of(A.bf16, A.width), true);
     const int64_t parts = parts_of(P, A.rows);
     if (A.rows > 0) {
         profile_before("norm_backward", st);

@@ -18,7 +18,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroup = 8;                 // rows that a thread has asked for at a time
-constexpr int kMaxParts = 256, kWorkgroups = 4096, kSlab = 64;      // parts of the rows; workgroups that are enough for a matrix; columns of a workgroup
+// Parts of the rows (us with 64 / 128 / 256: 60001 rows x 576 columns in bf16 94 / 80 / 76, 32000 x 40 52 / 42 / 41, x 2048 292 / 285 / 302), workgroups that are enough for a matrix
+// (1024 to 8192 are alike) and columns of a workgroup (32 / 64: 32000 x 1000 and their drafts' 164 / 166).
+constexpr int kMaxParts = 256, kWorkgroups = 4096, kSlab = 64;
 
 // 2^t, t <= 0 and finite; 0 below 2^-1074
 __device__ __forceinline__ double power_in_range(double t)
@@ -519,6 +521,7 @@ hipError_t launch_verify(const VerifyArgs& given, hipStream_t st)
     }
     const Plan P = plan_of(A.k, A.batch);
     A.lanes_log2 = P.lanes_log2; A.part_rows = P.part_rows; A.parts = P.parts;
+    // (us with 1 / 4 / 8 / 16 sequences side by side: 512 of 4 columns 895 / 386 / 292 / 302, 200 of 5 324 / 178 / 164 / 166, 8 of 5 62 / 43 / 41 / 41)
     A.seq_log2 = 0;
     while (A.seq_log2 < 4 && (1 << A.seq_log2) < A.sequences) ++A.seq_log2;
     char* at = A.ws;
