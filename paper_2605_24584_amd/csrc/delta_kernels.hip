@@ -11,11 +11,19 @@
 //   gQ = N K + scale gamma gY S0^T,   gK = N^T Q + (M + M^T) K - beta gamma dR S0^T + tail U G^T
 //   gbeta_i = dR_i.(v_i - gamma_i S0^T k_i) + sum_j M_ij k_i.k_j / beta_i,    and what goes to the decays from the same sums (k_delta_gradients).
 //
-// Four kernels.  k_delta_prepare forms T for every chunk and head, all chunks at once.  k_delta_walk goes over the chunks of a sequence with the state in
+// In chunks k_delta_prepare forms T for every chunk and head, all chunks at once.  k_delta_walk goes over the chunks of a sequence with the state in
 // accumulator registers: a wavefront owns 16 columns of the state, of U and of the results, and since an accumulator (a pair of them in bf16) IS a fragment of the
 // next product over the same rows, neither the state nor U passes through memory on its way from product to product.  k_delta_back is the walk from the last chunk
 // to the first, with the gradient of the state.  k_delta_gradients forms what is left of the gradients, all chunks at once, from the states, U, G and dR that the two
-// walks have written.
+// walks have written.  Long sequences are cut into stretches of chunks: a walk of all stretches at once finds what each does to a state (S -> turned S + added), k_delta_carry
+// joins these in order, and the walks then start from the stretches' own states.  k_delta_tokens takes sequences of a few tokens one token at a time.
+//
+// What bounds it (us, bf16, heads of 128): not memory, but products that wait for one another with one or two wavefronts on a SIMD, as many vector instructions beside them (splits into
+// parts, decays), and in the gradients LDS, of which a workgroup takes all.  8 x 4096 tokens of 16 heads, trained: prepare 106, walk 530, back 498, gradients 927 (the recurrence's operations and bytes
+// would take 220).  4 x 2048 of 16: prepare 40, stretches 94, carry 28, walk 86.  65536 of 8: 135, 346, 206, 274.  256 sequences of 5 tokens, token by token: 122, which is 0.54 GB of
+// states at 4.5 TB/s.
+// Chunks of half as many tokens make the walks slower (4 x 2048 268 -> 350, 8 x 4096 trained 2120 -> 3390): a chunk's waits stay, and there are twice as many.  Sixteen wavefronts for the gradients
+// spill.  Fragments asked for a step ahead took 8 x 4096 from 2120 to 2030, 65536 from 963 to 925.
 //
 // Numbers: sums, states and everything from which states come are fp32 numbers; in bf16 they enter products as sums of three bf16 numbers (exactly; of the nine
 // products of two such sums the three below 2^-24 are left out).  What only goes into a result that is rounded to bf16 enters as two (16 bits).  The
@@ -1744,7 +1752,7 @@ Cut cut_of(bool bf16, int64_t tokens, int64_t sequences, int heads, int dk, int 
     P.stretch = ((units + wanted - 1) / wanted + c - 1) / c * c;
     if (P.stretch < kLeastChunks * c) P.stretch = kLeastChunks * c;
     P.cut = longest > kPays * P.stretch;
-    if (!P.cut) P.stretch = longest < 1 ? 1 : longest;
+    if (!P.cut) P.stretch = longest + 1;               // (more than all tokens: so an empty sequence behind the last token has its place too)
     P.per_sequence = 1;
     if (equal && P.cut) P.per_sequence = (longest + P.stretch - 1) / P.stretch;
     P.slots = !P.cut ? sequences : equal ? sequences * P.per_sequence : tokens / P.stretch + sequences;

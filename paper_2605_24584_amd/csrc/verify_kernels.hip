@@ -10,6 +10,10 @@
 // Four launches: k_verify_rows reads both matrices once, and leaves maximum and sum of every column and part of the rows (and, for the greedy rule, the place of
 // the maximum); k_verify_judge, a wavefront per column, joins them and judges the draft; k_verify_left sums what is left of the refused columns over the same
 // parts of the rows; k_verify_draw, a workgroup per sequence, finds the part and then the row.  The second reading takes the refused columns alone.
+//
+// What bounds it: 64-bit vector instructions, some 43 a logit, not memory.  32000 rows x 1001 columns in fp32 with the drafts' logits: rows 91 us of 155 (0.26 GB: 2.8 TB/s), left 33, draw 17,
+// judge 14; 60001 x 576 in bf16, certain drafts: rows 54 of 80, draw 15, judge 8.  One column alone costs the four launches and the draw's two searches: 30 us.
+// Two columns a lane, and several parts a workgroup in k_verify_left, were no faster.
 #include "token_internal.h"
 
 namespace laplex {

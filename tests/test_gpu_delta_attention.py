@@ -152,6 +152,7 @@ SHAPES = [
     ([150], 1, 1, 256, 256, False), ([70], 2, 1, 256, 40, False), ([95], 1, 1, 40, 256, False), ([0, 0], 2, 2, 8, 8, True), ([400, 213], 1, 1, 48, 100, True),
     ([97, 65], 2, 2, 129, 65, True), ([33, 100], 3, 1, 192, 150, True), ([32, 31, 15, 16, 48], 2, 2, 128, 96, True), ([700], 2, 1, 64, 128, False), ([12, 12, 12], 4, 2, 128, 128, False), ([13, 13], 2, 2, 128, 128, False), ([9] * 3, 2, 1, 256, 33, False), ([11], 1, 1, 100, 256, False),
     ([10] * 70, 4, 4, 64, 64, False),
+    ([40, 0], 2, 1, 32, 48, True), ([0, 130, 0, 0], 2, 2, 64, 64, True), ([2100, 0, 0], 1, 1, 64, 64, True),
 ]
 
 
@@ -386,7 +387,8 @@ def test_two_calls_at_once():
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("lengths,heads,key_heads,dk,dv,packed,read", [
     ([2600], 2, 1, 64, 64, False, None), ([1, 2000, 0, 900], 4, 2, 96, 80, True, None), ([1500, 1500], 2, 2, 20, 130, False, None), ([1300], 1, 1, 200, 256, False, None),
-    ([1100, 1100, 1100], 2, 2, 48, 48, False, [1100, 77, 1027]), ([40, 1500, 30, 2000], 2, 2, 128, 128, True, [40, 1501, 7, 1025]), ([769, 5, 1025], 1, 1, 256, 64, True, None)])
+    ([1100, 1100, 1100], 2, 2, 48, 48, False, [1100, 77, 1027]), ([40, 1500, 30, 2000], 2, 2, 128, 128, True, [40, 1501, 7, 1025]), ([769, 5, 1025], 1, 1, 256, 64, True, None),
+    ([384, 385, 768, 769], 2, 1, 64, 48, True, None), ([769, 769], 2, 2, 32, 64, False, [768, 769])])
 def test_sequences_in_stretches(dtype, lengths, heads, key_heads, dk, dv, packed, read):
     """Sequences that are cut, with lengths that end inside, at and behind the edges of stretches; the state in place."""
     c = Case(seeded("stretches", lengths, heads, dk, dv), lengths, heads, key_heads, dk, dv, dtype, True, packed, read)
