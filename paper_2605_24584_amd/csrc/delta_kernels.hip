@@ -20,7 +20,7 @@
 //
 // What bounds it (us, bf16, heads of 128): not memory, but products that wait for one another with one or two wavefronts on a SIMD, as many vector instructions beside them (splits into
 // parts, decays), and in the gradients LDS, of which a workgroup takes all.  8 x 4096 tokens of 16 heads, trained: prepare 106, walk 530, back 498, gradients 927 (the recurrence's operations and bytes
-// would take 220).  4 x 2048 of 16: prepare 40, stretches 94, carry 28, walk 86.  65536 of 8: 135, 346, 206, 274.  256 sequences of 5 tokens, token by token: 122, which is 0.54 GB of
+// would take 220).  4 x 2048 of 16: prepare 40, stretches 94, carry 20, walk 86.  65536 of 8: 135, 340, 122, 270.  256 sequences of 5 tokens, token by token: 122, which is 0.54 GB of
 // states at 4.5 TB/s.
 // Chunks of half as many tokens make the walks slower (4 x 2048 268 -> 350, 8 x 4096 trained 2120 -> 3390): a chunk's waits stay, and there are twice as many.  Sixteen wavefronts for the gradients
 // spill.  Fragments asked for a step ahead took 8 x 4096 from 2120 to 2030, 65536 from 963 to 925.
@@ -1042,7 +1042,8 @@ k_delta_back(DeltaArgs A)
 
 // ----------------------------------------------------------------------------
 // The states that enter the stretches of a sequence that has several, in the places of what the stretches add: S_(n+1) = turned_n S_n + added_n from state_in on, or, back,
-// G_(n-1) = turned_n^T G_n + added_n from gstate_out on.  A wavefront to 16 columns, on the fp32 matrix instructions whatever the type.
+// G_(n-1) = turned_n^T G_n + added_n from gstate_out on.  A workgroup to 16 columns, on the fp32 matrix instructions whatever the type: a wavefront forms every fourth 16 rows, and hands them
+// to the others through LDS, since a step waits for the one before (65536 tokens of 8 heads of 128, 32 steps: 204 us with 16 columns to a wavefront, 122 so).
 // ----------------------------------------------------------------------------
 constexpr int kCarryWaves = 4;
 
@@ -1050,16 +1051,17 @@ template <int DK, bool BACK>
 __global__ void __launch_bounds__(64 * kCarryWaves)
 k_delta_carry(DeltaArgs A)
 {
-    constexpr int DT = DK / 16, SLICES = (DT + kCarryWaves - 1) / kCarryWaves, THREADS = 64 * kCarryWaves, PAD = DK + 4;
+    constexpr int DT = DK / 16, THREADS = 64 * kCarryWaves, PAD = DK + 4;
     constexpr int ROWS = DK > 192 ? 64 : DK > 128 ? 80 : DK, BLOCKS = (DK + ROWS - 1) / ROWS, N = (ROWS * DK / 4 + THREADS - 1) / THREADS;
     __shared__ __attribute__((aligned(16))) float M[ROWS * PAD];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-    const int h = blockIdx.x / SLICES, col = ((blockIdx.x % SLICES) * kCarryWaves + wave) * 16 + r16;
+    __shared__ f32x4 formed[DT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    // (a head's workgroups are `heads` apart: where that is a multiple of 8 they share an L2, and `turned` in it)
+    const int h = blockIdx.x % A.heads, col0 = blockIdx.x / A.heads * 16, col = col0 + r16;
     const int64_t b = (int64_t)blockIdx.z * kRows + blockIdx.y;
     if (b >= A.sequences) return;
     const int64_t begin = start_of(A, b), count = count_of(A, b, begin);
-    if (count <= kPays * A.stretch || (int)(blockIdx.x % SLICES) * kCarryWaves * 16 >= A.dv) return;
-    const bool live = (col & ~15) < A.dv;
+    if (count <= kPays * A.stretch || col0 >= A.dv) return;
     const int64_t stretches = (count + A.stretch - 1) / A.stretch, place = first_place(A, b, begin), step = (int64_t)A.heads * DK * DK;
     const float* const given = BACK ? A.gstate_out : A.state_in;
     float* const added = (BACK ? A.added_back : A.added) + (place * A.heads + h) * (int64_t)DK * DK;
@@ -1092,13 +1094,13 @@ k_delta_carry(DeltaArgs A)
         f32x4 next[DT];
 #pragma unroll
         for (int t = 0; t < DT; ++t)
+            if (t % kCarryWaves == wave)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) next[t][r] = live && !last ? here[(16 * t + 4 * g + r) * DK] : 0.0f;
-        if (live)
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) here[(16 * t + 4 * g + r) * DK] = S[t][r];
+                for (int r = 0; r < 4; ++r) {
+                    float* const at = here + (16 * t + 4 * g + r) * DK;
+                    next[t][r] = last ? 0.0f : *at;
+                    *at = S[t][r];
+                }
         if (last) break;
 #pragma unroll
         for (int block = 0; block < BLOCKS; ++block) {
@@ -1112,25 +1114,34 @@ k_delta_carry(DeltaArgs A)
             if (block + 1 < BLOCKS) ask(n, block + 1);
             else if (i + 2 < stretches) ask(number(i + 1), 0);
             // rows of the block are results ahead, what is summed over back
+            if constexpr (BACK) {
 #pragma unroll
-            for (int a = 0; a < ROWS / 16; ++a) {
-                const int mine = block * (ROWS / 16) + a;
-                if (mine >= DT) continue;
+                for (int c = 0; c < DT; ++c)
+                    if (c % kCarryWaves == wave)
 #pragma unroll
-                for (int c = 0; c < DT; ++c) {
-                    f32x4 f;
-                    if (BACK)
+                        for (int a = 0; a < ROWS / 16; ++a) {
+                            if (block * (ROWS / 16) + a >= DT) continue;
+                            f32x4 f;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) f[r] = M[(16 * a + 4 * g + r) * PAD + 16 * c + r16];
-                    else
-                        f = *reinterpret_cast<const f32x4*>(&M[(16 * a + r16) * PAD + 16 * c + 4 * g]);
-                    if (BACK) next[c] = mma(f, S[mine], next[c]);
-                    else next[mine] = mma(f, S[c], next[mine]);
+                            for (int r = 0; r < 4; ++r) f[r] = M[(16 * a + 4 * g + r) * PAD + 16 * c + r16];
+                            next[c] = mma(f, S[block * (ROWS / 16) + a], next[c]);
+                        }
+            } else {
+#pragma unroll
+                for (int a = 0; a < ROWS / 16; ++a) {
+                    const int mine = block * (ROWS / 16) + a;
+                    if (mine < DT && mine % kCarryWaves == wave)
+#pragma unroll
+                        for (int c = 0; c < DT; ++c) next[mine] = mma(*reinterpret_cast<const f32x4*>(&M[(16 * a + r16) * PAD + 16 * c + 4 * g]), S[c], next[mine]);
                 }
             }
         }
 #pragma unroll
-        for (int t = 0; t < DT; ++t) S[t] = next[t];
+        for (int t = 0; t < DT; ++t)
+            if (t % kCarryWaves == wave) formed[t][lane] = next[t];
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < DT; ++t) S[t] = formed[t][lane];
     }
 }
 
@@ -1793,7 +1804,7 @@ hipError_t walks_with(const DeltaArgs& A, int what, hipStream_t st)
 template <int DK>
 hipError_t carry_with(const DeltaArgs& A, bool back, hipStream_t st)
 {
-    const dim3 grid = grid_of((int64_t)A.heads * ((DK / 16 + kCarryWaves - 1) / kCarryWaves), A.sequences), block(64 * kCarryWaves);
+    const dim3 grid = grid_of((int64_t)A.heads * (DK / 16), A.sequences), block(64 * kCarryWaves);
     profile_before("delta_carry", st);
     if (back) hipLaunchKernelGGL((k_delta_carry<DK, true>), grid, block, 0, st, A);
     else hipLaunchKernelGGL((k_delta_carry<DK, false>), grid, block, 0, st, A);
