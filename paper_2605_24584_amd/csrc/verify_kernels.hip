@@ -91,6 +91,9 @@ k_verify_rows(VerifyArgs A)
     const int64_t first = part * A.part_rows + (int64_t)row_lane * kGroup, step = (int64_t)row_lanes * kGroup;
     const int64_t end = (part + 1) * A.part_rows < A.k ? (part + 1) * A.part_rows : A.k;
     Sum st{-INFINITY, 0.0};
+    // Logits further below the maximum than reach weigh 0.  An fp32 difference may be the maximum itself again (large logits, large c): there is a reach only
+    // where its own weight is 0, below 2^-1074.
+    float reach = -INFINITY;
     int64_t place = INT64_MAX;
     float ahead[kGroup];                               // the next rows are on their way while these are summed
     const auto ask = [&](int64_t row) {
@@ -117,10 +120,11 @@ k_verify_rows(VerifyArgs A)
             if (m > st.m) {
                 st.s *= weight_of(st.m, m, c);
                 st.m = m;
+                reach = m - far;
+                if (!(((double)m - (double)reach) * c >= 1100.0)) reach = -INFINITY;
             }
             // What is so far below the maximum that its weight is 0 is brought nearer, to where it is still 0: no further test in 64 bits.
-            const float reach = st.m - far;
-            if (reach > -3.4e38f) {
+            if (reach > -INFINITY) {
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) st.s += power_in_range(((double)fmaxf(v[i], reach) - (double)st.m) * c);
             } else {

@@ -235,3 +235,22 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for got, w in zip((accepted, following, logp, next_logp), want):
             assert torch.equal(got, w)
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rule", ["logits", "sure", "greedy"])
+@pytest.mark.parametrize("size,tau", [(1.0, 1e6), (1.0, 1e9), (1.0, 1e20), (1.0, 1e38), (1e4, 1.0), (1e4, 1e6), (1e10, 1.0), (1e30, 1.0), (1e30, 1e38), (1e-30, 1e30), (1e-38, 1.0)])
+def test_inverse_temperatures_and_logits_of_any_size(dtype, rule, size, tau):
+    """Where a step of a logit is more than a probability can fall: the likeliest tokens alone have weight, equal ones the same."""
+    r = seeded("any size", rule, size, tau)
+    c = Case(r, 5000, [4, 1, 0, 7, 3], dtype, rule == "logits")
+    for m in (c.y, c.z):
+        if m is not None:
+            m.mul_(size)
+    c.y[dev(r.random((5000, 15))) < 0.05] = -INF               # banned entries
+    c.y[:300, 3:6] = -INF
+    c.y[7:9, 9] = 9.0 * size                                    # two likeliest tokens
+    c.drafts = torch.where(dev(r.random(15)) < 0.6, c.y.argmax(0), c.drafts)
+    want = c.check(tau, tau, rule == "greedy")
+    assert (want[1][[0, 1, 3, 4]] >= 0).all()
+    c.check(tau, 1.0, rule == "greedy")
+    c.check(1.0, tau, rule == "greedy")
