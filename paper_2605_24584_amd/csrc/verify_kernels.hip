@@ -391,23 +391,34 @@ k_verify_draw(VerifyArgs A)
     const int64_t draft = C.mode == kVerifyOthers ? A.drafts[t] : -1;
     const double share = 1.0 / C.s, draft_share = 1.0 / C.draft_s;
     const double chance = A.next_chances[b];
+    int mode = C.mode;
+    // The weight of a row.  A part may be chosen only where one of its rows has some weight: a part's weight is the sum of these numbers, or no less than the largest of them and 0
+    // if that is.  (So p is not divided by its sum here: of the smallest weights that would leave 0 in the rows, though not in a part's sum.)
+    const auto row_weight = [&](int64_t r) {
+        const float y = to_float(static_cast<const T*>(A.y)[r * A.ldy + t]);
+        if (mode == kVerifyLeft) return left_of(A, C, share, draft_share, y, to_float(static_cast<const T*>(A.z)[r * A.ldz + t]));
+        return mode == kVerifyOthers && r == draft ? 0.0 : weight_of(y, C.m, A.c);
+    };
+    // The draft's part of the rows, without the draft, is summed again: a difference would hold the rounding of what is taken away.
+    const int64_t drafted = draft >= 0 ? draft / A.part_rows : -1;
+    double others = 0.0;
+    if (drafted >= 0) {
+        const int64_t begin = drafted * A.part_rows, end = begin + A.part_rows < A.k ? begin + A.part_rows : A.k;
+        double some = 0.0;
+        for (int64_t r = begin + x; r < end; r += kThreads) some += row_weight(r);
+        running(some, side, others);
+    }
     // the weights of the parts of the rows: a thread each
-    const auto part_weight = [&](int mode) {
+    const auto part_weight = [&]() {
         if (x >= A.parts) return 0.0;
         if (mode == kVerifyLeft) return A.left[x * A.sequences + b];
-        const float m = A.part_max[x * A.batch + t];
-        double w = A.part_sum[x * A.batch + t] * weight_of(m, C.m, A.c) * share;
-        if (mode == kVerifyOthers && draft / A.part_rows == x) {
-            w -= weight_of(to_float(static_cast<const T*>(A.y)[draft * A.ldy + t]), C.m, A.c) * share;
-            w = w > 0.0 ? w : 0.0;
-        }
-        return w;
+        if (mode == kVerifyOthers && x == drafted) return others;
+        return A.part_sum[x * A.batch + t] * weight_of(A.part_max[x * A.batch + t], C.m, A.c);
     };
-    int mode = C.mode;
-    double total, mine = part_weight(mode), sum = running(mine, side, total);
+    double total, mine = part_weight(), sum = running(mine, side, total);
     if (!(total > 0.0)) {                                 // nothing is left where it is refused: by rounding alone
         mode = kVerifyAll;
-        mine = part_weight(mode);
+        mine = part_weight();
         sum = running(mine, side, total);
     }
     const double bar = chance * total;
@@ -428,11 +439,6 @@ k_verify_draw(VerifyArgs A)
     // within it every thread takes some consecutive rows
     const int64_t begin = part * A.part_rows, end = begin + A.part_rows < A.k ? begin + A.part_rows : A.k;
     const int64_t each = (end - begin + kThreads - 1) / kThreads, r0 = begin + x * each, r1 = r0 + each < end ? r0 + each : end;
-    const auto row_weight = [&](int64_t r) {
-        const float y = to_float(static_cast<const T*>(A.y)[r * A.ldy + t]);
-        if (mode == kVerifyLeft) return left_of(A, C, share, draft_share, y, to_float(static_cast<const T*>(A.z)[r * A.ldz + t]));
-        return mode == kVerifyOthers && r == draft ? 0.0 : weight_of(y, C.m, A.c) * share;
-    };
     double rows = 0.0;
     for (int64_t r = r0; r < r1; ++r) rows += row_weight(r);
     double in_part;

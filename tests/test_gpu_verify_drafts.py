@@ -254,3 +254,46 @@ def test_inverse_temperatures_and_logits_of_any_size(dtype, rule, size, tau):
     assert (want[1][[0, 1, 3, 4]] >= 0).all()
     c.check(tau, 1.0, rule == "greedy")
     c.check(1.0, tau, rule == "greedy")
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,sequences", [(3000, 64), (3000, 3), (70000, 1)])
+def test_certain_draft_that_is_alone_in_its_part_of_the_rows(dtype, k, sequences):
+    """A refused draft with nothing but banned entries around it, before and behind all others: at either end of the chances the next token is the first or the last of the others."""
+    r = seeded("alone", k, sequences)
+    for at, chance in ((5, 0.0), (k - 9, 1.0 - 2.0 ** -53), (5, 0.5), (k - 9, 0.5)):
+        c = Case(r, k, [2] * sequences, dtype, False, spread=1.0, packed=False)
+        c.y[:600] = -INF
+        c.y[k - 600:] = -INF
+        c.y[at] = dev(r.normal(size=2 * sequences), dtype)
+        c.drafts.fill_(at)
+        c.chances.fill_(1.0 - 2.0 ** -53)
+        c.next_chances.fill_(chance)
+        want = c.check()
+        assert not want[0].any() and ((want[1] >= 600) & (want[1] < k - 600)).all()
+        assert chance == 0.5 or set(want[1]) == {600 if chance == 0.0 else k - 601}
+
+
+@pytest.mark.parametrize("rule", ["sure", "none"])
+def test_weights_at_the_end_of_the_numbers(rule):
+    """A part of the rows whose weights are the smallest number there is, which a division by the sum of all takes away: some token of those that are not banned is drawn."""
+    c = Case(seeded("smallest"), 4000, [2] * 40, F32, False, packed=False)
+    c.y.fill_(-INF)
+    c.y[:100] = -744.4                                          # e^-744.4 is 1.03 times 2^-1074
+    c.y[2000:2008] = 0.0
+    c.drafts.fill_(50 if rule == "sure" else -1)
+    c.chances.fill_(1.0 - 2.0 ** -53)
+    for chance in (0.0, 0.5, 1.0 - 2.0 ** -53):
+        c.next_chances.fill_(chance)
+        accepted, following, _, _ = c.run()
+        some = following.cpu().numpy()
+        assert not accepted.any() and (((some >= 0) & (some < 100)) | ((some >= 2000) & (some < 2008))).all()
+
+
+def test_certain_draft_that_has_nearly_all_the_weight():
+    """What the others weigh is formed from them: as the difference of two numbers near 1 it would be off by up to a tenth here."""
+    r = seeded("nearly all")
+    c = Case(r, 2500, [2] * 200, F32, False, spread=1.0, packed=False)
+    c.y[1200] = 41.0                                            # the others: some 4000 e^-41 = 6e-15
+    c.drafts.fill_(1200)
+    c.chances.fill_(1.0 - 2.0 ** -53)
+    assert not c.check()[0].any()
