@@ -26,10 +26,10 @@ constexpr int kGroup = 8;                 // rows that a thread has asked for at
 // (1024 to 8192 are alike) and columns of a workgroup (32 / 64: 32000 x 1000 and their drafts' 164 / 166).
 constexpr int kMaxParts = 256, kWorkgroups = 4096, kSlab = 64;
 
-// 2^t, t <= 0 and finite; 0 below 2^-1074
-__device__ __forceinline__ double power_in_range(double t)
+// 2^(c d), d <= 0 and c d finite; 0 below 2^-1074.  (The rest is written as one operation, so that the same numbers give the same bits wherever this is used.)
+__device__ __forceinline__ double power_in_range(double d, double c)
 {
-    const double n = __builtin_rint(t), f = t - n;
+    const double n = __builtin_rint(d * c), f = fma(d, c, -n);
     double s = 0x1.816193166d0f9p-40;                          // log(2)^13 / 13!, then 12, ...
     s = fma(s, f, 0x1.c3bd650fc2986p-36);
     s = fma(s, f, 0x1.e8cac7351bb25p-32);
@@ -47,13 +47,11 @@ __device__ __forceinline__ double power_in_range(double t)
     return __builtin_ldexp(s, (int)n);
 }
 
-// 2^t, t <= 0 (NaN for NaN)
-__device__ __forceinline__ double power_of_two(double t) { return t < -1100.0 ? 0.0 : power_in_range(t); }
-
 // 2^(c (y - m)) of a logit below the maximum m, which is finite or -inf (then there is nothing but -inf)
 __device__ __forceinline__ double weight_of(float y, float m, double c)
 {
-    return power_of_two(((double)y - (m == -INFINITY ? 0.0 : (double)m)) * c);
+    const double d = (double)y - (m == -INFINITY ? 0.0 : (double)m);
+    return d * c < -1100.0 ? 0.0 : power_in_range(d, c);      // (NaN for NaN)
 }
 
 struct Sum { float m; double s; };        // maximum and sum of 2^(c (y - m)); s is NaN where a logit is NaN or +inf
@@ -126,7 +124,7 @@ k_verify_rows(VerifyArgs A)
             // What is so far below the maximum that its weight is 0 is brought nearer, to where it is still 0: no further test in 64 bits.
             if (reach > -INFINITY) {
 #pragma unroll
-                for (int i = 0; i < kGroup; ++i) st.s += power_in_range(((double)fmaxf(v[i], reach) - (double)st.m) * c);
+                for (int i = 0; i < kGroup; ++i) st.s += power_in_range((double)fmaxf(v[i], reach) - (double)st.m, c);
             } else {
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) st.s += weight_of(v[i], st.m, c);
@@ -289,9 +287,11 @@ __device__ __forceinline__ void find_drawn(const VerifyArgs& A, int64_t b0, int 
     __syncthreads();
 }
 
-// share, draft_share: one over the columns' sums
+// share, draft_share: one over the columns' sums.  Both products are rounded before they are compared: a difference with one product exact would hold the other one's rounding
+// where both are alike, and such rows could be drawn.
 __device__ __forceinline__ double left_of(const VerifyArgs& A, const VerifyColumn& C, double share, double draft_share, float y, float z)
 {
+#pragma clang fp contract(off)
     const double p = weight_of(y, C.m, A.c) * share, q = weight_of(z, C.draft_m, A.draft_c) * draft_share, d = p - q;
     return d > 0.0 ? d : 0.0;
 }

@@ -297,3 +297,18 @@ def test_certain_draft_that_has_nearly_all_the_weight():
     c.drafts.fill_(1200)
     c.chances.fill_(1.0 - 2.0 ** -53)
     assert not c.check()[0].any()
+
+def test_entries_that_are_as_likely_under_both_are_never_drawn():
+    """Target and drafts differ in two entries that have changed places: what is left of a refused draft is one of them alone, up to the last chance."""
+    r = seeded("changed places")
+    for k in (40, 3000, 20000):
+        c = Case(r, k, [2] * 64, F32, spread=1.0, near=0.0, packed=False)
+        c.y[0], c.y[1] = 1.0, 2.0
+        c.z.copy_(c.y)
+        c.z[0], c.z[1] = 2.0, 1.0
+        c.drafts.fill_(0)
+        c.chances.fill_(1.0 - 2.0 ** -53)
+        for chance in (0.0, 0.5, 1.0 - 2.0 ** -53):
+            c.next_chances.fill_(chance)
+            accepted, following, _, _ = c.run(0.9, 0.9)
+            assert not bool(accepted.any()) and following.tolist() == [1] * 64
