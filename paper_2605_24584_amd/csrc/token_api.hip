@@ -488,7 +488,7 @@ int laplex_verify_drafts(const void* y, int64_t ldy, const void* draft_y, int64_
     LAPLEX_CHECK(check_array(next, sequences, 8, true));
     LAPLEX_CHECK(check_array(logp, batch, 4, false));
     LAPLEX_CHECK(check_array(next_logp, sequences, 4, false));
-    if (sequences == 0) return LAPLEX_OK;
+    if (sequences == 0 && (batch == 0 || !logp)) return LAPLEX_OK;
     LAPLEX_CHECK(check_ws(ws, ws_bytes, need));
     VerifyArgs A{};
     A.y = y; A.z = greedy ? nullptr : draft_y; A.ldy = ldy; A.ldz = ld_draft; A.k = k; A.batch = batch; A.sequences = sequences;

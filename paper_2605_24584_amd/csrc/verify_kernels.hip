@@ -197,6 +197,7 @@ k_verify_judge(VerifyArgs A)
             VerifyColumn none{};
             none.mode = kVerifyNone;
             A.columns[t] = none;
+            if (A.logp) A.logp[t] = 0.0f;
         }
         return;
     }
@@ -490,7 +491,7 @@ size_t verify_workspace(int64_t k, int64_t batch, int64_t sequences)
     return aligned(2 * most * 8) + aligned(2 * most * 4) + aligned(most * 8) + aligned(batch * sizeof(VerifyColumn)) + aligned(kMaxParts * sequences * 8);
 }
 
-// No columns at all: no sequence has a next token.
+// No columns, or no sequences: no sequence has a next token, no column a draft.
 __global__ void __launch_bounds__(kThreads)
 k_verify_none(VerifyArgs A)
 {
@@ -499,6 +500,8 @@ k_verify_none(VerifyArgs A)
         A.next[b] = -1;
         if (A.next_logp) A.next_logp[b] = 0.0f;
     }
+    if (A.logp)
+        for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < A.batch; t += (int64_t)gridDim.x * kThreads) A.logp[t] = 0.0f;
 }
 
 template <typename T>
@@ -529,8 +532,9 @@ static hipError_t launch_verify_of(const VerifyArgs& A, const Plan& P, hipStream
 hipError_t launch_verify(const VerifyArgs& given, hipStream_t st)
 {
     VerifyArgs A = given;
-    if (A.batch == 0) {
-        hipLaunchKernelGGL(k_verify_none, dim3((unsigned)((A.sequences + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, A);
+    if (A.batch == 0 || A.sequences == 0) {
+        const int64_t most = A.batch > A.sequences ? A.batch : A.sequences;
+        hipLaunchKernelGGL(k_verify_none, dim3((unsigned)((most + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, A);
         return hipGetLastError();
     }
     const Plan P = plan_of(A.k, A.batch);

@@ -312,3 +312,23 @@ def test_entries_that_are_as_likely_under_both_are_never_drawn():
             c.next_chances.fill_(chance)
             accepted, following, _, _ = c.run(0.9, 0.9)
             assert not bool(accepted.any()) and following.tolist() == [1] * 64
+
+@pytest.mark.parametrize("rule", ["logits", "sure", "greedy"])
+def test_columns_of_no_sequence(rule):
+    """Columns before the first sequence and behind the last one have no draft: their log probability is 0, whatever stood there; also where there is no sequence at all."""
+    r = seeded("outside", rule)
+    c = Case(r, 700, [12], F32, rule == "logits")
+    for starts in ([2, 5, 5, 9], [0, 0], [12, 12, 12], [4]):
+        b = len(starts) - 1
+        ws = torch.empty(max(1, B.laplex_verify_workspace_bytes(700, 12, b)), dtype=torch.uint8, device="cuda")
+        accepted, following = torch.full((b,), -7, device="cuda"), torch.full((b,), -7, device="cuda")
+        logp, next_logp = torch.full((12,), NAN, device="cuda"), torch.full((b,), NAN, device="cuda")
+        chances, next_chances = c.chances, dev(r.random(b), torch.float64)
+        B.laplex_verify_drafts(c.y, c.z, c.drafts, chances, next_chances, accepted, following, ws, logp, next_logp, sequences=b, starts=dev(np.array(starts), torch.int64),
+                               flags=B.LAPLEX_VERIFY_GREEDY if rule == "greedy" else 0)
+        want = O.verify_drafts(host(c.y), None if c.z is None else host(c.z), host(c.drafts).astype(np.int64), starts, 1.0, 1.0, host(chances), host(next_chances), rule == "greedy")
+        assert accepted.tolist() == want[0].tolist() and following.tolist() == want[1].tolist()
+        outside = [t for t in range(12) if t < starts[0] or t >= starts[-1]]
+        assert host(logp)[outside].tolist() == [0.0] * len(outside)
+        for got, w in ((host(logp), want[2]), (host(next_logp), want[3])):
+            assert (np.abs(got - w) <= U * (np.abs(w) + 1.0)).all()
