@@ -476,7 +476,9 @@ int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64
  * lengths (int64 device array of `sequences` numbers, or NULL): only the first lengths[b] rows of sequence b are read (all of them where it has fewer, none where that is
  * negative), and the rows behind them are left as they were, in y and in the gradients: what a batch with padding, or drafted tokens of which some were accepted, needs.
  * Keys are usually of length 1 and b_t from 0 to 1: then the state cannot grow from what it holds.  Rates >= 0 (+inf: nothing is left of the state;
- * from 1e5 on so too); other rates are carried as they are as long as exp(-sum of 64 of them) is a number.
+ * from 1e5 on so too).  Rates below 0 are carried as they are, but tokens are taken together in maps that hold factors of up to exp(-sum of up to 64 rates in a row): roundings
+ * grow by as much, and rates of -0.1 and below leave few digits.  In sequences of more than 192 tokens the maps of longer stretches must not overflow either: exp(-sum of any number of
+ * rates in a row) has to be an fp32 number, else the results may be NaN.  laplex_delta_attention_step takes rates below 0 like others.
  * Rows before a value that is not finite (in k, v, beta, or a NaN or -inf in rates) are not touched by it; from its token on the results and the state of its head may be NaN.  In q it reaches
  * its own row.  state_out may be state_in; nothing else may overlap.  1 <= dk, dv <= LAPLEX_ATTENTION_MAX_DIM; scale positive and finite.
  * Flags: LAPLEX_SAVE_SCANS (needs a workspace for training): what the gradients need stays in the workspace for laplex_delta_attention_backward with the same flag

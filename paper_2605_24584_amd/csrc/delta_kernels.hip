@@ -504,7 +504,7 @@ k_delta_walk(DeltaArgs A)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * t + 4 * g + r;
-            if (STATES) S[t][r] = part && row == col ? 1.0f : 0.0f;
+            if (STATES) S[t][r] = part && row == col && col < A.dk ? 1.0f : 0.0f;      // (nothing behind dk: no key takes of it what rates below 0 add)
             else if (s.several) S[t][r] = col < A.dv ? entering[row * DK] : 0.0f;
             else S[t][r] = A.state_in && row < A.dk && col < A.dv ? A.state_in[state_at + (int64_t)row * A.dv + col] : 0.0f;
         }

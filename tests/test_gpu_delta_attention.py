@@ -6,6 +6,8 @@ the sizes that the oracle gives: e = 16 sqrt(n + dk + dv + 64) U of the column's
 the sizes of the state's gradient.  The gradient of a rate is a sum of up to 64 tokens' terms, six each, with signs: 64 e.  In bf16 results are rounded once (H), and what
 enters products of them is carried in 16 bits at least: 2^-15 of the same sizes; states and the gradients of rates, beta and states are fp32 sums whatever the type.
 """
+import copy
+
 import numpy as np
 import pytest
 
@@ -404,3 +406,24 @@ def test_sequences_in_stretches(dtype, lengths, heads, key_heads, dk, dv, packed
     same = c.state.clone()
     B.laplex_delta_attention(c.q, c.k, c.v, c.rates, c.beta, z, c.workspace(False), c.scale, c.b, c.starts, c.read, same, same)
     assert torch.equal(z.nan_to_num(), y.nan_to_num()) and torch.equal(same, last)
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_growing_states_of_a_few_numbers(dtype):
+    """Rates below 0 in sequences that are cut: e^0.045 a token is e^92 over a stretch of 2048 tokens, more than fp32 holds, while keys of one number and weights near 1 take a tenth of the
+    state from token to token.  What lies beside that number of a key, as far as tiles are padded, may not grow.  A chunk's maps hold factors of up to exp(63 * 0.045) = 17, which
+    enlarge its roundings."""
+    c = Case(seeded("growing"), [8192], 64, 64, 1, 24, dtype, packed=False)
+    c.rates.fill_(-0.045)
+    c.beta.fill_(0.9)
+    one = copy.copy(c)                                          # the last head by itself
+    one.heads = one.key_heads = 1
+    for name in ("q", "k", "v", "rates", "beta", "gy"):
+        setattr(one, name, getattr(c, name)[:, -1:])
+    one.state, one.gstate = c.state[:, -1:], c.gstate[:, -1:]
+    one.e = lambda m: 17 * Case.e(one, m)
+    ws = c.workspace()
+    y, last = c.forward(ws, B.LAPLEX_SAVE_SCANS)
+    g = c.backward(ws, B.LAPLEX_SAVE_SCANS)
+    assert all(bool(torch.isfinite(t).all()) for t in (y, last, *g))
+    one.check_forward(y[:, -1:], last[:, -1:])
+    one.check_backward([t[:, -1:] for t in g])
