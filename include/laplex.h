@@ -471,7 +471,7 @@ int laplex_decay_attention_step(const void* q, int64_t ldq, const void* k, int64
  * Linear attention by the gated delta rule: the state forgets by a decay for each token and head, and a token corrects what the state holds for its key instead of
  * adding to it.  Per head of a sequence, with l_t = exp(-rates[t][head]), b_t = beta[t][head] and the state S (dk x dv; S0 = state_in, or zeros):
  *   S <- l_t S,   u_t = b_t (v_t - S^T k_t),   S <- S + k_t u_t^T,   y_t = scale S^T q_t,        t = 0 .. n-1
- * q, k [tokens][key_heads][dk], v, y [tokens][heads][dv]; head h of values uses head h / (heads / key_heads) of queries and keys (key_heads divides heads).
+ * q, k [tokens][key_heads][dk], v, y [tokens][heads][dv]; head h of values uses head h / (heads / key_heads) of queries and keys (key_heads divides heads; 0 only with 0 heads).
  * rates and beta: fp32 [tokens][heads], rows ldr and ldb floats apart, in device memory.  Sequences, starts and states as for laplex_decay_attention;
  * lengths (int64 device array of `sequences` numbers, or NULL): only the first lengths[b] rows of sequence b are read (all of them where it has fewer, none where that is
  * negative), and the rows behind them are left as they were, in y and in the gradients: what a batch with padding, or drafted tokens of which some were accepted, needs.

@@ -72,7 +72,7 @@ struct DeltaSizes { int64_t tokens, sequences, heads, key_heads, dk, dv; };
 int check_delta_sizes(int type, const DeltaSizes& s, bool equal)
 {
     LAPLEX_CHECK(check_attention_sizes(type, s.tokens, s.sequences, s.heads, s.dk, s.dv, equal));
-    return s.key_heads < 0 || (s.heads > 0 && (s.key_heads == 0 || s.heads % s.key_heads != 0)) ? LAPLEX_ERR_SIZE : LAPLEX_OK;
+    return s.heads == 0 ? (s.key_heads == 0 ? LAPLEX_OK : LAPLEX_ERR_SIZE) : s.key_heads < 1 || s.heads % s.key_heads != 0 ? LAPLEX_ERR_SIZE : LAPLEX_OK;
 }
 
 // float rows [tokens][heads]

@@ -81,6 +81,20 @@ def test_step_rejects_bad_arguments(L):
     assert call(sequences=0, q=None, k=None, v=None, y=None, rates=None, beta=None, state=None) == B.LAPLEX_OK
 
 
+def test_heads_of_keys_without_heads_of_values_are_refused(L):
+    """Their gradients would be sums over nothing, which no launch writes."""
+    out = ctypes.c_size_t(0)
+    bad = dict(heads=0, key_heads=2)
+    assert L.laplex_delta_attention_workspace_bytes(0, 12, 3, 0, 2, 16, 8, 1, ctypes.byref(out)) == B.LAPLEX_ERR_SIZE
+    for f, names in ((L.laplex_delta_attention, "q ldq k ldk v ldv type tokens sequences starts lengths heads key_heads dk dv rates ldr beta ldb scale state_in y ldy state_out ws wsb flags"),
+                     (L.laplex_delta_attention_backward, "q ldq k ldk v ldv type tokens sequences starts lengths heads key_heads dk dv rates ldr beta ldb scale state_in gy ldgy gstate_out "
+                      "gq ldgq gk ldgk gv ldgv grates ldgr gbeta ldgb gstate_in ws wsb flags"),
+                     (L.laplex_delta_attention_step, "q ldq k ldk v ldv type sequences heads key_heads dk dv rates ldr beta ldb scale state y ldy")):
+        call = caller(f, names, {**OK, "ldq": 32, "ldk": 32, "ldgq": 32, "ldgk": 32})
+        assert call(**bad) == B.LAPLEX_ERR_SIZE
+        assert call(heads=0, key_heads=0) == B.LAPLEX_OK
+
+
 def test_workspace(L):
     f = L.laplex_delta_attention_workspace_bytes
     out = ctypes.c_size_t(0)
