@@ -549,8 +549,8 @@ int laplex_logprob_backward(const void* y, int64_t ldy, int type, int64_t k, int
  *   mean = sum x / width,  rstd = (sum (x - mean)^2 / width + eps)^(-1/2),  y = (x - mean) rstd weight + bias
  * weight[width] and bias[width] may each be NULL (1, 0); mean[rows] and rstd[rows] (what the backward call needs) may each be NULL.  A row may be a
  * head of a token: with weight = width^(-1/2) queries and keys become (centred) vectors of length 1.  y may be x (in place, the same ld), else they must
- * not overlap.  eps positive and finite; 1 <= width <= LAPLEX_NORM_MAX_WIDTH; rows <= LAPLEX_NORM_MAX_ROWS.  The squares are summed in fp32: numbers from
- * 1e18 in magnitude on may give rows of zeros.  A row with a NaN or an infinity is NaN; others are not touched by it.
+ * not overlap.  eps positive and finite; 1 <= width <= LAPLEX_NORM_MAX_WIDTH; rows <= LAPLEX_NORM_MAX_ROWS.  Numbers and squares are summed in fp32: those from
+ * 1e18 in magnitude on may give rows of zeros, and where the sum of a row overflows NaN.  A row with a NaN or an infinity is NaN; others are not touched by it.
  */
 int laplex_layer_norm(const void* x, int64_t ldx, int type, int64_t rows, int64_t width, const float* weight, const float* bias, float eps,
                       void* y, int64_t ldy, float* mean, float* rstd, laplex_stream_t stream);

@@ -112,7 +112,7 @@ k_norm(NormArgs A)
 #pragma unroll
             for (int e = 0; e < N; ++e) sum[0] += v[i][e];
         row_sums<1, LANES>(sum, side[0]);
-        const float mean = sum[0] / width;      // (divided, not multiplied by 1 / width: rows of equal numbers have exactly their mean)
+        const float mean = sum[0] / width;      // (divided, not multiplied by 1 / width: rows of one number again and again have exactly it for a mean where their sum is exact)
         sum[0] = 0.0f;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i)
@@ -161,7 +161,7 @@ k_norm_long(NormArgs A)
             sum[0] += s;
         }
         row_sums<1, kThreads>(sum, side[0]);
-        const float mean = sum[0] / width;      // (divided, not multiplied by 1 / width: rows of equal numbers have exactly their mean)
+        const float mean = sum[0] / width;      // (divided, not multiplied by 1 / width: rows of one number again and again have exactly it for a mean where their sum is exact)
         sum[0] = 0.0f;
         for (int64_t at = (int64_t)threadIdx.x * N; at < A.width; at += step) {
             load_piece<T>(v, x, at, A.width);
