@@ -18,10 +18,13 @@
 // walks have written.  Long sequences are cut into stretches of chunks: a walk of all stretches at once finds what each does to a state (S -> turned S + added), k_delta_carry
 // joins these in order, and the walks then start from the stretches' own states.  k_delta_tokens takes sequences of a few tokens one token at a time.
 //
-// What bounds it (us, bf16, heads of 128): not memory, but products that wait for one another with one or two wavefronts on a SIMD, as many vector instructions beside them (splits into
-// parts, decays), and in the gradients LDS, of which a workgroup takes all.  8 x 4096 tokens of 16 heads, trained: prepare 106, walk 530, back 498, gradients 927 (the recurrence's operations and bytes
-// would take 220).  4 x 2048 of 16: prepare 40, stretches 94, carry 20, walk 86.  65536 of 8: 135, 340, 122, 270.  256 sequences of 5 tokens, token by token: 122, which is 0.54 GB of
-// states at 4.5 TB/s.
+// What bounds it (us, bf16, heads of 128): products that wait for one another with one or two wavefronts on a SIMD, as many vector instructions beside them (splits into
+// parts, decays), and in the gradients LDS, of which a workgroup takes all.  8 x 4096 tokens of 16 heads, trained: prepare 105, walk 517, back 483, gradients 908 (the recurrence's operations and bytes
+// would take 220).  There memory has a part in it too: the walks write states, their gradients, U and dR, 1.6 GB, and the gradients read them (counted: 0.95 GB written by the
+// walk, 0.81 by the walk back); there and back they would take 650 of the 1942 at a copy's rate.  4 x 2048 of 16: prepare 40, stretches 94, carry 21, walk 84.  65536 of 8: 136, 350, 122,
+// 274.  256 sequences of up to 5 tokens, token by token: 124 with the caches filled with other data before (114 among other calls), which is 0.54 GB of states at 4.4 TB/s.
+// Scratch (bytes a lane): the walk with results 44 (128 numbers, 8 wavefronts) and 28 (256), prepare 36 in bf16 up to 128 numbers, gradients 8 (96 numbers, bf16), tokens 12 (8 rows a
+// thread).
 // Chunks of half as many tokens make the walks slower (4 x 2048 268 -> 350, 8 x 4096 trained 2120 -> 3390): a chunk's waits stay, and there are twice as many.  Sixteen wavefronts for the gradients
 // spill.  Fragments asked for a step ahead took 8 x 4096 from 2120 to 2030, 65536 from 963 to 925.
 //
@@ -1588,7 +1591,7 @@ k_delta_gradients(DeltaArgs A)
 // ----------------------------------------------------------------------------
 // A few tokens of every sequence: the state in registers, token after token.  With e = S^T k and f = S^T q of the decayed state,
 //   u = beta (v - e),   y = scale (f + (k . q) u),   S <- S + k u^T:
-// both sums go over the state at once.  256 sequences of up to 5 tokens, 16 heads of 128: 129 us, 110 for the states' way through memory alone.  A workgroup takes a slice of the columns: `lanes` times VEC of them, the rest of its threads the rows.
+// both sums go over the state at once.  256 sequences of up to 5 tokens, 16 heads of 128: 124 us, 110 for the states' way through memory alone.  A workgroup takes a slice of the columns: `lanes` times VEC of them, the rest of its threads the rows.
 // ----------------------------------------------------------------------------
 constexpr int kTokenThreads = 256;
 
@@ -1713,7 +1716,8 @@ int64_t chunks_of(int64_t tokens, int64_t sequences, int c, bool equal)
     return equal ? sequences * ((sequences > 0 ? tokens / sequences + c - 1 : 0) / c) : tokens / c + sequences;
 }
 
-// Sequences of no more tokens than this go token by token.  us, token by token / in chunks, heads of 128: 256 sequences of 16 heads, 2 tokens 132 / 340, 5 185 / 334, 8 241 / 334,
+// Sequences of no more tokens than this go token by token, where all are of equal lengths (packed ones are as long as the device's numbers say, and go in chunks).  us of
+// single calls, of which one of next to no work takes 9, token by token / in chunks, heads of 128: 256 sequences of 16 heads, 2 tokens 132 / 340, 5 185 / 334, 8 241 / 334,
 // 16 393 / 336; 4 sequences 10.9 / 45, 16 / 44, 21 / 44, 35 / 44.
 constexpr int64_t kFewTokens = 12;
 
@@ -1745,11 +1749,13 @@ struct Cut { bool cut; int64_t stretch, per_sequence, slots, places; };
 
 // A workgroup of a walk takes most of a compute unit's LDS, so 256 of them fill the card: us with stretches for 128 / 256 / 512, 16 heads of 128 in bf16: 1 x 65536 tokens of 8
 // heads 1047 / 979 / 1145, 4 x 2048 247 / 227 / 278, 2 x 4096 for training 812 / 730 / 880; in fp32 256 / 512: 4 x 2048 437 / 471, 8 x 4096 for training 3203 / 4085.  Packed sequences of uneven
-// lengths leave places, and two workgroups of fp32 numbers fit a compute unit: 256 / 512 in fp32, 24 sequences of 30011 tokens, 6 heads of 96 and 80, for training 1792 / 1470, their results alone
-// 702 / 540, 16 of 32768 and 16 heads of 128 1656 / 1739; in bf16 16 of 32768 780 / 837, 8 of 32768 for training 2695 / 2737.
+// lengths leave places, and two workgroups of fp32 numbers fit a compute unit: 256 / 512 in fp32, over four draws of the lengths: 24 sequences of 30011 tokens, 6 heads of 96 and 80, for training
+// 1782 / 1690, their results alone 695 / 649; 16 of 32768, 16 heads of 128 1722 / 1550; 8 of 32768 for training 5559 / 4600; 12 of 20000, 8 heads of 64 358 / 291, for training 850 / 725; 40 of
+// 50000, 4 heads of 128 901 / 888; 4 of 9000, 16 heads of 96 536 / 461; 10 of 30000, 4 heads of 256 2067 / 1717.  In bf16 16 of 32768 780 / 837, 8 of 32768 for training 2695 / 2737.
 // Stretches of at least 2 / 4 / 8 chunks: 1 x 1024 123 / 112 / 132, 1 x 4096 222 / 222 / 203.
 // A cut costs the maps from state to state besides, about twice the work, and pays for sequences of more than three stretches (kPays).  Cut / whole: 1 x 512 (two stretches) 99 / 82, 8 x 4096 for
-// training (two) 2169 / 1958, 1 x 1024 (four) 112 / 133, 4 x 2048 (four) 231 / 248, 1 x 65536 927 / 6689.
+// training (two) 2169 / 1958, 1 x 1024 (four) 112 / 133, 4 x 2048 (four) 231 / 248, 1 x 65536 927 / 6689.  Packed, kPays 1 / 2 / 3 over eight draws of the lengths: 24 of 30011 in fp32 for
+// training 1542 / 1557 / 1598, 16 of 32768 in bf16 820 / 777 / 733: one number for both, which costs the one 4 % and gives the other 11 %.
 constexpr int64_t kLeastChunks = 4;
 int64_t workgroups_of(bool bf16, bool equal) { return bf16 || equal ? 256 : 512; }
 

@@ -9,7 +9,9 @@
 // workgroup (k_norm_parts) and added up in order by a second launch, so that the same call gives the same bits.  Longer rows are read again instead of held
 // (k_norm_*_long), and their columns are summed by a launch of their own.
 //
-// What bounds it: HBM.  In bf16 32768 rows of 4096: forward 131 us (4.1 TB/s), gradient 187 (4.3) and 7 for the join; 524288 rows of 128: 57 (4.7 TB/s) and 94 (4.3).  Weights held in registers
+// What bounds it: HBM.  In bf16 32768 rows of 4096: forward 135 us (4.0 TB/s), gradient 190 (4.2) and 7 for the join; 524288 rows of 128: 58 (4.6 TB/s) and 96 (4.2).  In fp32 (with the join)
+// 211 (5.1) and 341 (4.7), 124 (4.3) and 181 (4.4).  Rows that are not held, or barely, are far from that: 8192 x 16384 in bf16 274 (2.0) and 557 (1.5; the gradient's eight pieces a thread leave 196
+// bytes a lane in scratch and one wavefront a SIMD), in fp32, not held, 359 (3.0) and 700 (2.3); 2048 x 100000 in bf16 456 (1.8) and 1075 (1.1), of which the 819 MB of columns' sums are a part.  Weights held in registers
 // over a workgroup's rows, and not read again for each, took both directions of 32768 x 4096 from 517 to 332 us.  Reading the next row ahead is no faster: other workgroups of the compute unit do so.
 #include "token_internal.h"
 
@@ -379,8 +381,9 @@ Plan plan_of(int64_t pieces, bool two)
     return {0, 0};
 }
 
-// Forward, workgroups that go over the rows with the weights in registers: us with 1024 / 2048 / 4096 / one for each row, bf16: 32768 rows of 4096 130 / 136 / 133 / 150, 524288 of 128
-// 76 / 67 / 66 / 63.  Backward, workgroups that keep sums of columns, 512 / 1024 / 2048: 32768 of 4096 396 / 321 / 349, 524288 of 128 219 / 166 / 177; each has two turns at least where there are
+// Forward, workgroups that go over the rows with the weights in registers: us with 1024 / 2048 / 4096 / one for each row, bf16: 32768 rows of 4096 132 / 136 / 133 / 152, 524288 of 128
+// 77 / 69 / 68 / 63, 65536 of 1024 71 / 74 / 72 / 72, 16384 of 8192 204 / 207 / 210 / 222; fp32, the same rows: 219 / 211 / 207 / 195, 114 / 120 / 118 / 122, 122 / 110 / 110 / 125,
+// 214 / 205 / 203 / 212.  2048 and 4096 are alike within 2 %; each of the others loses a tenth somewhere.  Backward, workgroups that keep sums of columns, 512 / 1024 / 2048: 32768 of 4096 396 / 321 / 349, 524288 of 128 219 / 166 / 177; each has two turns at least where there are
 // more than 256, since it writes as much as a row of sums: 1024 of 8192 in 512 / 1024 parts 63 / 87.
 constexpr int64_t kForwardWorkgroups = 2048, kPartWorkgroups = 1024, kLeastParts = 256, kMostWorkgroups = int64_t(1) << 22;      // (a grid holds fewer than 2^32 threads)
 

@@ -11,8 +11,9 @@
 // the maximum); k_verify_judge, a wavefront per column, joins them and judges the draft; k_verify_left sums what is left of the refused columns over the same
 // parts of the rows; k_verify_draw, a workgroup per sequence, finds the part and then the row.  The second reading takes the refused columns alone.
 //
-// What bounds it: 64-bit vector instructions, some 43 a logit, not memory.  32000 rows x 1001 columns in fp32 with the drafts' logits: rows 91 us of 155 (0.26 GB: 2.8 TB/s), left 33, draw 17,
-// judge 14; 60001 x 576 in bf16, certain drafts: rows 54 of 80, draw 15, judge 8.  One column alone costs the four launches and the draw's two searches: 30 us.
+// What bounds it: 64-bit vector instructions, some 43 a logit, not memory.  32000 rows x 1001 columns in fp32 with the drafts' logits: rows 95 us (0.26 GB: 2.7 TB/s), left 32, draw 15,
+// judge 12, the call 138; 60001 x 576 in bf16, certain drafts: rows 55, draw 16 (1 of it for the draft's part, summed again), judge 7, the call 68.  Five columns of 32000 cost the four
+// launches and the draw's two searches: 26 us.  (Times at parts, workgroups and sequences side by side below are of single calls with all caches filled with other data, 10 to 25 us more.)
 // Two columns a lane, and several parts a workgroup in k_verify_left, were no faster.
 #include "token_internal.h"
 
